@@ -16,6 +16,14 @@
  *                     iteration, round by round (fetch, skip, emit,       App. E)
  *                     stop), into the same plan layout
  *
+ * What a trainer does with a collated tile once its model has answered:
+ *
+ *   odb_token_logprobs           log-probabilities of a tile's labels from its logits
+ *   odb_token_logprobs_backward  their gradient with respect to the logits
+ *   odb_policy_loss              clipped policy loss with a KL term, weighted per slot, and its
+ *                                gradient with respect to the log-probabilities
+ *   odb_preference_loss          loss over pairs of rows (paired log ratios) and its gradient
+ *
  * Conventions shared by every entry point
  *   - Pointers named d_* are device pointers (HIP global memory on the current device);
  *     all other pointers are host pointers.  The caller owns every buffer; the library
@@ -483,6 +491,219 @@ int odb_stream_plan(const odb_window_t* w, const int32_t* d_perm, int64_t budget
                     int64_t* d_slot_tokens, double* d_slot_tokens_approx, int32_t* d_left_views,
                     int64_t* d_left_off, odb_stream_round_t* h_trace, odb_stream_info_t* h_info,
                     void* d_ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------- losses over the tiles */
+
+/* A label that is not learnt: padding (odb_collate writes it) and whatever a caller masks. */
+#define ODB_LABEL_IGNORE (-100)
+
+typedef enum odb_dtype { ODB_FLOAT32 = 0, ODB_BFLOAT16 = 1, ODB_FLOAT16 = 2 } odb_dtype_t;
+
+/* The logits of one tile: element (i, c, v) is d_logits[i * row_stride + c * col_stride + v]. */
+typedef struct odb_logits {
+    int32_t dtype;          /* odb_dtype_t                                                    */
+    int32_t shift;          /* token (i, c) is scored by the logits at (i, c - shift): 1 for a
+                               model that predicts the next token, 0 for logits already aligned */
+    int64_t rows;           /* tile shape, >= 0; rows * cols < 2^31                           */
+    int64_t cols;
+    int64_t vocab;          /* V, 1 <= V < 2^31                                               */
+    int64_t row_stride;     /* in elements, >= 0                                              */
+    int64_t col_stride;
+    double  scale;          /* logits are multiplied by it (1 / temperature); finite, > 0     */
+    const void* d_logits;   /* aligned to its element                                         */
+} odb_logits_t;
+
+/*
+ * Log-probabilities of a tile's labels.  With y = label(i, c), z the logits that score it and
+ * a = scale:
+ *   largest = max_v z_v,   logsum = ln sum_v exp(a (z_v - largest))
+ *   logprob = a (z_y - largest) - logsum
+ *   entropy = logsum - sum_v p_v a (z_v - largest),   p_v = exp(a (z_v - largest) - logsum)
+ * A token counts if c >= shift and its label is not ODB_LABEL_IGNORE.  Every output of a token
+ * that does not count is 0 and its logits are not read (they may hold anything).
+ *
+ *   d_labels    [rows * cols] int32, as odb_collate writes them (or with more tokens masked)
+ *   d_logprob   [rows * cols] out
+ *   d_stats     [rows * cols * 2] out, or NULL: (largest, logsum) of every token, which the
+ *               backward call takes; ln sum_v exp(a z_v) = a * largest + logsum.  8-byte aligned
+ *   d_entropy   [rows * cols] out, or NULL
+ *   d_status    [1] device, or NULL: set to a nonzero value if a label lies outside [0, V) and
+ *               is not ODB_LABEL_IGNORE (that token does not count); never cleared here, so one
+ *               word may collect the errors of many calls
+ *
+ * Logits of -inf and of a type's lowest value are masked vocabulary entries.  A token whose
+ * logits are all -inf, or hold a NaN or +inf, gets NaN (no distribution); a label at -inf
+ * beside finite logits gets -inf.  Asynchronous (one kernel); needs no workspace.
+ */
+int odb_token_logprobs(const odb_logits_t* x, const int32_t* d_labels, float* d_logprob, float* d_stats,
+                       float* d_entropy, int32_t* d_status, void* stream);
+
+/*
+ * Gradient of the above: with g and h the gradients of a token's logprob and entropy,
+ *   d z_v = a (g ([v = y] - p_v) - h p_v (ln p_v + entropy)).
+ *
+ *   x, d_labels        as in the forward call
+ *   d_stats            [rows * cols * 2] as the forward call wrote them
+ *   d_grad_logprob     [rows * cols]; read only where the token counts
+ *   d_entropy,         [rows * cols] each, or both NULL (no gradient by the entropy)
+ *   d_grad_entropy
+ *   d_grad_logits      out, x's type: every element (i, c, v) of the tile is written at
+ *                      i * grad_row_stride + c * grad_col_stride + v, 0 where no token is
+ *                      scored.  Either x->d_logits with x's strides (in place) or memory that
+ *                      does not overlap it; the strides must not let elements overlap
+ *   d_status           as in the forward call
+ *
+ * Where g and h are both 0 the gradient is 0 and the logits are not read.  Asynchronous (one
+ * kernel); needs no workspace.
+ */
+int odb_token_logprobs_backward(const odb_logits_t* x, const int32_t* d_labels, const float* d_stats,
+                                const float* d_grad_logprob, const float* d_entropy, const float* d_grad_entropy,
+                                void* d_grad_logits, int64_t grad_row_stride, int64_t grad_col_stride,
+                                int32_t* d_status, void* stream);
+
+/*
+ * A run of a plan's slots and their labels.  The slot arrays are the plan's (odb_align_groups,
+ * odb_stream_plan) from the run's first slot on; offsets count from that slot's, so arrays
+ * parallel to the tiles (labels, log-probabilities, gradients) start at its first element and
+ * arrays parallel to the rows at its first row.  A whole plan is the run of all its slots.  Arrays
+ * of length 0 (a run of IDLE slots) may be NULL.
+ */
+typedef struct odb_tiles {
+    int64_t num_slots;               /* K, 0 <= K < 2^31                                       */
+    int64_t num_rows;                /* length of the arrays parallel to the rows, < 2^31      */
+    int64_t num_elems;               /* length of the arrays parallel to the tiles, <= 2^40    */
+    const int32_t* d_slot_rows;      /* [K]                                                    */
+    const int32_t* d_slot_maxlen;    /* [K]                                                    */
+    const int64_t* d_slot_row_off;   /* [K+1]                                                  */
+    const int64_t* d_slot_tile_off;  /* [K+1]                                                  */
+    const int32_t* d_labels;         /* [num_elems]; a token (i, c) of a tile counts if c >= shift
+                                        and its label is not ODB_LABEL_IGNORE                  */
+    int32_t shift;                   /* as in odb_logits_t: 0 or 1                             */
+    int32_t reserved0;               /* must be 0                                              */
+} odb_tiles_t;
+
+/* Bytes of device workspace that odb_policy_loss (num_ids = 0) and odb_preference_loss need for
+ * these tiles: a function of num_slots, num_rows, num_elems and num_ids alone.  0 on bad tiles. */
+size_t odb_loss_workspace_size(const odb_tiles_t* t, int64_t num_ids);
+
+/* KL term of a token, by x = logprob - ref_logprob. */
+typedef enum odb_kl {
+    ODB_KL_NONE = 0,
+    ODB_KL_LINEAR = 1,           /* x                                                          */
+    ODB_KL_SQUARE = 2,           /* x^2 / 2                                                    */
+    ODB_KL_EXP = 3               /* exp(-x) + x - 1                                            */
+} odb_kl_t;
+
+/* How a slot's counted tokens become one number. */
+typedef enum odb_reduce {
+    ODB_REDUCE_TOKEN_MEAN = 0,   /* mean over the counted tokens                               */
+    ODB_REDUCE_ROW_MEAN = 1,     /* mean over the rows with a counted token of the row's mean  */
+    ODB_REDUCE_SUM = 2
+} odb_reduce_t;
+
+typedef struct odb_policy_params {
+    int32_t kl;                  /* odb_kl_t                                                   */
+    int32_t reduce;              /* odb_reduce_t                                               */
+    int32_t token_advantage;     /* 0: one advantage per row, 1: one per element of the tiles  */
+    int32_t reserved0;           /* must be 0                                                  */
+    double  clip_low;            /* e_l in [0, 1] (1: no lower clip)                           */
+    double  clip_high;           /* e_h >= 0 (infinite: no upper clip)                         */
+    double  dual_clip;           /* bound c > 1 on the ratio where A < 0, or 0 (none)          */
+    double  kl_coef;
+    double  entropy_coef;
+    double  loss_scale;          /* factor of every slot's loss (W in Eq. 2's scaling)         */
+} odb_policy_params_t;
+
+/*
+ * Clipped policy loss with a KL term and an entropy bonus, and its gradient.  Per counted token,
+ * with ratio r = exp(d), d = logprob - old_logprob, and advantage A:
+ *   policy = max(-r A, -clip(r, 1 - e_l, 1 + e_h) A), and with a dual clip c, where A < 0,
+ *            the smaller of that and -c A;   0 where A = 0
+ * The loss of slot k, R being the reduction over its counted tokens, is
+ *   loss_k = loss_scale * slot_weight_k * (R(policy) + kl_coef R(KL) - entropy_coef R(entropy))
+ * and the gradients are those of sum_k loss_k.  Whether a ratio is clipped is decided on d, in
+ * 64 bits, against ln(1 - e_l), ln(1 + e_h) and ln c, strictly; a clipped token's policy term
+ * has no gradient.
+ *
+ *   d_logprob         [num_elems], as odb_token_logprobs writes them
+ *   d_old_logprob     [num_elems], or NULL: old = logprob, a ratio of 1 with gradient
+ *   d_ref_logprob     [num_elems]; needed unless kl is ODB_KL_NONE (then not read)
+ *   d_entropy         [num_elems], or NULL (then entropy_coef must be 0)
+ *   d_advantage       [num_rows], or [num_elems] with token_advantage
+ *   d_slot_weight     [K] fp64 (odb_loss_weights), or NULL: 1
+ *   d_slot_loss       [K] out
+ *   d_slot_means      [K * 4] out: R(policy), R(KL), R(entropy), R(ratio)
+ *   d_slot_counts     [K * 4] out: counted tokens, and of them those clipped below, above and by c
+ *   d_grad_logprob    [num_elems] out, or NULL
+ *   d_grad_entropy    [num_elems] out, or NULL (needs d_entropy)
+ *   d_status          [1] device, or NULL: set to a nonzero value if a slot's arrays contradict
+ *                     each other or leave the arrays' lengths (such a slot counts nothing and its
+ *                     gradients are not written); never cleared here
+ *   d_ws / ws_bytes   odb_loss_workspace_size(t, 0) bytes, 256-B aligned; calls in flight at
+ *                     once (captured graphs too) need workspaces of their own
+ *
+ * A token that does not count contributes nothing, whatever its inputs hold, and has gradient 0;
+ * a slot without counted tokens (an IDLE one among them) has loss, means and counts 0.  Elements
+ * behind the last slot are not written.  Sums run in 64 bits in a fixed order: results are the
+ * same bit for bit from call to call.  Asynchronous.
+ */
+int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* p, const float* d_logprob,
+                    const float* d_old_logprob, const float* d_ref_logprob, const float* d_entropy,
+                    const float* d_advantage, const double* d_slot_weight, float* d_slot_loss, float* d_slot_means,
+                    int64_t* d_slot_counts, float* d_grad_logprob, float* d_grad_entropy, int32_t* d_status,
+                    void* d_ws, size_t ws_bytes, void* stream);
+
+typedef enum odb_preference {
+    ODB_PREFERENCE_SIGMOID = 0,  /* -(1 - e) ln s(h) - e ln s(-h), s(h) = 1 / (1 + exp(-h))    */
+    ODB_PREFERENCE_HINGE = 1,    /* max(0, 1 - h)                                              */
+    ODB_PREFERENCE_SQUARE = 2    /* ((h - 1/2) / beta)^2                                       */
+} odb_preference_t;
+
+typedef struct odb_preference_params {
+    int32_t kind;                /* odb_preference_t                                           */
+    int32_t normalize;           /* 1: a row's log ratio is divided by its counted tokens      */
+    double  beta;                /* > 0                                                        */
+    double  margin;
+    double  label_smoothing;     /* e in [0, 1]; 0 unless kind is ODB_PREFERENCE_SIGMOID       */
+    double  loss_scale;          /* factor of every pair's loss                                */
+} odb_preference_params_t;
+
+/*
+ * Preference loss over pairs of rows, and its gradient.  A row's log ratio S is the sum over its
+ * counted tokens of logprob - ref_logprob (divided by their number with `normalize`; 0 for a row
+ * without any); a pair of a chosen row c and a rejected row r has
+ *   h = beta (S_c - S_r) - margin
+ * and the loss of its kind; the gradient is that of loss_scale * sum over pairs.
+ * The rows of a pair may lie in any tiles of the run: length-aware grouping parts them, so a
+ * trainer scores a whole run first, takes the gradient here and back-propagates tile by tile.
+ *
+ *   d_logprob         [num_elems], as odb_token_logprobs writes them
+ *   d_ref_logprob     [num_elems], or NULL: 0
+ *   d_row_ids         [num_rows] sample ids of the rows (the plan's d_emit_order), each in
+ *                     [0, num_ids), or NULL: then row i has id i and num_ids must be num_rows
+ *   num_ids           < 2^31
+ *   d_pair            [num_ids] by id a: 0 no pair; +(b + 1) a is chosen over id b; -(b + 1) a
+ *                     is rejected against id b.  b must name a with the other sign
+ *   d_loss            [1] out: loss_scale * sum over pairs
+ *   d_row_loss        [num_rows] out: loss_scale * loss of its pair at a chosen row, else 0
+ *   d_row_reward      [num_rows] out: beta * S
+ *   d_counts          [2] out: pairs, and of them those with S_c > S_r
+ *   d_grad_logprob    [num_elems] out, or NULL
+ *   d_status          [1] device, or NULL: set to a nonzero value if a slot's arrays contradict
+ *                     each other, an id lies outside [0, num_ids), or a row's id and the id it
+ *                     is paired with do not name each other (such a row has no pair); never
+ *                     cleared here
+ *   d_ws / ws_bytes   odb_loss_workspace_size(t, num_ids if d_row_ids else 0) bytes, 256-B
+ *                     aligned; calls in flight at once need workspaces of their own
+ *
+ * A pair counts if both ids have a row here.  If an id has several rows (sampler padding), the
+ * first of them is its row and the others have no pair.  Rows and elements behind the last slot
+ * are not written.  Sums run in 64 bits in a fixed order.  Asynchronous.
+ */
+int odb_preference_loss(const odb_tiles_t* t, const odb_preference_params_t* p, const float* d_logprob,
+                        const float* d_ref_logprob, const int32_t* d_row_ids, int64_t num_ids, const int32_t* d_pair,
+                        float* d_loss, float* d_row_loss, float* d_row_reward, int64_t* d_counts,
+                        float* d_grad_logprob, int32_t* d_status, void* d_ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -8,7 +8,7 @@ fails to load, every call raises.
 
 :class:`Pipeline` owns the device buffers of one window and runs the three stages
 (grouping, alignment, collation) in order on one stream, and on request the loss-scaling
-weights of the aligned plan.
+weights of the aligned plan, a policy loss and a preference loss over its tiles.
 """
 from __future__ import annotations
 
@@ -34,11 +34,18 @@ ODB_MODE_JOIN = 0
 ODB_MODE_NONJOIN_QUOTA = 1
 ODB_STOP_DRAINED, ODB_STOP_QUOTA, ODB_STOP_RANK_FINISHED = 0, 1, 2
 ODB_WEIGHT_SAMPLE, ODB_WEIGHT_TOKEN_APPROX, ODB_WEIGHT_TOKEN_EXACT = 0, 1, 2
+ODB_LABEL_IGNORE = -100
+ODB_FLOAT32, ODB_BFLOAT16, ODB_FLOAT16 = 0, 1, 2
+ODB_KL_NONE, ODB_KL_LINEAR, ODB_KL_SQUARE, ODB_KL_EXP = 0, 1, 2, 3
+ODB_REDUCE_TOKEN_MEAN, ODB_REDUCE_ROW_MEAN, ODB_REDUCE_SUM = 0, 1, 2
+ODB_PREFERENCE_SIGMOID, ODB_PREFERENCE_HINGE, ODB_PREFERENCE_SQUARE = 0, 1, 2
 
 EXPORTED = [
     "odb_status_string", "odb_last_error_message", "odb_workspace_size", "odb_form_groups",
     "odb_align_groups", "odb_collate", "odb_collate_status", "odb_check_coverage", "odb_loss_weights",
     "odb_length_sketch", "odb_stream_workspace_size", "odb_stream_plan", "odb_collate_static",
+    "odb_token_logprobs", "odb_token_logprobs_backward", "odb_loss_workspace_size", "odb_policy_loss",
+    "odb_preference_loss",
 ]
 ODB_COLLATE_STATIC_MAX_ROWS = 2097152
 
@@ -160,6 +167,69 @@ class StreamInfo(ctypes.Structure):
         return {f: getattr(self, f) for f, _ in self._fields_ if f != "reserved0"}
 
 
+class Logits(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("shift", ctypes.c_int32),
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("vocab", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64),
+        ("col_stride", ctypes.c_int64),
+        ("scale", ctypes.c_double),
+        ("d_logits", ctypes.c_void_p),
+    ]
+
+
+class TilesStruct(ctypes.Structure):
+    _fields_ = [
+        ("num_slots", ctypes.c_int64),
+        ("num_rows", ctypes.c_int64),
+        ("num_elems", ctypes.c_int64),
+        ("d_slot_rows", ctypes.c_void_p),
+        ("d_slot_maxlen", ctypes.c_void_p),
+        ("d_slot_row_off", ctypes.c_void_p),
+        ("d_slot_tile_off", ctypes.c_void_p),
+        ("d_labels", ctypes.c_void_p),
+        ("shift", ctypes.c_int32),
+        ("reserved0", ctypes.c_int32),
+    ]
+
+
+class PolicyParams(ctypes.Structure):
+    """Parameters of odb_policy_loss; keywords override the defaults below."""
+    _fields_ = [
+        ("kl", ctypes.c_int32),
+        ("reduce", ctypes.c_int32),
+        ("token_advantage", ctypes.c_int32),
+        ("reserved0", ctypes.c_int32),
+        ("clip_low", ctypes.c_double),
+        ("clip_high", ctypes.c_double),
+        ("dual_clip", ctypes.c_double),
+        ("kl_coef", ctypes.c_double),
+        ("entropy_coef", ctypes.c_double),
+        ("loss_scale", ctypes.c_double),
+    ]
+
+    def __init__(self, **kw):
+        super().__init__(**{**dict(clip_low=0.2, clip_high=0.2, loss_scale=1.0), **kw})
+
+
+class PreferenceParams(ctypes.Structure):
+    """Parameters of odb_preference_loss; keywords override the defaults below."""
+    _fields_ = [
+        ("kind", ctypes.c_int32),
+        ("normalize", ctypes.c_int32),
+        ("beta", ctypes.c_double),
+        ("margin", ctypes.c_double),
+        ("label_smoothing", ctypes.c_double),
+        ("loss_scale", ctypes.c_double),
+    ]
+
+    def __init__(self, **kw):
+        super().__init__(**{**dict(beta=0.1, loss_scale=1.0), **kw})
+
+
 _lib = None
 
 
@@ -201,6 +271,18 @@ def load():
         lib.odb_stream_plan.restype = ctypes.c_int
         lib.odb_stream_plan.argtypes = [W, P, I64, ctypes.POINTER(StreamParams), I64, P, P, P, P, P, P, P, P, P, P, P, P,
                                         P, ctypes.POINTER(StreamInfo), P, SZ, P]
+        T = ctypes.POINTER(TilesStruct)
+        lib.odb_token_logprobs.restype = ctypes.c_int
+        lib.odb_token_logprobs.argtypes = [ctypes.POINTER(Logits), P, P, P, P, P, P]
+        lib.odb_token_logprobs_backward.restype = ctypes.c_int
+        lib.odb_token_logprobs_backward.argtypes = [ctypes.POINTER(Logits), P, P, P, P, P, P, I64, I64, P, P]
+        lib.odb_loss_workspace_size.restype = SZ
+        lib.odb_loss_workspace_size.argtypes = [T, I64]
+        lib.odb_policy_loss.restype = ctypes.c_int
+        lib.odb_policy_loss.argtypes = [T, ctypes.POINTER(PolicyParams), P, P, P, P, P, P, P, P, P, P, P, P, P, SZ, P]
+        lib.odb_preference_loss.restype = ctypes.c_int
+        lib.odb_preference_loss.argtypes = [T, ctypes.POINTER(PreferenceParams), P, P, P, I64, P, P, P, P, P, P, P, P,
+                                            SZ, P]
         _lib = lib
     return _lib
 
@@ -350,7 +432,226 @@ def odb_length_sketch(win, ids, count, budget, ws, stream=None) -> dict:
     return d
 
 
-class Pipeline:
+def _array(t, dtype, least: int, name: str):
+    """Device pointer of an argument of the loss operators, its type, size and device checked
+    (None passes NULL)."""
+    if t is None:
+        return None
+    import torch
+    if t.dtype != getattr(torch, dtype):
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.numel() < least:
+        raise ValueError(f"{name}: {t.numel()} elements, {least} needed")
+    p = _dptr(t)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return p
+
+
+def _logits(x, shift, scale, name="logits"):
+    """Descriptor of a [rows, cols, vocab] tensor of logits; rows and columns may have any stride."""
+    import torch
+    types = {torch.float32: ODB_FLOAT32, torch.bfloat16: ODB_BFLOAT16, torch.float16: ODB_FLOAT16}
+    if x.dtype not in types:
+        raise ValueError(f"{name}: expected float32, bfloat16 or float16, got {x.dtype}")
+    if x.dim() != 3:
+        raise ValueError(f"{name}: expected [rows, cols, vocab], got {tuple(x.shape)}")
+    if x.stride(2) != 1 and x.size(2) > 1:
+        raise ValueError(f"{name}: the vocabulary must be contiguous")
+    if not x.is_cuda:
+        raise ValueError("expected a device tensor")
+    if x.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {x.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return Logits(types[x.dtype], int(shift), x.size(0), x.size(1), x.size(2), x.stride(0), x.stride(1), float(scale),
+                  x.data_ptr())
+
+
+def odb_token_logprobs(logits, labels, logprob, stats=None, entropy=None, status=None, shift=1, scale=1.0,
+                       stream=None):
+    """Log-probabilities of a tile's labels (int32, [rows, cols]) from its logits [rows, cols,
+    vocab]; ``stats`` (float32, [rows, cols, 2]) is what the backward call takes."""
+    x = _logits(logits, shift, scale)
+    n = x.rows * x.cols
+    _check(load().odb_token_logprobs(ctypes.byref(x), _array(labels, "int32", n, "labels"),
+                                     _array(logprob, "float32", n, "logprob"),
+                                     _array(stats, "float32", 2 * n, "stats"),
+                                     _array(entropy, "float32", n, "entropy"), _array(status, "int32", 1, "status"),
+                                     _stream(stream)))
+
+
+def odb_token_logprobs_backward(logits, labels, stats, grad_logprob, grad_logits, entropy=None, grad_entropy=None,
+                                status=None, shift=1, scale=1.0, stream=None):
+    """Gradient of :func:`odb_token_logprobs` with respect to the logits, written to
+    ``grad_logits`` (the logits' shape and type; may be the logits themselves)."""
+    x = _logits(logits, shift, scale)
+    g = _logits(grad_logits, shift, scale, "grad_logits")
+    if (g.dtype, g.rows, g.cols, g.vocab) != (x.dtype, x.rows, x.cols, x.vocab):
+        raise ValueError("grad_logits must have the shape and type of the logits")
+    n = x.rows * x.cols
+    _check(load().odb_token_logprobs_backward(ctypes.byref(x), _array(labels, "int32", n, "labels"),
+                                              _array(stats, "float32", 2 * n, "stats"),
+                                              _array(grad_logprob, "float32", n, "grad_logprob"),
+                                              _array(entropy, "float32", n, "entropy"),
+                                              _array(grad_entropy, "float32", n, "grad_entropy"), g.d_logits,
+                                              g.row_stride, g.col_stride, _array(status, "int32", 1, "status"),
+                                              _stream(stream)))
+
+
+class Tiles:
+    """A run of a plan's slots and their labels, with its C descriptor.
+
+    The slot arrays hold the run's slots (the offsets one entry more); ``labels`` and every array
+    parallel to the tiles start at the run's first element, arrays parallel to the rows at its
+    first row.  ``slots``, ``rows`` and ``elems`` are the run's ranges in the plan's arrays.
+    """
+
+    def __init__(self, slot_rows, slot_maxlen, slot_row_off, slot_tile_off, labels, num_rows: int, shift: int = 1,
+                 slots=None, rows=None, elems=None):
+        K = slot_rows.numel()
+        self.keep = (slot_rows, slot_maxlen, slot_row_off, slot_tile_off)
+        self.num_slots, self.num_rows, self.num_elems = K, int(num_rows), labels.numel()
+        self.slots = slice(0, K) if slots is None else slots
+        self.rows = slice(0, self.num_rows) if rows is None else rows
+        self.elems = slice(0, self.num_elems) if elems is None else elems
+        self.labels = labels
+        self.struct = TilesStruct(K, self.num_rows, self.num_elems, _array(slot_rows, "int32", K, "slot_rows"),
+                                  _array(slot_maxlen, "int32", K, "slot_maxlen"),
+                                  _array(slot_row_off, "int64", K + 1, "slot_row_off"),
+                                  _array(slot_tile_off, "int64", K + 1, "slot_tile_off"),
+                                  _array(labels, "int32", 0, "labels"), int(shift), 0)
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.struct)
+
+
+def odb_loss_workspace_size(tiles: Tiles, num_ids: int = 0) -> int:
+    v = load().odb_loss_workspace_size(tiles.ref, int(num_ids))
+    if v == 0:
+        _check(ODB_E_INVALID_ARG)
+    return int(v)
+
+
+def odb_policy_loss(tiles, params, logprob, advantage, slot_loss, slot_means, slot_counts, ws, old_logprob=None,
+                    ref_logprob=None, entropy=None, slot_weight=None, grad_logprob=None, grad_entropy=None,
+                    status=None, stream=None):
+    K, R, E = tiles.num_slots, tiles.num_rows, tiles.num_elems
+    f = lambda t, n, name: _array(t, "float32", n, name)
+    _check(load().odb_policy_loss(tiles.ref, ctypes.byref(params), f(logprob, E, "logprob"),
+                                  f(old_logprob, E, "old_logprob"), f(ref_logprob, E, "ref_logprob"),
+                                  f(entropy, E, "entropy"),
+                                  f(advantage, E if params.token_advantage else R, "advantage"),
+                                  _array(slot_weight, "float64", K, "slot_weight"), f(slot_loss, K, "slot_loss"),
+                                  f(slot_means, 4 * K, "slot_means"), _array(slot_counts, "int64", 4 * K, "slot_counts"),
+                                  f(grad_logprob, E, "grad_logprob"), f(grad_entropy, E, "grad_entropy"),
+                                  _array(status, "int32", 1, "status"), _dptr(ws), ws.numel() * ws.element_size(),
+                                  _stream(stream)))
+
+
+def odb_preference_loss(tiles, params, logprob, pair, loss, row_loss, row_reward, counts, ws, ref_logprob=None,
+                        row_ids=None, grad_logprob=None, status=None, stream=None):
+    R, E = tiles.num_rows, tiles.num_elems
+    f = lambda t, n, name: _array(t, "float32", n, name)
+    ids = R if row_ids is None or R == 0 else pair.numel()    # an empty tensor has no address
+    _check(load().odb_preference_loss(tiles.ref, ctypes.byref(params), f(logprob, E, "logprob"),
+                                      f(ref_logprob, E, "ref_logprob"), _array(row_ids, "int32", R, "row_ids"), ids,
+                                      _array(pair, "int32", ids, "pair"), f(loss, 1, "loss"),
+                                      f(row_loss, R, "row_loss"), f(row_reward, R, "row_reward"),
+                                      _array(counts, "int64", 2, "counts"), f(grad_logprob, E, "grad_logprob"),
+                                      _array(status, "int32", 1, "status"), _dptr(ws),
+                                      ws.numel() * ws.element_size(), _stream(stream)))
+
+
+class _PlanLosses:
+    """Losses over the tiles of a pipeline's plan.  Output buffers are kept and reused (views of
+    them are returned), so a call on another stream never writes freed memory; a policy and a
+    preference loss have buffers of their own.  Inputs are checked on the host; what the device
+    finds wrong with them is collected until :meth:`check_losses`."""
+
+    _loss_buffers = None
+
+    def tiles(self, labels=None, first: int = 0, count: Optional[int] = None, shift: int = 1) -> Tiles:
+        """The run of `count` slots from `first` on (default: all of the plan's).  ``labels`` is
+        parallel to the plan's tiles (default: the collate's).  A run that is not the whole plan
+        reads its four bounds from the device (one synchronisation)."""
+        K = self.num_slots
+        a, b = int(first), K if count is None else int(first) + int(count)
+        if not 0 <= a <= b <= K:
+            raise ValueError(f"slots [{a}, {b}) of a plan of {K}")
+        R = int(self.info["emitted_samples" if "emitted_samples" in self.info else "emitted_views"])
+        e, r = (0, int(self.info["padded_elems"])), (0, R)
+        if (a, b) != (0, K):
+            v = self.torch.stack([self.slot_tile_off[a], self.slot_tile_off[b], self.slot_row_off[a],
+                                  self.slot_row_off[b]]).tolist()
+            e, r = (v[0], v[1]), (v[2], v[3])
+        if labels is None:
+            if self.outputs is None:
+                raise ValueError("collate first, or pass labels")
+            labels = self.outputs[1]
+        return Tiles(self.slot_rows[a:b], self.slot_maxlen[a:b], self.slot_row_off[a:b + 1],
+                     self.slot_tile_off[a:b + 1], labels.reshape(-1)[e[0]:e[1]], r[1] - r[0], shift, slice(a, b),
+                     slice(*r), slice(*e))
+
+    def _loss_outputs(self, kind: str, sizes: dict):
+        """Kept buffers of at least the given sizes: {name: (elements, type)}."""
+        torch = self.torch
+        if self._loss_buffers is None:
+            self._loss_buffers = {"status": torch.zeros(1, dtype=torch.int32, device=self.device)}
+            _sync_current(self.device)
+        grown = False
+        for name, (n, dtype) in sizes.items():
+            t = self._loss_buffers.get((kind, name))
+            if t is None or t.numel() < n:
+                self._loss_buffers[kind, name] = torch.empty(max(n, 1), dtype=getattr(torch, dtype), device=self.device)
+                grown = True
+        if grown:
+            # buffers may be used on another stream than the one they were allocated on
+            _sync_current(self.device)
+        return [self._loss_buffers[kind, name][:n] for name, (n, _) in sizes.items()], self._loss_buffers["status"]
+
+    def policy_loss(self, tiles: Tiles, logprob, advantage, params: Optional[PolicyParams] = None, old_logprob=None,
+                    ref_logprob=None, entropy=None, slot_weight=None, stream=None):
+        """odb_policy_loss of a run's tiles, usually weighted by
+        ``loss_weights(mode)[0][tiles.slots]`` with ``params.loss_scale`` the number of ranks.
+        Returns (loss per slot, means [K, 4], counts [K, 4], gradient of the log-probabilities,
+        gradient of the entropies or None)."""
+        K, E = tiles.num_slots, tiles.num_elems
+        (ws, loss, means, counts, grad, gent), status = self._loss_outputs("policy", {
+            "ws": (odb_loss_workspace_size(tiles), "uint8"), "loss": (K, "float32"), "means": (4 * K, "float32"),
+            "counts": (4 * K, "int64"), "grad": (E, "float32"), "gent": (0 if entropy is None else E, "float32")})
+        gent = None if entropy is None else gent
+        odb_policy_loss(tiles, PolicyParams() if params is None else params, logprob, advantage, loss, means, counts,
+                        ws, old_logprob, ref_logprob, entropy, slot_weight, grad, gent, status, stream)
+        return loss, means.view(K, 4), counts.view(K, 4), grad, gent
+
+    def preference_loss(self, tiles: Tiles, logprob, pair, params: Optional[PreferenceParams] = None,
+                        ref_logprob=None, stream=None):
+        """odb_preference_loss of a run's tiles; ``pair`` is by sample id (the plan's emitted
+        ids).  Returns (loss, loss per row, reward per row, counts [2], gradient of the
+        log-probabilities)."""
+        R, E = tiles.num_rows, tiles.num_elems
+        (ws, loss, row_loss, reward, counts, grad), status = self._loss_outputs("preference", {
+            "ws": (odb_loss_workspace_size(tiles, pair.numel()), "uint8"), "loss": (1, "float32"),
+            "row_loss": (R, "float32"), "reward": (R, "float32"), "counts": (2, "int64"), "grad": (E, "float32")})
+        odb_preference_loss(tiles, PreferenceParams() if params is None else params, logprob, pair, loss, row_loss,
+                            reward, counts, ws, ref_logprob, self.emit_order[tiles.rows], grad, status, stream)
+        return loss, row_loss, reward, counts, grad
+
+    def check_losses(self, stream=None):
+        """Synchronises `stream` and raises if a loss since the last check met bad tiles or pairs."""
+        if self._loss_buffers is None:
+            return
+        st = self._loss_buffers["status"]
+        with self.torch.cuda.stream(stream if stream is not None else self.torch.cuda.current_stream()):
+            bad = int(st.item())
+            if bad:
+                st.zero_()
+                _sync_current(self.device)
+        if bad:
+            raise OdbError(ODB_E_INVALID_DATA, f"a loss met inconsistent tiles or pairs (device flags {bad})")
+
+
+class Pipeline(_PlanLosses):
     """Device buffers of one window and the three-stage call sequence.
 
     Slot arrays start at ``W * max_r n_r`` capacity unless ``slot_capacity`` is given;
@@ -475,7 +776,7 @@ def stream_round_bound(num_samples: int, num_ranks: int, buffer_size: int, rate)
     return q + (q + 1) * fill + 2
 
 
-class StreamPipeline:
+class StreamPipeline(_PlanLosses):
     """Device buffers of one streaming iteration (odb_stream_plan) and its collate and
     loss weights (odb_collate / odb_loss_weights on the streaming plan)."""
 

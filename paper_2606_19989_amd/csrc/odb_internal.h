@@ -53,7 +53,10 @@ enum : int32_t {
     kErrIdentity = 16,   // identity outside [0, num_identities)
     kErrCollate = 32,    // collate met an inconsistent plan
     kErrInternal = 64,
-    kErrSortedLen = 128  // a stage-1 sorted length differs from the sample's CSR length
+    kErrSortedLen = 128, // a stage-1 sorted length differs from the sample's CSR length
+    kErrLabel = 256,     // a label outside the vocabulary
+    kErrTiles = 512,     // a slot's arrays contradict each other or leave the arrays' lengths
+    kErrPair = 1024      // a row id out of range, or two ids that do not name each other
 };
 
 struct DevStatus {

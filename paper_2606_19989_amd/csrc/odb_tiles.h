@@ -1,0 +1,76 @@
+// Which slots a chunk of a run's elements touches, apart from the kernels so that it can be
+// checked on the host with slot arrays that contradict each other.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "odb.h"
+
+namespace odb {
+
+// Slot k of a run: its elements [lo, hi) and its first row, counted from the run's first.
+struct SlotView {
+    int64_t lo, hi;
+    int64_t row0;
+    int32_t rows, maxlen;
+    bool ok;    // the arrays agree and stay inside the run's lengths
+};
+
+// Differences of offsets that may hold anything.
+__host__ __device__ __forceinline__ int64_t offset_from(int64_t a, int64_t base) {
+    return (int64_t)((uint64_t)a - (uint64_t)base);
+}
+
+__host__ __device__ __forceinline__ SlotView slot_view(const odb_tiles_t& t, int64_t k, int64_t e_base,
+                                                       int64_t r_base) {
+    SlotView s;
+    s.lo = offset_from(t.d_slot_tile_off[k], e_base);
+    s.hi = offset_from(t.d_slot_tile_off[k + 1], e_base);
+    s.row0 = offset_from(t.d_slot_row_off[k], r_base);
+    const int64_t row1 = offset_from(t.d_slot_row_off[k + 1], r_base);
+    s.rows = t.d_slot_rows[k];
+    s.maxlen = t.d_slot_maxlen[k];
+    s.ok = s.rows >= 0 && s.maxlen >= 0 && (s.rows == 0) == (s.maxlen == 0) && 0 <= s.lo && s.lo <= s.hi &&
+           s.hi <= t.num_elems && 0 <= s.row0 && s.row0 <= row1 && row1 <= t.num_rows && row1 - s.row0 == s.rows &&
+           s.hi - s.lo == (int64_t)s.rows * s.maxlen;
+    return s;
+}
+
+// Last slot that starts at or before element e (0 if there is none), whatever the offsets hold.
+__host__ __device__ __forceinline__ int64_t slot_of(const odb_tiles_t& t, int64_t e_base, int64_t e) {
+    int64_t lo = 0, hi = t.num_slots;
+    while (hi - lo > 1) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (offset_from(t.d_slot_tile_off[mid], e_base) <= e) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// Elements of the run, never more than its arrays hold.
+__host__ __device__ __forceinline__ int64_t run_elems(const odb_tiles_t& t, int64_t e_base) {
+    const int64_t n = offset_from(t.d_slot_tile_off[t.num_slots], e_base);
+    return n < 0 ? 0 : n < t.num_elems ? n : t.num_elems;
+}
+
+// Rows of the run, never more than its arrays hold.
+__host__ __device__ __forceinline__ int64_t run_rows(const odb_tiles_t& t, int64_t r_base) {
+    const int64_t n = offset_from(t.d_slot_row_off[t.num_slots], r_base);
+    return n < 0 ? 0 : n < t.num_rows ? n : t.num_rows;
+}
+
+// Calls f(k, slot, a0, a1) for every sound slot k with elements [a0, a1) in [c0, c1), in order.
+template <typename F>
+__host__ __device__ __forceinline__ void chunk_slots(const odb_tiles_t& t, int64_t e_base, int64_t r_base, int64_t c0,
+                                                     int64_t c1, const F& f) {
+    if (c0 >= c1) return;
+    for (int64_t k = slot_of(t, e_base, c0); k < t.num_slots; ++k) {
+        const SlotView s = slot_view(t, k, e_base, r_base);
+        if (s.lo >= c1) break;
+        if (!s.ok || s.hi <= c0 || s.hi == s.lo) continue;
+        f(k, s, s.lo > c0 ? s.lo : c0, s.hi < c1 ? s.hi : c1);
+    }
+}
+
+}  // namespace odb
