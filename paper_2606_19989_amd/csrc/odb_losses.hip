@@ -4,11 +4,11 @@
 // The run's elements are cut into chunks of equal length wherever slots and rows end, so any mix
 // of tiles keeps every compute unit busy.  What a chunk adds to a slot (or a row) is a partial of
 // its own: going through the chunks b in order, the slot k never falls, so b + k names each pair
-// that occurs once and a slot's partials are neighbours.  They are summed in that order, in 64
-// bits, by whoever needs the sum: no atomics, the same result from call to call.
+// that occurs once and a slot's partials are neighbours.  They are summed in a fixed order, in 64
+// bits, by whoever needs the sum: no atomics on sums, the same result from call to call.
 //
-// The first pass reads the labels and leaves one bit per element (does it count?), which is all
-// that the later passes read of them: 4 bytes an element become 1/8.
+// A mean's weight is known only after the labels have been read.  That pass leaves one bit per
+// element (does it count?), which is all that the later ones read of them: 4 bytes become 1/8.
 #include <cmath>
 
 #include "odb_internal.h"
@@ -18,8 +18,8 @@ namespace odb {
 
 namespace {
 
-constexpr int kChunk = 4096;                   // elements of a chunk
-constexpr int kChunkWords = kChunk / 32;
+constexpr int kMaxChunk = 16384;               // elements of a chunk, at most
+constexpr int kWaves = kBlock / kWave;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLog2eLow = 1.92596299112661746887e-8f;   // log2 e - kLog2e
 constexpr float kLn2 = 0.69314718055994530942f;
@@ -31,7 +31,7 @@ typedef int int4u __attribute__((ext_vector_type(4), aligned(4)));
 struct SlotPart {
     double sum[4];      // policy, KL, entropy, ratio
     int32_t clipped[3];
-    int32_t pad;
+    int32_t counted;
 };
 
 struct RowInfo {
@@ -45,12 +45,21 @@ struct PairPart {
 };
 
 struct LossLayout {
-    size_t bits, slot_count, slot_part, row_sum, row_count, row_info, row_scale, pair_part, row_of;
+    size_t bits, slot_count, slot_part, row_sum, row_count, row_info, coef, pair_part, row_of;
     size_t total;
     int64_t chunks;
+    int32_t chunk;
 };
 
 constexpr int64_t kMaxElems = (int64_t)1 << 40;
+
+// Elements of a chunk.  A chunk's fixed cost is a search for its first slot and a reduction; more
+// chunks than the chip holds at once (2,048 blocks of 256 threads) only add to it.
+int32_t chunk_for(int64_t elems) {
+    if (elems >= (int64_t)1 << 25) return kMaxChunk;
+    if (elems >= (int64_t)1 << 23) return 4096;
+    return 1024;
+}
 
 int check_tiles(const odb_tiles_t* t) {
     if (!t) return set_error(ODB_E_INVALID_ARG, "tiles is NULL");
@@ -72,15 +81,16 @@ LossLayout loss_layout(const odb_tiles_t* t, int64_t num_ids) {
         o = (o + (size_t)(bytes > 0 ? bytes : 1) + 255) & ~size_t(255);
         return at;
     };
-    L.chunks = (t->num_elems + kChunk - 1) / kChunk;
+    L.chunk = chunk_for(t->num_elems);
+    L.chunks = (t->num_elems + L.chunk - 1) / L.chunk;
     const int64_t K = t->num_slots, R = t->num_rows;
-    L.bits = take(L.chunks * kChunkWords * 4);
+    L.bits = take(L.chunks * (L.chunk / 8));
     L.slot_count = take(4 * (L.chunks + K));
     L.slot_part = take((int64_t)sizeof(SlotPart) * (L.chunks + K));
     L.row_sum = take(8 * (L.chunks + R));
     L.row_count = take(4 * (L.chunks + R));
     L.row_info = take((int64_t)sizeof(RowInfo) * R);
-    L.row_scale = take(8 * R);
+    L.coef = take(8 * R);
     L.pair_part = take((int64_t)sizeof(PairPart) * (R / kBlock + 1));
     L.row_of = take(4 * num_ids);
     L.total = o;
@@ -96,167 +106,161 @@ int check_loss_workspace(const LossLayout& L, const void* d_ws, size_t ws_bytes)
     return ODB_OK;
 }
 
-// ------------------------------------------------------------------ first pass: rows and the mask
-// Per chunk and row: how many of its tokens count, and (SUM) the sum of logprob - ref over them.
-// Per chunk and slot: how many count.  A row is taken by the smallest power of two of lanes that
-// covers it four elements each, up to a wave; rows of more than 1,024 elements by the block.
-struct RowsArgs {
-    odb_tiles_t t;
-    const float* logprob;
-    const float* ref;
-    uint32_t* bits;
-    int32_t* slot_count;
-    double* row_sum;
-    int32_t* row_count;
-    RowInfo* row_info;
-    const int32_t* row_ids;
-    int32_t* row_of;
-    int64_t num_ids;
-    int64_t chunks;
-    int32_t* status;
-    bool rows;          // leave row partials
+// ------------------------------------------------------------------ shared by the passes
+// First slot of a chunk, 64 probes a step (one a lane; every lane of the wave must be active): two
+// loads one after the other for up to 4,096 slots, where halving the range takes twelve.
+__device__ __forceinline__ int64_t first_slot(const odb_tiles_t& t, int64_t e_base, int64_t c0) {
+    const int lane = threadIdx.x & (kWave - 1);
+    return search_slot(t.num_slots, [&](int64_t lo, int64_t step, int64_t hi) {
+        const int64_t at = lo + lane * step;
+        const uint64_t before = __ballot(at < hi && offset_from(t.d_slot_tile_off[at < hi ? at : lo], e_base) <= c0);
+        return before == ~0ull ? kProbes : __builtin_ctzll(~before);
+    });
+}
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_plus(double v) {
+    const long long u = __double_as_longlong(v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)u, CTRL, ROWS, 0xf, true);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, ROWS, 0xf, true);
+    return v + __longlong_as_double((long long)(((unsigned long long)hi << 32) | lo));
+}
+
+// Sum over the 64 lanes in a fixed order, on every lane; all lanes must be active.
+__device__ __forceinline__ double wave_total(double v) {
+    v = dpp_plus<0x111, 0xf>(v);
+    v = dpp_plus<0x112, 0xf>(v);
+    v = dpp_plus<0x114, 0xf>(v);
+    v = dpp_plus<0x118, 0xf>(v);
+    v = dpp_plus<0x142, 0xa>(v);
+    v = dpp_plus<0x143, 0xc>(v);
+    const long long u = __double_as_longlong(v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)u, kWave - 1);
+    const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(u >> 32), kWave - 1);
+    return __longlong_as_double((long long)(((unsigned long long)hi << 32) | lo));
+}
+
+__device__ __forceinline__ int wave_total(int v) { return wave_last(wave_scan_dpp<OpAdd>(v)); }
+
+template <typename T>
+__device__ __forceinline__ T block_total(T v) {
+    __shared__ T s_part[kWaves];
+    v = wave_total(v);
+    __syncthreads();
+    if ((threadIdx.x & (kWave - 1)) == 0) s_part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    T sum = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) sum += s_part[i];
+    return sum;
+}
+
+// Four values from position o on of an array that ends at `limit`; what lies behind is `fill`.
+template <typename V4, typename T>
+__device__ __forceinline__ V4 load4(const T* p, int o, int limit, T fill) {
+    if (o + 4 <= limit) return *reinterpret_cast<const V4*>(p + o);
+    V4 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = o + j < limit ? p[o + j] : fill;
+    return v;
+}
+
+__device__ __forceinline__ int4u load_labels(const int32_t* labels, int o, int limit) {
+    return load4<int4u>(labels, o, limit, (int32_t)ODB_LABEL_IGNORE);
+}
+
+__device__ __forceinline__ float4u load_floats(const float* p, int o, int limit) {
+    return load4<float4u>(p, o, limit, 0.0f);
+}
+
+// A thread's group of four elements of a chunk, from position o (a multiple of 4) on: which of them
+// lie in the slot, and row and column of the first.  The column is negative where the slot starts
+// inside the group.
+struct Group {
+    int o;
+    uint32_t mask;
+    int row, col;
+
+    // Walks one element on.
+    __device__ __forceinline__ void next(int maxlen) {
+        if (++col == maxlen) {
+            col = 0;
+            ++row;
+        }
+    }
 };
 
-constexpr int kLongRow = 1024;
+// A slot's elements [a0, a1) of the chunk that starts at c0, as positions [o0, o1) in it; threads
+// take groups kBlock apart.  Rows count from the slot's first.
+struct Span {
+    int o0, o1, maxlen;
+    int row_a, col_a;           // of element a0
+    int rows_by, cols_by;       // what a thread's next group is ahead
 
-__device__ __forceinline__ void mark(uint32_t* s_bits, int at, uint32_t nibble) {
-    if (!nibble) return;
-    const uint64_t w = (uint64_t)nibble << (at & 31);
-    atomicOr(&s_bits[at >> 5], (uint32_t)w);
-    if (w >> 32) atomicOr(&s_bits[(at >> 5) + 1], (uint32_t)(w >> 32));
-}
+    __device__ __forceinline__ Span(const SlotView& s, int64_t a0, int64_t a1, int64_t c0)
+        : o0((int)(a0 - c0)), o1((int)(a1 - c0)), maxlen(s.maxlen), row_a((int)((a0 - s.lo) / s.maxlen)),
+          col_a((int)((a0 - s.lo) - (int64_t)row_a * s.maxlen)), rows_by(4 * kBlock / s.maxlen),
+          cols_by(4 * kBlock - rows_by * s.maxlen) {}
 
-// Elements [a, b) of the run, four a lane of the `lanes` that share a row: count and sum.
-template <bool SUM>
-__device__ __forceinline__ void row_run(const RowsArgs& A, int64_t a, int64_t b, int64_t first_counted, int lane,
-                                        int lanes, int64_t c0, uint32_t* s_bits, int* count, double* sum) {
-    for (int64_t e = a + 4 * lane; e < b; e += 4 * lanes) {
-        uint32_t nibble = 0;
-        if (e + 4 <= b) {
-            const int4u y = *reinterpret_cast<const int4u*>(A.t.d_labels + e);
-            float4u p = {0, 0, 0, 0}, r = {0, 0, 0, 0};
-            if (SUM) {
-                p = *reinterpret_cast<const float4u*>(A.logprob + e);
-                if (A.ref) r = *reinterpret_cast<const float4u*>(A.ref + e);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bool on = y[j] != ODB_LABEL_IGNORE && e + j >= first_counted;
-                nibble |= (uint32_t)on << j;
-                if (SUM && on) *sum += (double)p[j] - (double)r[j];
-            }
+    __device__ __forceinline__ uint32_t mask_at(int o) const {
+        return (o0 > o ? 0xfu << (o0 - o) : 0xfu) & (o1 - o >= 4 ? 0xfu : 0xfu >> (4 - (o1 - o)));
+    }
+
+    // The thread's first group; its o may lie behind the span.
+    __device__ __forceinline__ Group first() const {
+        Group q;
+        q.o = (o0 & ~3) + 4 * (int)threadIdx.x;
+        const int x = q.o - o0;      // negative only in the group in which the slot starts, where col_a is 0
+        q.row = row_a;
+        q.col = x;
+        if (x >= 0) {
+            const uint32_t c = (uint32_t)col_a + (uint32_t)x, r = c / (uint32_t)maxlen;
+            q.row += (int)r;
+            q.col = (int)(c - r * (uint32_t)maxlen);
+        }
+        q.mask = mask_at(q.o);
+        return q;
+    }
+
+    __device__ __forceinline__ void advance(Group* q) const {
+        q->o += 4 * kBlock;
+        q->row += rows_by;
+        if (q->col >= maxlen - cols_by) {    // no sum of two columns: they may pass 2^31
+            q->col -= maxlen - cols_by;
+            ++q->row;
         } else {
-            for (int j = 0; j < 4 && e + j < b; ++j) {
-                const bool on = A.t.d_labels[e + j] != ODB_LABEL_IGNORE && e + j >= first_counted;
-                nibble |= (uint32_t)on << j;
-                if (SUM && on) *sum += (double)A.logprob[e + j] - (A.ref ? (double)A.ref[e + j] : 0.0);
-            }
+            q->col += cols_by;
         }
-        *count += __builtin_popcount(nibble);
-        mark(s_bits, (int)(e - c0), nibble);
+        q->mask = mask_at(q->o);
     }
-}
+};
 
-template <bool SUM>
-__global__ void __launch_bounds__(kBlock) loss_rows_kernel(RowsArgs A) {
-    __shared__ uint32_t s_bits[kChunkWords];
-    const odb_tiles_t& t = A.t;
-    const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
-    const int64_t total = run_elems(t, e_base);
-    for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
-        const int64_t c0 = b * kChunk, c1 = c0 + kChunk < total ? c0 + kChunk : total;
-        for (int i = threadIdx.x; i < kChunkWords; i += kBlock) s_bits[i] = 0;
-        __syncthreads();
-        chunk_slots(t, e_base, r_base, c0, c1, [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
-            const int64_t row_a = (a0 - s.lo) / s.maxlen, row_b = (a1 - 1 - s.lo) / s.maxlen;
-            int slot_count = 0;
-            const bool wide = s.maxlen > kLongRow;
-            int lanes = 1;
-            while (lanes < kWave && 4 * lanes < s.maxlen) lanes *= 2;
-            if (wide) lanes = kBlock;
-            const int lane = threadIdx.x & (lanes - 1);
-            const int step = kBlock / lanes;
-            // every group goes round as often as the first, so that no lane leaves a shuffle alone
-            for (int64_t r0 = row_a; r0 <= row_b; r0 += step) {
-                const int64_t r = r0 + threadIdx.x / lanes;
-                const bool live = r <= row_b;
-                const int64_t start = s.lo + r * s.maxlen;
-                int count = 0;
-                double sum = 0.0;
-                if (live) {
-                    const int64_t x0 = start > a0 ? start : a0, x1 = start + s.maxlen < a1 ? start + s.maxlen : a1;
-                    row_run<SUM>(A, x0, x1, start + t.shift, lane, lanes, c0, s_bits, &count, &sum);
-                }
-                for (int d = (wide ? kWave : lanes) / 2; d > 0; d >>= 1) {
-                    count += __shfl_xor(count, d, kWave);
-                    if (SUM) sum += __shfl_xor(sum, d, kWave);
-                }
-                if (wide) {
-                    __shared__ int w_count[kBlock / kWave];
-                    __shared__ double w_sum[kBlock / kWave];
-                    const int w = threadIdx.x / kWave;
-                    if ((threadIdx.x & (kWave - 1)) == 0) {
-                        w_count[w] = count;
-                        w_sum[w] = sum;
-                    }
-                    __syncthreads();
-                    count = 0;
-                    sum = 0.0;
+// Which of a group's elements count.
+__device__ __forceinline__ uint32_t count_mask(Group q, const int4u& y, int maxlen, int shift) {
+    uint32_t on = 0;
 #pragma unroll
-                    for (int j = 0; j < kBlock / kWave; ++j) {
-                        count += w_count[j];
-                        sum += w_sum[j];
-                    }
-                    __syncthreads();
-                }
-                if (live && lane == 0) {
-                    const int64_t row = s.row0 + r;
-                    slot_count += count;
-                    if (A.rows) {
-                        A.row_count[b + row] = count;
-                        if (SUM) A.row_sum[b + row] = sum;
-                        if (start >= c0) {   // the row starts here
-                            const int64_t last = (start + s.maxlen - 1) / kChunk;
-                            A.row_info[row] = RowInfo{(int32_t)b, (int32_t)(last - b + 1)};
-                            if (A.row_of) {
-                                const int32_t id = A.row_ids[row];
-                                if (id >= 0 && id < A.num_ids) atomicMin(&A.row_of[id], (int32_t)row);
-                            }
-                        }
-                    }
-                }
-            }
-            slot_count = block_sum(slot_count);
-            if (threadIdx.x == 0) A.slot_count[b + k] = slot_count;
-        });
-        __syncthreads();
-        for (int i = threadIdx.x; i < kChunkWords; i += kBlock) A.bits[b * kChunkWords + i] = s_bits[i];
-        __syncthreads();
+    for (int j = 0; j < 4; ++j) {
+        on |= (uint32_t)(y[j] != ODB_LABEL_IGNORE && q.col >= shift) << j;
+        q.next(maxlen);
     }
-    if (A.status)
-        for (int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x; k < t.num_slots; k += (int64_t)gridDim.x * kBlock)
-            if (!slot_view(t, k, e_base, r_base).ok) *A.status = kErrTiles;
+    return on & q.mask;
 }
 
-__global__ void __launch_bounds__(kBlock) fill_rows_kernel(int32_t* row_of, int64_t n) {
-    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock)
-        row_of[i] = INT32_MAX;
+__device__ __forceinline__ void store4(float* p, const Group& q, const float v[4]) {
+    if (q.mask == 0xf) {
+        const float4u x = {v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<float4u*>(p + q.o) = x;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (q.mask >> j & 1) p[q.o + j] = v[j];
+    }
 }
 
-// Sum of a row's partials; nothing is read outside them whatever the row's record holds.
-__device__ __forceinline__ int row_total(const int32_t* row_count, const double* row_sum, const RowInfo* info,
-                                         int64_t chunks, int64_t row, double* sum) {
-    const RowInfo f = info[row];
-    int count = 0;
-    double s = 0.0;
-    if (f.first >= 0 && f.chunks > 0 && (int64_t)f.first + f.chunks <= chunks) {
-        for (int64_t b = f.first; b < (int64_t)f.first + f.chunks; ++b) {
-            count += row_count[b + row];
-            if (sum) s += row_sum[b + row];
-        }
-    }
-    if (sum) *sum = s;
-    return count;
+// Elements from c0 to the arrays' end, as far as a chunk's positions go.
+__device__ __forceinline__ int chunk_limit(const odb_tiles_t& t, int64_t c0) {
+    const int64_t n = t.num_elems - c0;
+    return (int)(n < 2 * kMaxChunk ? n : 2 * kMaxChunk);
 }
 
 // ------------------------------------------------------------------ policy loss
@@ -273,35 +277,102 @@ struct PolicyArgs {
     int64_t* slot_counts;
     float* grad;
     float* grad_entropy;
-    const uint32_t* bits;
-    const int32_t* slot_count;
+    uint32_t* bits;
+    int32_t* slot_count;        // counted tokens (token mean) or complete rows with any (row mean)
     SlotPart* slot_part;
-    const int32_t* row_count;
-    const RowInfo* row_info;
-    double* row_scale;
+    int32_t* row_count;
+    int32_t* status;
     int64_t chunks;
     double at_low, at_high, at_dual;    // ln(1 - e_l), ln(1 + e_h), ln c
     double kl_coef, entropy_coef, loss_scale;
     float low, high, dual;              // 1 - e_l, 1 + e_h, c
-    int32_t kl, reduce;
+    int32_t kl, reduce, chunk;
     bool token_advantage;
 };
 
-// Weight of a row's token under the mean of row means: 1 / (the row's tokens * the slot's rows).
-__global__ void __launch_bounds__(kBlock) row_scale_kernel(PolicyArgs A) {
+// Rows of a slot that one block weighs in LDS.
+constexpr int kLdsRows = 4096;
+
+// Adds a group's counted elements to its rows, the first of them `row0`.
+__device__ __forceinline__ void add_to_rows(int* s_rows, Group q, uint32_t on, int maxlen, int row0) {
+    if (q.col <= maxlen - 4) {
+        if (on) atomicAdd(&s_rows[q.row - row0], __builtin_popcount(on));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (on >> j & 1) atomicAdd(&s_rows[q.row - row0], 1);
+        q.next(maxlen);
+    }
+}
+
+// First pass of a mean: the bits, and per chunk and slot the counted tokens, or (ROWS) per chunk and
+// row the counted tokens and per chunk and slot the rows with any that lie wholly in the chunk.
+template <bool ROWS>
+__global__ void __launch_bounds__(kBlock) policy_count_kernel(PolicyArgs A) {
+    __shared__ uint8_t s_nibble[kMaxChunk / 4];
+    __shared__ int s_rows[ROWS ? kLdsRows : 1];
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
-    for (int64_t k = blockIdx.x; k < t.num_slots; k += gridDim.x) {
-        const SlotView s = slot_view(t, k, e_base, r_base);
-        if (!s.ok || s.rows == 0) continue;   // uniform
-        int rows = 0;
-        for (int i = threadIdx.x; i < s.rows; i += kBlock)
-            rows += row_total(A.row_count, nullptr, A.row_info, A.chunks, s.row0 + i, nullptr) > 0;
-        rows = block_sum(rows);
-        for (int i = threadIdx.x; i < s.rows; i += kBlock) {
-            const int n = row_total(A.row_count, nullptr, A.row_info, A.chunks, s.row0 + i, nullptr);
-            A.row_scale[s.row0 + i] = n > 0 ? 1.0 / ((double)n * rows) : 0.0;
+    const int64_t total = run_elems(t, e_base);
+    for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
+        const int64_t c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
+        if (c0 >= c1) break;
+        const int32_t* labels = t.d_labels + c0;
+        const int limit = chunk_limit(t, c0);
+        for (int i = threadIdx.x; i < A.chunk / 16; i += kBlock) reinterpret_cast<uint32_t*>(s_nibble)[i] = 0;
+        __syncthreads();
+        chunk_slots(t, e_base, r_base, first_slot(t, e_base, c0), c0, c1,
+                    [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+            const Span p(s, a0, a1, c0);
+            const int rows = (int)((a1 - 1 - s.lo) / s.maxlen) - p.row_a + 1;
+            const bool lds = ROWS && rows <= kLdsRows;
+            if (lds) {
+                for (int i = threadIdx.x; i < rows; i += kBlock) s_rows[i] = 0;
+                __syncthreads();
+            }
+            int count = 0;
+            Group q = p.first();
+#pragma unroll 4
+            for (; q.o < p.o1; p.advance(&q)) {
+                const uint32_t on = count_mask(q, load_labels(labels, q.o, limit), p.maxlen, t.shift);
+                if (on) s_nibble[q.o / 4] |= (uint8_t)on;
+                if (lds)
+                    add_to_rows(s_rows, q, on, p.maxlen, p.row_a);
+                else
+                    count += __builtin_popcount(on);
+            }
+            if (ROWS) {
+                // a row counts here if it starts and ends here; the others are joined by who needs the slot's rows
+                __syncthreads();
+                count = 0;
+                for (int i = threadIdx.x; i < rows; i += kBlock) {
+                    const int64_t start = s.lo + (int64_t)(p.row_a + i) * s.maxlen;
+                    int n = 0;
+                    if (lds) {
+                        n = s_rows[i];
+                    } else {     // rows of a few elements
+                        for (int64_t e = start > a0 ? start : a0; e < start + s.maxlen && e < a1; ++e)
+                            n += s_nibble[(e - c0) / 4] >> ((e - c0) & 3) & 1;
+                    }
+                    A.row_count[b + s.row0 + p.row_a + i] = n;
+                    count += n > 0 && start >= c0 && start + s.maxlen <= c0 + A.chunk;
+                }
+            }
+            count = block_total(count);
+            if (threadIdx.x == 0) A.slot_count[b + k] = count;
+            __syncthreads();
+        });
+        for (int i = threadIdx.x; i < A.chunk / 32; i += kBlock) {
+            const uint2 w = reinterpret_cast<const uint2*>(s_nibble)[i];
+            // eight bytes of four bits to one word
+            uint32_t v = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                v |= (w.x >> (8 * j) & 0xf) << (4 * j) | (w.y >> (8 * j) & 0xf) << (16 + 4 * j);
+            A.bits[b * (A.chunk / 32) + i] = v;
         }
+        __syncthreads();
     }
 }
 
@@ -338,28 +409,36 @@ struct TokenTerms {
     int clip;    // 0 none, 1 below, 2 above, 3 by the dual bound
 };
 
-__device__ __forceinline__ TokenTerms policy_token(const PolicyArgs& A, float lp, float old, float ref, float adv) {
+// The bounds on lp - old, rounded to fp32.
+struct Bounds {
+    float low, high, dual;
+};
+
+__device__ __forceinline__ TokenTerms policy_token(const PolicyArgs& A, const Bounds& B, float lp, float old, float ref,
+                                                   float adv) {
     TokenTerms o;
-    // the comparisons are made on the difference itself; its fp32 rounding is enough for the rest
-    const double d = A.old ? (double)lp - (double)old : 0.0;
-    o.ratio = A.old ? exp_near(lp - old) : 1.0f;
+    o.ratio = 1.0f;
     o.clip = 0;
-    float bound = o.ratio;
-    if (adv > 0.0f) {
-        if (d > A.at_high) {
-            o.clip = 2;
-            bound = A.high;
+    float bound = 1.0f;
+    if (A.old) {
+        const float d = lp - old;
+        bound = o.ratio = exp_near(d);
+        // rounding keeps order: the rounded difference decides unless it equals a rounded bound
+        const float up = adv > 0.0f ? B.high : B.dual;
+        bool above = d > up, below = d < B.low;
+        if (__builtin_expect(d == up || d == B.low, 0)) {
+            const double x = (double)lp - (double)old;
+            above = x > (adv > 0.0f ? A.at_high : A.at_dual);
+            below = x < A.at_low;
         }
-    } else if (adv < 0.0f) {
-        if (d < A.at_low) {
-            o.clip = 1;
-            bound = A.low;
-        } else if (d > A.at_dual) {
-            o.clip = 3;
-            bound = A.dual;
-        }
+        below = below && adv < 0.0f;
+        o.clip = below ? 1 : above ? (adv > 0.0f ? 2 : 3) : 0;
+        bound = below ? A.low : above ? (adv > 0.0f ? A.high : A.dual) : bound;
     }
-    o.policy = adv == 0.0f ? 0.0f : -bound * adv;
+    // no ratio clips an advantage of 0 (nor a NaN), and an overflowing one must not make it NaN
+    const bool none = adv == 0.0f;
+    o.clip = none || adv != adv ? 0 : o.clip;
+    o.policy = none ? 0.0f : -bound * adv;
     o.grad = o.clip ? 0.0f : o.policy;
     o.kl = o.kl_grad = 0.0f;
     if (A.kl != ODB_KL_NONE) {
@@ -378,99 +457,263 @@ __device__ __forceinline__ TokenTerms policy_token(const PolicyArgs& A, float lp
     return o;
 }
 
+// What a thread has of a slot's part: a chunk gives it at most 64 elements, so four counts of
+// tokens by their clip (none among them) fit a word.
+struct PolicySums {
+    double sum[4] = {0, 0, 0, 0};
+    uint32_t clips = 0;
+};
+static_assert(kMaxChunk / kBlock <= 255, "counts of a byte");
+
+// The chunk's part of every array, and what does not change from group to group.
+struct PolicyChunk {
+    const float* logprob;
+    const float* old;
+    const float* ref;
+    const float* entropy;
+    const float* advantage;     // of the chunk (per token) or of the slot (per row)
+    float* grad;
+    float* grad_entropy;
+    int limit;
+    float kl_coef, entropy_coef;
+    Bounds bounds;
+};
+
+// A group's tokens: its part of the sums, its gradients.  weight(row, &f, &gs) gives the weight of a
+// row's token in the slot's mean and the factor of its gradient.  What does not count has all its
+// inputs replaced by 0.  Within a group the sums are formed in fp32.
+template <typename Weight>
+__device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyChunk& C, Group q, uint32_t on, int maxlen,
+                                             const Weight& weight, PolicySums& S) {
+    float g[4] = {0, 0, 0, 0}, ge[4] = {0, 0, 0, 0};
+    const Group q0 = q;
+    if (on) {      // what does not count is not read
+        const float4u zero = {0, 0, 0, 0};
+        const float4u lp = load_floats(C.logprob, q.o, C.limit);
+        const float4u old = A.old ? load_floats(C.old, q.o, C.limit) : zero;
+        const float4u ref = A.kl != ODB_KL_NONE ? load_floats(C.ref, q.o, C.limit) : zero;
+        const float4u H = A.entropy ? load_floats(C.entropy, q.o, C.limit) : zero;
+        const bool one_row = q.col <= maxlen - 4;
+        float4u adv;
+        float f[4], gs[4];
+        if (one_row) {
+            weight(q.row, &f[0], &gs[0]);
+            if (!A.token_advantage) adv[0] = C.advantage[q.row];
+#pragma unroll
+            for (int j = 1; j < 4; ++j) {
+                f[j] = f[0];
+                gs[j] = gs[0];
+                if (!A.token_advantage) adv[j] = adv[0];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f[j] = gs[j] = adv[j] = 0.0f;
+                if (on >> j & 1) {
+                    weight(q.row, &f[j], &gs[j]);
+                    if (!A.token_advantage) adv[j] = C.advantage[q.row];
+                }
+                q.next(maxlen);
+            }
+        }
+        if (A.token_advantage) adv = load_floats(C.advantage, q.o, C.limit);
+        float sum[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool live = on >> j & 1;
+            const TokenTerms o = policy_token(A, C.bounds, live ? lp[j] : 0.0f, live ? old[j] : 0.0f,
+                                              live ? ref[j] : 0.0f, live ? adv[j] : 0.0f);
+            const float w = live ? f[j] : 0.0f;
+            sum[0] = fmaf(w, o.policy, sum[0]);
+            sum[1] = fmaf(w, o.kl, sum[1]);
+            if (A.entropy) sum[2] = fmaf(w, live ? H[j] : 0.0f, sum[2]);
+            sum[3] = fmaf(w, o.ratio, sum[3]);
+            S.clips += live ? 1u << (8 * o.clip) : 0u;
+            const float k = live ? gs[j] : 0.0f;
+            g[j] = k * fmaf(C.kl_coef, o.kl_grad, o.grad);
+            ge[j] = -C.entropy_coef * k;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) S.sum[j] += sum[j];
+    }
+    if (A.grad) store4(C.grad, q0, g);
+    if (A.grad_entropy) store4(C.grad_entropy, q0, ge);
+}
+
+// Sums of the block's part of a slot, to its partial.
+__device__ __forceinline__ void leave_part(const PolicyArgs& A, const PolicySums& S, double same, int64_t at) {
+    __shared__ SlotPart s_part[kWaves];
+    SlotPart p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p.sum[j] = wave_total(S.sum[j]);
+    p.counted = wave_total((int)(S.clips & 0xff));
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+        p.clipped[j] = wave_total((int)(S.clips >> (8 * (j + 1)) & 0xff));
+        p.counted += p.clipped[j];
+    }
+    if ((threadIdx.x & (kWave - 1)) == 0) s_part[threadIdx.x / kWave] = p;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kWaves; ++w) {
+            for (int j = 0; j < 4; ++j) p.sum[j] += s_part[w].sum[j];
+            for (int j = 0; j < 3; ++j) p.clipped[j] += s_part[w].clipped[j];
+            p.counted += s_part[w].counted;
+        }
+        for (int j = 0; j < 4; ++j) p.sum[j] *= same;
+        A.slot_part[at] = p;
+    }
+    __syncthreads();
+}
+
+// Counted tokens of a row, over the chunks it touches.
+__device__ __forceinline__ int row_tokens(const PolicyArgs& A, const SlotView& s, int64_t row) {
+    const int64_t start = s.lo + row * s.maxlen;
+    int n = 0;
+    for (int64_t b = start / A.chunk; b <= (start + s.maxlen - 1) / A.chunk; ++b) n += A.row_count[b + s.row0 + row];
+    return n;
+}
+
+// Sum over a slot's chunks, one a lane, of f(chunk): a whole number that may pass 2^31.
+template <typename F>
+__device__ __forceinline__ double slot_total(const PolicyArgs& A, const SlotView& s, const F& f) {
+    const int64_t first = s.lo / A.chunk, last = (s.hi - 1) / A.chunk;
+    double n = 0;
+    for (int64_t j = first + (threadIdx.x & (kWave - 1)); j <= last; j += kWave) n += f(j);
+    return wave_total(n);
+}
+
+// The loss and its gradient, the elements that count given by the bits (LABELS: by the labels; a sum
+// needs no weights and so no pass before).
+template <bool ROWS, bool LABELS>
 __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
+    __shared__ double s_weight[ROWS ? kLdsRows : 1];
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int64_t total = run_elems(t, e_base);
     for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
-        const int64_t c0 = b * kChunk, c1 = c0 + kChunk < total ? c0 + kChunk : total;
-        chunk_slots(t, e_base, r_base, c0, c1, [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
-            double weight = 1.0;     // of a token in the slot's mean, where it is the same for all
-            if (A.reduce == ODB_REDUCE_TOKEN_MEAN) {
-                int64_t n = 0;
-                for (int64_t j = s.lo / kChunk; j <= (s.hi - 1) / kChunk; ++j) n += A.slot_count[j + k];
-                weight = n > 0 ? 1.0 / (double)n : 0.0;
-            }
+        const int64_t c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
+        if (c0 >= c1) break;
+        const int limit = chunk_limit(t, c0);
+        const uint32_t* bits = A.bits + b * (A.chunk / 32);
+        chunk_slots(t, e_base, r_base, first_slot(t, e_base, c0), c0, c1,
+                    [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+            const Span p(s, a0, a1, c0);
             const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
-            const int64_t row_a = (a0 - s.lo) / s.maxlen;
-            const uint32_t col_a = (uint32_t)((a0 - s.lo) - row_a * s.maxlen);
-            double sum[4] = {0, 0, 0, 0};
-            int clipped[3] = {0, 0, 0};
-            for (int64_t e = a0 + threadIdx.x; e < a1; e += kBlock) {
-                const uint32_t x = col_a + (uint32_t)(e - a0);
-                const int64_t row = s.row0 + row_a + x / (uint32_t)s.maxlen;
-                const bool on = A.bits[e / 32] >> (e & 31) & 1;
-                float g = 0.0f, ge = 0.0f;
-                if (on) {
-                    const float adv = A.advantage[A.token_advantage ? e : row];
-                    const TokenTerms o = policy_token(A, A.logprob[e], A.old ? A.old[e] : 0.0f,
-                                                      A.kl != ODB_KL_NONE ? A.ref[e] : 0.0f, adv);
-                    const double w = A.reduce == ODB_REDUCE_ROW_MEAN ? A.row_scale[row] : weight;
-                    sum[0] += w * o.policy;
-                    sum[1] += w * o.kl;
-                    if (A.entropy) sum[2] += w * A.entropy[e];
-                    sum[3] += w * o.ratio;
-                    clipped[0] += o.clip == 1;
-                    clipped[1] += o.clip == 2;
-                    clipped[2] += o.clip == 3;
-                    g = (float)(scale * w * ((double)o.grad + A.kl_coef * (double)o.kl_grad));
-                    ge = (float)(-A.entropy_coef * scale * w);
-                }
-                if (A.grad) A.grad[e] = g;
-                if (A.grad_entropy) A.grad_entropy[e] = ge;
+            double same = 1.0;       // weight of every token, where rows have none of their own
+            double rows = 0;         // of the slot, with a counted token
+            const int here = (int)((a1 - 1 - s.lo) / s.maxlen) - p.row_a + 1;
+            const bool lds = ROWS && here <= kLdsRows;
+            if (ROWS) {
+                // whole rows of every chunk, and those that start in it and go on
+                rows = slot_total(A, s, [&](int64_t j) {
+                    const int64_t end = (j + 1) * A.chunk;
+                    int n = A.slot_count[j + k];
+                    if (end < s.hi && (end - s.lo) % s.maxlen) {
+                        const int64_t row = (end - s.lo) / s.maxlen;
+                        if (s.lo + row * s.maxlen >= j * A.chunk) n += row_tokens(A, s, row) > 0;
+                    }
+                    return n;
+                });
+            } else if (!LABELS) {
+                const double n = slot_total(A, s, [&](int64_t j) { return A.slot_count[j + k]; });
+                same = n > 0 ? 1.0 / n : 0.0;
             }
-            SlotPart p;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) p.sum[j] = block_sum(sum[j]);
-#pragma unroll
-            for (int j = 0; j < 3; ++j) p.clipped[j] = block_sum(clipped[j]);
-            p.pad = 0;
-            if (threadIdx.x == 0) A.slot_part[b + k] = p;
+            auto row_weight = [&](int row) {
+                const int n = row_tokens(A, s, row);
+                return n > 0 ? 1.0 / ((double)n * rows) : 0.0;
+            };
+            if (lds) {
+                for (int i = threadIdx.x; i < here; i += kBlock) s_weight[i] = row_weight(p.row_a + i);
+                __syncthreads();
+            }
+            const float factor = (float)(scale * same);
+            auto weight = [&](int row, float* f, float* gs) {
+                if (ROWS) {
+                    const double w = lds ? s_weight[row - p.row_a] : row_weight(row);
+                    *f = (float)w;
+                    *gs = (float)(scale * w);
+                } else {
+                    *f = 1.0f;
+                    *gs = factor;
+                }
+            };
+            PolicyChunk C;
+            C.logprob = A.logprob + c0;
+            C.old = A.old + c0;
+            C.ref = A.ref + c0;
+            C.entropy = A.entropy + c0;
+            C.advantage = A.advantage + (A.token_advantage ? c0 : s.row0);
+            C.grad = A.grad + c0;
+            C.grad_entropy = A.grad_entropy + c0;
+            C.limit = limit;
+            C.kl_coef = (float)A.kl_coef;
+            C.entropy_coef = (float)A.entropy_coef;
+            C.bounds = Bounds{(float)A.at_low, (float)A.at_high, (float)A.at_dual};
+            PolicySums S;
+            Group q = p.first();
+            for (; q.o < p.o1; p.advance(&q)) {
+                const uint32_t on = LABELS ? count_mask(q, load_labels(t.d_labels + c0, q.o, limit), p.maxlen, t.shift)
+                                           : bits[q.o / 32] >> (q.o & 31) & q.mask;
+                policy_group(A, C, q, on, p.maxlen, weight, S);
+            }
+            leave_part(A, S, same, b + k);
         });
     }
 }
 
-// The slots' numbers from their chunks' partials, a thread a slot.
+// The slots' numbers from their chunks' partials, a wave a slot.
 __global__ void __launch_bounds__(kBlock) policy_slots_kernel(PolicyArgs A) {
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
-    for (int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x; k < t.num_slots; k += (int64_t)gridDim.x * kBlock) {
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int64_t k = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave; k < t.num_slots;
+         k += (int64_t)gridDim.x * kWaves) {
         const SlotView s = slot_view(t, k, e_base, r_base);
         double sum[4] = {0, 0, 0, 0};
-        int64_t n = 0, clipped[3] = {0, 0, 0};
-        if (s.ok && s.hi > s.lo) {
-            for (int64_t j = s.lo / kChunk; j <= (s.hi - 1) / kChunk; ++j) {
+        double n = 0, clipped[3] = {0, 0, 0};     // whole numbers below 2^41
+        if (!s.ok) {
+            if (A.status && lane == 0) *A.status = kErrTiles;
+        } else if (s.hi > s.lo) {
+            for (int64_t j = s.lo / A.chunk + lane; j <= (s.hi - 1) / A.chunk; j += kWave) {
                 const SlotPart p = A.slot_part[j + k];
-                n += A.slot_count[j + k];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[i] += p.sum[i];
 #pragma unroll
                 for (int i = 0; i < 3; ++i) clipped[i] += p.clipped[i];
+                n += p.counted;
             }
         }
-        const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
-        A.slot_loss[k] = n > 0 ? (float)(scale * (sum[0] + A.kl_coef * sum[1] - A.entropy_coef * sum[2])) : 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) A.slot_means[4 * k + i] = (float)sum[i];
-        A.slot_counts[4 * k] = n;
+        for (int i = 0; i < 4; ++i) sum[i] = wave_total(sum[i]);
 #pragma unroll
-        for (int i = 0; i < 3; ++i) A.slot_counts[4 * k + 1 + i] = clipped[i];
+        for (int i = 0; i < 3; ++i) clipped[i] = wave_total(clipped[i]);
+        n = wave_total(n);
+        if (lane == 0) {
+            const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
+            A.slot_loss[k] = n > 0 ? (float)(scale * (sum[0] + A.kl_coef * sum[1] - A.entropy_coef * sum[2])) : 0.0f;
+            for (int i = 0; i < 4; ++i) A.slot_means[4 * k + i] = (float)sum[i];
+            A.slot_counts[4 * k] = (int64_t)n;
+            for (int i = 0; i < 3; ++i) A.slot_counts[4 * k + 1 + i] = (int64_t)clipped[i];
+        }
     }
 }
 
 // ------------------------------------------------------------------ preference loss
 struct PairArgs {
     odb_tiles_t t;
+    const float* logprob;
+    const float* ref;
     const int32_t* row_ids;
     const int32_t* pair;
     int64_t num_ids;
-    const int32_t* row_of;
-    const int32_t* row_count;
-    const double* row_sum;
-    const RowInfo* row_info;
+    int32_t* row_of;
+    int32_t* row_count;
+    double* row_sum;
+    RowInfo* row_info;
     double* coef;
     PairPart* part;
-    const uint32_t* bits;
+    uint32_t* bits;
     float* loss;
     float* row_loss;
     float* row_reward;
@@ -479,13 +722,154 @@ struct PairArgs {
     int32_t* status;
     int64_t chunks;
     double beta, margin, smoothing, loss_scale;
-    int32_t kind;
+    int32_t kind, chunk;
     bool normalize;
 };
 
+constexpr int kLongRow = 1024;
+constexpr int kAhead = 4;          // groups of a lane whose loads are under way together
+
+__device__ __forceinline__ void mark(uint32_t* s_bits, int at, uint32_t nibble) {
+    if (!nibble) return;
+    const uint64_t w = (uint64_t)nibble << (at & 31);
+    atomicOr(&s_bits[at >> 5], (uint32_t)w);
+    if (w >> 32) atomicOr(&s_bits[(at >> 5) + 1], (uint32_t)(w >> 32));
+}
+
+// Positions [a, b) of a chunk, which lie in one row: four a lane of the `lanes` that share it.  How
+// many count (from position `from` on), and the sum of logprob - ref over them.
+__device__ __forceinline__ void row_run(const PairArgs& A, int64_t c0, int limit, int a, int b, int from, int lane,
+                                        int lanes, uint32_t* s_bits, int* count, double* sum) {
+    const int32_t* labels = A.t.d_labels + c0;
+    const float* logprob = A.logprob + c0;
+    const float* ref = A.ref + c0;
+    for (int o0 = a + 4 * lane; o0 < b; o0 += 4 * kAhead * lanes) {
+        int4u y[kAhead];
+        float4u p[kAhead], r[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int o = o0 + 4 * i * lanes;
+            if (o < b) {
+                y[i] = load_labels(labels, o, limit);
+                p[i] = load_floats(logprob, o, limit);
+                if (A.ref) r[i] = load_floats(ref, o, limit);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int o = o0 + 4 * i * lanes;
+            if (o < b) {
+                uint32_t on = b - o >= 4 ? 0xfu : 0xfu >> (4 - (b - o));
+                if (o < from) on &= 0xfu << (from - o < 4 ? from - o : 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (y[i][j] == ODB_LABEL_IGNORE) on &= ~(1u << j);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const double x = A.ref ? (double)p[i][j] - (double)r[i][j] : (double)p[i][j];
+                    *sum += on >> j & 1 ? x : 0.0;
+                }
+                *count += __builtin_popcount(on);
+                mark(s_bits, o, on);
+            }
+        }
+    }
+}
+
+// First pass: the bits, and per chunk and row how many tokens count and the sum over them.  A row is
+// taken by the smallest power of two of lanes that covers it four elements each, up to a wave; rows
+// of more than 1,024 elements by the block.
+__global__ void __launch_bounds__(kBlock) row_sums_kernel(PairArgs A) {
+    __shared__ uint32_t s_bits[kMaxChunk / 32];
+    const odb_tiles_t& t = A.t;
+    const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
+    const int64_t total = run_elems(t, e_base);
+    const int words = A.chunk / 32;
+    for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
+        const int64_t c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
+        if (c0 >= c1) break;
+        const int limit = chunk_limit(t, c0);
+        for (int i = threadIdx.x; i < words; i += kBlock) s_bits[i] = 0;
+        __syncthreads();
+        chunk_slots(t, e_base, r_base, first_slot(t, e_base, c0), c0, c1,
+                    [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+            const int64_t row_a = (a0 - s.lo) / s.maxlen, row_b = (a1 - 1 - s.lo) / s.maxlen;
+            const bool wide = s.maxlen > kLongRow;
+            int lanes = 1;
+            while (lanes < kWave && 4 * lanes < s.maxlen) lanes *= 2;
+            if (wide) lanes = kBlock;
+            const int lane = threadIdx.x & (lanes - 1);
+            const int step = kBlock / lanes;
+            // every group goes round as often as the first, so that no lane leaves a reduction alone
+            for (int64_t r0 = row_a; r0 <= row_b; r0 += step) {
+                const int64_t r = r0 + threadIdx.x / lanes;
+                const bool live = r <= row_b;
+                const int64_t start = s.lo + r * s.maxlen;
+                int count = 0;
+                double sum = 0.0;
+                if (live) {
+                    const int64_t x0 = start > a0 ? start : a0, x1 = start + s.maxlen < a1 ? start + s.maxlen : a1;
+                    // the row's start may lie far before the chunk
+                    const int from = start + t.shift > c0 ? (int)(start + t.shift - c0) : 0;
+                    row_run(A, c0, limit, (int)(x0 - c0), (int)(x1 - c0), from, lane, lanes, s_bits, &count, &sum);
+                }
+                if (wide) {
+                    count = block_total(count);
+                    sum = block_total(sum);
+                } else if (lanes == kWave) {
+                    count = wave_total(count);
+                    sum = wave_total(sum);
+                } else {
+                    for (int d = lanes / 2; d > 0; d >>= 1) {
+                        count += __shfl_xor(count, d, kWave);
+                        sum += __shfl_xor(sum, d, kWave);
+                    }
+                }
+                if (live && lane == 0) {
+                    const int64_t row = s.row0 + r;
+                    A.row_count[b + row] = count;
+                    A.row_sum[b + row] = sum;
+                    if (start >= c0) {   // the row starts here
+                        const int64_t last = (start + s.maxlen - 1) / A.chunk;
+                        A.row_info[row] = RowInfo{(int32_t)b, (int32_t)(last - b + 1)};
+                        if (A.row_of) {
+                            const int32_t id = A.row_ids[row];
+                            if (id >= 0 && id < A.num_ids) atomicMin(&A.row_of[id], (int32_t)row);
+                        }
+                    }
+                }
+            }
+        });
+        __syncthreads();
+        for (int i = threadIdx.x; i < words; i += kBlock) A.bits[b * words + i] = s_bits[i];
+        __syncthreads();
+    }
+    if (A.status)
+        for (int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x; k < t.num_slots; k += (int64_t)gridDim.x * kBlock)
+            if (!slot_view(t, k, e_base, r_base).ok) *A.status = kErrTiles;
+}
+
+// Clears the entries of the ids that have a row.  The others hold anything: an entry is believed
+// only if the row that it names has the id.
+__global__ void __launch_bounds__(kBlock) clear_rows_kernel(PairArgs A) {
+    const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
+    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < rows; i += (int64_t)gridDim.x * kBlock) {
+        const int32_t id = A.row_ids[i];
+        if (id >= 0 && id < A.num_ids) A.row_of[id] = INT32_MAX;
+    }
+}
+
+// A row's log ratio; nothing is read outside its partials whatever its record holds.
 __device__ __forceinline__ double log_ratio(const PairArgs& A, int64_t row, int* count) {
-    double s;
-    const int n = row_total(A.row_count, A.row_sum, A.row_info, A.chunks, row, &s);
+    const RowInfo f = A.row_info[row];
+    int n = 0;
+    double s = 0.0;
+    if (f.first >= 0 && f.chunks > 0 && (int64_t)f.first + f.chunks <= A.chunks) {
+        for (int64_t b = f.first; b < (int64_t)f.first + f.chunks; ++b) {
+            n += A.row_count[b + row];
+            s += A.row_sum[b + row];
+        }
+    }
     *count = n;
     return n == 0 ? 0.0 : A.normalize ? s / n : s;
 }
@@ -509,7 +893,7 @@ __device__ __forceinline__ int64_t partner_row(const PairArgs& A, int64_t row, i
     if (!A.row_ids) return other < rows ? other : -1;
     if (A.row_of[id] != row) return -1;        // a later row of an id that has one already
     const int64_t j = A.row_of[other];
-    return j < rows ? j : -1;
+    return j >= 0 && j < rows && A.row_ids[j] == other ? j : -1;
 }
 
 __global__ void __launch_bounds__(kBlock) pairs_kernel(PairArgs A) {
@@ -529,7 +913,7 @@ __global__ void __launch_bounds__(kBlock) pairs_kernel(PairArgs A) {
             const double h = A.beta * (chosen ? S - T : T - S) - A.margin;
             double dh;
             if (A.kind == ODB_PREFERENCE_SIGMOID) {
-                const double q = exp(-fabs(h)), soft = log1p(q);       // -ln s(|h|)
+                const double q = exp(-fabs(h)), soft = log1p(q);           // -ln s(|h|)
                 const double far = 1.0 / (1.0 + q), near = q / (1.0 + q);  // s(|h|), s(-|h|)
                 const double up = h >= 0 ? far : near, down = h >= 0 ? near : far;
                 loss = (1.0 - A.smoothing) * (soft + (h < 0 ? -h : 0.0)) + A.smoothing * (soft + (h > 0 ? h : 0.0));
@@ -557,9 +941,9 @@ __global__ void __launch_bounds__(kBlock) pairs_kernel(PairArgs A) {
         A.row_reward[row] = (float)(A.beta * S);
     }
     PairPart p;
-    p.loss = block_sum(loss);
-    p.pairs = block_sum(pairs);
-    p.right = block_sum(right);
+    p.loss = block_total(loss);
+    p.pairs = block_total(pairs);
+    p.right = block_total(right);
     if (threadIdx.x == 0) A.part[blockIdx.x] = p;
 }
 
@@ -567,35 +951,52 @@ __global__ void __launch_bounds__(kBlock) pairs_kernel(PairArgs A) {
 __global__ void __launch_bounds__(kBlock) pairs_grad_kernel(PairArgs A, int64_t parts) {
     const odb_tiles_t& t = A.t;
     if (blockIdx.x == 0) {
-        double loss = 0.0;
-        int64_t pairs = 0, right = 0;
+        double loss = 0.0, pairs = 0.0, right = 0.0;    // whole numbers below 2^31
         for (int64_t i = threadIdx.x; i < parts; i += kBlock) {
             loss += A.part[i].loss;
             pairs += A.part[i].pairs;
             right += A.part[i].right;
         }
-        loss = block_sum(loss);
-        pairs = block_sum(pairs);
-        right = block_sum(right);
+        loss = block_total(loss);
+        pairs = block_total(pairs);
+        right = block_total(right);
         if (threadIdx.x == 0) {
             *A.loss = (float)loss;
-            A.counts[0] = pairs;
-            A.counts[1] = right;
+            A.counts[0] = (int64_t)pairs;
+            A.counts[1] = (int64_t)right;
         }
     }
     if (!A.grad || t.num_slots == 0) return;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int64_t total = run_elems(t, e_base);
     for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
-        const int64_t c0 = b * kChunk, c1 = c0 + kChunk < total ? c0 + kChunk : total;
-        chunk_slots(t, e_base, r_base, c0, c1, [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
-            const int64_t row_a = (a0 - s.lo) / s.maxlen;
-            const uint32_t col_a = (uint32_t)((a0 - s.lo) - row_a * s.maxlen);
-            for (int64_t e = a0 + threadIdx.x; e < a1; e += kBlock) {
-                const uint32_t x = col_a + (uint32_t)(e - a0);
-                const int64_t row = s.row0 + row_a + x / (uint32_t)s.maxlen;
-                const bool on = A.bits[e / 32] >> (e & 31) & 1;
-                A.grad[e] = on ? (float)A.coef[row] : 0.0f;
+        const int64_t c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
+        if (c0 >= c1) break;
+        const uint32_t* bits = A.bits + b * (A.chunk / 32);
+        chunk_slots(t, e_base, r_base, first_slot(t, e_base, c0), c0, c1,
+                    [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+            const Span p(s, a0, a1, c0);
+            const double* coef = A.coef + s.row0;
+            Group q = p.first();
+#pragma unroll 4
+            for (; q.o < p.o1; p.advance(&q)) {
+                const uint32_t on = bits[q.o / 32] >> (q.o & 31) & q.mask;
+                float v[4] = {0, 0, 0, 0};
+                if (on) {
+                    if (q.col <= p.maxlen - 4) {
+                        const float c = (float)coef[q.row];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] = on >> j & 1 ? c : 0.0f;
+                    } else {
+                        Group r = q;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (on >> j & 1) v[j] = (float)coef[r.row];
+                            r.next(p.maxlen);
+                        }
+                    }
+                }
+                store4(A.grad + c0, q, v);
             }
         });
     }
@@ -606,18 +1007,6 @@ int check_tile_arrays(const odb_tiles_t* t) {
         return set_error(ODB_E_INVALID_ARG, "slot arrays must not be NULL");
     if (t->num_elems > 0 && !t->d_labels) return set_error(ODB_E_INVALID_ARG, "d_labels must not be NULL");
     return ODB_OK;
-}
-
-void rows_args(RowsArgs* r, const odb_tiles_t* t, const LossLayout& L, void* ws, int32_t* status) {
-    *r = RowsArgs{};
-    r->t = *t;
-    r->bits = ws_at<uint32_t>(ws, L.bits);
-    r->slot_count = ws_at<int32_t>(ws, L.slot_count);
-    r->row_sum = ws_at<double>(ws, L.row_sum);
-    r->row_count = ws_at<int32_t>(ws, L.row_count);
-    r->row_info = ws_at<RowInfo>(ws, L.row_info);
-    r->chunks = L.chunks;
-    r->status = status;
 }
 
 }  // namespace
@@ -666,9 +1055,6 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     ODB_TRY(check_loss_workspace(L, d_ws, ws_bytes));
 
     hipStream_t s = static_cast<hipStream_t>(stream);
-    RowsArgs r;
-    rows_args(&r, t, L, d_ws, d_status);
-    r.rows = p->reduce == ODB_REDUCE_ROW_MEAN;
     PolicyArgs a{};
     a.t = *t;
     a.logprob = d_logprob;
@@ -682,13 +1068,13 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     a.slot_counts = d_slot_counts;
     a.grad = d_grad_logprob;
     a.grad_entropy = d_grad_entropy;
-    a.bits = r.bits;
-    a.slot_count = r.slot_count;
+    a.bits = ws_at<uint32_t>(d_ws, L.bits);
+    a.slot_count = ws_at<int32_t>(d_ws, L.slot_count);
     a.slot_part = ws_at<SlotPart>(d_ws, L.slot_part);
-    a.row_count = r.row_count;
-    a.row_info = r.row_info;
-    a.row_scale = ws_at<double>(d_ws, L.row_scale);
+    a.row_count = ws_at<int32_t>(d_ws, L.row_count);
+    a.status = d_status;
     a.chunks = L.chunks;
+    a.chunk = L.chunk;
     a.at_low = std::log1p(-p->clip_low);
     a.at_high = std::log1p(p->clip_high);
     a.at_dual = p->dual_clip > 0.0 ? std::log(p->dual_clip) : HUGE_VAL;
@@ -701,16 +1087,22 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     a.kl = p->kl;
     a.reduce = p->reduce;
     a.token_advantage = p->token_advantage;
-    const dim3 chunks(grid_for(L.chunks, 1));
-    hipLaunchKernelGGL(loss_rows_kernel<false>, chunks, dim3(kBlock), 0, s, r);
-    ODB_LAUNCHED();
-    if (r.rows) {
-        hipLaunchKernelGGL(row_scale_kernel, dim3(grid_for(t->num_slots, 1)), dim3(kBlock), 0, s, a);
+    const dim3 grid(grid_for(L.chunks, 1)), block(kBlock);
+    if (L.chunks > 0) {
+        if (p->reduce == ODB_REDUCE_TOKEN_MEAN) {
+            hipLaunchKernelGGL(policy_count_kernel<false>, grid, block, 0, s, a);
+            ODB_LAUNCHED();
+            hipLaunchKernelGGL((policy_kernel<false, false>), grid, block, 0, s, a);
+        } else if (p->reduce == ODB_REDUCE_ROW_MEAN) {
+            hipLaunchKernelGGL(policy_count_kernel<true>, grid, block, 0, s, a);
+            ODB_LAUNCHED();
+            hipLaunchKernelGGL((policy_kernel<true, false>), grid, block, 0, s, a);
+        } else {
+            hipLaunchKernelGGL((policy_kernel<false, true>), grid, block, 0, s, a);
+        }
         ODB_LAUNCHED();
     }
-    hipLaunchKernelGGL(policy_kernel, chunks, dim3(kBlock), 0, s, a);
-    ODB_LAUNCHED();
-    hipLaunchKernelGGL(policy_slots_kernel, dim3(grid_for(t->num_slots, kBlock)), dim3(kBlock), 0, s, a);
+    hipLaunchKernelGGL(policy_slots_kernel, dim3(grid_for(t->num_slots, kWaves)), block, 0, s, a);
     ODB_LAUNCHED();
     return ODB_OK;
 }
@@ -744,26 +1136,20 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
     ODB_TRY(check_loss_workspace(L, d_ws, ws_bytes));
 
     hipStream_t s = static_cast<hipStream_t>(stream);
-    RowsArgs r;
-    rows_args(&r, t, L, d_ws, d_status);
-    r.logprob = d_logprob;
-    r.ref = d_ref_logprob;
-    r.row_ids = d_row_ids;
-    r.row_of = d_row_ids ? ws_at<int32_t>(d_ws, L.row_of) : nullptr;
-    r.num_ids = num_ids;
-    r.rows = true;
     PairArgs a{};
     a.t = *t;
+    a.logprob = d_logprob;
+    a.ref = d_ref_logprob;
     a.row_ids = d_row_ids;
     a.pair = d_pair;
     a.num_ids = num_ids;
-    a.row_of = r.row_of;
-    a.row_count = r.row_count;
-    a.row_sum = r.row_sum;
-    a.row_info = r.row_info;
-    a.coef = ws_at<double>(d_ws, L.row_scale);
+    a.row_of = d_row_ids ? ws_at<int32_t>(d_ws, L.row_of) : nullptr;
+    a.row_count = ws_at<int32_t>(d_ws, L.row_count);
+    a.row_sum = ws_at<double>(d_ws, L.row_sum);
+    a.row_info = ws_at<RowInfo>(d_ws, L.row_info);
+    a.coef = ws_at<double>(d_ws, L.coef);
     a.part = ws_at<PairPart>(d_ws, L.pair_part);
-    a.bits = r.bits;
+    a.bits = ws_at<uint32_t>(d_ws, L.bits);
     a.loss = d_loss;
     a.row_loss = d_row_loss;
     a.row_reward = d_row_reward;
@@ -771,6 +1157,7 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
     a.grad = any ? d_grad_logprob : nullptr;
     a.status = d_status;
     a.chunks = any ? L.chunks : 0;
+    a.chunk = L.chunk;
     a.beta = p->beta;
     a.margin = p->margin;
     a.smoothing = p->label_smoothing;
@@ -779,12 +1166,11 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
     a.normalize = p->normalize;
     const int64_t parts = any ? (t->num_rows + kBlock - 1) / kBlock : 0;
     if (any) {
-        if (d_row_ids && num_ids > 0) {
-            hipLaunchKernelGGL(fill_rows_kernel, dim3(grid_for(num_ids, kBlock, (int64_t)num_cus() * 8)), dim3(kBlock),
-                               0, s, r.row_of, num_ids);
+        if (a.row_of && parts > 0) {
+            hipLaunchKernelGGL(clear_rows_kernel, dim3(grid_for(parts, 1)), dim3(kBlock), 0, s, a);
             ODB_LAUNCHED();
         }
-        hipLaunchKernelGGL(loss_rows_kernel<true>, dim3(grid_for(L.chunks, 1)), dim3(kBlock), 0, s, r);
+        hipLaunchKernelGGL(row_sums_kernel, dim3(grid_for(L.chunks, 1)), dim3(kBlock), 0, s, a);
         ODB_LAUNCHED();
         if (parts > 0) {
             hipLaunchKernelGGL(pairs_kernel, dim3((unsigned)parts), dim3(kBlock), 0, s, a);

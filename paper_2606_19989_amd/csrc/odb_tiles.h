@@ -38,12 +38,20 @@ __host__ __device__ __forceinline__ SlotView slot_view(const odb_tiles_t& t, int
     return s;
 }
 
-// Last slot that starts at or before element e (0 if there is none), whatever the offsets hold.
-__host__ __device__ __forceinline__ int64_t slot_of(const odb_tiles_t& t, int64_t e_base, int64_t e) {
-    int64_t lo = 0, hi = t.num_slots;
+// Probes of one step of the search below, one a lane.
+constexpr int kProbes = 64;
+
+// Last slot of [0, slots) that starts at or before an element (0 if there is none), whatever the
+// offsets hold: probe(lo, step, hi) is the first i < kProbes whose slot lo + i * step does not or is
+// not below hi, else kProbes.
+template <typename Probe>
+__host__ __device__ __forceinline__ int64_t search_slot(int64_t slots, const Probe& probe) {
+    int64_t lo = 0, hi = slots;
     while (hi - lo > 1) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (offset_from(t.d_slot_tile_off[mid], e_base) <= e) lo = mid; else hi = mid;
+        const int64_t step = (hi - lo + kProbes - 1) / kProbes;
+        const int n = probe(lo, step, hi);
+        if (n > 1) lo += (n - 1) * step;
+        hi = lo + step < hi ? lo + step : hi;
     }
     return lo;
 }
@@ -60,12 +68,12 @@ __host__ __device__ __forceinline__ int64_t run_rows(const odb_tiles_t& t, int64
     return n < 0 ? 0 : n < t.num_rows ? n : t.num_rows;
 }
 
-// Calls f(k, slot, a0, a1) for every sound slot k with elements [a0, a1) in [c0, c1), in order.
+// Calls f(k, slot, a0, a1) for every sound slot k >= first with elements [a0, a1) in [c0, c1), in
+// order, until one starts behind them.
 template <typename F>
-__host__ __device__ __forceinline__ void chunk_slots(const odb_tiles_t& t, int64_t e_base, int64_t r_base, int64_t c0,
-                                                     int64_t c1, const F& f) {
-    if (c0 >= c1) return;
-    for (int64_t k = slot_of(t, e_base, c0); k < t.num_slots; ++k) {
+__host__ __device__ __forceinline__ void chunk_slots(const odb_tiles_t& t, int64_t e_base, int64_t r_base,
+                                                     int64_t first, int64_t c0, int64_t c1, const F& f) {
+    for (int64_t k = first; k < t.num_slots; ++k) {
         const SlotView s = slot_view(t, k, e_base, r_base);
         if (s.lo >= c1) break;
         if (!s.ok || s.hi <= c0 || s.hi == s.lo) continue;
