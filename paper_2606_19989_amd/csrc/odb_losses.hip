@@ -19,10 +19,14 @@ namespace odb {
 namespace {
 
 constexpr int kMaxChunk = 16384;               // elements of a chunk, at most
+constexpr int kOneChunk = 4096;                // elements of a run that one block takes
 constexpr int kWaves = kBlock / kWave;
+static_assert(kWaves == 4, "a wave takes a quarter of a chunk");
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLog2eLow = 1.92596299112661746887e-8f;   // log2 e - kLog2e
 constexpr float kLn2 = 0.69314718055994530942f;
+
+constexpr int32_t kIgnore = ODB_LABEL_IGNORE;
 
 typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef int int4u __attribute__((ext_vector_type(4), aligned(4)));
@@ -35,8 +39,8 @@ struct SlotPart {
 };
 
 struct RowInfo {
-    int32_t first;      // chunk in which the row starts
-    int32_t chunks;     // chunks it touches
+    int32_t first;      // quarter of a chunk in which the row starts
+    int32_t parts;      // quarters it touches
 };
 
 struct PairPart {
@@ -45,7 +49,7 @@ struct PairPart {
 };
 
 struct LossLayout {
-    size_t bits, slot_count, slot_part, row_sum, row_count, row_info, coef, pair_part, row_of;
+    size_t bits, chunk_slot, slot_count, slot_part, row_sum, row_count, row_info, coef, pair_part, row_of;
     size_t total;
     int64_t chunks;
     int32_t chunk;
@@ -58,7 +62,7 @@ constexpr int64_t kMaxElems = (int64_t)1 << 40;
 int32_t chunk_for(int64_t elems) {
     if (elems >= (int64_t)1 << 25) return kMaxChunk;
     if (elems >= (int64_t)1 << 23) return 4096;
-    return 1024;
+    return elems > kOneChunk ? 1024 : kOneChunk;
 }
 
 int check_tiles(const odb_tiles_t* t) {
@@ -85,10 +89,11 @@ LossLayout loss_layout(const odb_tiles_t* t, int64_t num_ids) {
     L.chunks = (t->num_elems + L.chunk - 1) / L.chunk;
     const int64_t K = t->num_slots, R = t->num_rows;
     L.bits = take(L.chunks * (L.chunk / 8));
+    L.chunk_slot = take(4 * L.chunks);
     L.slot_count = take(4 * (L.chunks + K));
     L.slot_part = take((int64_t)sizeof(SlotPart) * (L.chunks + K));
-    L.row_sum = take(8 * (L.chunks + R));
-    L.row_count = take(4 * (L.chunks + R));
+    L.row_sum = take(8 * (kWaves * L.chunks + R));
+    L.row_count = take(4 * (kWaves * L.chunks + R));
     L.row_info = take((int64_t)sizeof(RowInfo) * R);
     L.coef = take(8 * R);
     L.pair_part = take((int64_t)sizeof(PairPart) * (R / kBlock + 1));
@@ -155,22 +160,32 @@ __device__ __forceinline__ T block_total(T v) {
     return sum;
 }
 
-// Four values from position o on of an array that ends at `limit`; what lies behind is `fill`.
-template <typename V4, typename T>
-__device__ __forceinline__ V4 load4(const T* p, int o, int limit, T fill) {
-    if (o + 4 <= limit) return *reinterpret_cast<const V4*>(p + o);
-    V4 v;
+// Four values of an array from position o of a chunk on, without a branch: past `last`, the position
+// of the array's last four, those are read instead and put in their places afterwards by `settle`, so
+// that loads of many groups go out together.  SAFE, for arrays that may hold fewer than four: each is
+// read on its own where not all are there, and the others are `fill` at once.
+template <typename V4, bool SAFE, typename T>
+__device__ __forceinline__ V4 load4(const T* p, int o, int last, T fill) {
+    if (SAFE && o > last) {
+        V4 v;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = o + j < limit ? p[o + j] : fill;
-    return v;
+        for (int j = 0; j < 4; ++j) v[j] = o + j < last + 4 ? p[o + j] : fill;
+        return v;
+    }
+    return *reinterpret_cast<const V4*>(p + (o < last ? o : last));
 }
 
-__device__ __forceinline__ int4u load_labels(const int32_t* labels, int o, int limit) {
-    return load4<int4u>(labels, o, limit, (int32_t)ODB_LABEL_IGNORE);
-}
-
-__device__ __forceinline__ float4u load_floats(const float* p, int o, int limit) {
-    return load4<float4u>(p, o, limit, 0.0f);
+// What lies behind the array becomes `fill`.
+template <bool SAFE, typename V4, typename T>
+__device__ __forceinline__ void settle(V4* v, int o, int last, T fill) {
+    if (SAFE || o <= last) return;
+    for (int d = last; d < o; ++d) {
+        (*v)[0] = (*v)[1];
+        (*v)[1] = (*v)[2];
+        (*v)[2] = (*v)[3];
+        (*v)[3] = fill;
+        if (d - last >= 3) break;
+    }
 }
 
 // A thread's group of four elements of a chunk, from position o (a multiple of 4) on: which of them
@@ -190,26 +205,31 @@ struct Group {
     }
 };
 
-// A slot's elements [a0, a1) of the chunk that starts at c0, as positions [o0, o1) in it; threads
-// take groups kBlock apart.  Rows count from the slot's first.
+// A slot's elements [a0, a1) of the chunk that starts at c0, as positions [o0, o1) in it; `threads`
+// threads take its groups in turn.  Rows count from the slot's first.
 struct Span {
     int o0, o1, maxlen;
-    int row_a, col_a;           // of element a0
-    int rows_by, cols_by;       // what a thread's next group is ahead
+    int row_a, col_a;               // of element a0
+    int ahead, rows_by, cols_by;    // from a thread's group to its next
 
-    __device__ __forceinline__ Span(const SlotView& s, int64_t a0, int64_t a1, int64_t c0)
+    __device__ __forceinline__ Span(const SlotView& s, int64_t a0, int64_t a1, int64_t c0, int threads)
         : o0((int)(a0 - c0)), o1((int)(a1 - c0)), maxlen(s.maxlen), row_a((int)((a0 - s.lo) / s.maxlen)),
-          col_a((int)((a0 - s.lo) - (int64_t)row_a * s.maxlen)), rows_by(4 * kBlock / s.maxlen),
-          cols_by(4 * kBlock - rows_by * s.maxlen) {}
+          col_a((int)((a0 - s.lo) - (int64_t)row_a * s.maxlen)), ahead(4 * threads), rows_by(ahead / s.maxlen),
+          cols_by(ahead - rows_by * s.maxlen) {}
 
     __device__ __forceinline__ uint32_t mask_at(int o) const {
         return (o0 > o ? 0xfu << (o0 - o) : 0xfu) & (o1 - o >= 4 ? 0xfu : 0xfu >> (4 - (o1 - o)));
     }
 
-    // The thread's first group; its o may lie behind the span.
-    __device__ __forceinline__ Group first() const {
+    // Row of position o >= o0.
+    __device__ __forceinline__ int row_at(int o) const {
+        return row_a + (int)(((uint32_t)col_a + (uint32_t)(o - o0)) / (uint32_t)maxlen);
+    }
+
+    // First group of a thread; its o may lie behind the span.
+    __device__ __forceinline__ Group first(int thread) const {
         Group q;
-        q.o = (o0 & ~3) + 4 * (int)threadIdx.x;
+        q.o = (o0 & ~3) + 4 * thread;
         const int x = q.o - o0;      // negative only in the group in which the slot starts, where col_a is 0
         q.row = row_a;
         q.col = x;
@@ -218,12 +238,12 @@ struct Span {
             q.row += (int)r;
             q.col = (int)(c - r * (uint32_t)maxlen);
         }
-        q.mask = mask_at(q.o);
+        q.mask = q.o < o1 ? mask_at(q.o) : 0;
         return q;
     }
 
     __device__ __forceinline__ void advance(Group* q) const {
-        q->o += 4 * kBlock;
+        q->o += ahead;
         q->row += rows_by;
         if (q->col >= maxlen - cols_by) {    // no sum of two columns: they may pass 2^31
             q->col -= maxlen - cols_by;
@@ -231,7 +251,7 @@ struct Span {
         } else {
             q->col += cols_by;
         }
-        q->mask = mask_at(q->o);
+        q->mask = q->o < o1 ? mask_at(q->o) : 0;
     }
 };
 
@@ -257,9 +277,18 @@ __device__ __forceinline__ void store4(float* p, const Group& q, const float v[4
     }
 }
 
-// Elements from c0 to the arrays' end, as far as a chunk's positions go.
-__device__ __forceinline__ int chunk_limit(const odb_tiles_t& t, int64_t c0) {
-    const int64_t n = t.num_elems - c0;
+// A chunk's bits to LDS; the block meets before and after.
+__device__ __forceinline__ void load_bits(uint32_t* s_bits, const uint32_t* bits, int64_t b, int chunk) {
+    const int words = chunk / 32;
+    __syncthreads();
+    for (int i = threadIdx.x; i < words; i += kBlock) s_bits[i] = bits[b * words + i];
+    __syncthreads();
+}
+
+// Position in a chunk of the arrays' last four elements, as far as a chunk's positions go; negative in
+// a last chunk of fewer.
+__device__ __forceinline__ int last_four(const odb_tiles_t& t, int64_t c0) {
+    const int64_t n = t.num_elems - 4 - c0;
     return (int)(n < 2 * kMaxChunk ? n : 2 * kMaxChunk);
 }
 
@@ -278,6 +307,7 @@ struct PolicyArgs {
     float* grad;
     float* grad_entropy;
     uint32_t* bits;
+    int32_t* chunk_slot;        // first slot of every chunk, left by the first pass
     int32_t* slot_count;        // counted tokens (token mean) or complete rows with any (row mean)
     SlotPart* slot_part;
     int32_t* row_count;
@@ -286,9 +316,12 @@ struct PolicyArgs {
     double at_low, at_high, at_dual;    // ln(1 - e_l), ln(1 + e_h), ln c
     double kl_coef, entropy_coef, loss_scale;
     float low, high, dual;              // 1 - e_l, 1 + e_h, c
-    int32_t kl, reduce, chunk;
-    bool token_advantage;
+    int32_t chunk, chunk_log2;
+    bool token_advantage, on_policy;    // on_policy: no old log-probabilities, the ratio is 1
 };
+
+// Groups of a thread whose loads are under way together.
+constexpr int kAhead = 4;
 
 // Rows of a slot that one block weighs in LDS.
 constexpr int kLdsRows = 4096;
@@ -319,12 +352,14 @@ __global__ void __launch_bounds__(kBlock) policy_count_kernel(PolicyArgs A) {
         const int64_t c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
         if (c0 >= c1) break;
         const int32_t* labels = t.d_labels + c0;
-        const int limit = chunk_limit(t, c0);
+        const int last = last_four(t, c0);
         for (int i = threadIdx.x; i < A.chunk / 16; i += kBlock) reinterpret_cast<uint32_t*>(s_nibble)[i] = 0;
+        const int64_t k0 = first_slot(t, e_base, c0);
+        if (threadIdx.x == 0) A.chunk_slot[b] = (int32_t)k0;
         __syncthreads();
-        chunk_slots(t, e_base, r_base, first_slot(t, e_base, c0), c0, c1,
+        chunk_slots(t, e_base, r_base, k0, c0, c1,
                     [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
-            const Span p(s, a0, a1, c0);
+            const Span p(s, a0, a1, c0, kBlock);
             const int rows = (int)((a1 - 1 - s.lo) / s.maxlen) - p.row_a + 1;
             const bool lds = ROWS && rows <= kLdsRows;
             if (lds) {
@@ -332,15 +367,22 @@ __global__ void __launch_bounds__(kBlock) policy_count_kernel(PolicyArgs A) {
                 __syncthreads();
             }
             int count = 0;
-            Group q = p.first();
-#pragma unroll 4
-            for (; q.o < p.o1; p.advance(&q)) {
-                const uint32_t on = count_mask(q, load_labels(labels, q.o, limit), p.maxlen, t.shift);
-                if (on) s_nibble[q.o / 4] |= (uint8_t)on;
-                if (lds)
-                    add_to_rows(s_rows, q, on, p.maxlen, p.row_a);
-                else
-                    count += __builtin_popcount(on);
+            Group q = p.first((int)threadIdx.x);
+            for (int o = p.o0 & ~3; o < p.o1; o += kAhead * p.ahead) {     // uniform
+                int4u y[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) y[i] = load4<int4u, false>(labels, q.o + i * p.ahead, last, kIgnore);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    settle<false>(&y[i], q.o, last, kIgnore);
+                    const uint32_t on = count_mask(q, y[i], p.maxlen, t.shift);
+                    if (on) s_nibble[q.o / 4] |= (uint8_t)on;
+                    if (lds)
+                        add_to_rows(s_rows, q, on, p.maxlen, p.row_a);
+                    else
+                        count += __builtin_popcount(on);
+                    p.advance(&q);
+                }
             }
             if (ROWS) {
                 // a row counts here if it starts and ends here; the others are joined by who needs the slot's rows
@@ -384,13 +426,11 @@ __device__ __forceinline__ float exp_near(float d) {
     return fabsf(u) < 200.0f ? fmaf(e * lost, kLn2, e) : e;
 }
 
-// exp(d) - 1 - d: below 1 by its series (the next term is under 2^-31 of the sum), where the
+// exp(d) - 1 - d: below 3/4 by its series (the next term is under 2^-27 of the sum), where the
 // difference would cancel.
 __device__ __forceinline__ float exp_less_line(float d) {
-    if (fabsf(d) < 1.0f) {
-        float q = 1.0f / 479001600.0f;
-        q = fmaf(q, d, 1.0f / 39916800.0f);
-        q = fmaf(q, d, 1.0f / 3628800.0f);
+    if (fabsf(d) < 0.75f) {
+        float q = 1.0f / 3628800.0f;
         q = fmaf(q, d, 1.0f / 362880.0f);
         q = fmaf(q, d, 1.0f / 40320.0f);
         q = fmaf(q, d, 1.0f / 5040.0f);
@@ -406,7 +446,7 @@ __device__ __forceinline__ float exp_less_line(float d) {
 
 struct TokenTerms {
     float policy, ratio, kl, grad, kl_grad;
-    int clip;    // 0 none, 1 below, 2 above, 3 by the dual bound
+    bool below, above, dual;    // clipped
 };
 
 // The bounds on lp - old, rounded to fp32.
@@ -414,56 +454,49 @@ struct Bounds {
     float low, high, dual;
 };
 
+template <int KL>
 __device__ __forceinline__ TokenTerms policy_token(const PolicyArgs& A, const Bounds& B, float lp, float old, float ref,
                                                    float adv) {
     TokenTerms o;
-    o.ratio = 1.0f;
-    o.clip = 0;
-    float bound = 1.0f;
-    if (A.old) {
-        const float d = lp - old;
-        bound = o.ratio = exp_near(d);
-        // rounding keeps order: the rounded difference decides unless it equals a rounded bound
-        const float up = adv > 0.0f ? B.high : B.dual;
-        bool above = d > up, below = d < B.low;
-        if (__builtin_expect(d == up || d == B.low, 0)) {
-            const double x = (double)lp - (double)old;
-            above = x > (adv > 0.0f ? A.at_high : A.at_dual);
-            below = x < A.at_low;
-        }
-        below = below && adv < 0.0f;
-        o.clip = below ? 1 : above ? (adv > 0.0f ? 2 : 3) : 0;
-        bound = below ? A.low : above ? (adv > 0.0f ? A.high : A.dual) : bound;
+    const float d = A.on_policy ? 0.0f : lp - old;
+    const bool pos = adv > 0.0f, neg = adv < 0.0f;     // neither for 0 and NaN: nothing is clipped
+    const float up = pos ? B.high : neg ? B.dual : INFINITY, low = neg ? B.low : -INFINITY;
+    bool over = d > up, under = d < low;
+    // rounding keeps order: the rounded difference decides unless it equals a rounded bound
+    if (__builtin_expect(d == up || d == low, 0)) {
+        const double x = A.on_policy ? 0.0 : (double)lp - (double)old;
+        over = x > (pos ? A.at_high : neg ? A.at_dual : HUGE_VAL);
+        under = neg && x < A.at_low;
     }
-    // no ratio clips an advantage of 0 (nor a NaN), and an overflowing one must not make it NaN
-    const bool none = adv == 0.0f;
-    o.clip = none || adv != adv ? 0 : o.clip;
-    o.policy = none ? 0.0f : -bound * adv;
-    o.grad = o.clip ? 0.0f : o.policy;
+    o.ratio = exp_near(d);
+    float bound = over ? (pos ? A.high : A.dual) : o.ratio;
+    bound = under ? A.low : bound;
+    o.below = under;
+    o.above = over && pos;
+    o.dual = over && neg;
+    o.policy = adv == 0.0f ? 0.0f : -bound * adv;     // an overflowing ratio must not make it NaN
+    o.grad = over || under ? 0.0f : o.policy;
     o.kl = o.kl_grad = 0.0f;
-    if (A.kl != ODB_KL_NONE) {
-        const float x = lp - ref;
-        if (A.kl == ODB_KL_LINEAR) {
-            o.kl = x;
-            o.kl_grad = 1.0f;
-        } else if (A.kl == ODB_KL_SQUARE) {
-            o.kl = 0.5f * x * x;
-            o.kl_grad = x;
-        } else {
-            o.kl = exp_less_line(-x);
-            o.kl_grad = x - o.kl;    // 1 - exp(-x)
-        }
+    const float x = lp - ref;
+    if (KL == ODB_KL_LINEAR) {
+        o.kl = x;
+        o.kl_grad = 1.0f;
+    } else if (KL == ODB_KL_SQUARE) {
+        o.kl = 0.5f * x * x;
+        o.kl_grad = x;
+    } else if (KL == ODB_KL_EXP) {
+        o.kl = exp_less_line(-x);
+        o.kl_grad = x - o.kl;    // 1 - exp(-x)
     }
     return o;
 }
 
-// What a thread has of a slot's part: a chunk gives it at most 64 elements, so four counts of
-// tokens by their clip (none among them) fit a word.
+// A thread's sums, and the wave's counts.
 struct PolicySums {
     double sum[4] = {0, 0, 0, 0};
-    uint32_t clips = 0;
+    int counted = 0;            // the thread's
+    int clipped[3] = {0, 0, 0};
 };
-static_assert(kMaxChunk / kBlock <= 255, "counts of a byte");
 
 // The chunk's part of every array, and what does not change from group to group.
 struct PolicyChunk {
@@ -474,84 +507,134 @@ struct PolicyChunk {
     const float* advantage;     // of the chunk (per token) or of the slot (per row)
     float* grad;
     float* grad_entropy;
-    int limit;
+    int last;
     float kl_coef, entropy_coef;
     Bounds bounds;
 };
 
-// A group's tokens: its part of the sums, its gradients.  weight(row, &f, &gs) gives the weight of a
-// row's token in the slot's mean and the factor of its gradient.  What does not count has all its
-// inputs replaced by 0.  Within a group the sums are formed in fp32.
-template <typename Weight>
-__device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyChunk& C, Group q, uint32_t on, int maxlen,
-                                             const Weight& weight, PolicySums& S) {
+// A group's inputs on their way.  A group in which nothing counts reads the chunk's first elements
+// instead, as all such do: no traffic, and no branch that parts the loads.
+struct PolicyLoads {
+    float4u lp, old, ref, H, adv;
+    int o;
+    uint32_t on;
+};
+
+template <int KL, bool SAFE>
+__device__ __forceinline__ PolicyLoads policy_load(const PolicyArgs& A, const PolicyChunk& C, Group q, uint32_t on,
+                                                   int maxlen, int row_a) {
+    PolicyLoads L;
+    L.on = on;
+    L.o = on ? q.o : 0;
+    L.lp = load4<float4u, SAFE>(C.logprob, L.o, C.last, 0.0f);
+    L.old = load4<float4u, SAFE>(C.old, L.o, C.last, 0.0f);
+    if (KL != ODB_KL_NONE) L.ref = load4<float4u, SAFE>(C.ref, L.o, C.last, 0.0f);
+    if (A.entropy) L.H = load4<float4u, SAFE>(C.entropy, L.o, C.last, 0.0f);
+    if (A.token_advantage) {
+        L.adv = load4<float4u, SAFE>(C.advantage, L.o, C.last, 0.0f);
+    } else {
+        L.adv[0] = C.advantage[on ? q.row : row_a];
+        L.adv[1] = L.adv[2] = L.adv[3] = L.adv[0];
+        if (on && q.col > maxlen - 4) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (on >> j & 1) L.adv[j] = C.advantage[q.row];
+                q.next(maxlen);
+            }
+        }
+    }
+    return L;
+}
+
+// A group's part of the sums, and its gradients.  weight(row, &f, &gs) gives the weight of a row's
+// token in the slot's mean and the factor of its gradient (ROWS: they differ from row to row).  What
+// does not count has its inputs replaced by 0, which makes all but the ratio and the KL term's slope
+// 0.  Within a group the sums are formed in fp32.  The whole wave takes part.
+template <int KL, bool ROWS, bool SAFE, typename Weight>
+__device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyChunk& C, Group q, PolicyLoads L,
+                                             int maxlen, const Weight& weight, PolicySums& S) {
     float g[4] = {0, 0, 0, 0}, ge[4] = {0, 0, 0, 0};
-    const Group q0 = q;
-    if (on) {      // what does not count is not read
-        const float4u zero = {0, 0, 0, 0};
-        const float4u lp = load_floats(C.logprob, q.o, C.limit);
-        const float4u old = A.old ? load_floats(C.old, q.o, C.limit) : zero;
-        const float4u ref = A.kl != ODB_KL_NONE ? load_floats(C.ref, q.o, C.limit) : zero;
-        const float4u H = A.entropy ? load_floats(C.entropy, q.o, C.limit) : zero;
-        const bool one_row = q.col <= maxlen - 4;
-        float4u adv;
+    if (__any(L.on != 0)) {
+        if (!SAFE && L.o > C.last) {
+            settle<SAFE>(&L.lp, L.o, C.last, 0.0f);
+            settle<SAFE>(&L.old, L.o, C.last, 0.0f);
+            if (KL != ODB_KL_NONE) settle<SAFE>(&L.ref, L.o, C.last, 0.0f);
+            if (A.entropy) settle<SAFE>(&L.H, L.o, C.last, 0.0f);
+            if (A.token_advantage) settle<SAFE>(&L.adv, L.o, C.last, 0.0f);
+        }
         float f[4], gs[4];
-        if (one_row) {
-            weight(q.row, &f[0], &gs[0]);
-            if (!A.token_advantage) adv[0] = C.advantage[q.row];
+        if (!ROWS) {
+            weight(0, &f[0], &gs[0]);
 #pragma unroll
             for (int j = 1; j < 4; ++j) {
                 f[j] = f[0];
                 gs[j] = gs[0];
-                if (!A.token_advantage) adv[j] = adv[0];
             }
         } else {
+            Group r = q;
+            float w = 0.0f, k = 0.0f;
+            int have = -1;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                f[j] = gs[j] = adv[j] = 0.0f;
-                if (on >> j & 1) {
-                    weight(q.row, &f[j], &gs[j]);
-                    if (!A.token_advantage) adv[j] = C.advantage[q.row];
+                if ((L.on >> j & 1) && r.row != have) {
+                    weight(r.row, &w, &k);
+                    have = r.row;
                 }
-                q.next(maxlen);
+                f[j] = w;
+                gs[j] = k;
+                r.next(maxlen);
             }
         }
-        if (A.token_advantage) adv = load_floats(C.advantage, q.o, C.limit);
         float sum[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const bool live = on >> j & 1;
-            const TokenTerms o = policy_token(A, C.bounds, live ? lp[j] : 0.0f, live ? old[j] : 0.0f,
-                                              live ? ref[j] : 0.0f, live ? adv[j] : 0.0f);
-            const float w = live ? f[j] : 0.0f;
-            sum[0] = fmaf(w, o.policy, sum[0]);
-            sum[1] = fmaf(w, o.kl, sum[1]);
-            if (A.entropy) sum[2] = fmaf(w, live ? H[j] : 0.0f, sum[2]);
-            sum[3] = fmaf(w, o.ratio, sum[3]);
-            S.clips += live ? 1u << (8 * o.clip) : 0u;
-            const float k = live ? gs[j] : 0.0f;
-            g[j] = k * fmaf(C.kl_coef, o.kl_grad, o.grad);
-            ge[j] = -C.entropy_coef * k;
+            const bool live = L.on >> j & 1;
+            const TokenTerms o = policy_token<KL>(A, C.bounds, live ? L.lp[j] : 0.0f, live ? L.old[j] : 0.0f,
+                                                  KL == ODB_KL_NONE ? 0.0f : live ? L.ref[j] : 0.0f,
+                                                  live ? L.adv[j] : 0.0f);
+            const float ratio = live ? o.ratio : 0.0f;
+            const float slope = KL == ODB_KL_LINEAR ? (live ? o.kl_grad : 0.0f) : o.kl_grad;
+            if (ROWS) {
+                sum[0] = fmaf(f[j], o.policy, sum[0]);
+                sum[1] = fmaf(f[j], o.kl, sum[1]);
+                sum[3] = fmaf(f[j], ratio, sum[3]);
+            } else {
+                sum[0] += o.policy;
+                sum[1] += o.kl;
+                sum[3] += ratio;
+            }
+            S.clipped[0] += __popcll(__ballot(o.below));
+            S.clipped[1] += __popcll(__ballot(o.above));
+            S.clipped[2] += __popcll(__ballot(o.dual));
+            g[j] = gs[j] * fmaf(C.kl_coef, slope, o.grad);
+        }
+        if (A.entropy) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool live = L.on >> j & 1;
+                sum[2] = fmaf(ROWS ? f[j] : 1.0f, live ? L.H[j] : 0.0f, sum[2]);
+                ge[j] = live ? -C.entropy_coef * gs[j] : 0.0f;
+            }
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) S.sum[j] += sum[j];
+        S.counted += __builtin_popcount(L.on);
     }
-    if (A.grad) store4(C.grad, q0, g);
-    if (A.grad_entropy) store4(C.grad_entropy, q0, ge);
+    if (q.mask) {
+        if (A.grad) store4(C.grad, q, g);
+        if (A.grad_entropy) store4(C.grad_entropy, q, ge);
+    }
 }
 
-// Sums of the block's part of a slot, to its partial.
-__device__ __forceinline__ void leave_part(const PolicyArgs& A, const PolicySums& S, double same, int64_t at) {
+// The block's part of a slot from its threads', on thread 0.
+__device__ __forceinline__ SlotPart block_part(const PolicySums& S, double same) {
     __shared__ SlotPart s_part[kWaves];
     SlotPart p;
 #pragma unroll
     for (int j = 0; j < 4; ++j) p.sum[j] = wave_total(S.sum[j]);
-    p.counted = wave_total((int)(S.clips & 0xff));
+    p.counted = wave_total(S.counted);
 #pragma unroll
-    for (int j = 0; j < 3; ++j) {
-        p.clipped[j] = wave_total((int)(S.clips >> (8 * (j + 1)) & 0xff));
-        p.counted += p.clipped[j];
-    }
+    for (int j = 0; j < 3; ++j) p.clipped[j] = S.clipped[j];
     if ((threadIdx.x & (kWave - 1)) == 0) s_part[threadIdx.x / kWave] = p;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -561,44 +644,85 @@ __device__ __forceinline__ void leave_part(const PolicyArgs& A, const PolicySums
             p.counted += s_part[w].counted;
         }
         for (int j = 0; j < 4; ++j) p.sum[j] *= same;
-        A.slot_part[at] = p;
     }
     __syncthreads();
+    return p;
+}
+
+// A slot's numbers from its sums.
+__device__ __forceinline__ void leave_slot(const PolicyArgs& A, int64_t k, const double sum[4], int64_t counted,
+                                           const int64_t clipped[3]) {
+    const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
+    A.slot_loss[k] = counted > 0 ? (float)(scale * (sum[0] + A.kl_coef * sum[1] - A.entropy_coef * sum[2])) : 0.0f;
+    for (int i = 0; i < 4; ++i) A.slot_means[4 * k + i] = (float)sum[i];
+    A.slot_counts[4 * k] = counted;
+    for (int i = 0; i < 3; ++i) A.slot_counts[4 * k + 1 + i] = clipped[i];
+}
+
+__device__ __forceinline__ PolicyChunk policy_chunk(const PolicyArgs& A, const SlotView& s, int64_t c0) {
+    PolicyChunk C;
+    C.logprob = A.logprob + c0;
+    C.old = A.old + c0;
+    C.ref = A.ref + c0;
+    C.entropy = A.entropy + c0;
+    C.advantage = A.advantage + (A.token_advantage ? c0 : s.row0);
+    C.grad = A.grad + c0;
+    C.grad_entropy = A.grad_entropy + c0;
+    C.last = last_four(A.t, c0);
+    C.kl_coef = (float)A.kl_coef;
+    C.entropy_coef = (float)A.entropy_coef;
+    C.bounds = Bounds{(float)A.at_low, (float)A.at_high, (float)A.at_dual};
+    return C;
+}
+
+// The block's part of a slot: counted(group) tells which elements count.
+template <int KL, bool ROWS, bool SAFE, typename Counted, typename Weight>
+__device__ __forceinline__ void policy_span(const PolicyArgs& A, const PolicyChunk& C, const Span& p,
+                                            const Counted& counted, const Weight& weight, PolicySums& S) {
+    // uniform over the block: a wave's lanes stay together, those behind the slot with nothing to do
+    Group q = p.first((int)threadIdx.x);
+    for (int o = p.o0 & ~3; o < p.o1; o += p.ahead, p.advance(&q)) {
+        const PolicyLoads L = policy_load<KL, SAFE>(A, C, q, q.mask ? counted(q) : 0, p.maxlen, p.row_a);
+        policy_group<KL, ROWS, SAFE>(A, C, q, L, p.maxlen, weight, S);
+    }
 }
 
 // Counted tokens of a row, over the chunks it touches.
 __device__ __forceinline__ int row_tokens(const PolicyArgs& A, const SlotView& s, int64_t row) {
     const int64_t start = s.lo + row * s.maxlen;
     int n = 0;
-    for (int64_t b = start / A.chunk; b <= (start + s.maxlen - 1) / A.chunk; ++b) n += A.row_count[b + s.row0 + row];
+    const int64_t last = (start + s.maxlen - 1) >> A.chunk_log2;
+    for (int64_t b = start >> A.chunk_log2; b <= last; ++b) n += A.row_count[b + s.row0 + row];
     return n;
 }
 
 // Sum over a slot's chunks, one a lane, of f(chunk): a whole number that may pass 2^31.
 template <typename F>
 __device__ __forceinline__ double slot_total(const PolicyArgs& A, const SlotView& s, const F& f) {
-    const int64_t first = s.lo / A.chunk, last = (s.hi - 1) / A.chunk;
+    const int64_t first = s.lo >> A.chunk_log2, last = (s.hi - 1) >> A.chunk_log2;
     double n = 0;
     for (int64_t j = first + (threadIdx.x & (kWave - 1)); j <= last; j += kWave) n += f(j);
     return wave_total(n);
 }
 
-// The loss and its gradient, the elements that count given by the bits (LABELS: by the labels; a sum
+// The loss and its gradient, the elements that count given by the bits (by the labels for a sum, which
 // needs no weights and so no pass before).
-template <bool ROWS, bool LABELS>
+template <int KL, int REDUCE>
 __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
+    constexpr bool ROWS = REDUCE == ODB_REDUCE_ROW_MEAN, LABELS = REDUCE == ODB_REDUCE_SUM;
     __shared__ double s_weight[ROWS ? kLdsRows : 1];
+    __shared__ uint32_t s_bits[LABELS ? 1 : kMaxChunk / 32];
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int64_t total = run_elems(t, e_base);
     for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
         const int64_t c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
         if (c0 >= c1) break;
-        const int limit = chunk_limit(t, c0);
-        const uint32_t* bits = A.bits + b * (A.chunk / 32);
-        chunk_slots(t, e_base, r_base, first_slot(t, e_base, c0), c0, c1,
+        const int64_t k0 = LABELS ? first_slot(t, e_base, c0) : (int64_t)A.chunk_slot[b];
+        if (!LABELS) load_bits(s_bits, A.bits, b, A.chunk);
+        chunk_slots(t, e_base, r_base, k0, c0, c1,
                     [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
-            const Span p(s, a0, a1, c0);
+            const Span p(s, a0, a1, c0, kBlock);
             const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
             double same = 1.0;       // weight of every token, where rows have none of their own
             double rows = 0;         // of the slot, with a counted token
@@ -638,29 +762,81 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
                     *gs = factor;
                 }
             };
-            PolicyChunk C;
-            C.logprob = A.logprob + c0;
-            C.old = A.old + c0;
-            C.ref = A.ref + c0;
-            C.entropy = A.entropy + c0;
-            C.advantage = A.advantage + (A.token_advantage ? c0 : s.row0);
-            C.grad = A.grad + c0;
-            C.grad_entropy = A.grad_entropy + c0;
-            C.limit = limit;
-            C.kl_coef = (float)A.kl_coef;
-            C.entropy_coef = (float)A.entropy_coef;
-            C.bounds = Bounds{(float)A.at_low, (float)A.at_high, (float)A.at_dual};
+            const PolicyChunk C = policy_chunk(A, s, c0);
+            auto counted = [&](const Group& q) {
+                if (!LABELS) return s_bits[q.o / 32] >> (q.o & 31) & q.mask;
+                int4u y = load4<int4u, false>(t.d_labels + c0, q.o, C.last, kIgnore);
+                settle<false>(&y, q.o, C.last, kIgnore);
+                return count_mask(q, y, p.maxlen, t.shift);
+            };
             PolicySums S;
-            Group q = p.first();
-            for (; q.o < p.o1; p.advance(&q)) {
-                const uint32_t on = LABELS ? count_mask(q, load_labels(t.d_labels + c0, q.o, limit), p.maxlen, t.shift)
-                                           : bits[q.o / 32] >> (q.o & 31) & q.mask;
-                policy_group(A, C, q, on, p.maxlen, weight, S);
-            }
-            leave_part(A, S, same, b + k);
+            policy_span<KL, ROWS, false>(A, C, p, counted, weight, S);
+            const SlotPart part = block_part(S, same);
+            if (threadIdx.x == 0) A.slot_part[b + k] = part;
         });
     }
 }
+
+// A run of one chunk, in one launch of one block: 6 us for 256 elements where the passes take 12.
+template <int KL>
+__global__ void __launch_bounds__(kBlock) policy_one_kernel(PolicyArgs A, int reduce) {
+    __shared__ uint8_t s_nibble[kOneChunk / 4];
+    __shared__ int s_rows[kOneChunk];
+    const odb_tiles_t& t = A.t;
+    const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
+    const int64_t total = run_elems(t, e_base), none[3] = {0, 0, 0};
+    const double nothing[4] = {0, 0, 0, 0};
+    for (int64_t k = threadIdx.x; k < t.num_slots; k += kBlock) {
+        leave_slot(A, k, nothing, 0, none);
+        if (A.status && !slot_view(t, k, e_base, r_base).ok) *A.status = kErrTiles;
+    }
+    __syncthreads();
+    if (total == 0) return;
+    chunk_slots(t, e_base, r_base, first_slot(t, e_base, 0), 0, total,
+                [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+        const Span p(s, a0, a1, 0, kBlock);
+        const PolicyChunk C = policy_chunk(A, s, 0);
+        for (int i = threadIdx.x; i < s.rows; i += kBlock) s_rows[i] = 0;
+        __syncthreads();
+        int count = 0;
+        for (Group q = p.first((int)threadIdx.x); q.o < p.o1; p.advance(&q)) {
+            const uint32_t on = count_mask(q, load4<int4u, true>(t.d_labels, q.o, C.last, kIgnore), p.maxlen, t.shift);
+            s_nibble[q.o / 4] = (uint8_t)on;
+            count += __builtin_popcount(on);
+            if (reduce == ODB_REDUCE_ROW_MEAN) add_to_rows(s_rows, q, on, p.maxlen, 0);
+        }
+        __syncthreads();
+        if (reduce == ODB_REDUCE_ROW_MEAN) {
+            count = 0;
+            for (int i = threadIdx.x; i < s.rows; i += kBlock) count += s_rows[i] > 0;
+        }
+        count = block_total(count);
+        const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
+        const double same = reduce == ODB_REDUCE_SUM ? 1.0 : count > 0 ? 1.0 / count : 0.0;
+        auto weight = [&](int row, float* f, float* gs) {
+            const double w = reduce == ODB_REDUCE_ROW_MEAN ? 1.0 / ((double)s_rows[row] * count) : same;
+            *f = (float)w;
+            *gs = (float)(scale * w);
+        };
+        PolicySums S;
+        policy_span<KL, true, true>(A, C, p, [&](const Group& q) { return (uint32_t)s_nibble[q.o / 4]; }, weight, S);
+        const SlotPart part = block_part(S, 1.0);
+        if (threadIdx.x == 0) {
+            const int64_t clipped[3] = {part.clipped[0], part.clipped[1], part.clipped[2]};
+            leave_slot(A, k, part.sum, part.counted, clipped);
+        }
+    });
+}
+
+using PolicyOneKernel = void (*)(PolicyArgs, int);
+const PolicyOneKernel policy_one_kernels[4] = {policy_one_kernel<0>, policy_one_kernel<1>, policy_one_kernel<2>,
+                                               policy_one_kernel<3>};
+
+using PolicyKernel = void (*)(PolicyArgs);
+#define ODB_POLICY_KERNELS(KL) {policy_kernel<KL, 0>, policy_kernel<KL, 1>, policy_kernel<KL, 2>}
+const PolicyKernel policy_kernels[4][3] = {ODB_POLICY_KERNELS(0), ODB_POLICY_KERNELS(1), ODB_POLICY_KERNELS(2),
+                                           ODB_POLICY_KERNELS(3)};   // by odb_kl_t and odb_reduce_t
+#undef ODB_POLICY_KERNELS
 
 // The slots' numbers from their chunks' partials, a wave a slot.
 __global__ void __launch_bounds__(kBlock) policy_slots_kernel(PolicyArgs A) {
@@ -675,7 +851,7 @@ __global__ void __launch_bounds__(kBlock) policy_slots_kernel(PolicyArgs A) {
         if (!s.ok) {
             if (A.status && lane == 0) *A.status = kErrTiles;
         } else if (s.hi > s.lo) {
-            for (int64_t j = s.lo / A.chunk + lane; j <= (s.hi - 1) / A.chunk; j += kWave) {
+            for (int64_t j = (s.lo >> A.chunk_log2) + lane; j <= (s.hi - 1) >> A.chunk_log2; j += kWave) {
                 const SlotPart p = A.slot_part[j + k];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[i] += p.sum[i];
@@ -690,11 +866,8 @@ __global__ void __launch_bounds__(kBlock) policy_slots_kernel(PolicyArgs A) {
         for (int i = 0; i < 3; ++i) clipped[i] = wave_total(clipped[i]);
         n = wave_total(n);
         if (lane == 0) {
-            const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
-            A.slot_loss[k] = n > 0 ? (float)(scale * (sum[0] + A.kl_coef * sum[1] - A.entropy_coef * sum[2])) : 0.0f;
-            for (int i = 0; i < 4; ++i) A.slot_means[4 * k + i] = (float)sum[i];
-            A.slot_counts[4 * k] = (int64_t)n;
-            for (int i = 0; i < 3; ++i) A.slot_counts[4 * k + 1 + i] = (int64_t)clipped[i];
+            const int64_t c[3] = {(int64_t)clipped[0], (int64_t)clipped[1], (int64_t)clipped[2]};
+            leave_slot(A, k, sum, (int64_t)n, c);
         }
     }
 }
@@ -714,6 +887,7 @@ struct PairArgs {
     double* coef;
     PairPart* part;
     uint32_t* bits;
+    int32_t* chunk_slot;
     float* loss;
     float* row_loss;
     float* row_reward;
@@ -722,124 +896,179 @@ struct PairArgs {
     int32_t* status;
     int64_t chunks;
     double beta, margin, smoothing, loss_scale;
-    int32_t kind, chunk;
+    int32_t kind, chunk, quarter_log2;
     bool normalize;
 };
 
-constexpr int kLongRow = 1024;
-constexpr int kAhead = 4;          // groups of a lane whose loads are under way together
+constexpr int kShortRow = 64;      // rows up to here are taken several at a time
+constexpr int kRowAhead = 2;       // groups of a lane whose loads (two or three each) are under way together
 
-__device__ __forceinline__ void mark(uint32_t* s_bits, int at, uint32_t nibble) {
-    if (!nibble) return;
-    const uint64_t w = (uint64_t)nibble << (at & 31);
-    atomicOr(&s_bits[at >> 5], (uint32_t)w);
-    if (w >> 32) atomicOr(&s_bits[(at >> 5) + 1], (uint32_t)(w >> 32));
-}
-
-// Positions [a, b) of a chunk, which lie in one row: four a lane of the `lanes` that share it.  How
-// many count (from position `from` on), and the sum of logprob - ref over them.
-__device__ __forceinline__ void row_run(const PairArgs& A, int64_t c0, int limit, int a, int b, int from, int lane,
-                                        int lanes, uint32_t* s_bits, int* count, double* sum) {
-    const int32_t* labels = A.t.d_labels + c0;
-    const float* logprob = A.logprob + c0;
-    const float* ref = A.ref + c0;
-    for (int o0 = a + 4 * lane; o0 < b; o0 += 4 * kAhead * lanes) {
-        int4u y[kAhead];
-        float4u p[kAhead], r[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int o = o0 + 4 * i * lanes;
-            if (o < b) {
-                y[i] = load_labels(labels, o, limit);
-                p[i] = load_floats(logprob, o, limit);
-                if (A.ref) r[i] = load_floats(ref, o, limit);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int o = o0 + 4 * i * lanes;
-            if (o < b) {
-                uint32_t on = b - o >= 4 ? 0xfu : 0xfu >> (4 - (b - o));
-                if (o < from) on &= 0xfu << (from - o < 4 ? from - o : 4);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (y[i][j] == ODB_LABEL_IGNORE) on &= ~(1u << j);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const double x = A.ref ? (double)p[i][j] - (double)r[i][j] : (double)p[i][j];
-                    *sum += on >> j & 1 ? x : 0.0;
-                }
-                *count += __builtin_popcount(on);
-                mark(s_bits, o, on);
-            }
+// What a wave leaves of a row in its quarter of a chunk, by its lane 0; the records count quarters.
+__device__ __forceinline__ void leave_row(const PairArgs& A, const SlotView& s, int64_t part, int64_t c0, int row,
+                                          int count, double sum, int lane) {
+    if (lane != 0) return;
+    const int64_t at = s.row0 + row, start = s.lo + (int64_t)row * s.maxlen;
+    A.row_count[part + at] = count;
+    A.row_sum[part + at] = sum;
+    if (start >= c0) {   // the row starts here
+        const int64_t last = (start + s.maxlen - 1) >> A.quarter_log2;
+        A.row_info[at] = RowInfo{(int32_t)part, (int32_t)(last - part + 1)};
+        if (A.row_of) {
+            const int32_t id = A.row_ids[at];
+            if (id >= 0 && id < A.num_ids) atomicMin(&A.row_of[id], (int32_t)at);
         }
     }
 }
 
-// First pass: the bits, and per chunk and row how many tokens count and the sum over them.  A row is
-// taken by the smallest power of two of lanes that covers it four elements each, up to a wave; rows
-// of more than 1,024 elements by the block.
-__global__ void __launch_bounds__(kBlock) row_sums_kernel(PairArgs A) {
-    __shared__ uint32_t s_bits[kMaxChunk / 32];
+// The lowest n of four bits.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 4 ? 0xfu : (1u << n) - 1; }
+
+// Elements that count of a group and, one by one, logprob - ref.
+struct RowTerms {
+    uint32_t on;
+    double x[4];
+};
+
+template <bool REF>
+__device__ __forceinline__ RowTerms row_terms(const int4u& y, const float4u& p, const float4u& r, uint32_t mask) {
+    RowTerms o;
+    o.on = mask;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (y[j] == ODB_LABEL_IGNORE) o.on &= ~(1u << j);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const double x = REF ? (double)p[j] - (double)r[j] : (double)p[j];
+        o.x[j] = o.on >> j & 1 ? x : 0.0;
+    }
+    return o;
+}
+
+// First pass: the bits, and per quarter of a chunk and row how many tokens count and the sum over
+// them.  A wave takes a quarter.  Rows of more than 64 elements are summed across the wave as its 256
+// elements at a time come in and are left where they end: the loads do not wait for the reductions.
+// Shorter ones are taken by the smallest power of two of lanes that covers them four elements each.
+template <bool REF, bool SAFE>
+__device__ __forceinline__ void row_sums(const PairArgs& A) {
+    __shared__ uint32_t s_bits[SAFE ? kOneChunk / 32 : kMaxChunk / 32];
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int64_t total = run_elems(t, e_base);
-    const int words = A.chunk / 32;
+    const int words = A.chunk / 32, quarter = A.chunk / kWaves;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
-        const int64_t c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
-        if (c0 >= c1) break;
-        const int limit = chunk_limit(t, c0);
+        if (b * A.chunk >= total) break;
         for (int i = threadIdx.x; i < words; i += kBlock) s_bits[i] = 0;
         __syncthreads();
-        chunk_slots(t, e_base, r_base, first_slot(t, e_base, c0), c0, c1,
-                    [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
-            const int64_t row_a = (a0 - s.lo) / s.maxlen, row_b = (a1 - 1 - s.lo) / s.maxlen;
-            const bool wide = s.maxlen > kLongRow;
-            int lanes = 1;
-            while (lanes < kWave && 4 * lanes < s.maxlen) lanes *= 2;
-            if (wide) lanes = kBlock;
-            const int lane = threadIdx.x & (lanes - 1);
-            const int step = kBlock / lanes;
-            // every group goes round as often as the first, so that no lane leaves a reduction alone
-            for (int64_t r0 = row_a; r0 <= row_b; r0 += step) {
-                const int64_t r = r0 + threadIdx.x / lanes;
-                const bool live = r <= row_b;
-                const int64_t start = s.lo + r * s.maxlen;
-                int count = 0;
-                double sum = 0.0;
-                if (live) {
-                    const int64_t x0 = start > a0 ? start : a0, x1 = start + s.maxlen < a1 ? start + s.maxlen : a1;
-                    // the row's start may lie far before the chunk
-                    const int from = start + t.shift > c0 ? (int)(start + t.shift - c0) : 0;
-                    row_run(A, c0, limit, (int)(x0 - c0), (int)(x1 - c0), from, lane, lanes, s_bits, &count, &sum);
-                }
-                if (wide) {
-                    count = block_total(count);
-                    sum = block_total(sum);
-                } else if (lanes == kWave) {
-                    count = wave_total(count);
-                    sum = wave_total(sum);
-                } else {
-                    for (int d = lanes / 2; d > 0; d >>= 1) {
-                        count += __shfl_xor(count, d, kWave);
-                        sum += __shfl_xor(sum, d, kWave);
-                    }
-                }
-                if (live && lane == 0) {
-                    const int64_t row = s.row0 + r;
-                    A.row_count[b + row] = count;
-                    A.row_sum[b + row] = sum;
-                    if (start >= c0) {   // the row starts here
-                        const int64_t last = (start + s.maxlen - 1) / A.chunk;
-                        A.row_info[row] = RowInfo{(int32_t)b, (int32_t)(last - b + 1)};
-                        if (A.row_of) {
-                            const int32_t id = A.row_ids[row];
-                            if (id >= 0 && id < A.num_ids) atomicMin(&A.row_of[id], (int32_t)row);
+        const int64_t part = b * kWaves + wave, c0 = part * quarter, c1 = c0 + quarter < total ? c0 + quarter : total;
+        uint32_t* bits = s_bits + wave * (quarter / 32);
+        const int64_t k0 = c0 < c1 ? first_slot(t, e_base, c0) : 0;
+        if (threadIdx.x == 0) A.chunk_slot[b] = (int32_t)k0;     // the first wave's quarter starts the chunk
+        const int last = last_four(t, c0);
+        const int32_t* labels = t.d_labels + c0;
+        const float* logprob = A.logprob + c0;
+        const float* ref = A.ref + c0;
+        if (c0 < c1)
+            chunk_slots(t, e_base, r_base, k0, c0, c1, [&](int64_t, const SlotView& s, int64_t a0, int64_t a1) {
+                if (s.maxlen > kShortRow) {
+                    const int o0 = (int)(a0 - c0), o1 = (int)(a1 - c0);
+                    int row = (int)((a0 - s.lo) / s.maxlen);
+                    // the current row's positions in the quarter; its start may lie before, its end behind
+                    int64_t ends = s.lo + ((int64_t)row + 1) * s.maxlen - c0;
+                    int begin = ends - s.maxlen >= 0 ? (int)(ends - s.maxlen) + t.shift : 0;
+                    int count = 0;          // of the wave
+                    double sum = 0.0;       // of the lane
+                    for (int o = o0 & ~3; o < o1; o += 4 * kWave * kRowAhead) {   // uniform
+                        int4u y[kRowAhead];
+                        float4u lp[kRowAhead], rf[kRowAhead];
+#pragma unroll
+                        for (int i = 0; i < kRowAhead; ++i) {
+                            const int at = o + 4 * (kWave * i + lane);
+                            y[i] = load4<int4u, SAFE>(labels, at, last, kIgnore);
+                            lp[i] = load4<float4u, SAFE>(logprob, at, last, 0.0f);
+                            if (REF) rf[i] = load4<float4u, SAFE>(ref, at, last, 0.0f);
+                        }
+#pragma unroll
+                        for (int i = 0; i < kRowAhead; ++i) {
+                            const int from = o + 4 * kWave * i, at = from + 4 * lane;
+                            if (from >= o1) break;     // uniform
+                            const int to = from + 4 * kWave < o1 ? from + 4 * kWave : o1;
+                            uint32_t real = 0, on = 0;
+                            double x[4] = {0, 0, 0, 0};
+                            if (!SAFE && at > last) {
+                                settle<SAFE>(&y[i], at, last, kIgnore);
+                                settle<SAFE>(&lp[i], at, last, 0.0f);
+                                if (REF) settle<SAFE>(&rf[i], at, last, 0.0f);
+                            }
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                real |= (uint32_t)(y[i][j] != ODB_LABEL_IGNORE) << j;
+                                x[j] = REF ? (double)lp[i][j] - (double)rf[i][j] : (double)lp[i][j];
+                            }
+                            for (;;) {     // the rows in these 256 elements; uniform
+                                const int z = ends < to ? (int)ends : to;
+                                const uint32_t mine = real & low_bits(z - at) & ~low_bits(begin - at);   // none behind the slot
+                                on |= mine;
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    const bool live = mine >> j & 1;
+                                    sum += live ? x[j] : 0.0;
+                                    count += __popcll(__ballot(live));
+                                }
+                                if (ends > to || (ends == to && to == o1)) break;
+                                leave_row(A, s, part, c0, row, count, wave_total(sum), lane);
+                                count = 0;
+                                sum = 0.0;
+                                ++row;
+                                begin = (int)ends + t.shift;
+                                ends += s.maxlen;
+                                if (begin - t.shift >= to) break;
+                            }
+                            if (on) atomicOr(&bits[at >> 5], on << (at & 31));
                         }
                     }
+                    leave_row(A, s, part, c0, row, count, wave_total(sum), lane);
+                } else {
+                    const int row_a = (int)((a0 - s.lo) / s.maxlen), row_b = (int)((a1 - 1 - s.lo) / s.maxlen);
+                    int lanes = 1;
+                    while (4 * lanes < s.maxlen) lanes *= 2;
+                    const int sub = lane & (lanes - 1);
+                    // every group of lanes goes round as often as the first, so that none leaves a reduction alone
+                    for (int r0 = row_a; r0 <= row_b; r0 += kWave / lanes) {
+                        const int r = r0 + lane / lanes;
+                        int count = 0;
+                        double sum = 0.0;
+                        if (r <= row_b) {
+                            // positions in the quarter; a row's start may lie before it
+                            const int start = (int)(s.lo + (int64_t)r * s.maxlen - c0);
+                            const int x0 = start > (int)(a0 - c0) ? start : (int)(a0 - c0);
+                            const int x1 = start + s.maxlen < (int)(a1 - c0) ? start + s.maxlen : (int)(a1 - c0);
+                            const int o = x0 + 4 * sub, from = start + t.shift;
+                            if (o < x1) {
+                                uint32_t mask = x1 - o >= 4 ? 0xfu : 0xfu >> (4 - (x1 - o));
+                                if (o < from) mask &= 0xfu << (from - o < 4 ? from - o : 4);
+                                int4u y = load4<int4u, SAFE>(labels, o, last, kIgnore);
+                                float4u lp = load4<float4u, SAFE>(logprob, o, last, 0.0f), rf = {0, 0, 0, 0};
+                                if (REF) rf = load4<float4u, SAFE>(ref, o, last, 0.0f);
+                                settle<SAFE>(&y, o, last, kIgnore);
+                                settle<SAFE>(&lp, o, last, 0.0f);
+                                if (REF) settle<SAFE>(&rf, o, last, 0.0f);
+                                const RowTerms v = row_terms<REF>(y, lp, rf, mask);
+                                count = __builtin_popcount(v.on);
+                                sum = (v.x[0] + v.x[1]) + (v.x[2] + v.x[3]);
+                                const uint64_t w = (uint64_t)v.on << (o & 31);
+                                if ((uint32_t)w) atomicOr(&bits[o >> 5], (uint32_t)w);
+                                if (w >> 32) atomicOr(&bits[(o >> 5) + 1], (uint32_t)(w >> 32));
+                            }
+                        }
+                        for (int d = lanes / 2; d > 0; d >>= 1) {
+                            count += __shfl_xor(count, d, kWave);
+                            sum += __shfl_xor(sum, d, kWave);
+                        }
+                        if (r <= row_b) leave_row(A, s, part, c0, r, count, sum, sub);
+                    }
                 }
-            }
-        });
+            });
         __syncthreads();
         for (int i = threadIdx.x; i < words; i += kBlock) A.bits[b * words + i] = s_bits[i];
         __syncthreads();
@@ -849,9 +1078,14 @@ __global__ void __launch_bounds__(kBlock) row_sums_kernel(PairArgs A) {
             if (!slot_view(t, k, e_base, r_base).ok) *A.status = kErrTiles;
 }
 
+template <bool REF>
+__global__ void __launch_bounds__(kBlock) row_sums_kernel(PairArgs A) {
+    row_sums<REF, false>(A);
+}
+
 // Clears the entries of the ids that have a row.  The others hold anything: an entry is believed
 // only if the row that it names has the id.
-__global__ void __launch_bounds__(kBlock) clear_rows_kernel(PairArgs A) {
+__device__ __forceinline__ void clear_rows(const PairArgs& A) {
     const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
     for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < rows; i += (int64_t)gridDim.x * kBlock) {
         const int32_t id = A.row_ids[i];
@@ -859,13 +1093,15 @@ __global__ void __launch_bounds__(kBlock) clear_rows_kernel(PairArgs A) {
     }
 }
 
+__global__ void __launch_bounds__(kBlock) clear_rows_kernel(PairArgs A) { clear_rows(A); }
+
 // A row's log ratio; nothing is read outside its partials whatever its record holds.
 __device__ __forceinline__ double log_ratio(const PairArgs& A, int64_t row, int* count) {
     const RowInfo f = A.row_info[row];
     int n = 0;
     double s = 0.0;
-    if (f.first >= 0 && f.chunks > 0 && (int64_t)f.first + f.chunks <= A.chunks) {
-        for (int64_t b = f.first; b < (int64_t)f.first + f.chunks; ++b) {
+    if (f.first >= 0 && f.parts > 0 && (int64_t)f.first + f.parts <= kWaves * A.chunks) {
+        for (int64_t b = f.first; b < (int64_t)f.first + f.parts; ++b) {
             n += A.row_count[b + row];
             s += A.row_sum[b + row];
         }
@@ -891,115 +1127,173 @@ __device__ __forceinline__ int64_t partner_row(const PairArgs& A, int64_t row, i
     }
     *chosen = v > 0;
     if (!A.row_ids) return other < rows ? other : -1;
-    if (A.row_of[id] != row) return -1;        // a later row of an id that has one already
-    const int64_t j = A.row_of[other];
+    // written by atomics, in one block's case in this launch: read behind the first cache
+    auto row_of = [&](int64_t i) {
+        return (int64_t)__hip_atomic_load(&A.row_of[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    };
+    if (row_of(id) != row) return -1;        // a later row of an id that has one already
+    const int64_t j = row_of(other);
     return j >= 0 && j < rows && A.row_ids[j] == other ? j : -1;
+}
+
+// What a thread's rows add up to.
+struct PairSums {
+    double loss = 0.0;
+    int pairs = 0, right = 0;
+};
+
+// A row's loss (at the chosen row of a pair) and reward, if `out`, and the factor of its tokens' gradients.
+__device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64_t rows, bool out, PairSums* sums) {
+    int n, m;
+    const double S = log_ratio(A, row, &n);
+    bool chosen;
+    const int64_t j = partner_row(A, row, rows, &chosen);
+    double c = 0.0, loss = 0.0;
+    if (j >= 0) {
+        const double T = log_ratio(A, j, &m);
+        const double h = A.beta * (chosen ? S - T : T - S) - A.margin;
+        double dh;
+        if (A.kind == ODB_PREFERENCE_SIGMOID) {
+            const double q = exp(-fabs(h)), soft = log1p(q);           // -ln s(|h|)
+            const double far = 1.0 / (1.0 + q), near = q / (1.0 + q);  // s(|h|), s(-|h|)
+            const double up = h >= 0 ? far : near, down = h >= 0 ? near : far;
+            loss = (1.0 - A.smoothing) * (soft + (h < 0 ? -h : 0.0)) + A.smoothing * (soft + (h > 0 ? h : 0.0));
+            dh = A.smoothing * up - (1.0 - A.smoothing) * down;
+        } else if (A.kind == ODB_PREFERENCE_HINGE) {
+            loss = h < 1.0 ? 1.0 - h : 0.0;
+            dh = h < 1.0 ? -1.0 : 0.0;
+        } else {
+            loss = (h - 0.5) / A.beta;
+            dh = 2.0 * loss / A.beta;
+            loss *= loss;
+        }
+        c = A.loss_scale * A.beta * (chosen ? dh : -dh);
+        if (A.normalize) c /= n > 0 ? n : 1;
+        loss = chosen ? A.loss_scale * loss : 0.0;
+        sums->loss += loss;
+        sums->pairs += chosen;
+        sums->right += chosen && S > T;
+    }
+    if (out) {
+        A.row_loss[row] = (float)loss;
+        A.row_reward[row] = (float)(A.beta * S);
+    }
+    return c;
 }
 
 __global__ void __launch_bounds__(kBlock) pairs_kernel(PairArgs A) {
     const odb_tiles_t& t = A.t;
     const int64_t rows = run_rows(t, t.d_slot_row_off[0]);
     const int64_t row = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    double loss = 0.0;
-    int pairs = 0, right = 0;
-    if (row < rows) {
-        int n, m;
-        const double S = log_ratio(A, row, &n);
-        bool chosen;
-        const int64_t j = partner_row(A, row, rows, &chosen);
-        double c = 0.0;
-        if (j >= 0) {
-            const double T = log_ratio(A, j, &m);
-            const double h = A.beta * (chosen ? S - T : T - S) - A.margin;
-            double dh;
-            if (A.kind == ODB_PREFERENCE_SIGMOID) {
-                const double q = exp(-fabs(h)), soft = log1p(q);           // -ln s(|h|)
-                const double far = 1.0 / (1.0 + q), near = q / (1.0 + q);  // s(|h|), s(-|h|)
-                const double up = h >= 0 ? far : near, down = h >= 0 ? near : far;
-                loss = (1.0 - A.smoothing) * (soft + (h < 0 ? -h : 0.0)) + A.smoothing * (soft + (h > 0 ? h : 0.0));
-                dh = A.smoothing * up - (1.0 - A.smoothing) * down;
-            } else if (A.kind == ODB_PREFERENCE_HINGE) {
-                loss = h < 1.0 ? 1.0 - h : 0.0;
-                dh = h < 1.0 ? -1.0 : 0.0;
-            } else {
-                loss = (h - 0.5) / A.beta;
-                dh = 2.0 * loss / A.beta;
-                loss *= loss;
-            }
-            c = A.loss_scale * A.beta * (chosen ? dh : -dh);
-            if (A.normalize) c /= n > 0 ? n : 1;
-            loss *= A.loss_scale;
-            if (chosen) {
-                pairs = 1;
-                right = S > T;
-            } else {
-                loss = 0.0;
-            }
-        }
-        A.coef[row] = c;
-        A.row_loss[row] = (float)loss;
-        A.row_reward[row] = (float)(A.beta * S);
-    }
+    PairSums sums;
+    if (row < rows) A.coef[row] = pair_row(A, row, rows, true, &sums);
     PairPart p;
-    p.loss = block_total(loss);
-    p.pairs = block_total(pairs);
-    p.right = block_total(right);
+    p.loss = block_total(sums.loss);
+    p.pairs = block_total(sums.pairs);
+    p.right = block_total(sums.right);
     if (threadIdx.x == 0) A.part[blockIdx.x] = p;
 }
 
-// Gradients of the tiles; the first block also sums what the pairs left.
-__global__ void __launch_bounds__(kBlock) pairs_grad_kernel(PairArgs A, int64_t parts) {
-    const odb_tiles_t& t = A.t;
-    if (blockIdx.x == 0) {
-        double loss = 0.0, pairs = 0.0, right = 0.0;    // whole numbers below 2^31
-        for (int64_t i = threadIdx.x; i < parts; i += kBlock) {
-            loss += A.part[i].loss;
-            pairs += A.part[i].pairs;
-            right += A.part[i].right;
-        }
-        loss = block_total(loss);
-        pairs = block_total(pairs);
-        right = block_total(right);
-        if (threadIdx.x == 0) {
-            *A.loss = (float)loss;
-            A.counts[0] = (int64_t)pairs;
-            A.counts[1] = (int64_t)right;
-        }
+// The totals from the threads' sums (whole numbers below 2^31).
+__device__ __forceinline__ void leave_totals(const PairArgs& A, double loss, double pairs, double right) {
+    loss = block_total(loss);
+    pairs = block_total(pairs);
+    right = block_total(right);
+    if (threadIdx.x == 0) {
+        *A.loss = (float)loss;
+        A.counts[0] = (int64_t)pairs;
+        A.counts[1] = (int64_t)right;
     }
-    if (!A.grad || t.num_slots == 0) return;
+}
+
+// Gradients of the block's chunks from the factors of the rows.
+template <int CHUNK>
+__device__ __forceinline__ void pairs_grad(const PairArgs& A, const double* coef) {
+    __shared__ uint32_t s_bits[CHUNK / 32];
+    const odb_tiles_t& t = A.t;
+    if (!A.grad) return;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int64_t total = run_elems(t, e_base);
     for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
         const int64_t c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
         if (c0 >= c1) break;
-        const uint32_t* bits = A.bits + b * (A.chunk / 32);
-        chunk_slots(t, e_base, r_base, first_slot(t, e_base, c0), c0, c1,
-                    [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
-            const Span p(s, a0, a1, c0);
-            const double* coef = A.coef + s.row0;
-            Group q = p.first();
+        const int64_t k0 = A.chunk_slot[b];
+        load_bits(s_bits, A.bits, b, A.chunk);
+        chunk_slots(t, e_base, r_base, k0, c0, c1,
+                    [&](int64_t, const SlotView& s, int64_t a0, int64_t a1) {
+            const Span p(s, a0, a1, c0, kBlock);
+            const double* of_row = coef + s.row0;
+            Group q = p.first((int)threadIdx.x);
 #pragma unroll 4
             for (; q.o < p.o1; p.advance(&q)) {
-                const uint32_t on = bits[q.o / 32] >> (q.o & 31) & q.mask;
-                float v[4] = {0, 0, 0, 0};
-                if (on) {
-                    if (q.col <= p.maxlen - 4) {
-                        const float c = (float)coef[q.row];
+                const uint32_t on = s_bits[q.o / 32] >> (q.o & 31) & q.mask;
+                const float c = (float)of_row[q.row];
+                float v[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) v[j] = on >> j & 1 ? c : 0.0f;
-                    } else {
-                        Group r = q;
+                for (int j = 0; j < 4; ++j) v[j] = on >> j & 1 ? c : 0.0f;
+                if (q.col > p.maxlen - 4) {
+                    Group r = q;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (on >> j & 1) v[j] = (float)coef[r.row];
-                            r.next(p.maxlen);
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        if (on >> j & 1) v[j] = (float)of_row[r.row];
+                        r.next(p.maxlen);
                     }
                 }
                 store4(A.grad + c0, q, v);
             }
         });
     }
+}
+
+// Gradients of the tiles; the first block also sums what the pairs left.
+__global__ void __launch_bounds__(kBlock) pairs_grad_kernel(PairArgs A, int64_t parts) {
+    if (blockIdx.x == 0) {
+        double loss = 0.0, pairs = 0.0, right = 0.0;
+        for (int64_t i = threadIdx.x; i < parts; i += kBlock) {
+            loss += A.part[i].loss;
+            pairs += A.part[i].pairs;
+            right += A.part[i].right;
+        }
+        leave_totals(A, loss, pairs, right);
+    }
+    pairs_grad<kMaxChunk>(A, A.coef);
+}
+
+constexpr int64_t kFewChunks = 1024;
+
+// The same for runs of at most kBlock rows: every block forms all their factors, which costs it what
+// waiting for a kernel that does would, and the first one leaves the rows' numbers.
+__global__ void __launch_bounds__(kBlock) few_rows_kernel(PairArgs A) {
+    __shared__ double s_coef[kBlock];
+    const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
+    PairSums sums;
+    s_coef[threadIdx.x] = threadIdx.x < rows ? pair_row(A, threadIdx.x, rows, blockIdx.x == 0, &sums) : 0.0;
+    if (blockIdx.x == 0) leave_totals(A, sums.loss, sums.pairs, sums.right);
+    __syncthreads();
+    pairs_grad<kMaxChunk>(A, s_coef);
+}
+
+__global__ void no_pairs_kernel(PairArgs A) {
+    *A.loss = 0.0f;
+    A.counts[0] = A.counts[1] = 0;
+}
+
+// A run of one chunk, in one launch of one block.
+template <bool REF>
+__global__ void __launch_bounds__(kBlock) pairs_one_kernel(PairArgs A) {
+    if (A.row_of) {
+        clear_rows(A);
+        __threadfence();     // before the atomics on the same entries
+        __syncthreads();
+    }
+    row_sums<REF, true>(A);
+    __syncthreads();
+    const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
+    PairSums sums;
+    for (int64_t row = threadIdx.x; row < rows; row += kBlock) A.coef[row] = pair_row(A, row, rows, true, &sums);
+    leave_totals(A, sums.loss, sums.pairs, sums.right);
+    __syncthreads();
+    pairs_grad<kOneChunk>(A, A.coef);
 }
 
 int check_tile_arrays(const odb_tiles_t* t) {
@@ -1058,7 +1352,8 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     PolicyArgs a{};
     a.t = *t;
     a.logprob = d_logprob;
-    a.old = d_old_logprob;
+    a.old = d_old_logprob ? d_old_logprob : d_logprob;
+    a.on_policy = !d_old_logprob;
     a.ref = d_ref_logprob;
     a.entropy = d_entropy;
     a.advantage = d_advantage;
@@ -1069,12 +1364,14 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     a.grad = d_grad_logprob;
     a.grad_entropy = d_grad_entropy;
     a.bits = ws_at<uint32_t>(d_ws, L.bits);
+    a.chunk_slot = ws_at<int32_t>(d_ws, L.chunk_slot);
     a.slot_count = ws_at<int32_t>(d_ws, L.slot_count);
     a.slot_part = ws_at<SlotPart>(d_ws, L.slot_part);
     a.row_count = ws_at<int32_t>(d_ws, L.row_count);
     a.status = d_status;
     a.chunks = L.chunks;
     a.chunk = L.chunk;
+    a.chunk_log2 = __builtin_ctz((unsigned)L.chunk);
     a.at_low = std::log1p(-p->clip_low);
     a.at_high = std::log1p(p->clip_high);
     a.at_dual = p->dual_clip > 0.0 ? std::log(p->dual_clip) : HUGE_VAL;
@@ -1084,24 +1381,20 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     a.low = (float)(1.0 - p->clip_low);
     a.high = (float)(1.0 + p->clip_high);
     a.dual = (float)p->dual_clip;
-    a.kl = p->kl;
-    a.reduce = p->reduce;
     a.token_advantage = p->token_advantage;
     const dim3 grid(grid_for(L.chunks, 1)), block(kBlock);
-    if (L.chunks > 0) {
-        if (p->reduce == ODB_REDUCE_TOKEN_MEAN) {
-            hipLaunchKernelGGL(policy_count_kernel<false>, grid, block, 0, s, a);
-            ODB_LAUNCHED();
-            hipLaunchKernelGGL((policy_kernel<false, false>), grid, block, 0, s, a);
-        } else if (p->reduce == ODB_REDUCE_ROW_MEAN) {
-            hipLaunchKernelGGL(policy_count_kernel<true>, grid, block, 0, s, a);
-            ODB_LAUNCHED();
-            hipLaunchKernelGGL((policy_kernel<true, false>), grid, block, 0, s, a);
-        } else {
-            hipLaunchKernelGGL((policy_kernel<false, true>), grid, block, 0, s, a);
-        }
+    if (L.chunks <= 1) {
+        hipLaunchKernelGGL(policy_one_kernels[p->kl], dim3(1), block, 0, s, a, (int)p->reduce);
+        ODB_LAUNCHED();
+        return ODB_OK;
+    }
+    if (p->reduce != ODB_REDUCE_SUM) {
+        hipLaunchKernelGGL(p->reduce == ODB_REDUCE_ROW_MEAN ? policy_count_kernel<true> : policy_count_kernel<false>,
+                           grid, block, 0, s, a);
         ODB_LAUNCHED();
     }
+    hipLaunchKernelGGL(policy_kernels[p->kl][p->reduce], grid, block, 0, s, a);
+    ODB_LAUNCHED();
     hipLaunchKernelGGL(policy_slots_kernel, dim3(grid_for(t->num_slots, kWaves)), block, 0, s, a);
     ODB_LAUNCHED();
     return ODB_OK;
@@ -1150,34 +1443,50 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
     a.coef = ws_at<double>(d_ws, L.coef);
     a.part = ws_at<PairPart>(d_ws, L.pair_part);
     a.bits = ws_at<uint32_t>(d_ws, L.bits);
+    a.chunk_slot = ws_at<int32_t>(d_ws, L.chunk_slot);
     a.loss = d_loss;
     a.row_loss = d_row_loss;
     a.row_reward = d_row_reward;
     a.counts = d_counts;
-    a.grad = any ? d_grad_logprob : nullptr;
+    a.grad = d_grad_logprob;
     a.status = d_status;
-    a.chunks = any ? L.chunks : 0;
+    a.chunks = L.chunks;
     a.chunk = L.chunk;
+    a.quarter_log2 = __builtin_ctz((unsigned)L.chunk) - 2;
     a.beta = p->beta;
     a.margin = p->margin;
     a.smoothing = p->label_smoothing;
     a.loss_scale = p->loss_scale;
     a.kind = p->kind;
     a.normalize = p->normalize;
-    const int64_t parts = any ? (t->num_rows + kBlock - 1) / kBlock : 0;
-    if (any) {
-        if (a.row_of && parts > 0) {
-            hipLaunchKernelGGL(clear_rows_kernel, dim3(grid_for(parts, 1)), dim3(kBlock), 0, s, a);
-            ODB_LAUNCHED();
-        }
-        hipLaunchKernelGGL(row_sums_kernel, dim3(grid_for(L.chunks, 1)), dim3(kBlock), 0, s, a);
+    const dim3 block(kBlock), grid(grid_for(L.chunks, 1));
+    if (!any) {
+        hipLaunchKernelGGL(no_pairs_kernel, dim3(1), dim3(1), 0, s, a);
         ODB_LAUNCHED();
-        if (parts > 0) {
-            hipLaunchKernelGGL(pairs_kernel, dim3((unsigned)parts), dim3(kBlock), 0, s, a);
-            ODB_LAUNCHED();
-        }
+        return ODB_OK;
     }
-    hipLaunchKernelGGL(pairs_grad_kernel, dim3(a.grad ? grid_for(L.chunks, 1) : 1), dim3(kBlock), 0, s, a, parts);
+    if (L.chunks <= 1) {
+        hipLaunchKernelGGL(d_ref_logprob ? pairs_one_kernel<true> : pairs_one_kernel<false>, dim3(1), block, 0, s, a);
+        ODB_LAUNCHED();
+        return ODB_OK;
+    }
+    const int64_t parts = (t->num_rows + kBlock - 1) / kBlock;
+    if (a.row_of && parts > 0) {
+        hipLaunchKernelGGL(clear_rows_kernel, dim3(grid_for(parts, 1)), block, 0, s, a);
+        ODB_LAUNCHED();
+    }
+    hipLaunchKernelGGL(d_ref_logprob ? row_sums_kernel<true> : row_sums_kernel<false>, grid, block, 0, s, a);
+    ODB_LAUNCHED();
+    if (parts <= 1 && L.chunks <= kFewChunks) {
+        hipLaunchKernelGGL(few_rows_kernel, grid, block, 0, s, a);
+        ODB_LAUNCHED();
+        return ODB_OK;
+    }
+    if (parts > 0) {
+        hipLaunchKernelGGL(pairs_kernel, dim3((unsigned)parts), block, 0, s, a);
+        ODB_LAUNCHED();
+    }
+    hipLaunchKernelGGL(pairs_grad_kernel, a.grad ? grid : dim3(1), block, 0, s, a, parts);
     ODB_LAUNCHED();
     return ODB_OK;
 }

@@ -408,6 +408,32 @@ def test_policy_loss(name, shift):
             assert v is None or torch.equal(v, again[k]), k
 
 
+def test_fewer_than_four_elements():
+    """Runs whose arrays end before a group of four does, at each of their addresses."""
+    torch = _torch()
+    for E in (1, 2, 3, 4, 5):
+        for off in range(4):
+            plan = Plan([[E]])
+            rng = np.random.default_rng(E)
+            y = plan.labels(rng)
+            lp, old, kref, H = (v.astype(np.float32) for v in _inputs(plan, rng, y != IGNORE))
+            adv = np.ones(1, np.float32)
+            at = lambda v: torch.from_numpy(np.concatenate([np.zeros(off, v.dtype), v])).cuda()[off:]
+            tiles = _tiles(plan, y, 0, 0, 0)
+            for n, o in enumerate(POLICY_OPTIONS):
+                p = _policy_params({**o, "token_advantage": 0})
+                p["entropy_coef"] = 0.0
+                want = ref.policy_loss(plan, y, 0, p, lp, old, kref, None, adv, None)
+                out, status = _policy_run(tiles, plan, p, at(lp), at(old), at(kref), None, at(adv), None, extra=0)
+                assert int(status.item()) == 0
+                assert np.allclose(out["grad"].cpu().numpy(), want["grad"], rtol=200 * U, atol=1e-7)
+            p = dict(kind=0, normalize=0, beta=1.0, margin=0.0, label_smoothing=0.0, loss_scale=1.0)
+            out, status = _preference_run(tiles, plan, p, at(lp), at(kref), None, torch.zeros(1, dtype=torch.int32,
+                                                                                             device="cuda"), 0, 0)
+            _check_preference(out, ref.preference_loss(plan, y, 0, p, lp, kref, None, np.zeros(1, np.int32)), plan, p,
+                              lp, kref, y != IGNORE)
+
+
 def test_policy_clips_are_decided_on_the_exact_difference():
     """Differences of one fp32 step around each bound, and equal to it."""
     torch = _torch()
