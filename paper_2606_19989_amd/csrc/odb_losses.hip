@@ -55,7 +55,7 @@ struct LossLayout {
     int32_t chunk;
 };
 
-constexpr int64_t kMaxElems = (int64_t)1 << 40;
+constexpr int64_t kMaxElems = (int64_t)1 << 37;
 
 // Elements of a chunk.  A chunk's fixed cost is a search for its first slot and a reduction; more
 // chunks than the chip holds at once (2,048 blocks of 256 threads) only add to it.
@@ -71,7 +71,7 @@ int check_tiles(const odb_tiles_t* t) {
         return set_error(ODB_E_INVALID_ARG, "num_slots must be in [0, 2^31)");
     if (t->num_rows < 0 || t->num_rows > INT32_MAX) return set_error(ODB_E_INVALID_ARG, "num_rows must be in [0, 2^31)");
     if (t->num_elems < 0 || t->num_elems > kMaxElems)
-        return set_error(ODB_E_INVALID_ARG, "num_elems must be in [0, 2^40]");
+        return set_error(ODB_E_INVALID_ARG, "num_elems must be in [0, 2^37]");
     if (t->shift != 0 && t->shift != 1) return set_error(ODB_E_INVALID_ARG, "shift must be 0 or 1 (got %d)", t->shift);
     if (t->reserved0 != 0) return set_error(ODB_E_INVALID_ARG, "tiles.reserved0 must be 0");
     return ODB_OK;
@@ -160,32 +160,19 @@ __device__ __forceinline__ T block_total(T v) {
     return sum;
 }
 
-// Four values of an array from position o of a chunk on, without a branch: past `last`, the position
-// of the array's last four, those are read instead and put in their places afterwards by `settle`, so
-// that loads of many groups go out together.  SAFE, for arrays that may hold fewer than four: each is
-// read on its own where not all are there, and the others are `fill` at once.
+// Four values of an array from position o of a chunk on.  SAFE, for where they may end behind the array,
+// whose last four are at `last`: each is read on its own then, and the others are `fill`.  Otherwise a
+// position past `last` reads that one, so that loads of many groups go out without a branch between them.
 template <typename V4, bool SAFE, typename T>
 __device__ __forceinline__ V4 load4(const T* p, int o, int last, T fill) {
-    if (SAFE && o > last) {
+    if (SAFE) {
         V4 v;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = o + j < last + 4 ? p[o + j] : fill;
         return v;
     }
-    return *reinterpret_cast<const V4*>(p + (o < last ? o : last));
-}
-
-// What lies behind the array becomes `fill`.
-template <bool SAFE, typename V4, typename T>
-__device__ __forceinline__ void settle(V4* v, int o, int last, T fill) {
-    if (SAFE || o <= last) return;
-    for (int d = last; d < o; ++d) {
-        (*v)[0] = (*v)[1];
-        (*v)[1] = (*v)[2];
-        (*v)[2] = (*v)[3];
-        (*v)[3] = fill;
-        if (d - last >= 3) break;
-    }
+    const uint32_t at = 4u * (uint32_t)(o < last ? o : last);    // one 32-bit offset to the chunk's address
+    return *reinterpret_cast<const V4*>(reinterpret_cast<const char*>(p) + at);
 }
 
 // A thread's group of four elements of a chunk, from position o (a multiple of 4) on: which of them
@@ -286,11 +273,13 @@ __device__ __forceinline__ void load_bits(uint32_t* s_bits, const uint32_t* bits
 }
 
 // Position in a chunk of the arrays' last four elements, as far as a chunk's positions go; negative in
-// a last chunk of fewer.
+// a last chunk of fewer.  Whether a span's groups reach past them:
 __device__ __forceinline__ int last_four(const odb_tiles_t& t, int64_t c0) {
     const int64_t n = t.num_elems - 4 - c0;
     return (int)(n < 2 * kMaxChunk ? n : 2 * kMaxChunk);
 }
+
+__device__ __forceinline__ bool at_end(int o1, int last) { return ((o1 + 3) & ~3) > last + 4; }
 
 // ------------------------------------------------------------------ policy loss
 struct PolicyArgs {
@@ -348,73 +337,73 @@ __global__ void __launch_bounds__(kBlock) policy_count_kernel(PolicyArgs A) {
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int64_t total = run_elems(t, e_base);
-    for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
-        const int64_t c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
-        if (c0 >= c1) break;
-        const int32_t* labels = t.d_labels + c0;
-        const int last = last_four(t, c0);
-        for (int i = threadIdx.x; i < A.chunk / 16; i += kBlock) reinterpret_cast<uint32_t*>(s_nibble)[i] = 0;
-        const int64_t k0 = first_slot(t, e_base, c0);
-        if (threadIdx.x == 0) A.chunk_slot[b] = (int32_t)k0;
-        __syncthreads();
-        chunk_slots(t, e_base, r_base, k0, c0, c1,
-                    [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
-            const Span p(s, a0, a1, c0, kBlock);
-            const int rows = (int)((a1 - 1 - s.lo) / s.maxlen) - p.row_a + 1;
-            const bool lds = ROWS && rows <= kLdsRows;
-            if (lds) {
-                for (int i = threadIdx.x; i < rows; i += kBlock) s_rows[i] = 0;
-                __syncthreads();
-            }
-            int count = 0;
-            Group q = p.first((int)threadIdx.x);
+    const int64_t b = blockIdx.x, c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
+    if (c0 >= c1) return;
+    const int32_t* labels = t.d_labels + c0;
+    const int last = last_four(t, c0);
+    for (int i = threadIdx.x; i < A.chunk / 16; i += kBlock) reinterpret_cast<uint32_t*>(s_nibble)[i] = 0;
+    const int64_t k0 = first_slot(t, e_base, c0);
+    if (threadIdx.x == 0) A.chunk_slot[b] = (int32_t)k0;
+    __syncthreads();
+    chunk_slots(t, e_base, r_base, k0, c0, c1, [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+        const Span p(s, a0, a1, c0, kBlock);
+        const int rows = (int)((a1 - 1 - s.lo) / s.maxlen) - p.row_a + 1;
+        const bool lds = ROWS && rows <= kLdsRows;
+        if (lds) {
+            for (int i = threadIdx.x; i < rows; i += kBlock) s_rows[i] = 0;
+            __syncthreads();
+        }
+        int count = 0;
+        Group q = p.first((int)threadIdx.x);
+        auto take = [&](const int4u& y) {
+            const uint32_t on = count_mask(q, y, p.maxlen, t.shift);
+            if (on) s_nibble[q.o / 4] |= (uint8_t)on;
+            if (lds)
+                add_to_rows(s_rows, q, on, p.maxlen, p.row_a);
+            else
+                count += __builtin_popcount(on);
+            p.advance(&q);
+        };
+        if (at_end(p.o1, last)) {
+            while (q.o < p.o1) take(load4<int4u, true>(labels, q.o, last, kIgnore));
+        } else {
             for (int o = p.o0 & ~3; o < p.o1; o += kAhead * p.ahead) {     // uniform
                 int4u y[kAhead];
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) y[i] = load4<int4u, false>(labels, q.o + i * p.ahead, last, kIgnore);
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    settle<false>(&y[i], q.o, last, kIgnore);
-                    const uint32_t on = count_mask(q, y[i], p.maxlen, t.shift);
-                    if (on) s_nibble[q.o / 4] |= (uint8_t)on;
-                    if (lds)
-                        add_to_rows(s_rows, q, on, p.maxlen, p.row_a);
-                    else
-                        count += __builtin_popcount(on);
-                    p.advance(&q);
-                }
+                for (int i = 0; i < kAhead; ++i) take(y[i]);
             }
-            if (ROWS) {
-                // a row counts here if it starts and ends here; the others are joined by who needs the slot's rows
-                __syncthreads();
-                count = 0;
-                for (int i = threadIdx.x; i < rows; i += kBlock) {
-                    const int64_t start = s.lo + (int64_t)(p.row_a + i) * s.maxlen;
-                    int n = 0;
-                    if (lds) {
-                        n = s_rows[i];
-                    } else {     // rows of a few elements
-                        for (int64_t e = start > a0 ? start : a0; e < start + s.maxlen && e < a1; ++e)
-                            n += s_nibble[(e - c0) / 4] >> ((e - c0) & 3) & 1;
-                    }
-                    A.row_count[b + s.row0 + p.row_a + i] = n;
-                    count += n > 0 && start >= c0 && start + s.maxlen <= c0 + A.chunk;
-                }
-            }
-            count = block_total(count);
-            if (threadIdx.x == 0) A.slot_count[b + k] = count;
-            __syncthreads();
-        });
-        for (int i = threadIdx.x; i < A.chunk / 32; i += kBlock) {
-            const uint2 w = reinterpret_cast<const uint2*>(s_nibble)[i];
-            // eight bytes of four bits to one word
-            uint32_t v = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                v |= (w.x >> (8 * j) & 0xf) << (4 * j) | (w.y >> (8 * j) & 0xf) << (16 + 4 * j);
-            A.bits[b * (A.chunk / 32) + i] = v;
         }
+        if (ROWS) {
+            // a row counts here if it starts and ends here; the others are joined by who needs the slot's rows
+            __syncthreads();
+            count = 0;
+            for (int i = threadIdx.x; i < rows; i += kBlock) {
+                const int64_t start = s.lo + (int64_t)(p.row_a + i) * s.maxlen;
+                int n = 0;
+                if (lds) {
+                    n = s_rows[i];
+                } else {     // rows of a few elements
+                    for (int64_t e = start > a0 ? start : a0; e < start + s.maxlen && e < a1; ++e)
+                        n += s_nibble[(e - c0) / 4] >> ((e - c0) & 3) & 1;
+                }
+                A.row_count[b + s.row0 + p.row_a + i] = n;
+                count += n > 0 && start >= c0 && start + s.maxlen <= c0 + A.chunk;
+            }
+        }
+        count = block_total(count);
+        if (threadIdx.x == 0) A.slot_count[b + k] = count;
         __syncthreads();
+    });
+    for (int i = threadIdx.x; i < A.chunk / 32; i += kBlock) {
+        const uint2 w = reinterpret_cast<const uint2*>(s_nibble)[i];
+        // eight bytes of four bits to one word
+        uint32_t v = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v |= (w.x >> (8 * j) & 0xf) << (4 * j) | (w.y >> (8 * j) & 0xf) << (16 + 4 * j);
+        A.bits[b * (A.chunk / 32) + i] = v;
     }
 }
 
@@ -426,75 +415,38 @@ __device__ __forceinline__ float exp_near(float d) {
     return fabsf(u) < 200.0f ? fmaf(e * lost, kLn2, e) : e;
 }
 
-// exp(d) - 1 - d: below 3/4 by its series (the next term is under 2^-27 of the sum), where the
+// exp(d) - 1 - d: below 3/2 by its series (the next term is under 2^-31 of the sum), where the
 // difference would cancel.
-__device__ __forceinline__ float exp_less_line(float d) {
-    if (fabsf(d) < 0.75f) {
-        float q = 1.0f / 3628800.0f;
-        q = fmaf(q, d, 1.0f / 362880.0f);
-        q = fmaf(q, d, 1.0f / 40320.0f);
-        q = fmaf(q, d, 1.0f / 5040.0f);
-        q = fmaf(q, d, 1.0f / 720.0f);
-        q = fmaf(q, d, 1.0f / 120.0f);
-        q = fmaf(q, d, 1.0f / 24.0f);
-        q = fmaf(q, d, 1.0f / 6.0f);
-        q = fmaf(q, d, 0.5f);
-        return q * d * d;
-    }
-    return exp_near(d) - 1.0f - d;
+constexpr float kSeries = 1.5f;
+
+__device__ __forceinline__ float less_line_series(float d) {
+    float q = 1.0f / 87178291200.0f;
+    q = fmaf(q, d, 1.0f / 6227020800.0f);
+    q = fmaf(q, d, 1.0f / 479001600.0f);
+    q = fmaf(q, d, 1.0f / 39916800.0f);
+    q = fmaf(q, d, 1.0f / 3628800.0f);
+    q = fmaf(q, d, 1.0f / 362880.0f);
+    q = fmaf(q, d, 1.0f / 40320.0f);
+    q = fmaf(q, d, 1.0f / 5040.0f);
+    q = fmaf(q, d, 1.0f / 720.0f);
+    q = fmaf(q, d, 1.0f / 120.0f);
+    q = fmaf(q, d, 1.0f / 24.0f);
+    q = fmaf(q, d, 1.0f / 6.0f);
+    q = fmaf(q, d, 0.5f);
+    return q * d * d;
 }
 
-struct TokenTerms {
-    float policy, ratio, kl, grad, kl_grad;
-    bool below, above, dual;    // clipped
-};
+__device__ __forceinline__ float less_line_far(float d) { return exp_near(d) - 1.0f - d; }
 
 // The bounds on lp - old, rounded to fp32.
 struct Bounds {
     float low, high, dual;
 };
 
-template <int KL>
-__device__ __forceinline__ TokenTerms policy_token(const PolicyArgs& A, const Bounds& B, float lp, float old, float ref,
-                                                   float adv) {
-    TokenTerms o;
-    const float d = A.on_policy ? 0.0f : lp - old;
-    const bool pos = adv > 0.0f, neg = adv < 0.0f;     // neither for 0 and NaN: nothing is clipped
-    const float up = pos ? B.high : neg ? B.dual : INFINITY, low = neg ? B.low : -INFINITY;
-    bool over = d > up, under = d < low;
-    // rounding keeps order: the rounded difference decides unless it equals a rounded bound
-    if (__builtin_expect(d == up || d == low, 0)) {
-        const double x = A.on_policy ? 0.0 : (double)lp - (double)old;
-        over = x > (pos ? A.at_high : neg ? A.at_dual : HUGE_VAL);
-        under = neg && x < A.at_low;
-    }
-    o.ratio = exp_near(d);
-    float bound = over ? (pos ? A.high : A.dual) : o.ratio;
-    bound = under ? A.low : bound;
-    o.below = under;
-    o.above = over && pos;
-    o.dual = over && neg;
-    o.policy = adv == 0.0f ? 0.0f : -bound * adv;     // an overflowing ratio must not make it NaN
-    o.grad = over || under ? 0.0f : o.policy;
-    o.kl = o.kl_grad = 0.0f;
-    const float x = lp - ref;
-    if (KL == ODB_KL_LINEAR) {
-        o.kl = x;
-        o.kl_grad = 1.0f;
-    } else if (KL == ODB_KL_SQUARE) {
-        o.kl = 0.5f * x * x;
-        o.kl_grad = x;
-    } else if (KL == ODB_KL_EXP) {
-        o.kl = exp_less_line(-x);
-        o.kl_grad = x - o.kl;    // 1 - exp(-x)
-    }
-    return o;
-}
-
-// A thread's sums, and the wave's counts.
+// A thread's part of a slot.
 struct PolicySums {
     double sum[4] = {0, 0, 0, 0};
-    int counted = 0;            // the thread's
+    int counted = 0;
     int clipped[3] = {0, 0, 0};
 };
 
@@ -516,22 +468,21 @@ struct PolicyChunk {
 // instead, as all such do: no traffic, and no branch that parts the loads.
 struct PolicyLoads {
     float4u lp, old, ref, H, adv;
-    int o;
     uint32_t on;
 };
 
-template <int KL, bool SAFE>
+template <int KL, bool ENT, bool SAFE>
 __device__ __forceinline__ PolicyLoads policy_load(const PolicyArgs& A, const PolicyChunk& C, Group q, uint32_t on,
                                                    int maxlen, int row_a) {
     PolicyLoads L;
     L.on = on;
-    L.o = on ? q.o : 0;
-    L.lp = load4<float4u, SAFE>(C.logprob, L.o, C.last, 0.0f);
-    L.old = load4<float4u, SAFE>(C.old, L.o, C.last, 0.0f);
-    if (KL != ODB_KL_NONE) L.ref = load4<float4u, SAFE>(C.ref, L.o, C.last, 0.0f);
-    if (A.entropy) L.H = load4<float4u, SAFE>(C.entropy, L.o, C.last, 0.0f);
+    const int o = on ? q.o : 0;
+    L.lp = load4<float4u, SAFE>(C.logprob, o, C.last, 0.0f);
+    L.old = load4<float4u, SAFE>(C.old, o, C.last, 0.0f);
+    if (KL != ODB_KL_NONE) L.ref = load4<float4u, SAFE>(C.ref, o, C.last, 0.0f);
+    if (ENT) L.H = load4<float4u, SAFE>(C.entropy, o, C.last, 0.0f);
     if (A.token_advantage) {
-        L.adv = load4<float4u, SAFE>(C.advantage, L.o, C.last, 0.0f);
+        L.adv = load4<float4u, SAFE>(C.advantage, o, C.last, 0.0f);
     } else {
         L.adv[0] = C.advantage[on ? q.row : row_a];
         L.adv[1] = L.adv[2] = L.adv[3] = L.adv[0];
@@ -548,28 +499,51 @@ __device__ __forceinline__ PolicyLoads policy_load(const PolicyArgs& A, const Po
 
 // A group's part of the sums, and its gradients.  weight(row, &f, &gs) gives the weight of a row's
 // token in the slot's mean and the factor of its gradient (ROWS: they differ from row to row).  What
-// does not count has its inputs replaced by 0, which makes all but the ratio and the KL term's slope
-// 0.  Within a group the sums are formed in fp32.  The whole wave takes part.
-template <int KL, bool ROWS, bool SAFE, typename Weight>
-__device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyChunk& C, Group q, PolicyLoads L,
+// does not count has its inputs replaced by 0, which makes all but the ratio and the linear KL term's
+// slope 0.  Within a group the sums are formed in fp32.  Four tokens go through without a branch but
+// the one of the rare cases.
+template <int KL, bool ROWS, bool ENT, typename Weight>
+__device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyChunk& C, Group q, const PolicyLoads& L,
                                              int maxlen, const Weight& weight, PolicySums& S) {
     float g[4] = {0, 0, 0, 0}, ge[4] = {0, 0, 0, 0};
     if (__any(L.on != 0)) {
-        if (!SAFE && L.o > C.last) {
-            settle<SAFE>(&L.lp, L.o, C.last, 0.0f);
-            settle<SAFE>(&L.old, L.o, C.last, 0.0f);
-            if (KL != ODB_KL_NONE) settle<SAFE>(&L.ref, L.o, C.last, 0.0f);
-            if (A.entropy) settle<SAFE>(&L.H, L.o, C.last, 0.0f);
-            if (A.token_advantage) settle<SAFE>(&L.adv, L.o, C.last, 0.0f);
+        float d[4], x[4], adv[4], kl[4];
+        bool over[4], under[4], rare = false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool live = L.on >> j & 1;
+            const float lp = live ? L.lp[j] : 0.0f;
+            adv[j] = live ? L.adv[j] : 0.0f;
+            d[j] = lp - (live ? L.old[j] : 0.0f);
+            d[j] = A.on_policy ? 0.0f : d[j];
+            // neither bound for advantages of 0 and NaN: nothing is clipped
+            const bool pos = adv[j] > 0.0f, neg = adv[j] < 0.0f;
+            const float up = pos ? C.bounds.high : neg ? C.bounds.dual : INFINITY, low = neg ? C.bounds.low : -INFINITY;
+            over[j] = d[j] > up;
+            under[j] = d[j] < low;
+            // rounding keeps order: the rounded difference decides unless it equals a rounded bound
+            rare |= d[j] == up || d[j] == low;
+            if (KL != ODB_KL_NONE) x[j] = lp - (live ? L.ref[j] : 0.0f);
+            if (KL == ODB_KL_EXP) {
+                kl[j] = less_line_series(-x[j]);
+                rare |= fabsf(x[j]) >= kSeries;
+            }
+        }
+        if (__builtin_expect(rare, 0)) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool live = L.on >> j & 1, pos = adv[j] > 0.0f, neg = adv[j] < 0.0f;
+                const double z = A.on_policy || !live ? 0.0 : (double)L.lp[j] - (double)L.old[j];
+                over[j] = z > (pos ? A.at_high : neg ? A.at_dual : HUGE_VAL);
+                under[j] = neg && z < A.at_low;
+                if (KL == ODB_KL_EXP && fabsf(x[j]) >= kSeries) kl[j] = less_line_far(-x[j]);
+            }
         }
         float f[4], gs[4];
         if (!ROWS) {
             weight(0, &f[0], &gs[0]);
 #pragma unroll
-            for (int j = 1; j < 4; ++j) {
-                f[j] = f[0];
-                gs[j] = gs[0];
-            }
+            for (int j = 1; j < 4; ++j) gs[j] = gs[0];
         } else {
             Group r = q;
             float w = 0.0f, k = 0.0f;
@@ -588,36 +562,38 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
         float sum[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const bool live = L.on >> j & 1;
-            const TokenTerms o = policy_token<KL>(A, C.bounds, live ? L.lp[j] : 0.0f, live ? L.old[j] : 0.0f,
-                                                  KL == ODB_KL_NONE ? 0.0f : live ? L.ref[j] : 0.0f,
-                                                  live ? L.adv[j] : 0.0f);
-            const float ratio = live ? o.ratio : 0.0f;
-            const float slope = KL == ODB_KL_LINEAR ? (live ? o.kl_grad : 0.0f) : o.kl_grad;
-            if (ROWS) {
-                sum[0] = fmaf(f[j], o.policy, sum[0]);
-                sum[1] = fmaf(f[j], o.kl, sum[1]);
-                sum[3] = fmaf(f[j], ratio, sum[3]);
+            const bool live = L.on >> j & 1, pos = adv[j] > 0.0f;
+            const float ratio = exp_near(d[j]);
+            float bound = over[j] ? (pos ? A.high : A.dual) : ratio;
+            bound = under[j] ? A.low : bound;
+            const float policy = adv[j] == 0.0f ? 0.0f : -bound * adv[j];   // an overflowing ratio must not make it NaN
+            const float slope = over[j] || under[j] ? 0.0f : policy;
+            float kl_slope = 0.0f;
+            if (KL == ODB_KL_LINEAR) {
+                kl[j] = x[j];
+                kl_slope = live ? 1.0f : 0.0f;
+            } else if (KL == ODB_KL_SQUARE) {
+                kl[j] = 0.5f * x[j] * x[j];
+                kl_slope = x[j];
+            } else if (KL == ODB_KL_EXP) {
+                kl_slope = x[j] - kl[j];    // 1 - exp(-x)
             } else {
-                sum[0] += o.policy;
-                sum[1] += o.kl;
-                sum[3] += ratio;
+                kl[j] = 0.0f;
             }
-            S.clipped[0] += __popcll(__ballot(o.below));
-            S.clipped[1] += __popcll(__ballot(o.above));
-            S.clipped[2] += __popcll(__ballot(o.dual));
-            g[j] = gs[j] * fmaf(C.kl_coef, slope, o.grad);
-        }
-        if (A.entropy) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bool live = L.on >> j & 1;
-                sum[2] = fmaf(ROWS ? f[j] : 1.0f, live ? L.H[j] : 0.0f, sum[2]);
-                ge[j] = live ? -C.entropy_coef * gs[j] : 0.0f;
-            }
+            const float w = ROWS ? f[j] : 1.0f;
+            sum[0] = fmaf(w, policy, sum[0]);
+            if (KL != ODB_KL_NONE) sum[1] = fmaf(w, kl[j], sum[1]);
+            if (ENT) sum[2] = fmaf(w, live ? L.H[j] : 0.0f, sum[2]);
+            sum[3] = fmaf(w, live ? ratio : 0.0f, sum[3]);
+            S.clipped[0] += under[j];
+            S.clipped[1] += over[j] && pos;
+            S.clipped[2] += over[j] && !pos;
+            g[j] = gs[j] * fmaf(C.kl_coef, kl_slope, slope);
+            if (ENT) ge[j] = live ? -C.entropy_coef * gs[j] : 0.0f;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) S.sum[j] += sum[j];
+        for (int j = 0; j < 4; ++j)
+            if ((KL != ODB_KL_NONE || j != 1) && (ENT || j != 2)) S.sum[j] += sum[j];
         S.counted += __builtin_popcount(L.on);
     }
     if (q.mask) {
@@ -634,7 +610,7 @@ __device__ __forceinline__ SlotPart block_part(const PolicySums& S, double same)
     for (int j = 0; j < 4; ++j) p.sum[j] = wave_total(S.sum[j]);
     p.counted = wave_total(S.counted);
 #pragma unroll
-    for (int j = 0; j < 3; ++j) p.clipped[j] = S.clipped[j];
+    for (int j = 0; j < 3; ++j) p.clipped[j] = wave_total(S.clipped[j]);
     if ((threadIdx.x & (kWave - 1)) == 0) s_part[threadIdx.x / kWave] = p;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -676,14 +652,14 @@ __device__ __forceinline__ PolicyChunk policy_chunk(const PolicyArgs& A, const S
 }
 
 // The block's part of a slot: counted(group) tells which elements count.
-template <int KL, bool ROWS, bool SAFE, typename Counted, typename Weight>
+template <int KL, bool ROWS, bool ENT, bool SAFE, typename Counted, typename Weight>
 __device__ __forceinline__ void policy_span(const PolicyArgs& A, const PolicyChunk& C, const Span& p,
                                             const Counted& counted, const Weight& weight, PolicySums& S) {
     // uniform over the block: a wave's lanes stay together, those behind the slot with nothing to do
     Group q = p.first((int)threadIdx.x);
     for (int o = p.o0 & ~3; o < p.o1; o += p.ahead, p.advance(&q)) {
-        const PolicyLoads L = policy_load<KL, SAFE>(A, C, q, q.mask ? counted(q) : 0, p.maxlen, p.row_a);
-        policy_group<KL, ROWS, SAFE>(A, C, q, L, p.maxlen, weight, S);
+        const PolicyLoads L = policy_load<KL, ENT, SAFE>(A, C, q, q.mask ? counted(q) : 0, p.maxlen, p.row_a);
+        policy_group<KL, ROWS, ENT>(A, C, q, L, p.maxlen, weight, S);
     }
 }
 
@@ -707,7 +683,7 @@ __device__ __forceinline__ double slot_total(const PolicyArgs& A, const SlotView
 
 // The loss and its gradient, the elements that count given by the bits (by the labels for a sum, which
 // needs no weights and so no pass before).
-template <int KL, int REDUCE>
+template <int KL, int REDUCE, bool ENT>
 __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
     constexpr bool ROWS = REDUCE == ODB_REDUCE_ROW_MEAN, LABELS = REDUCE == ODB_REDUCE_SUM;
     __shared__ double s_weight[ROWS ? kLdsRows : 1];
@@ -715,66 +691,70 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int64_t total = run_elems(t, e_base);
-    for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
-        const int64_t c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
-        if (c0 >= c1) break;
-        const int64_t k0 = LABELS ? first_slot(t, e_base, c0) : (int64_t)A.chunk_slot[b];
-        if (!LABELS) load_bits(s_bits, A.bits, b, A.chunk);
-        chunk_slots(t, e_base, r_base, k0, c0, c1,
-                    [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
-            const Span p(s, a0, a1, c0, kBlock);
-            const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
-            double same = 1.0;       // weight of every token, where rows have none of their own
-            double rows = 0;         // of the slot, with a counted token
-            const int here = (int)((a1 - 1 - s.lo) / s.maxlen) - p.row_a + 1;
-            const bool lds = ROWS && here <= kLdsRows;
-            if (ROWS) {
-                // whole rows of every chunk, and those that start in it and go on
-                rows = slot_total(A, s, [&](int64_t j) {
-                    const int64_t end = (j + 1) * A.chunk;
-                    int n = A.slot_count[j + k];
-                    if (end < s.hi && (end - s.lo) % s.maxlen) {
-                        const int64_t row = (end - s.lo) / s.maxlen;
-                        if (s.lo + row * s.maxlen >= j * A.chunk) n += row_tokens(A, s, row) > 0;
-                    }
-                    return n;
-                });
-            } else if (!LABELS) {
-                const double n = slot_total(A, s, [&](int64_t j) { return A.slot_count[j + k]; });
-                same = n > 0 ? 1.0 / n : 0.0;
-            }
-            auto row_weight = [&](int row) {
-                const int n = row_tokens(A, s, row);
-                return n > 0 ? 1.0 / ((double)n * rows) : 0.0;
-            };
-            if (lds) {
-                for (int i = threadIdx.x; i < here; i += kBlock) s_weight[i] = row_weight(p.row_a + i);
-                __syncthreads();
-            }
-            const float factor = (float)(scale * same);
-            auto weight = [&](int row, float* f, float* gs) {
-                if (ROWS) {
-                    const double w = lds ? s_weight[row - p.row_a] : row_weight(row);
-                    *f = (float)w;
-                    *gs = (float)(scale * w);
-                } else {
-                    *f = 1.0f;
-                    *gs = factor;
+    const int64_t b = blockIdx.x, c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
+    if (c0 >= c1) return;
+    const int64_t k0 = LABELS ? first_slot(t, e_base, c0) : (int64_t)A.chunk_slot[b];
+    if (!LABELS) load_bits(s_bits, A.bits, b, A.chunk);
+    chunk_slots(t, e_base, r_base, k0, c0, c1, [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+        const Span p(s, a0, a1, c0, kBlock);
+        const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
+        double same = 1.0;       // weight of every token, where rows have none of their own
+        double rows = 0;         // of the slot, with a counted token
+        const int here = (int)((a1 - 1 - s.lo) / s.maxlen) - p.row_a + 1;
+        const bool lds = ROWS && here <= kLdsRows;
+        if (ROWS) {
+            // whole rows of every chunk, and those that start in it and go on
+            rows = slot_total(A, s, [&](int64_t j) {
+                const int64_t end = (j + 1) * A.chunk;
+                int n = A.slot_count[j + k];
+                if (end < s.hi && (end - s.lo) % s.maxlen) {
+                    const int64_t row = (end - s.lo) / s.maxlen;
+                    if (s.lo + row * s.maxlen >= j * A.chunk) n += row_tokens(A, s, row) > 0;
                 }
+                return n;
+            });
+        } else if (!LABELS) {
+            const double n = slot_total(A, s, [&](int64_t j) { return A.slot_count[j + k]; });
+            same = n > 0 ? 1.0 / n : 0.0;
+        }
+        auto row_weight = [&](int row) {
+            const int n = row_tokens(A, s, row);
+            return n > 0 ? 1.0 / ((double)n * rows) : 0.0;
+        };
+        if (lds) {
+            for (int i = threadIdx.x; i < here; i += kBlock) s_weight[i] = row_weight(p.row_a + i);
+            __syncthreads();
+        }
+        const float factor = (float)(scale * same);
+        auto weight = [&](int row, float* f, float* gs) {
+            if (ROWS) {
+                const double w = lds ? s_weight[row - p.row_a] : row_weight(row);
+                *f = (float)w;
+                *gs = (float)(scale * w);
+            } else {
+                *f = 1.0f;
+                *gs = factor;
+            }
+        };
+        const PolicyChunk C = policy_chunk(A, s, c0);
+        auto from_bits = [&](const Group& q) { return s_bits[q.o / 32] >> (q.o & 31) & q.mask; };
+        PolicySums S;
+        if (at_end(p.o1, C.last)) {
+            auto from_labels = [&](const Group& q) {
+                return count_mask(q, load4<int4u, true>(t.d_labels + c0, q.o, C.last, kIgnore), p.maxlen, t.shift);
             };
-            const PolicyChunk C = policy_chunk(A, s, c0);
-            auto counted = [&](const Group& q) {
-                if (!LABELS) return s_bits[q.o / 32] >> (q.o & 31) & q.mask;
-                int4u y = load4<int4u, false>(t.d_labels + c0, q.o, C.last, kIgnore);
-                settle<false>(&y, q.o, C.last, kIgnore);
-                return count_mask(q, y, p.maxlen, t.shift);
+            if (LABELS) policy_span<KL, ROWS, ENT, true>(A, C, p, from_labels, weight, S);
+            else policy_span<KL, ROWS, ENT, true>(A, C, p, from_bits, weight, S);
+        } else {
+            auto from_labels = [&](const Group& q) {
+                return count_mask(q, load4<int4u, false>(t.d_labels + c0, q.o, C.last, kIgnore), p.maxlen, t.shift);
             };
-            PolicySums S;
-            policy_span<KL, ROWS, false>(A, C, p, counted, weight, S);
-            const SlotPart part = block_part(S, same);
-            if (threadIdx.x == 0) A.slot_part[b + k] = part;
-        });
-    }
+            if (LABELS) policy_span<KL, ROWS, ENT, false>(A, C, p, from_labels, weight, S);
+            else policy_span<KL, ROWS, ENT, false>(A, C, p, from_bits, weight, S);
+        }
+        const SlotPart part = block_part(S, same);
+        if (threadIdx.x == 0) A.slot_part[b + k] = part;
+    });
 }
 
 // A run of one chunk, in one launch of one block: 6 us for 256 elements where the passes take 12.
@@ -819,7 +799,9 @@ __global__ void __launch_bounds__(kBlock) policy_one_kernel(PolicyArgs A, int re
             *gs = (float)(scale * w);
         };
         PolicySums S;
-        policy_span<KL, true, true>(A, C, p, [&](const Group& q) { return (uint32_t)s_nibble[q.o / 4]; }, weight, S);
+        auto counted = [&](const Group& q) { return (uint32_t)s_nibble[q.o / 4]; };
+        if (A.entropy) policy_span<KL, true, true, true>(A, C, p, counted, weight, S);
+        else policy_span<KL, true, false, true>(A, C, p, counted, weight, S);
         const SlotPart part = block_part(S, 1.0);
         if (threadIdx.x == 0) {
             const int64_t clipped[3] = {part.clipped[0], part.clipped[1], part.clipped[2]};
@@ -833,9 +815,11 @@ const PolicyOneKernel policy_one_kernels[4] = {policy_one_kernel<0>, policy_one_
                                                policy_one_kernel<3>};
 
 using PolicyKernel = void (*)(PolicyArgs);
-#define ODB_POLICY_KERNELS(KL) {policy_kernel<KL, 0>, policy_kernel<KL, 1>, policy_kernel<KL, 2>}
-const PolicyKernel policy_kernels[4][3] = {ODB_POLICY_KERNELS(0), ODB_POLICY_KERNELS(1), ODB_POLICY_KERNELS(2),
-                                           ODB_POLICY_KERNELS(3)};   // by odb_kl_t and odb_reduce_t
+#define ODB_POLICY_KERNELS(KL) \
+    {{policy_kernel<KL, 0, false>, policy_kernel<KL, 1, false>, policy_kernel<KL, 2, false>}, \
+     {policy_kernel<KL, 0, true>, policy_kernel<KL, 1, true>, policy_kernel<KL, 2, true>}}
+const PolicyKernel policy_kernels[4][2][3] = {ODB_POLICY_KERNELS(0), ODB_POLICY_KERNELS(1), ODB_POLICY_KERNELS(2),
+                                              ODB_POLICY_KERNELS(3)};   // by odb_kl_t, entropies and odb_reduce_t
 #undef ODB_POLICY_KERNELS
 
 // The slots' numbers from their chunks' partials, a wave a slot.
@@ -843,7 +827,7 @@ __global__ void __launch_bounds__(kBlock) policy_slots_kernel(PolicyArgs A) {
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int lane = threadIdx.x & (kWave - 1);
-    for (int64_t k = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave; k < t.num_slots;
+    for (int64_t k = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); k < t.num_slots;
          k += (int64_t)gridDim.x * kWaves) {
         const SlotView s = slot_view(t, k, e_base, r_base);
         double sum[4] = {0, 0, 0, 0};
@@ -923,164 +907,158 @@ __device__ __forceinline__ void leave_row(const PairArgs& A, const SlotView& s, 
 // The lowest n of four bits.
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 4 ? 0xfu : (1u << n) - 1; }
 
-// Elements that count of a group and, one by one, logprob - ref.
-struct RowTerms {
-    uint32_t on;
-    double x[4];
-};
-
-template <bool REF>
-__device__ __forceinline__ RowTerms row_terms(const int4u& y, const float4u& p, const float4u& r, uint32_t mask) {
-    RowTerms o;
-    o.on = mask;
+// The wave's part of a slot with longer rows: positions [a0, a1) - c0 of its quarter.
+template <bool REF, bool SAFE>
+__device__ __forceinline__ void long_rows(const PairArgs& A, const SlotView& s, int64_t part, int64_t c0, int64_t a0,
+                                          int64_t a1, int last, int lane, uint32_t* bits) {
+    const int32_t* labels = A.t.d_labels + c0;
+    const float* logprob = A.logprob + c0;
+    const float* ref = A.ref + c0;
+    const int o0 = (int)(a0 - c0), o1 = (int)(a1 - c0), shift = A.t.shift;
+    int row = (int)((a0 - s.lo) / s.maxlen);
+    // the current row's positions in the quarter; its start may lie before, its end behind
+    int64_t ends = s.lo + ((int64_t)row + 1) * s.maxlen - c0;
+    int begin = ends - s.maxlen >= 0 ? (int)(ends - s.maxlen) + shift : 0;
+    int count = 0;          // of the lane
+    double sum = 0.0;
+    for (int o = o0 & ~3; o < o1; o += 4 * kWave * kRowAhead) {   // uniform
+        int4u y[kRowAhead];
+        float4u lp[kRowAhead], rf[kRowAhead];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (y[j] == ODB_LABEL_IGNORE) o.on &= ~(1u << j);
+        for (int i = 0; i < kRowAhead; ++i) {
+            const int at = o + 4 * (kWave * i + lane);
+            y[i] = load4<int4u, SAFE>(labels, at, last, kIgnore);
+            lp[i] = load4<float4u, SAFE>(logprob, at, last, 0.0f);
+            if (REF) rf[i] = load4<float4u, SAFE>(ref, at, last, 0.0f);
+        }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const double x = REF ? (double)p[j] - (double)r[j] : (double)p[j];
-        o.x[j] = o.on >> j & 1 ? x : 0.0;
+        for (int i = 0; i < kRowAhead; ++i) {
+            const int from = o + 4 * kWave * i, at = from + 4 * lane;
+            if (from >= o1) break;     // uniform
+            const int to = from + 4 * kWave < o1 ? from + 4 * kWave : o1;
+            uint32_t real = 0, on = 0;
+            double x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                real |= (uint32_t)(y[i][j] != ODB_LABEL_IGNORE) << j;
+                x[j] = REF ? (double)lp[i][j] - (double)rf[i][j] : (double)lp[i][j];
+            }
+            for (;;) {     // the rows in these 256 elements; uniform
+                const int z = ends < to ? (int)ends : to;
+                const uint32_t mine = real & low_bits(z - at) & ~low_bits(begin - at);   // none behind the slot
+                on |= mine;
+                count += __builtin_popcount(mine);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum += mine >> j & 1 ? x[j] : 0.0;
+                if (ends > to || (ends == to && to == o1)) break;
+                leave_row(A, s, part, c0, row, wave_total(count), wave_total(sum), lane);
+                count = 0;
+                sum = 0.0;
+                ++row;
+                begin = (int)ends + shift;
+                ends += s.maxlen;
+                if (begin - shift >= to) break;
+            }
+            if (on) atomicOr(&bits[at >> 5], on << (at & 31));
+        }
     }
-    return o;
+    leave_row(A, s, part, c0, row, wave_total(count), wave_total(sum), lane);
+}
+
+// The same with rows of up to 64 elements, taken by the smallest power of two of lanes that covers them
+// four elements each.
+template <bool REF>
+__device__ __forceinline__ void short_rows(const PairArgs& A, const SlotView& s, int64_t part, int64_t c0, int64_t a0,
+                                           int64_t a1, int last, int lane, uint32_t* bits) {
+    const int row_a = (int)((a0 - s.lo) / s.maxlen), row_b = (int)((a1 - 1 - s.lo) / s.maxlen);
+    const int o0 = (int)(a0 - c0), o1 = (int)(a1 - c0);
+    int lanes = 1;
+    while (4 * lanes < s.maxlen) lanes *= 2;
+    const int sub = lane & (lanes - 1);
+    // every group of lanes goes round as often as the first, so that none leaves a reduction alone
+    for (int r0 = row_a; r0 <= row_b; r0 += kWave / lanes) {
+        const int r = r0 + lane / lanes;
+        int count = 0;
+        double sum = 0.0;
+        if (r <= row_b) {
+            // positions in the quarter; a row's start may lie before it
+            const int start = (int)(s.lo + (int64_t)r * s.maxlen - c0);
+            const int x0 = start > o0 ? start : o0, x1 = start + s.maxlen < o1 ? start + s.maxlen : o1;
+            const int o = x0 + 4 * sub, from = start + A.t.shift;
+            if (o < x1) {
+                uint32_t on = low_bits(x1 - o) & ~low_bits(from - o);
+                int4u y;
+                float4u p, q = {0, 0, 0, 0};
+                if (o <= last) {
+                    y = load4<int4u, false>(A.t.d_labels + c0, o, last, kIgnore);
+                    p = load4<float4u, false>(A.logprob + c0, o, last, 0.0f);
+                    if (REF) q = load4<float4u, false>(A.ref + c0, o, last, 0.0f);
+                } else {
+                    y = load4<int4u, true>(A.t.d_labels + c0, o, last, kIgnore);
+                    p = load4<float4u, true>(A.logprob + c0, o, last, 0.0f);
+                    if (REF) q = load4<float4u, true>(A.ref + c0, o, last, 0.0f);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (y[j] == ODB_LABEL_IGNORE) on &= ~(1u << j);
+                    const double x = REF ? (double)p[j] - (double)q[j] : (double)p[j];
+                    sum += on >> j & 1 ? x : 0.0;
+                }
+                count = __builtin_popcount(on);
+                const uint64_t w = (uint64_t)on << (o & 31);
+                if ((uint32_t)w) atomicOr(&bits[o >> 5], (uint32_t)w);
+                if (w >> 32) atomicOr(&bits[(o >> 5) + 1], (uint32_t)(w >> 32));
+            }
+        }
+        for (int d = lanes / 2; d > 0; d >>= 1) {
+            count += __shfl_xor(count, d, kWave);
+            sum += __shfl_xor(sum, d, kWave);
+        }
+        if (r <= row_b) leave_row(A, s, part, c0, r, count, sum, sub);
+    }
 }
 
 // First pass: the bits, and per quarter of a chunk and row how many tokens count and the sum over
 // them.  A wave takes a quarter.  Rows of more than 64 elements are summed across the wave as its 256
-// elements at a time come in and are left where they end: the loads do not wait for the reductions.
-// Shorter ones are taken by the smallest power of two of lanes that covers them four elements each.
-template <bool REF, bool SAFE>
-__device__ __forceinline__ void row_sums(const PairArgs& A) {
-    __shared__ uint32_t s_bits[SAFE ? kOneChunk / 32 : kMaxChunk / 32];
+// elements at a time come in and are left where they end.
+template <bool REF>
+__device__ __forceinline__ void row_sums(const PairArgs& A, uint32_t* s_bits) {
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int64_t total = run_elems(t, e_base);
     const int words = A.chunk / 32, quarter = A.chunk / kWaves;
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
-        if (b * A.chunk >= total) break;
-        for (int i = threadIdx.x; i < words; i += kBlock) s_bits[i] = 0;
-        __syncthreads();
-        const int64_t part = b * kWaves + wave, c0 = part * quarter, c1 = c0 + quarter < total ? c0 + quarter : total;
-        uint32_t* bits = s_bits + wave * (quarter / 32);
-        const int64_t k0 = c0 < c1 ? first_slot(t, e_base, c0) : 0;
+    // (uniform over the wave, which the compiler does not see by itself)
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t b = blockIdx.x;
+    if (A.status)
+        for (int64_t k = b * kBlock + threadIdx.x; k < t.num_slots; k += (int64_t)gridDim.x * kBlock)
+            if (!slot_view(t, k, e_base, r_base).ok) *A.status = kErrTiles;
+    if (b * A.chunk >= total) return;
+    for (int i = threadIdx.x; i < words; i += kBlock) s_bits[i] = 0;
+    __syncthreads();
+    const int64_t part = b * kWaves + wave, c0 = part * quarter, c1 = c0 + quarter < total ? c0 + quarter : total;
+    if (c0 < c1) {
+        const int64_t k0 = first_slot(t, e_base, c0);
         if (threadIdx.x == 0) A.chunk_slot[b] = (int32_t)k0;     // the first wave's quarter starts the chunk
         const int last = last_four(t, c0);
-        const int32_t* labels = t.d_labels + c0;
-        const float* logprob = A.logprob + c0;
-        const float* ref = A.ref + c0;
-        if (c0 < c1)
-            chunk_slots(t, e_base, r_base, k0, c0, c1, [&](int64_t, const SlotView& s, int64_t a0, int64_t a1) {
-                if (s.maxlen > kShortRow) {
-                    const int o0 = (int)(a0 - c0), o1 = (int)(a1 - c0);
-                    int row = (int)((a0 - s.lo) / s.maxlen);
-                    // the current row's positions in the quarter; its start may lie before, its end behind
-                    int64_t ends = s.lo + ((int64_t)row + 1) * s.maxlen - c0;
-                    int begin = ends - s.maxlen >= 0 ? (int)(ends - s.maxlen) + t.shift : 0;
-                    int count = 0;          // of the wave
-                    double sum = 0.0;       // of the lane
-                    for (int o = o0 & ~3; o < o1; o += 4 * kWave * kRowAhead) {   // uniform
-                        int4u y[kRowAhead];
-                        float4u lp[kRowAhead], rf[kRowAhead];
-#pragma unroll
-                        for (int i = 0; i < kRowAhead; ++i) {
-                            const int at = o + 4 * (kWave * i + lane);
-                            y[i] = load4<int4u, SAFE>(labels, at, last, kIgnore);
-                            lp[i] = load4<float4u, SAFE>(logprob, at, last, 0.0f);
-                            if (REF) rf[i] = load4<float4u, SAFE>(ref, at, last, 0.0f);
-                        }
-#pragma unroll
-                        for (int i = 0; i < kRowAhead; ++i) {
-                            const int from = o + 4 * kWave * i, at = from + 4 * lane;
-                            if (from >= o1) break;     // uniform
-                            const int to = from + 4 * kWave < o1 ? from + 4 * kWave : o1;
-                            uint32_t real = 0, on = 0;
-                            double x[4] = {0, 0, 0, 0};
-                            if (!SAFE && at > last) {
-                                settle<SAFE>(&y[i], at, last, kIgnore);
-                                settle<SAFE>(&lp[i], at, last, 0.0f);
-                                if (REF) settle<SAFE>(&rf[i], at, last, 0.0f);
-                            }
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                real |= (uint32_t)(y[i][j] != ODB_LABEL_IGNORE) << j;
-                                x[j] = REF ? (double)lp[i][j] - (double)rf[i][j] : (double)lp[i][j];
-                            }
-                            for (;;) {     // the rows in these 256 elements; uniform
-                                const int z = ends < to ? (int)ends : to;
-                                const uint32_t mine = real & low_bits(z - at) & ~low_bits(begin - at);   // none behind the slot
-                                on |= mine;
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    const bool live = mine >> j & 1;
-                                    sum += live ? x[j] : 0.0;
-                                    count += __popcll(__ballot(live));
-                                }
-                                if (ends > to || (ends == to && to == o1)) break;
-                                leave_row(A, s, part, c0, row, count, wave_total(sum), lane);
-                                count = 0;
-                                sum = 0.0;
-                                ++row;
-                                begin = (int)ends + t.shift;
-                                ends += s.maxlen;
-                                if (begin - t.shift >= to) break;
-                            }
-                            if (on) atomicOr(&bits[at >> 5], on << (at & 31));
-                        }
-                    }
-                    leave_row(A, s, part, c0, row, count, wave_total(sum), lane);
-                } else {
-                    const int row_a = (int)((a0 - s.lo) / s.maxlen), row_b = (int)((a1 - 1 - s.lo) / s.maxlen);
-                    int lanes = 1;
-                    while (4 * lanes < s.maxlen) lanes *= 2;
-                    const int sub = lane & (lanes - 1);
-                    // every group of lanes goes round as often as the first, so that none leaves a reduction alone
-                    for (int r0 = row_a; r0 <= row_b; r0 += kWave / lanes) {
-                        const int r = r0 + lane / lanes;
-                        int count = 0;
-                        double sum = 0.0;
-                        if (r <= row_b) {
-                            // positions in the quarter; a row's start may lie before it
-                            const int start = (int)(s.lo + (int64_t)r * s.maxlen - c0);
-                            const int x0 = start > (int)(a0 - c0) ? start : (int)(a0 - c0);
-                            const int x1 = start + s.maxlen < (int)(a1 - c0) ? start + s.maxlen : (int)(a1 - c0);
-                            const int o = x0 + 4 * sub, from = start + t.shift;
-                            if (o < x1) {
-                                uint32_t mask = x1 - o >= 4 ? 0xfu : 0xfu >> (4 - (x1 - o));
-                                if (o < from) mask &= 0xfu << (from - o < 4 ? from - o : 4);
-                                int4u y = load4<int4u, SAFE>(labels, o, last, kIgnore);
-                                float4u lp = load4<float4u, SAFE>(logprob, o, last, 0.0f), rf = {0, 0, 0, 0};
-                                if (REF) rf = load4<float4u, SAFE>(ref, o, last, 0.0f);
-                                settle<SAFE>(&y, o, last, kIgnore);
-                                settle<SAFE>(&lp, o, last, 0.0f);
-                                if (REF) settle<SAFE>(&rf, o, last, 0.0f);
-                                const RowTerms v = row_terms<REF>(y, lp, rf, mask);
-                                count = __builtin_popcount(v.on);
-                                sum = (v.x[0] + v.x[1]) + (v.x[2] + v.x[3]);
-                                const uint64_t w = (uint64_t)v.on << (o & 31);
-                                if ((uint32_t)w) atomicOr(&bits[o >> 5], (uint32_t)w);
-                                if (w >> 32) atomicOr(&bits[(o >> 5) + 1], (uint32_t)(w >> 32));
-                            }
-                        }
-                        for (int d = lanes / 2; d > 0; d >>= 1) {
-                            count += __shfl_xor(count, d, kWave);
-                            sum += __shfl_xor(sum, d, kWave);
-                        }
-                        if (r <= row_b) leave_row(A, s, part, c0, r, count, sum, sub);
-                    }
-                }
-            });
-        __syncthreads();
-        for (int i = threadIdx.x; i < words; i += kBlock) A.bits[b * words + i] = s_bits[i];
-        __syncthreads();
+        uint32_t* bits = s_bits + wave * (quarter / 32);
+        chunk_slots(t, e_base, r_base, k0, c0, c1, [&](int64_t, const SlotView& s, int64_t a0, int64_t a1) {
+            if (s.maxlen <= kShortRow)
+                short_rows<REF>(A, s, part, c0, a0, a1, last, lane, bits);
+            else if (at_end((int)(a1 - c0), last))
+                long_rows<REF, true>(A, s, part, c0, a0, a1, last, lane, bits);
+            else
+                long_rows<REF, false>(A, s, part, c0, a0, a1, last, lane, bits);
+        });
     }
-    if (A.status)
-        for (int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x; k < t.num_slots; k += (int64_t)gridDim.x * kBlock)
-            if (!slot_view(t, k, e_base, r_base).ok) *A.status = kErrTiles;
+    __syncthreads();
+    for (int i = threadIdx.x; i < words; i += kBlock) A.bits[b * words + i] = s_bits[i];
 }
 
 template <bool REF>
 __global__ void __launch_bounds__(kBlock) row_sums_kernel(PairArgs A) {
-    row_sums<REF, false>(A);
+    __shared__ uint32_t s_bits[kMaxChunk / 32];
+    row_sums<REF>(A, s_bits);
 }
 
 // Clears the entries of the ids that have a row.  The others hold anything: an entry is believed
@@ -1206,47 +1184,43 @@ __device__ __forceinline__ void leave_totals(const PairArgs& A, double loss, dou
     }
 }
 
-// Gradients of the block's chunks from the factors of the rows.
-template <int CHUNK>
-__device__ __forceinline__ void pairs_grad(const PairArgs& A, const double* coef) {
-    __shared__ uint32_t s_bits[CHUNK / 32];
+// Gradients of the block's chunk from the factors of the rows.
+__device__ __forceinline__ void pairs_grad(const PairArgs& A, const double* coef, uint32_t* s_bits) {
     const odb_tiles_t& t = A.t;
     if (!A.grad) return;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int64_t total = run_elems(t, e_base);
-    for (int64_t b = blockIdx.x; b < A.chunks; b += gridDim.x) {   // uniform
-        const int64_t c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
-        if (c0 >= c1) break;
-        const int64_t k0 = A.chunk_slot[b];
-        load_bits(s_bits, A.bits, b, A.chunk);
-        chunk_slots(t, e_base, r_base, k0, c0, c1,
-                    [&](int64_t, const SlotView& s, int64_t a0, int64_t a1) {
-            const Span p(s, a0, a1, c0, kBlock);
-            const double* of_row = coef + s.row0;
-            Group q = p.first((int)threadIdx.x);
+    const int64_t b = blockIdx.x, c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
+    if (c0 >= c1) return;
+    const int64_t k0 = A.chunk_slot[b];
+    load_bits(s_bits, A.bits, b, A.chunk);
+    chunk_slots(t, e_base, r_base, k0, c0, c1, [&](int64_t, const SlotView& s, int64_t a0, int64_t a1) {
+        const Span p(s, a0, a1, c0, kBlock);
+        const double* of_row = coef + s.row0;
+        Group q = p.first((int)threadIdx.x);
 #pragma unroll 4
-            for (; q.o < p.o1; p.advance(&q)) {
-                const uint32_t on = s_bits[q.o / 32] >> (q.o & 31) & q.mask;
-                const float c = (float)of_row[q.row];
-                float v[4];
+        for (; q.o < p.o1; p.advance(&q)) {
+            const uint32_t on = s_bits[q.o / 32] >> (q.o & 31) & q.mask;
+            const float c = (float)of_row[q.row];
+            float v[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = on >> j & 1 ? c : 0.0f;
-                if (q.col > p.maxlen - 4) {
-                    Group r = q;
+            for (int j = 0; j < 4; ++j) v[j] = on >> j & 1 ? c : 0.0f;
+            if (q.col > p.maxlen - 4) {
+                Group r = q;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (on >> j & 1) v[j] = (float)of_row[r.row];
-                        r.next(p.maxlen);
-                    }
+                for (int j = 0; j < 4; ++j) {
+                    if (on >> j & 1) v[j] = (float)of_row[r.row];
+                    r.next(p.maxlen);
                 }
-                store4(A.grad + c0, q, v);
             }
-        });
-    }
+            store4(A.grad + c0, q, v);
+        }
+    });
 }
 
 // Gradients of the tiles; the first block also sums what the pairs left.
 __global__ void __launch_bounds__(kBlock) pairs_grad_kernel(PairArgs A, int64_t parts) {
+    __shared__ uint32_t s_bits[kMaxChunk / 32];
     if (blockIdx.x == 0) {
         double loss = 0.0, pairs = 0.0, right = 0.0;
         for (int64_t i = threadIdx.x; i < parts; i += kBlock) {
@@ -1256,7 +1230,7 @@ __global__ void __launch_bounds__(kBlock) pairs_grad_kernel(PairArgs A, int64_t 
         }
         leave_totals(A, loss, pairs, right);
     }
-    pairs_grad<kMaxChunk>(A, A.coef);
+    pairs_grad(A, A.coef, s_bits);
 }
 
 constexpr int64_t kFewChunks = 1024;
@@ -1265,12 +1239,13 @@ constexpr int64_t kFewChunks = 1024;
 // waiting for a kernel that does would, and the first one leaves the rows' numbers.
 __global__ void __launch_bounds__(kBlock) few_rows_kernel(PairArgs A) {
     __shared__ double s_coef[kBlock];
+    __shared__ uint32_t s_bits[kMaxChunk / 32];
     const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
     PairSums sums;
     s_coef[threadIdx.x] = threadIdx.x < rows ? pair_row(A, threadIdx.x, rows, blockIdx.x == 0, &sums) : 0.0;
     if (blockIdx.x == 0) leave_totals(A, sums.loss, sums.pairs, sums.right);
     __syncthreads();
-    pairs_grad<kMaxChunk>(A, s_coef);
+    pairs_grad(A, s_coef, s_bits);
 }
 
 __global__ void no_pairs_kernel(PairArgs A) {
@@ -1281,19 +1256,20 @@ __global__ void no_pairs_kernel(PairArgs A) {
 // A run of one chunk, in one launch of one block.
 template <bool REF>
 __global__ void __launch_bounds__(kBlock) pairs_one_kernel(PairArgs A) {
+    __shared__ uint32_t s_bits[kOneChunk / 32];
     if (A.row_of) {
         clear_rows(A);
         __threadfence();     // before the atomics on the same entries
         __syncthreads();
     }
-    row_sums<REF, true>(A);
+    row_sums<REF>(A, s_bits);
     __syncthreads();
     const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
     PairSums sums;
     for (int64_t row = threadIdx.x; row < rows; row += kBlock) A.coef[row] = pair_row(A, row, rows, true, &sums);
     leave_totals(A, sums.loss, sums.pairs, sums.right);
     __syncthreads();
-    pairs_grad<kOneChunk>(A, A.coef);
+    pairs_grad(A, A.coef, s_bits);
 }
 
 int check_tile_arrays(const odb_tiles_t* t) {
@@ -1382,7 +1358,7 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     a.high = (float)(1.0 + p->clip_high);
     a.dual = (float)p->dual_clip;
     a.token_advantage = p->token_advantage;
-    const dim3 grid(grid_for(L.chunks, 1)), block(kBlock);
+    const dim3 grid((unsigned)L.chunks), block(kBlock);     // at most 2^23 blocks
     if (L.chunks <= 1) {
         hipLaunchKernelGGL(policy_one_kernels[p->kl], dim3(1), block, 0, s, a, (int)p->reduce);
         ODB_LAUNCHED();
@@ -1393,7 +1369,7 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
                            grid, block, 0, s, a);
         ODB_LAUNCHED();
     }
-    hipLaunchKernelGGL(policy_kernels[p->kl][p->reduce], grid, block, 0, s, a);
+    hipLaunchKernelGGL(policy_kernels[p->kl][d_entropy ? 1 : 0][p->reduce], grid, block, 0, s, a);
     ODB_LAUNCHED();
     hipLaunchKernelGGL(policy_slots_kernel, dim3(grid_for(t->num_slots, kWaves)), block, 0, s, a);
     ODB_LAUNCHED();
@@ -1459,7 +1435,7 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
     a.loss_scale = p->loss_scale;
     a.kind = p->kind;
     a.normalize = p->normalize;
-    const dim3 block(kBlock), grid(grid_for(L.chunks, 1));
+    const dim3 block(kBlock), grid((unsigned)L.chunks);     // at most 2^23 blocks
     if (!any) {
         hipLaunchKernelGGL(no_pairs_kernel, dim3(1), dim3(1), 0, s, a);
         ODB_LAUNCHED();
