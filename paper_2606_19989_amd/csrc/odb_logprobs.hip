@@ -26,25 +26,54 @@ constexpr float kFarBelow = -16384.0f;   // base-2 exponent whose power is 0, fi
 typedef __bf16 bf16_t;
 typedef _Float16 fp16_t;
 
-// 16 bytes of logits: N values.  Rows of an odd vocabulary start at any element, so the loads are
-// declared with the element's alignment; global memory serves 16-byte accesses at any address.
+// 16 bytes of logits: N values.  Rows of an odd vocabulary start at any element; global memory serves
+// 16-byte accesses at any address.  The forward call makes use of that, so that a row's sums run in the
+// same order wherever it lies.  The gradient is written in the alignment of its own rows: up to N - 1
+// elements one by one, then 16 bytes at a time (2,545 positions of 65,537 bf16 logits: 79 us, 120 us
+// without).
+typedef unsigned u4a2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned u4a4 __attribute__((ext_vector_type(4), aligned(4)));
+template <int ALIGN>
+struct Words {
+    typedef u4a2 type;
+};
+template <>
+struct Words<4> {
+    typedef u4a4 type;
+};
+
 template <typename T>
 struct alignas(sizeof(T)) Vec {
     static constexpr int N = 16 / sizeof(T);
     T v[N];
 };
 
-template <typename T>
+template <bool ONCE, typename T>
 __device__ __forceinline__ Vec<T> load_vec(const T* p) {
+    const auto* q = reinterpret_cast<const typename Words<sizeof(T)>::type*>(p);
+    const auto w = ONCE ? __builtin_nontemporal_load(q) : *q;
     Vec<T> r;
-    __builtin_memcpy(&r, p, 16);
+    __builtin_memcpy(&r, &w, 16);
     return r;
 }
 
 template <typename T>
 __device__ __forceinline__ void store_vec(T* p, const Vec<T>& r) {
-    __builtin_memcpy(p, &r, 16);
+    typename Words<sizeof(T)>::type w;
+    __builtin_memcpy(&w, &r, 16);
+    __builtin_nontemporal_store(w, reinterpret_cast<typename Words<sizeof(T)>::type*>(p));
 }
+
+// Elements before the first 16-byte boundary of a row, at most n.
+template <typename T>
+__device__ __forceinline__ int head_of(const T* p, int64_t n) {
+    const int h = (int)(-reinterpret_cast<uintptr_t>(p) & 15) / (int)sizeof(T);
+    return h < n ? h : (int)n;
+}
+
+constexpr int kAhead = 4;    // 16-byte loads of a thread that are under way together
+
+__device__ __forceinline__ int64_t at_most(int64_t v, int64_t most) { return v < most ? v : most; }
 
 struct Acc {
     float m, s, t;
@@ -96,12 +125,7 @@ __device__ __forceinline__ Acc acc_join(Acc a, Acc b, float k) {
     return a;
 }
 
-// Token of a position, or -1: position q = (i, c) of the tile.
-struct Token {
-    int64_t at;     // index of the token in the tile
-    int32_t label;  // -1: not scored
-};
-
+// Label of a token, or -1 if it is not scored.
 __device__ __forceinline__ int32_t read_label(const int32_t* labels, int64_t at, int64_t vocab, int32_t* status,
                                               bool report) {
     const int32_t y = labels[at];
@@ -113,7 +137,8 @@ __device__ __forceinline__ int32_t read_label(const int32_t* labels, int64_t at,
     return y;
 }
 
-// A group of G threads takes a position; blocks of max(G, 256) threads.
+// A group of G threads (a divisor of a wave or whole waves) takes a position; blocks of max(G, 256)
+// threads.  G is 8 at least, so that a thread has at most one of the elements outside the 16-byte groups.
 template <typename T, bool ENT, int G>
 __global__ void __launch_bounds__(G > kBlock ? G : kBlock) token_logprobs_kernel(odb_logits_t x,
                                                                                 const int32_t* __restrict__ labels,
@@ -144,21 +169,20 @@ __global__ void __launch_bounds__(G > kBlock ? G : kBlock) token_logprobs_kernel
                      (int64_t)(c - (uint32_t)x.shift) * x.col_stride;
         const float zy = (float)z[y];
         Acc r{kLowest, 0.0f, 0.0f};
-        const int64_t whole = V / N * N;
-        int64_t v = (int64_t)t * N;
-        for (; v + 3 * G * N < whole; v += 4 * G * N) {
-            Vec<T> w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = load_vec(z + v + j * G * N);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc_vec<T, ENT>(r, w[j], k);
-        }
-        for (; v < whole; v += G * N) acc_vec<T, ENT>(r, load_vec(z + v), k);
-        if (whole + t < V) {
-            const float f = (float)z[whole + t];
+        auto one = [&](float f) {
             if (f > r.m) acc_rescale<ENT>(r, f, k);
             acc_term<ENT>(r, f, k);
+        };
+        const int64_t whole = V / N * N;
+        for (int64_t v = (int64_t)t * N; v < whole; v += kAhead * G * N) {
+            Vec<T> w[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) w[j] = load_vec<true>(z + at_most(v + j * G * N, whole - N));
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                if (v + j * G * N < whole) acc_vec<T, ENT>(r, w[j], k);
         }
+        if (whole + t < V) one((float)z[whole + t]);
 #pragma unroll
         for (int d = (G < kWave ? G : kWave) / 2; d > 0; d >>= 1) {
             Acc o{__shfl_xor(r.m, d, kWave), __shfl_xor(r.s, d, kWave), ENT ? __shfl_xor(r.t, d, kWave) : 0.0f};
@@ -193,7 +217,6 @@ __global__ void __launch_bounds__(G > kBlock ? G : kBlock) token_logprobs_backwa
     const int t = threadIdx.x & (G - 1);
     const float a = (float)x.scale, k = a * kLog2e;
     const int64_t V = x.vocab;
-    const int64_t whole = V / N * N;
     for (int64_t q = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G; q < n;
          q += (int64_t)gridDim.x * (kThreads / G)) {
         const uint32_t i = (uint32_t)q / (uint32_t)x.cols, c = (uint32_t)q - i * (uint32_t)x.cols;
@@ -205,12 +228,16 @@ __global__ void __launch_bounds__(G > kBlock ? G : kBlock) token_logprobs_backwa
             if (ENT) h = grad_entropy[at];
         }
         T* d = grad + (int64_t)i * grs + (int64_t)c * gcs;
+        const int head = head_of(d, V);    // the stores' alignment: half a line written costs more than read
+        const int64_t whole = (V - head) / N * N;
+        T* db = d + head;
         if (y < 0 || (g == 0.0f && h == 0.0f)) {
             Vec<T> zero;
 #pragma unroll
             for (int j = 0; j < N; ++j) zero.v[j] = (T)0.0f;
-            for (int64_t v = (int64_t)t * N; v < whole; v += G * N) store_vec(d + v, zero);
-            if (whole + t < V) d[whole + t] = (T)0.0f;
+            if (t < head) d[t] = (T)0.0f;
+            for (int64_t v = (int64_t)t * N; v < whole; v += G * N) store_vec(db + v, zero);
+            if (head + whole + t < V) db[whole + t] = (T)0.0f;
             continue;
         }
         const T* z = static_cast<const T*>(x.d_logits) + (int64_t)i * x.row_stride + (int64_t)c * x.col_stride;
@@ -223,34 +250,39 @@ __global__ void __launch_bounds__(G > kBlock ? G : kBlock) token_logprobs_backwa
             const float p = __builtin_amdgcn_exp2f(u) * inv;
             return ENT ? -p * (c0 + c1 * fmaxf(u, kFarBelow)) : -p * c0;
         };
-        for (int64_t v = (int64_t)t * N; v < whole; v += 4 * G * N) {
-            Vec<T> w[4];
+        auto store_one = [&](int64_t v) {
+            float o = one((float)z[v]);
+            if (v == y) o += ag;
+            d[v] = (T)o;
+        };
+        if (t < head) store_one(t);
+        const T* zb = z + head;
+        const int64_t yb = y - head;
+        auto store_group = [&](const Vec<T>& w, int64_t v) {
+            float o[N];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (v + j * G * N < whole) w[j] = load_vec(z + v + j * G * N);
+            for (int e = 0; e < N; ++e) o[e] = one((float)w.v[e]);
+            if ((uint64_t)(yb - v) < (uint64_t)N) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t b = v + j * G * N;
-                if (b >= whole) break;
-                float o[N];
-#pragma unroll
-                for (int e = 0; e < N; ++e) o[e] = one((float)w[j].v[e]);
-                if ((uint64_t)(y - b) < (uint64_t)N) {
-#pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (b + e == y) o[e] += ag;
-                }
-                Vec<T> r;
-#pragma unroll
-                for (int e = 0; e < N; ++e) r.v[e] = (T)o[e];
-                store_vec(d + b, r);
+                for (int e = 0; e < N; ++e)
+                    if (v + e == yb) o[e] += ag;
             }
+            Vec<T> r;
+#pragma unroll
+            for (int e = 0; e < N; ++e) r.v[e] = (T)o[e];
+            store_vec(db + v, r);
+        };
+        for (int64_t v = (int64_t)t * N; v < whole; v += kAhead * G * N) {
+            Vec<T> w[kAhead];
+            // in place: those past the row's end read what this thread has yet to write or another has written,
+            // and drop it
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) w[j] = load_vec<false>(zb + at_most(v + j * G * N, whole - N));
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                if (v + j * G * N < whole) store_group(w[j], v + j * G * N);
         }
-        if (whole + t < V) {
-            float o = one((float)z[whole + t]);
-            if (whole + t == y) o += ag;
-            d[whole + t] = (T)o;
-        }
+        if (head + whole + t < V) store_one(head + whole + t);
     }
 }
 
@@ -285,38 +317,80 @@ int check_tile(const odb_logits_t* x, const void* p, int64_t rs, int64_t cs, con
     return ODB_OK;
 }
 
-constexpr int64_t kWaveVocab = 2048;
+// Threads of a position, by the bytes of its logits.  Too many leave the reduction and the label's load
+// in front of too little work, too few leave loads unissued.  us for about 600 MB of logits (N positions
+// of V), the last two lines for few positions; 2 x 600 MB for the gradient:
+//   bytes of a row     forward 64 / 256 / 512 threads    backward 64 / 256 / 512 / 1,024
+//   4 KB               109 / 246 / 463                   198 / 325 / 567 / 1049
+//   16 KB               95 / 122 / 189                   222 / 201 / 245 / 403
+//   32 KB               98 /  96 / 123                   219 / 212 / 195 / 284
+//   64 KB              103 /  98 / 110                   250 / 229 / 207 / 203
+//   128 KB             120 / 101 /  97                   283 / 263 / 249 / 215
+//   64 KB x 32        14.7 / 8.4 / 7.2                   14.3 / 6.9 / 6.1 / 5.8
+//   304 KB x 1          58 /  19 /  13                    53 /  17 /  12 /  11
+enum Group { kGroup8, kGroup32, kGroup64, kGroup256, kGroup512, kGroup1024 };
 
-template <typename T>
+Group group_for(const odb_logits_t* x, bool backward) {
+    const int64_t row = x->vocab * (x->dtype == ODB_FLOAT32 ? 4 : 2);
+    if (x->rows * x->cols <= 2 * (int64_t)num_cus())
+        return row <= 1024 ? kGroup64 : row <= 32768 ? kGroup256 : backward && row > 49152 ? kGroup1024 : kGroup512;
+    if (row <= 1024) return kGroup8;
+    if (row <= 2048) return kGroup32;
+    if (!backward) return row <= 16384 ? kGroup64 : row <= 98304 ? kGroup256 : kGroup512;
+    return row <= 8192 ? kGroup64 : row <= 24576 ? kGroup256 : row <= 49152 ? kGroup512 : kGroup1024;
+}
+
+template <typename T, int G>
 void launch_forward(const odb_logits_t* x, const int32_t* labels, float* logprob, float* stats, float* entropy,
                     int32_t* status, hipStream_t s) {
-    const int64_t n = x->rows * x->cols;
-    if (x->vocab <= kWaveVocab) {
-        const dim3 grid(grid_for(n, kBlock / kWave));
-        hipLaunchKernelGGL((entropy ? token_logprobs_kernel<T, true, kWave> : token_logprobs_kernel<T, false, kWave>),
-                           grid, dim3(kBlock), 0, s, *x, labels, logprob, stats, entropy, status);
-    } else {
-        hipLaunchKernelGGL((entropy ? token_logprobs_kernel<T, true, kBlock> : token_logprobs_kernel<T, false, kBlock>),
-                           dim3(grid_for(n, 1)), dim3(kBlock), 0, s, *x, labels, logprob, stats, entropy, status);
-    }
+    constexpr int kThreads = G > kBlock ? G : kBlock;
+    hipLaunchKernelGGL((entropy ? token_logprobs_kernel<T, true, G> : token_logprobs_kernel<T, false, G>),
+                       dim3(grid_for(x->rows * x->cols, kThreads / G)), dim3(kThreads), 0, s, *x, labels, logprob, stats,
+                       entropy, status);
 }
 
 template <typename T>
-void launch_backward(const odb_logits_t* x, const int32_t* labels, const float* stats, const float* gl,
-                     const float* entropy, const float* ge, void* grad, int64_t grs, int64_t gcs, int32_t* status,
-                     hipStream_t s) {
-    const int64_t n = x->rows * x->cols;
-    T* g = static_cast<T*>(grad);
-    if (x->vocab <= kWaveVocab) {
-        const dim3 grid(grid_for(n, kBlock / kWave));
-        hipLaunchKernelGGL((ge ? token_logprobs_backward_kernel<T, true, kWave>
-                               : token_logprobs_backward_kernel<T, false, kWave>),
-                           grid, dim3(kBlock), 0, s, *x, labels, stats, gl, entropy, ge, g, grs, gcs, status);
-    } else {
-        hipLaunchKernelGGL((ge ? token_logprobs_backward_kernel<T, true, kBlock>
-                               : token_logprobs_backward_kernel<T, false, kBlock>),
-                           dim3(grid_for(n, 1)), dim3(kBlock), 0, s, *x, labels, stats, gl, entropy, ge, g, grs, gcs,
-                           status);
+void forward(const odb_logits_t* x, const int32_t* labels, float* logprob, float* stats, float* entropy,
+             int32_t* status, hipStream_t s) {
+    switch (group_for(x, false)) {
+        case kGroup8: return launch_forward<T, 8>(x, labels, logprob, stats, entropy, status, s);
+        case kGroup32: return launch_forward<T, 32>(x, labels, logprob, stats, entropy, status, s);
+        case kGroup64: return launch_forward<T, 64>(x, labels, logprob, stats, entropy, status, s);
+        case kGroup256: return launch_forward<T, 256>(x, labels, logprob, stats, entropy, status, s);
+        default: return launch_forward<T, 512>(x, labels, logprob, stats, entropy, status, s);
+    }
+}
+
+struct BackwardArgs {
+    const int32_t* labels;
+    const float* stats;
+    const float* grad_logprob;
+    const float* entropy;
+    const float* grad_entropy;
+    void* grad;
+    int64_t row_stride, col_stride;
+    int32_t* status;
+};
+
+template <typename T, int G>
+void launch_backward(const odb_logits_t* x, const BackwardArgs& a, hipStream_t s) {
+    constexpr int kThreads = G > kBlock ? G : kBlock;
+    hipLaunchKernelGGL((a.entropy ? token_logprobs_backward_kernel<T, true, G>
+                                  : token_logprobs_backward_kernel<T, false, G>),
+                       dim3(grid_for(x->rows * x->cols, kThreads / G)), dim3(kThreads), 0, s, *x, a.labels, a.stats,
+                       a.grad_logprob, a.entropy, a.grad_entropy, static_cast<T*>(a.grad), a.row_stride, a.col_stride,
+                       a.status);
+}
+
+template <typename T>
+void backward(const odb_logits_t* x, const BackwardArgs& a, hipStream_t s) {
+    switch (group_for(x, true)) {
+        case kGroup8: return launch_backward<T, 8>(x, a, s);
+        case kGroup32: return launch_backward<T, 32>(x, a, s);
+        case kGroup64: return launch_backward<T, 64>(x, a, s);
+        case kGroup256: return launch_backward<T, 256>(x, a, s);
+        case kGroup512: return launch_backward<T, 512>(x, a, s);
+        default: return launch_backward<T, 1024>(x, a, s);
     }
 }
 
@@ -336,11 +410,11 @@ extern "C" int odb_token_logprobs(const odb_logits_t* x, const int32_t* d_labels
         return set_error(ODB_E_INVALID_ARG, "d_stats must be 8-byte aligned");
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (x->dtype == ODB_FLOAT32)
-        launch_forward<float>(x, d_labels, d_logprob, d_stats, d_entropy, d_status, s);
+        forward<float>(x, d_labels, d_logprob, d_stats, d_entropy, d_status, s);
     else if (x->dtype == ODB_BFLOAT16)
-        launch_forward<bf16_t>(x, d_labels, d_logprob, d_stats, d_entropy, d_status, s);
+        forward<bf16_t>(x, d_labels, d_logprob, d_stats, d_entropy, d_status, s);
     else
-        launch_forward<fp16_t>(x, d_labels, d_logprob, d_stats, d_entropy, d_status, s);
+        forward<fp16_t>(x, d_labels, d_logprob, d_stats, d_entropy, d_status, s);
     ODB_LAUNCHED();
     return ODB_OK;
 }
@@ -370,15 +444,14 @@ extern "C" int odb_token_logprobs_backward(const odb_logits_t* x, const int32_t*
     if (!d_entropy != !d_grad_entropy)
         return set_error(ODB_E_INVALID_ARG, "d_entropy and d_grad_entropy come together or not at all");
     hipStream_t s = static_cast<hipStream_t>(stream);
+    const BackwardArgs a{d_labels, d_stats, d_grad_logprob, d_entropy, d_grad_entropy, d_grad_logits,
+                         grad_row_stride, grad_col_stride, d_status};
     if (x->dtype == ODB_FLOAT32)
-        launch_backward<float>(x, d_labels, d_stats, d_grad_logprob, d_entropy, d_grad_entropy, d_grad_logits,
-                               grad_row_stride, grad_col_stride, d_status, s);
+        backward<float>(x, a, s);
     else if (x->dtype == ODB_BFLOAT16)
-        launch_backward<bf16_t>(x, d_labels, d_stats, d_grad_logprob, d_entropy, d_grad_entropy, d_grad_logits,
-                                grad_row_stride, grad_col_stride, d_status, s);
+        backward<bf16_t>(x, a, s);
     else
-        launch_backward<fp16_t>(x, d_labels, d_stats, d_grad_logprob, d_entropy, d_grad_entropy, d_grad_logits,
-                                grad_row_stride, grad_col_stride, d_status, s);
+        backward<fp16_t>(x, a, s);
     ODB_LAUNCHED();
     return ODB_OK;
 }
