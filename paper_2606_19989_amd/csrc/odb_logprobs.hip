@@ -320,20 +320,25 @@ int check_tile(const odb_logits_t* x, const void* p, int64_t rs, int64_t cs, con
 // Threads of a position, by the bytes of its logits.  Too many leave the reduction and the label's load
 // in front of too little work, too few leave loads unissued.  us for about 600 MB of logits (N positions
 // of V), the last two lines for few positions; 2 x 600 MB for the gradient:
-//   bytes of a row     forward 64 / 256 / 512 threads    backward 64 / 256 / 512 / 1,024
-//   4 KB               109 / 246 / 463                   198 / 325 / 567 / 1049
-//   16 KB               95 / 122 / 189                   222 / 201 / 245 / 403
-//   32 KB               98 /  96 / 123                   219 / 212 / 195 / 284
-//   64 KB              103 /  98 / 110                   250 / 229 / 207 / 203
-//   128 KB             120 / 101 /  97                   283 / 263 / 249 / 215
-//   64 KB x 32        14.7 / 8.4 / 7.2                   14.3 / 6.9 / 6.1 / 5.8
-//   304 KB x 1          58 /  19 /  13                    53 /  17 /  12 /  11
+//   bytes of a row     forward 64 / 256 / 512 / 1,024 threads    backward 64 / 256 / 512 / 1,024
+//   4 KB               109 / 246 / 463 / 1320                    198 / 325 / 567 / 1049
+//   16 KB               95 / 122 / 189 /  412                    222 / 201 / 245 / 403
+//   32 KB               98 /  96 / 123 /  267                    219 / 212 / 195 / 284
+//   64 KB              103 /  98 / 110 /  207                    250 / 229 / 207 / 203
+//   128 KB             120 / 101 /  97 /  147                    283 / 263 / 249 / 215
+//   64 KB x 32        14.7 / 8.4 / 7.2 /  7.7                    14.3 / 6.9 / 6.1 / 5.8
+//   304 KB x 1          58 /  19 /  13 /   12                     53 /  17 /  12 /  11
+// Rows of 128 bytes, 4.7 M: 1,682 with a wave a row, 245 with 8 threads; of 512 bytes 461 and 106; of
+// 1 KB 240 and 99; of 2 KB 160, and 110 with 32.
 enum Group { kGroup8, kGroup32, kGroup64, kGroup256, kGroup512, kGroup1024 };
 
 Group group_for(const odb_logits_t* x, bool backward) {
     const int64_t row = x->vocab * (x->dtype == ODB_FLOAT32 ? 4 : 2);
     if (x->rows * x->cols <= 2 * (int64_t)num_cus())
-        return row <= 1024 ? kGroup64 : row <= 32768 ? kGroup256 : backward && row > 49152 ? kGroup1024 : kGroup512;
+        return row <= 1024    ? kGroup64
+               : row <= 32768 ? kGroup256
+               : row <= (backward ? 49152 : 131072) ? kGroup512
+                                                    : kGroup1024;
     if (row <= 1024) return kGroup8;
     if (row <= 2048) return kGroup32;
     if (!backward) return row <= 16384 ? kGroup64 : row <= 98304 ? kGroup256 : kGroup512;
@@ -357,7 +362,8 @@ void forward(const odb_logits_t* x, const int32_t* labels, float* logprob, float
         case kGroup32: return launch_forward<T, 32>(x, labels, logprob, stats, entropy, status, s);
         case kGroup64: return launch_forward<T, 64>(x, labels, logprob, stats, entropy, status, s);
         case kGroup256: return launch_forward<T, 256>(x, labels, logprob, stats, entropy, status, s);
-        default: return launch_forward<T, 512>(x, labels, logprob, stats, entropy, status, s);
+        case kGroup512: return launch_forward<T, 512>(x, labels, logprob, stats, entropy, status, s);
+        default: return launch_forward<T, 1024>(x, labels, logprob, stats, entropy, status, s);
     }
 }
 
