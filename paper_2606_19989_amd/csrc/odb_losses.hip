@@ -38,9 +38,13 @@ struct SlotPart {
     int32_t counted;
 };
 
+// A row's sum and count where it lies in one part (a wave's quarter of a chunk), otherwise the parts
+// that it touches, whose partials hold them.
 struct RowInfo {
-    int32_t first;      // quarter of a chunk in which the row starts
-    int32_t parts;      // quarters it touches
+    double sum;
+    int32_t count;
+    int32_t parts, first;
+    int32_t pad;
 };
 
 struct PairPart {
@@ -889,21 +893,19 @@ struct PairArgs {
 constexpr int kShortRow = 64;      // rows up to here are taken several at a time
 constexpr int kRowAhead = 2;       // groups of a lane whose loads (two or three each) are under way together
 
-// What a wave leaves of a row in its quarter of a chunk, by its lane 0; the records count quarters.
+// What a wave leaves of a row in its quarter of a chunk, by its lane 0.
 __device__ __forceinline__ void leave_row(const PairArgs& A, const SlotView& s, int64_t part, int64_t c0, int row,
                                           int count, double sum, int lane) {
     if (lane != 0) return;
     const int64_t at = s.row0 + row, start = s.lo + (int64_t)row * s.maxlen;
+    const int64_t last = (start + s.maxlen - 1) >> A.quarter_log2;
+    if (start >= c0) {   // the row starts here
+        const bool whole = last == part;
+        A.row_info[at] = RowInfo{whole ? sum : 0.0, whole ? count : 0, (int32_t)(last - part + 1), (int32_t)part, 0};
+        if (whole) return;
+    }
     A.row_count[part + at] = count;
     A.row_sum[part + at] = sum;
-    if (start >= c0) {   // the row starts here
-        const int64_t last = (start + s.maxlen - 1) >> A.quarter_log2;
-        A.row_info[at] = RowInfo{(int32_t)part, (int32_t)(last - part + 1)};
-        if (A.row_of) {
-            const int32_t id = A.row_ids[at];
-            if (id >= 0 && id < A.num_ids) atomicMin(&A.row_of[id], (int32_t)at);
-        }
-    }
 }
 
 // The lowest n of four bits.
@@ -1035,6 +1037,13 @@ __device__ __forceinline__ void row_sums(const PairArgs& A, uint32_t* s_bits) {
     if (A.status)
         for (int64_t k = b * kBlock + threadIdx.x; k < t.num_slots; k += (int64_t)gridDim.x * kBlock)
             if (!slot_view(t, k, e_base, r_base).ok) *A.status = kErrTiles;
+    if (A.row_of) {      // the ids' first rows, beside the tiles
+        const int64_t rows = run_rows(t, r_base);
+        for (int64_t i = b * kBlock + threadIdx.x; i < rows; i += (int64_t)gridDim.x * kBlock) {
+            const int32_t id = A.row_ids[i];
+            if (id >= 0 && id < A.num_ids) atomicMin(&A.row_of[id], (int32_t)i);
+        }
+    }
     if (b * A.chunk >= total) return;
     for (int i = threadIdx.x; i < words; i += kBlock) s_bits[i] = 0;
     __syncthreads();
@@ -1075,12 +1084,11 @@ __device__ __forceinline__ void clear_rows(const PairArgs& A) {
 
 __global__ void __launch_bounds__(kBlock) clear_rows_kernel(PairArgs A) { clear_rows(A); }
 
-// A row's log ratio; nothing is read outside its partials whatever its record holds.
-__device__ __forceinline__ double log_ratio(const PairArgs& A, int64_t row, int* count) {
-    const RowInfo f = A.row_info[row];
-    int n = 0;
-    double s = 0.0;
-    if (f.first >= 0 && f.parts > 0 && (int64_t)f.first + f.parts <= kWaves * A.chunks) {
+// A row's log ratio from its record; nothing is read outside its partials whatever that holds.
+__device__ __forceinline__ double log_ratio(const PairArgs& A, int64_t row, const RowInfo& f, int* count) {
+    int n = f.count;
+    double s = f.sum;
+    if (f.parts > 1 && f.first >= 0 && (int64_t)f.first + f.parts <= kWaves * A.chunks) {
         for (int64_t b = f.first; b < (int64_t)f.first + f.parts; ++b) {
             n += A.row_count[b + row];
             s += A.row_sum[b + row];
@@ -1090,7 +1098,8 @@ __device__ __forceinline__ double log_ratio(const PairArgs& A, int64_t row, int*
     return n == 0 ? 0.0 : A.normalize ? s / n : s;
 }
 
-// Row of a row's partner (-1: none here), and whether the row is the chosen one.
+// Row of a row's partner (-1: none here), and whether the row is the chosen one.  What may be needed is
+// loaded at once, from the first entry where there is none: two waits instead of five.
 __device__ __forceinline__ int64_t partner_row(const PairArgs& A, int64_t row, int64_t rows, bool* chosen) {
     const int64_t id = A.row_ids ? A.row_ids[row] : row;
     *chosen = false;
@@ -1101,19 +1110,21 @@ __device__ __forceinline__ int64_t partner_row(const PairArgs& A, int64_t row, i
     const int64_t v = A.pair[id];
     if (v == 0) return -1;
     const int64_t other = (v < 0 ? -v : v) - 1;
-    if (other >= A.num_ids || A.pair[other] != (v < 0 ? id + 1 : -(id + 1))) {
-        if (A.status) *A.status = kErrPair;
-        return -1;
-    }
-    *chosen = v > 0;
-    if (!A.row_ids) return other < rows ? other : -1;
+    const int64_t at = other < A.num_ids ? other : 0;
     // written by atomics, in one block's case in this launch: read behind the first cache
     auto row_of = [&](int64_t i) {
         return (int64_t)__hip_atomic_load(&A.row_of[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     };
-    if (row_of(id) != row) return -1;        // a later row of an id that has one already
-    const int64_t j = row_of(other);
-    return j >= 0 && j < rows && A.row_ids[j] == other ? j : -1;
+    const int64_t back = A.pair[at], first = A.row_of ? row_of(id) : row;
+    const int64_t j = A.row_of ? row_of(at) : at;
+    if (other >= A.num_ids || back != (v < 0 ? id + 1 : -(id + 1))) {
+        if (A.status) *A.status = kErrPair;
+        return -1;
+    }
+    *chosen = v > 0;
+    // a later row of an id that has one already, or a partner without a row
+    if (first != row || j < 0 || j >= rows) return -1;
+    return j;
 }
 
 // What a thread's rows add up to.
@@ -1125,12 +1136,19 @@ struct PairSums {
 // A row's loss (at the chosen row of a pair) and reward, if `out`, and the factor of its tokens' gradients.
 __device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64_t rows, bool out, PairSums* sums) {
     int n, m;
-    const double S = log_ratio(A, row, &n);
+    const RowInfo mine = A.row_info[row];
     bool chosen;
-    const int64_t j = partner_row(A, row, rows, &chosen);
+    int64_t j = partner_row(A, row, rows, &chosen);
+    const RowInfo its = A.row_info[j >= 0 ? j : row];
+    // an id's entry is believed only if the row that it names has the id
+    if (j >= 0 && A.row_of) {
+        const int64_t v = A.pair[A.row_ids[row]];
+        if (A.row_ids[j] != (v < 0 ? -v : v) - 1) j = -1;
+    }
+    const double S = log_ratio(A, row, mine, &n);
     double c = 0.0, loss = 0.0;
     if (j >= 0) {
-        const double T = log_ratio(A, j, &m);
+        const double T = log_ratio(A, j, its, &m);
         const double h = A.beta * (chosen ? S - T : T - S) - A.margin;
         double dh;
         if (A.kind == ODB_PREFERENCE_SIGMOID) {
