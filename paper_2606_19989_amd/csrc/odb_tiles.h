@@ -1,5 +1,6 @@
-// Which slots a chunk of a run's elements touches, apart from the kernels so that it can be
-// checked on the host with slot arrays that contradict each other.
+// Which slots a chunk of a run's elements touches, and which rows and columns its elements are of,
+// apart from the kernels so that they can be checked on the host, with slot arrays that contradict
+// each other and at any lengths.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -80,5 +81,76 @@ __host__ __device__ __forceinline__ void chunk_slots(const odb_tiles_t& t, int64
         f(k, s, s.lo > c0 ? s.lo : c0, s.hi < c1 ? s.hi : c1);
     }
 }
+
+// A thread's group of four elements of a chunk, from position o (a multiple of 4) on: which of them
+// lie in the slot, and row and column of the first.  The column is negative where the slot starts
+// inside the group.
+struct Group {
+    int o;
+    uint32_t mask;
+    int row, col;
+
+    // Walks one element on.
+    __host__ __device__ __forceinline__ void next(int maxlen) {
+        if (++col == maxlen) {
+            col = 0;
+            ++row;
+        }
+    }
+};
+
+// A slot's elements [a0, a1) of the chunk that starts at c0, as positions [o0, o1) in it; `threads`
+// threads take its groups in turn.  Rows count from the slot's first.
+struct Span {
+    int o0, o1, maxlen;
+    int row_a, col_a;               // of element a0
+    int ahead, rows_by, cols_by;    // from a thread's group to its next
+
+    __host__ __device__ __forceinline__ Span(const SlotView& s, int64_t a0, int64_t a1, int64_t c0, int threads)
+        : o0((int)(a0 - c0)), o1((int)(a1 - c0)), maxlen(s.maxlen), row_a((int)((a0 - s.lo) / s.maxlen)),
+          col_a((int)((a0 - s.lo) - (int64_t)row_a * s.maxlen)), ahead(4 * threads), rows_by(ahead / s.maxlen),
+          cols_by(ahead - rows_by * s.maxlen) {}
+
+    __host__ __device__ __forceinline__ uint32_t mask_at(int o) const {
+        return (o0 > o ? 0xfu << (o0 - o) : 0xfu) & (o1 - o >= 4 ? 0xfu : 0xfu >> (4 - (o1 - o)));
+    }
+
+    // Row of position o >= o0.
+    __host__ __device__ __forceinline__ int row_at(int o) const {
+        return row_a + (int)(((uint32_t)col_a + (uint32_t)(o - o0)) / (uint32_t)maxlen);
+    }
+
+    // First group of a thread; its o may lie behind the span.
+    __host__ __device__ __forceinline__ Group first(int thread) const {
+        Group q;
+        q.o = (o0 & ~3) + 4 * thread;
+        const int x = q.o - o0;      // negative only in the group in which the slot starts, where col_a is 0
+        q.row = row_a;
+        q.col = x;
+        if (x >= 0) {
+            const uint32_t c = (uint32_t)col_a + (uint32_t)x, r = c / (uint32_t)maxlen;
+            q.row += (int)r;
+            q.col = (int)(c - r * (uint32_t)maxlen);
+        }
+        q.mask = q.o < o1 ? mask_at(q.o) : 0;
+        return q;
+    }
+
+    __host__ __device__ __forceinline__ void advance(Group* q) const {
+        q->o += ahead;
+        q->row += rows_by;
+        if (q->col >= maxlen - cols_by) {    // no sum of two columns: they may pass 2^31
+            q->col -= maxlen - cols_by;
+            ++q->row;
+        } else {
+            q->col += cols_by;
+        }
+        while (q->col < 0) {    // behind the group in which the slot starts, where a step is fewer than 3 columns
+            q->col += maxlen;
+            --q->row;
+        }
+        q->mask = q->o < o1 ? mask_at(q->o) : 0;
+    }
+};
 
 }  // namespace odb

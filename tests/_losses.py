@@ -200,3 +200,67 @@ def preference_loss(plan, labels, shift, p, lp, ref, row_ids, pair):
         right += S[r] > S[q]
     return dict(loss=math.fsum(row_loss), row_loss=row_loss, reward=p["beta"] * S, counts=np.array([pairs, right]),
                 grad=np.where(on, coef[plan.row_of], 0.0))
+
+
+# ------------------------------------------------------------------ large runs, on the GPU in 64 bits
+class Maps:
+    """Row, column and slot of every element, and sums over a row's or a slot's elements."""
+
+    def __init__(self, plan, device):
+        import torch
+        rows, maxlen = torch.from_numpy(plan.rows).long().to(device), torch.from_numpy(plan.maxlen).long().to(device)
+        self.by_row = torch.repeat_interleave(maxlen, rows)
+        self.by_slot, self.rows_of_slot = rows * maxlen, rows
+        start = torch.cumsum(self.by_row, 0) - self.by_row
+        self.row = torch.repeat_interleave(torch.arange(plan.R, device=device), self.by_row)
+        self.slot = torch.repeat_interleave(torch.arange(plan.K, device=device), rows)[self.row]
+        self.col = torch.arange(plan.E, device=device) - start[self.row]
+
+    @staticmethod
+    def sum(v, lengths):
+        import torch
+        return torch.segment_reduce(v.double(), "sum", lengths=lengths, initial=0.0, unsafe=True)
+
+
+def policy_loss_torch(m, labels, shift, p, lp, old, ref, adv):
+    """Loss, means, counts and gradient (kl 3, an advantage per row, no slot weights)."""
+    import torch
+    on = (labels != IGNORE) & (m.col >= shift)
+    n_slot, n_row = m.sum(on, m.by_slot), m.sum(on, m.by_row)
+    n_rows = m.sum(n_row > 0, m.rows_of_slot)
+    zero = torch.zeros((), dtype=torch.float64, device=on.device)
+    w = [lambda: 1 / n_slot[m.slot], lambda: 1 / (n_row[m.row] * n_rows[m.slot]), lambda: zero + 1][p["reduce"]]()
+    w = torch.where(on, w, zero)
+    d, A, x = lp.double() - old.double(), adv[m.row].double(), lp.double() - ref.double()
+    r = d.exp()
+    low = on & (A < 0) & (d < math.log1p(-p["clip_low"]))
+    high = on & (A > 0) & (d > math.log1p(p["clip_high"]))
+    pol = -torch.where(high, 1 + p["clip_high"], torch.where(low, 1 - p["clip_low"], r)) * A
+    kl = torch.expm1(-x) + x
+    means = [m.sum(w * v, m.by_slot) for v in (pol, kl, r * 0, r)]
+    mags = [m.sum(w * v.abs(), m.by_slot) for v in (pol, kl, r * 0, r)]
+    slope = torch.where(low | high, zero, pol)
+    counts = torch.stack([n_slot, m.sum(low, m.by_slot), m.sum(high, m.by_slot), n_slot * 0], 1).long()
+    s = p["loss_scale"]
+    return dict(loss=s * (means[0] + p["kl_coef"] * means[1]), means=torch.stack(means, 1), mags=torch.stack(mags, 1),
+                counts=counts, grad=s * w * (slope - p["kl_coef"] * torch.expm1(-x)),
+                grad_mag=s * w * (slope.abs() + p["kl_coef"] * torch.maximum(x.abs(), torch.expm1(-x).abs())))
+
+
+def preference_loss_torch(m, labels, shift, p, lp, ref, row_ids, pair):
+    """Loss, rows' losses and rewards, counts and gradient of the sigmoid; every id has one row."""
+    import torch
+    on = (labels != IGNORE) & (m.col >= shift)
+    zero = torch.zeros((), dtype=torch.float64, device=on.device)
+    S = m.sum(torch.where(on, lp.double() - ref.double(), zero), m.by_row)
+    row_of = torch.empty_like(row_ids).long()
+    row_of[row_ids.long()] = torch.arange(row_ids.numel(), device=on.device)
+    a = torch.nonzero(pair > 0)[:, 0]
+    c, r = row_of[a], row_of[pair[a].long() - 1]
+    h = p["beta"] * (S[c] - S[r])
+    loss, coef = torch.zeros_like(S), torch.zeros_like(S)
+    loss[c] = p["loss_scale"] * torch.nn.functional.softplus(-h)
+    coef[c] = -p["loss_scale"] * p["beta"] * torch.sigmoid(-h)
+    coef[r] = -coef[c]
+    return dict(loss=loss.sum(), row_loss=loss, reward=p["beta"] * S, grad=torch.where(on, coef[m.row], zero),
+                counts=torch.stack([torch.tensor(a.numel(), device=on.device), (S[c] > S[r]).sum()]))

@@ -1,7 +1,7 @@
 // Walks the chunks of runs of tiles as the loss kernels do, over slot arrays that are sound and
 // over ones that contradict each other, and checks every index that follows from them against
 // the arrays' lengths before it would be used; over sound arrays, that every element is met once
-// and that partials b + k are met once.  Prints one line per mistake, returns 1 if there was any.
+// that partials b + k are met once, and that rows and columns are those of plain division.  Prints one line per mistake, returns 1 if there was any.
 #include <cstdio>
 #include <random>
 #include <vector>
@@ -50,6 +50,27 @@ void walk(const odb_tiles_t& t, bool sound) {
             // the chunks that the slot's partials are summed over
             if (s.lo / kChunk > b || (s.hi - 1) / kChunk < b || (s.hi - 1) / kChunk >= chunks) return fail("span", s.lo, s.hi);
             part[b + k] += 1;
+            // rows and columns as the threads of a block, or the lanes of a wave, walk them
+            for (const int threads : {2, 8}) {
+                const odb::Span p(s, a0, a1, c0, threads);
+                int64_t seen = 0;
+                for (int thread = 0; thread < threads; ++thread) {
+                    for (odb::Group q = p.first(thread); q.o < p.o1; p.advance(&q)) {
+                        odb::Group r = q;
+                        for (int j = 0; j < 4; ++j) {
+                            const int64_t e = c0 + q.o + j;
+                            if (((q.mask >> j) & 1) != (uint32_t)(e >= a0 && e < a1)) return fail("mask", e, a0);
+                            if (q.mask >> j & 1) {
+                                ++seen;
+                                if (r.row != (e - s.lo) / s.maxlen || r.col != (e - s.lo) % s.maxlen)
+                                    return fail("row and column", r.row, r.col);
+                            }
+                            r.next(s.maxlen);
+                        }
+                    }
+                }
+                if (seen != a1 - a0) return fail("elements of a span", seen, a1 - a0);
+            }
             for (int64_t e = a0; e < a1; ++e) met[e] += 1;
         });
     }
@@ -74,7 +95,7 @@ int main() {
         for (int64_t k = 0; k < K; ++k) {
             const bool idle = pick(0, 3) == 0;
             rows[k] = idle ? 0 : (int32_t)pick(1, 9);
-            maxlen[k] = idle ? 0 : (int32_t)pick(1, run % 2 || K > 12 ? 7 : 200);
+            maxlen[k] = idle ? 0 : (int32_t)pick(1, run % 2 || K > 12 ? 9 : 200);
             row_off[k + 1] = row_off[k] + rows[k];
             tile_off[k + 1] = tile_off[k] + (int64_t)rows[k] * maxlen[k];
         }

@@ -635,6 +635,65 @@ def test_contradicting_tiles_are_reported():
         assert int(status.item()) != 0, (field, at)
 
 
+@pytest.mark.parametrize("elems", [60_000, 9_000_000, 34_000_000])
+def test_large_runs(elems):
+    """Runs of many tiles whose rows divide, or nearly divide, every step of the kernels, and whose
+    tiles start at any element; each size takes another length of chunk."""
+    torch = _torch()
+    rng = np.random.default_rng(elems)
+    lens = [1, 2, 3, 4, 5, 7, 8, 16, 31, 32, 33, 64, 65, 100, 128, 255, 256, 257, 341, 480, 511, 512, 513, 1000, 1023,
+            1024, 1025, 2048, 4096, 4097, 5000, 8192]
+    groups, total, k = [], 0, 0
+    while total < elems:
+        l = lens[k % len(lens)] if k < 4 * len(lens) else int(rng.integers(1, 1500))
+        n = max(1, int(rng.integers(1000, min(60_000, elems // 20)) // l))
+        if l == 1:
+            n = min(n, 3000)
+        groups.append([max(1, l - int(v)) for v in rng.integers(0, 1 + l // 9, n - 1)] + [l])
+        total += n * l
+        k += 1
+        if k % 7 == 0:
+            groups.append([])
+    plan = Plan(groups, base=(11, 1 << 34))
+    log(f"large run: {plan.K} tiles, {plan.R} rows, {plan.E} elements")
+    y_host = plan.labels(rng, 0.3, 0.05)
+    tiles = _tiles(plan, y_host, 1, 0, 0)
+    y = tiles.labels
+    maps = ref.Maps(plan, "cuda")
+    gen = torch.Generator("cuda").manual_seed(elems)
+    r = lambda n, sd: torch.randn(n, generator=gen, device="cuda") * sd
+    lp = -r(plan.E, 2).abs()
+    old, kref, adv = lp + r(plan.E, 0.2), lp + r(plan.E, 0.4), r(plan.R, 1)
+    for reduce in range(3):
+        p = _policy_params(dict(kl=3, reduce=reduce))
+        out, status = _policy_run(tiles, plan, p, lp, old, kref, None, adv, None, extra=0)
+        assert int(status.item()) == 0
+        want = ref.policy_loss_torch(maps, y, 1, p, lp, old, kref, adv)
+        assert torch.equal(out["counts"], want["counts"])
+        C = (80 + 2 * 2) * U        # no ratio is further off than exp(2): 10 standard deviations
+        mag = p["loss_scale"] * (want["mags"][:, 0] + p["kl_coef"] * want["mags"][:, 1])
+        assert torch.all((out["loss"].double() - want["loss"]).abs() <= C * mag + 2 * U * want["loss"].abs())
+        assert torch.all((out["means"].double() - want["means"]).abs() <= C * want["mags"] + 1e-12)
+        assert torch.all((out["grad"].double() - want["grad"]).abs() <= 2 * C * want["grad_mag"])
+        again, _ = _policy_run(tiles, plan, p, lp, old, kref, None, adv, None, extra=0)
+        for key, v in out.items():
+            assert v is None or torch.equal(v, again[key]), key
+    ids = torch.randperm(plan.R, generator=gen, device="cuda").int()
+    at = torch.randperm(plan.R, generator=gen, device="cuda")
+    pair = torch.zeros(plan.R, dtype=torch.int32, device="cuda")
+    a, b = at[0:plan.R // 2 * 2:2], at[1:plan.R // 2 * 2:2]
+    pair[a], pair[b] = (b + 1).int(), -(a + 1).int()
+    p = dict(kind=0, normalize=0, beta=0.05, margin=0.0, label_smoothing=0.0, loss_scale=0.125)
+    out, status = _preference_run(tiles, plan, p, lp, kref, ids, pair, 0, 0)
+    assert int(status.item()) == 0
+    want = ref.preference_loss_torch(maps, y, 1, p, lp, kref, ids, pair)
+    # 64-bit sums of at most 8,192 terms of size 10, rounded once; the total adds 2^20 of them
+    near = lambda x, w: torch.all((x.double() - w).abs() <= 1.01 * U * w.abs() + 1e-9)
+    assert torch.equal(out["counts"], want["counts"])
+    assert near(out["row_loss"], want["row_loss"]) and near(out["reward"], want["reward"])
+    assert near(out["grad"], want["grad"]) and near(out["loss"], want["loss"].reshape(1))
+
+
 def test_tiles_past_32_bits():
     """More than 2^31 elements in one slot of two rows: positions, the mean and the last elements."""
     import paper_2606_19989_amd as odb
