@@ -571,7 +571,7 @@ int odb_token_logprobs_backward(const odb_logits_t* x, const int32_t* d_labels, 
 typedef struct odb_tiles {
     int64_t num_slots;               /* K, 0 <= K < 2^31                                       */
     int64_t num_rows;                /* length of the arrays parallel to the rows, < 2^31      */
-    int64_t num_elems;               /* length of the arrays parallel to the tiles, <= 2^37    */
+    int64_t num_elems;               /* length of the arrays parallel to the tiles, <= 2^36    */
     const int32_t* d_slot_rows;      /* [K]                                                    */
     const int32_t* d_slot_maxlen;    /* [K]                                                    */
     const int64_t* d_slot_row_off;   /* [K+1]                                                  */

@@ -9,6 +9,7 @@
 //
 // A mean's weight is known only after the labels have been read.  That pass leaves one bit per
 // element (does it count?), which is all that the later ones read of them: 4 bytes become 1/8.
+#include <algorithm>
 #include <cmath>
 
 #include "odb_internal.h"
@@ -18,8 +19,9 @@ namespace odb {
 
 namespace {
 
-constexpr int kMaxChunk = 16384;               // elements of a chunk, at most
+constexpr int kMaxChunk = 8192;                // elements of a chunk, at most
 constexpr int kOneChunk = 4096;                // elements of a run that one block takes
+constexpr int kOneSlots = 4096;                // and its slots: an empty one, too, has its numbers to write
 constexpr int kWaves = kBlock / kWave;
 static_assert(kWaves == 4, "a wave takes a quarter of a chunk");
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -59,14 +61,25 @@ struct LossLayout {
     int32_t chunk;
 };
 
-constexpr int64_t kMaxElems = (int64_t)1 << 37;
+constexpr int64_t kMaxElems = (int64_t)1 << 36;    // 2^23 chunks: a grid's threads stay below 2^32
 
-// Elements of a chunk.  A chunk's fixed cost is a search for its first slot and a reduction; more
-// chunks than the chip holds at once (2,048 blocks of 256 threads) only add to it.
+// Elements of a chunk, a power of two: as many chunks as keep the chip busy (it holds 2,048 blocks of 256
+// threads), but not more, since each costs a search for its first slot and a reduction.  us of a whole call
+// with chunks of 1,024 / 2,048 / 4,096 / 8,192 / 16,384, tiles of up to 32,768 tokens:
+//   elements    policy, mean over tokens      preference, rows of about 480
+//   2^17         13 /  13 /  16 /  21 /  32    15 /  16 /  17 /  20 /  25
+//   2^20         25 /  22 /  23 /  28 /  44    25 /  23 /  25 /  33 /  38
+//   2^21         39 /  30 /  29 /  35 /  48    36 /  28 /  30 /  41 /  45
+//   2^22         57 /  45 /  38 /  41 /  53    51 /  39 /  40 /  50 /  54
+//   2^23         93 /  67 /  56 /  53 /  63    79 /  57 /  53 /  53 /  61
+//   2^25        310 / 208 / 155 / 138 / 145   244 / 158 / 130 / 127 / 131
+//   2^28       2469 /1538 /1049 / 918 / 968  2007 /1294 /1076 / 979 / 984
+// Up to 4,096 elements one block takes the run in one launch: 7 us, where the passes take 12.
 int32_t chunk_for(int64_t elems) {
-    if (elems >= (int64_t)1 << 25) return kMaxChunk;
-    if (elems >= (int64_t)1 << 23) return 4096;
-    return elems > kOneChunk ? 1024 : kOneChunk;
+    if (elems <= kOneChunk) return kOneChunk;
+    int32_t chunk = 1024;
+    while (chunk < kMaxChunk && elems >= chunk * (int64_t)2048) chunk *= 2;
+    return chunk;
 }
 
 int check_tiles(const odb_tiles_t* t) {
@@ -75,7 +88,7 @@ int check_tiles(const odb_tiles_t* t) {
         return set_error(ODB_E_INVALID_ARG, "num_slots must be in [0, 2^31)");
     if (t->num_rows < 0 || t->num_rows > INT32_MAX) return set_error(ODB_E_INVALID_ARG, "num_rows must be in [0, 2^31)");
     if (t->num_elems < 0 || t->num_elems > kMaxElems)
-        return set_error(ODB_E_INVALID_ARG, "num_elems must be in [0, 2^37]");
+        return set_error(ODB_E_INVALID_ARG, "num_elems must be in [0, 2^36]");
     if (t->shift != 0 && t->shift != 1) return set_error(ODB_E_INVALID_ARG, "shift must be 0 or 1 (got %d)", t->shift);
     if (t->reserved0 != 0) return set_error(ODB_E_INVALID_ARG, "tiles.reserved0 must be 0");
     return ODB_OK;
@@ -116,15 +129,27 @@ int check_loss_workspace(const LossLayout& L, const void* d_ws, size_t ws_bytes)
 }
 
 // ------------------------------------------------------------------ shared by the passes
-// First slot of a chunk, 64 probes a step (one a lane; every lane of the wave must be active): two
-// loads one after the other for up to 4,096 slots, where halving the range takes twelve.
-__device__ __forceinline__ int64_t first_slot(const odb_tiles_t& t, int64_t e_base, int64_t c0) {
+// Last slot from `from` on that starts at or before element e, 64 probes a step (one a lane; every lane of
+// the wave must be active): two loads one after the other for up to 4,096 slots, where halving the range
+// takes twelve.
+__device__ __forceinline__ int64_t slot_at(const odb_tiles_t& t, int64_t e_base, int64_t from, int64_t e) {
     const int lane = threadIdx.x & (kWave - 1);
-    return search_slot(t.num_slots, [&](int64_t lo, int64_t step, int64_t hi) {
+    return search_slot(from, t.num_slots, [&](int64_t lo, int64_t step, int64_t hi) {
         const int64_t at = lo + lane * step;
-        const uint64_t before = __ballot(at < hi && offset_from(t.d_slot_tile_off[at < hi ? at : lo], e_base) <= c0);
+        const uint64_t before = __ballot(at < hi && offset_from(t.d_slot_tile_off[at < hi ? at : lo], e_base) <= e);
         return before == ~0ull ? kProbes : __builtin_ctzll(~before);
     });
+}
+
+__device__ __forceinline__ int64_t first_slot(const odb_tiles_t& t, int64_t e_base, int64_t c0) {
+    return slot_at(t, e_base, 0, c0);
+}
+
+// The slots with elements in [c0, c1), from slot k0 on; every lane of the wave must be active.
+template <typename F>
+__device__ __forceinline__ void each_slot(const odb_tiles_t& t, int64_t e_base, int64_t r_base, int64_t k0, int64_t c0,
+                                          int64_t c1, const F& f) {
+    chunk_slots(t, e_base, r_base, k0, c0, c1, [&](int64_t from, int64_t e) { return slot_at(t, e_base, from, e); }, f);
 }
 
 template <int CTRL, int ROWS>
@@ -284,7 +309,7 @@ __global__ void __launch_bounds__(kBlock) policy_count_kernel(PolicyArgs A) {
     const int64_t k0 = first_slot(t, e_base, c0);
     if (threadIdx.x == 0) A.chunk_slot[b] = (int32_t)k0;
     __syncthreads();
-    chunk_slots(t, e_base, r_base, k0, c0, c1, [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+    each_slot(t, e_base, r_base, k0, c0, c1, [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
         const Span p(s, a0, a1, c0, kBlock);
         const int rows = (int)((a1 - 1 - s.lo) / s.maxlen) - p.row_a + 1;
         const bool lds = ROWS && rows <= kLdsRows;
@@ -351,7 +376,7 @@ __device__ __forceinline__ float exp_near(float d) {
     const float u = d * kLog2e;
     const float e = __builtin_amdgcn_exp2f(u);
     const float lost = fmaf(d, kLog2eLow, fmaf(d, kLog2e, -u));
-    return fabsf(u) < 200.0f ? fmaf(e * lost, kLn2, e) : e;
+    return u > -200.0f && u < 128.0f ? fmaf(e * lost, kLn2, e) : e;    // outside: 0 and infinity
 }
 
 // exp(d) - 1 - d: below 3/2 by its series (the next term is under 2^-31 of the sum), where the
@@ -527,7 +552,7 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
             S.clipped[0] += under[j];
             S.clipped[1] += over[j] && pos;
             S.clipped[2] += over[j] && !pos;
-            g[j] = gs[j] * fmaf(C.kl_coef, kl_slope, slope);
+            g[j] = gs[j] * (C.kl_coef != 0.0f ? fmaf(C.kl_coef, kl_slope, slope) : slope);
             if (ENT) ge[j] = live ? -C.entropy_coef * gs[j] : 0.0f;
         }
 #pragma unroll
@@ -568,7 +593,8 @@ __device__ __forceinline__ SlotPart block_part(const PolicySums& S, double same)
 __device__ __forceinline__ void leave_slot(const PolicyArgs& A, int64_t k, const double sum[4], int64_t counted,
                                            const int64_t clipped[3]) {
     const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
-    A.slot_loss[k] = counted > 0 ? (float)(scale * (sum[0] + A.kl_coef * sum[1] - A.entropy_coef * sum[2])) : 0.0f;
+    const double kl = A.kl_coef != 0.0 ? A.kl_coef * sum[1] : 0.0;      // a term that is only watched may overflow
+    A.slot_loss[k] = counted > 0 ? (float)(scale * (sum[0] + kl - A.entropy_coef * sum[2])) : 0.0f;
     for (int i = 0; i < 4; ++i) A.slot_means[4 * k + i] = (float)sum[i];
     A.slot_counts[4 * k] = counted;
     for (int i = 0; i < 3; ++i) A.slot_counts[4 * k + 1 + i] = clipped[i];
@@ -634,7 +660,7 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
     if (c0 >= c1) return;
     const int64_t k0 = LABELS ? first_slot(t, e_base, c0) : (int64_t)A.chunk_slot[b];
     if (!LABELS) load_bits(s_bits, A.bits, b, A.chunk);
-    chunk_slots(t, e_base, r_base, k0, c0, c1, [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+    each_slot(t, e_base, r_base, k0, c0, c1, [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
         const Span p(s, a0, a1, c0, kBlock);
         const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
         double same = 1.0;       // weight of every token, where rows have none of their own
@@ -711,8 +737,8 @@ __global__ void __launch_bounds__(kBlock) policy_one_kernel(PolicyArgs A, int re
     }
     __syncthreads();
     if (total == 0) return;
-    chunk_slots(t, e_base, r_base, first_slot(t, e_base, 0), 0, total,
-                [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+    each_slot(t, e_base, r_base, first_slot(t, e_base, 0), 0, total,
+              [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
         const Span p(s, a0, a1, 0, kBlock);
         const PolicyChunk C = policy_chunk(A, s, 0);
         for (int i = threadIdx.x; i < s.rows; i += kBlock) s_rows[i] = 0;
@@ -986,7 +1012,7 @@ __device__ __forceinline__ void row_sums(const PairArgs& A, uint32_t* s_bits) {
         if (threadIdx.x == 0) A.chunk_slot[b] = (int32_t)k0;     // the first wave's quarter starts the chunk
         const int last = last_four(t, c0);
         uint32_t* bits = s_bits + wave * (quarter / 32);
-        chunk_slots(t, e_base, r_base, k0, c0, c1, [&](int64_t, const SlotView& s, int64_t a0, int64_t a1) {
+        each_slot(t, e_base, r_base, k0, c0, c1, [&](int64_t, const SlotView& s, int64_t a0, int64_t a1) {
             if (s.maxlen <= kShortRow)
                 short_rows<REF>(A, s, part, c0, a0, a1, last, lane, bits);
             else if (at_end((int)(a1 - c0), last))
@@ -1088,7 +1114,9 @@ __device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64
             const double q = exp(-fabs(h)), soft = log1p(q);           // -ln s(|h|)
             const double far = 1.0 / (1.0 + q), near = q / (1.0 + q);  // s(|h|), s(-|h|)
             const double up = h >= 0 ? far : near, down = h >= 0 ? near : far;
-            loss = (1.0 - A.smoothing) * (soft + (h < 0 ? -h : 0.0)) + A.smoothing * (soft + (h > 0 ? h : 0.0));
+            // no product of 0 and an infinite side: a rejected label at -inf makes h infinite
+            loss = (A.smoothing < 1.0 ? (1.0 - A.smoothing) * (soft + (h < 0 ? -h : 0.0)) : 0.0) +
+                   (A.smoothing > 0.0 ? A.smoothing * (soft + (h > 0 ? h : 0.0)) : 0.0);
             dh = A.smoothing * up - (1.0 - A.smoothing) * down;
         } else if (A.kind == ODB_PREFERENCE_HINGE) {
             loss = h < 1.0 ? 1.0 - h : 0.0;
@@ -1147,7 +1175,7 @@ __device__ __forceinline__ void pairs_grad(const PairArgs& A, const double* coef
     if (c0 >= c1) return;
     const int64_t k0 = A.chunk_slot[b];
     load_bits(s_bits, A.bits, b, A.chunk);
-    chunk_slots(t, e_base, r_base, k0, c0, c1, [&](int64_t, const SlotView& s, int64_t a0, int64_t a1) {
+    each_slot(t, e_base, r_base, k0, c0, c1, [&](int64_t, const SlotView& s, int64_t a0, int64_t a1) {
         const Span p(s, a0, a1, c0, kBlock);
         const double* of_row = coef + s.row0;
         Group q = p.first((int)threadIdx.x);
@@ -1312,18 +1340,20 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     a.dual = (float)p->dual_clip;
     a.token_advantage = p->token_advantage;
     const dim3 grid((unsigned)L.chunks), block(kBlock);     // at most 2^23 blocks
-    if (L.chunks <= 1) {
+    if (L.chunks <= 1 && t->num_slots <= kOneSlots) {
         hipLaunchKernelGGL(policy_one_kernels[p->kl], dim3(1), block, 0, s, a, (int)p->reduce);
         ODB_LAUNCHED();
         return ODB_OK;
     }
-    if (p->reduce != ODB_REDUCE_SUM) {
+    if (L.chunks > 0 && p->reduce != ODB_REDUCE_SUM) {
         hipLaunchKernelGGL(p->reduce == ODB_REDUCE_ROW_MEAN ? policy_count_kernel<true> : policy_count_kernel<false>,
                            grid, block, 0, s, a);
         ODB_LAUNCHED();
     }
-    hipLaunchKernelGGL(policy_kernels[p->kl][d_entropy ? 1 : 0][p->reduce], grid, block, 0, s, a);
-    ODB_LAUNCHED();
+    if (L.chunks > 0) {
+        hipLaunchKernelGGL(policy_kernels[p->kl][d_entropy ? 1 : 0][p->reduce], grid, block, 0, s, a);
+        ODB_LAUNCHED();
+    }
     hipLaunchKernelGGL(policy_slots_kernel, dim3(grid_for(t->num_slots, kWaves)), block, 0, s, a);
     ODB_LAUNCHED();
     return ODB_OK;
@@ -1388,13 +1418,13 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
     a.loss_scale = p->loss_scale;
     a.kind = p->kind;
     a.normalize = p->normalize;
-    const dim3 block(kBlock), grid((unsigned)L.chunks);     // at most 2^23 blocks
+    const dim3 block(kBlock);
     if (!any) {
         hipLaunchKernelGGL(no_pairs_kernel, dim3(1), dim3(1), 0, s, a);
         ODB_LAUNCHED();
         return ODB_OK;
     }
-    if (L.chunks <= 1) {
+    if (L.chunks <= 1 && t->num_slots <= kOneSlots) {
         hipLaunchKernelGGL(d_ref_logprob ? pairs_one_kernel<true> : pairs_one_kernel<false>, dim3(1), block, 0, s, a);
         ODB_LAUNCHED();
         return ODB_OK;
@@ -1404,8 +1434,12 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
         hipLaunchKernelGGL(clear_rows_kernel, dim3(grid_for(parts, 1)), block, 0, s, a);
         ODB_LAUNCHED();
     }
-    hipLaunchKernelGGL(d_ref_logprob ? row_sums_kernel<true> : row_sums_kernel<false>, grid, block, 0, s, a);
+    // at most 2^23 blocks; those behind the chunks only look over the slots
+    const dim3 sums((unsigned)std::max(L.chunks, (t->num_slots + kOneSlots - 1) / kOneSlots));
+    hipLaunchKernelGGL(d_ref_logprob ? row_sums_kernel<true> : row_sums_kernel<false>, sums, block, 0, s, a);
     ODB_LAUNCHED();
+    // without gradients the first block is all that the last kernel has to do
+    const dim3 grid((unsigned)(a.grad ? std::max(L.chunks, (int64_t)1) : 1));
     if (parts <= 1 && L.chunks <= kFewChunks) {
         hipLaunchKernelGGL(few_rows_kernel, grid, block, 0, s, a);
         ODB_LAUNCHED();
@@ -1415,7 +1449,7 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
         hipLaunchKernelGGL(pairs_kernel, dim3((unsigned)parts), block, 0, s, a);
         ODB_LAUNCHED();
     }
-    hipLaunchKernelGGL(pairs_grad_kernel, a.grad ? grid : dim3(1), block, 0, s, a, parts);
+    hipLaunchKernelGGL(pairs_grad_kernel, grid, block, 0, s, a, parts);
     ODB_LAUNCHED();
     return ODB_OK;
 }

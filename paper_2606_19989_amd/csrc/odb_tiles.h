@@ -42,12 +42,11 @@ __host__ __device__ __forceinline__ SlotView slot_view(const odb_tiles_t& t, int
 // Probes of one step of the search below, one a lane.
 constexpr int kProbes = 64;
 
-// Last slot of [0, slots) that starts at or before an element (0 if there is none), whatever the
+// Last slot of [lo, hi) that starts at or before an element (lo if there is none), whatever the
 // offsets hold: probe(lo, step, hi) is the first i < kProbes whose slot lo + i * step does not or is
 // not below hi, else kProbes.
 template <typename Probe>
-__host__ __device__ __forceinline__ int64_t search_slot(int64_t slots, const Probe& probe) {
-    int64_t lo = 0, hi = slots;
+__host__ __device__ __forceinline__ int64_t search_slot(int64_t lo, int64_t hi, const Probe& probe) {
     while (hi - lo > 1) {
         const int64_t step = (hi - lo + kProbes - 1) / kProbes;
         const int n = probe(lo, step, hi);
@@ -70,15 +69,23 @@ __host__ __device__ __forceinline__ int64_t run_rows(const odb_tiles_t& t, int64
 }
 
 // Calls f(k, slot, a0, a1) for every sound slot k >= first with elements [a0, a1) in [c0, c1), in
-// order, until one starts behind them.
-template <typename F>
+// order, until one starts behind them.  last_at(from, e) is the last slot >= from that starts at or
+// before element e: where many empty slots (idle ranks' steps) lie together it finds the one behind them.
+template <typename LastAt, typename F>
 __host__ __device__ __forceinline__ void chunk_slots(const odb_tiles_t& t, int64_t e_base, int64_t r_base,
-                                                     int64_t first, int64_t c0, int64_t c1, const F& f) {
-    for (int64_t k = first; k < t.num_slots; ++k) {
+                                                     int64_t first, int64_t c0, int64_t c1, const LastAt& last_at,
+                                                     const F& f) {
+    int64_t k = first;
+    while (k < t.num_slots) {
         const SlotView s = slot_view(t, k, e_base, r_base);
         if (s.lo >= c1) break;
-        if (!s.ok || s.hi <= c0 || s.hi == s.lo) continue;
-        f(k, s, s.lo > c0 ? s.lo : c0, s.hi < c1 ? s.hi : c1);
+        if (s.ok && s.hi == s.lo) {
+            const int64_t next = last_at(k, s.lo);
+            k = next > k ? next : k + 1;
+            continue;
+        }
+        if (s.ok && s.hi > c0) f(k, s, s.lo > c0 ? s.lo : c0, s.hi < c1 ? s.hi : c1);
+        ++k;
     }
 }
 

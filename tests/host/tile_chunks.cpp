@@ -27,20 +27,24 @@ void walk(const odb_tiles_t& t, bool sound) {
     for (int64_t b = 0; b < chunks; ++b) {
         const int64_t c0 = b * kChunk, c1 = c0 + kChunk < total ? c0 + kChunk : total;
         if (c0 >= c1) continue;
-        const int64_t first = odb::search_slot(t.num_slots, [&](int64_t lo, int64_t step, int64_t hi) {
-            for (int i = 0; i < odb::kProbes; ++i) {
-                const int64_t at = lo + i * step;
-                if (at >= hi) return i;
-                if (at < 0 || at >= t.num_slots) fail("probe", at, t.num_slots);
-                if (odb::offset_from(t.d_slot_tile_off[at], e_base) > c0) return i;
-            }
-            return odb::kProbes;
-        });
+        auto last_at = [&](int64_t from, int64_t e) {
+            return odb::search_slot(from, t.num_slots, [&](int64_t lo, int64_t step, int64_t hi) {
+                for (int i = 0; i < odb::kProbes; ++i) {
+                    const int64_t at = lo + i * step;
+                    if (at >= hi) return i;
+                    if (at < 0 || at >= t.num_slots) fail("probe", at, t.num_slots);
+                    if (odb::offset_from(t.d_slot_tile_off[at], e_base) > e) return i;
+                }
+                return odb::kProbes;
+            });
+        };
+        const int64_t first = last_at(0, c0);
         if (first < 0 || first >= t.num_slots) {
             fail("first slot", first, t.num_slots);
             continue;
         }
-        odb::chunk_slots(t, e_base, r_base, first, c0, c1, [&](int64_t k, const odb::SlotView& s, int64_t a0, int64_t a1) {
+        odb::chunk_slots(t, e_base, r_base, first, c0, c1, last_at,
+                         [&](int64_t k, const odb::SlotView& s, int64_t a0, int64_t a1) {
             if (k < 0 || k >= t.num_slots) return fail("slot", k, t.num_slots);
             if (b + k >= (int64_t)part.size()) return fail("partial", b, k);
             if (a0 < c0 || a1 > c1 || a0 >= a1 || a1 > t.num_elems) return fail("range", a0, a1);
@@ -86,14 +90,15 @@ void walk(const odb_tiles_t& t, bool sound) {
 int main() {
     std::mt19937_64 rng(11);
     auto pick = [&](int64_t lo, int64_t hi) { return lo + (int64_t)(rng() % (uint64_t)(hi - lo + 1)); };
-    for (int run = 0; run < 4000; ++run) {
-        const int64_t K = run % 50 == 0 ? pick(60, 9000) : pick(1, 12);
+    for (int run = 0; run < 4200; ++run) {
+        const bool sparse = run >= 4000;    // many idle slots between those with rows
+        const int64_t K = sparse || run % 50 == 0 ? pick(60, 9000) : pick(1, 12);
         std::vector<int32_t> rows(K), maxlen(K);
         std::vector<int64_t> row_off(K + 1), tile_off(K + 1);
         row_off[0] = pick(0, 1000);
         tile_off[0] = pick(0, 1000);
         for (int64_t k = 0; k < K; ++k) {
-            const bool idle = pick(0, 3) == 0;
+            const bool idle = sparse ? pick(0, 400) > 0 : pick(0, 3) == 0;
             rows[k] = idle ? 0 : (int32_t)pick(1, 9);
             maxlen[k] = idle ? 0 : (int32_t)pick(1, run % 2 || K > 12 ? 9 : 200);
             row_off[k + 1] = row_off[k] + rows[k];

@@ -258,6 +258,37 @@ def test_other_orders_of_rows_and_columns():
         odb.odb_token_logprobs_backward(z, y, st, g, z[:1, :1].expand(3, 6, 300))
 
 
+def test_more_positions_than_a_grid_holds():
+    """34 M positions of five logits, more than 2^20 blocks take at once."""
+    import paper_2606_19989_amd as odb
+    torch = _torch()
+    n, V = 34_000_003, 5
+    log(f"{n} positions")
+    gen = torch.Generator("cuda").manual_seed(1)
+    z = torch.randn(1, n, V, generator=gen, device="cuda").half()
+    y = torch.randint(0, V, (1, n), generator=gen, device="cuda", dtype=torch.int32)
+    y[0, ::7] = IGNORE
+    lp, H = torch.empty(1, n, device="cuda"), torch.empty(1, n, device="cuda")
+    st = torch.empty(1, n, 2, device="cuda")
+    odb.odb_token_logprobs(z, y, lp, stats=st, entropy=H, shift=0)
+    on = y[0] != IGNORE
+    want = torch.log_softmax(z[0].double(), -1)
+    at = want.gather(1, y[0].long().clamp(min=0)[:, None])[:, 0]
+    # logits of at most 8: the sum of five powers, its logarithm and the difference, all of size 20 or less
+    assert float((lp[0].double() - at)[on].abs().max()) <= 32 * 20 * U
+    assert float(lp[0][~on].abs().max()) == 0.0
+    want = want.exp_()
+    del at
+    dz = torch.empty_like(z)
+    odb.odb_token_logprobs_backward(z, y, st, torch.ones_like(lp), dz, shift=0)
+    want = -want
+    want[on] += torch.nn.functional.one_hot(y[0][on].long(), V)
+    want[~on] = 0.0
+    # rounded to fp16 (2^-11 of at most 1), or to its smallest step
+    assert float((dz[0].double() - want).abs().max()) <= 2.0 ** -11 + 64 * U
+    assert float(dz[0][~on].abs().max()) == 0.0
+
+
 def test_logits_past_32_bits():
     """A tile of more than 2^32 bytes (and 2^31 elements) of logits: the last rows are right."""
     import paper_2606_19989_amd as odb
@@ -585,6 +616,122 @@ def test_preference_far_margins_stay_finite():
         assert out["row_loss"].tolist() == [0.0, 0.0, 10000.0 + kind, 0.0]
 
 
+def test_labels_without_probability_in_a_pair():
+    """Log ratios of -inf and +inf: the loss of the pair's right order is 0, the other's infinite."""
+    torch = _torch()
+    inf = math.inf
+    plan = Plan([[2, 2, 2, 2]])
+    lp = np.array([-1, -1, -inf, -1, -1, -inf, -1, -1], np.float32)      # row 1 and row 2
+    pair = np.array([2, -1, 4, -3], np.int32)                             # 0 over 1, 2 over 3
+    tiles = _tiles(plan, np.ones(plan.E, np.int32), 0, 0, 0)
+    dev = lambda x: torch.from_numpy(x).cuda()
+    for kind, smoothing, losses, slopes in ((0, 0.0, (0.0, inf), (0.0, -0.5)), (0, 1.0, (inf, 0.0), (0.5, 0.0)),
+                                            (0, 0.25, (inf, inf), (0.125, -0.375)), (1, 0.0, (0.0, inf), (0.0, -0.5))):
+        p = dict(kind=kind, normalize=0, beta=0.5, margin=0.0, label_smoothing=smoothing, loss_scale=1.0)
+        out, status = _preference_run(tiles, plan, p, dev(lp), None, None, dev(pair), 0, 0)
+        assert int(status.item()) == 0
+        assert out["row_loss"].tolist() == [losses[0], 0.0, losses[1], 0.0]
+        assert out["reward"].tolist() == [-1.0, -inf, -inf, -1.0] and out["counts"].tolist() == [2, 1]
+        a, b = slopes
+        assert out["grad"].tolist() == [a, a, -a, -a, b, b, -b, -b]
+
+
+def test_watched_kl_term_may_overflow():
+    """With a coefficient of 0 the KL term is only reported: neither the loss nor the gradient takes part in it."""
+    torch = _torch()
+    dev = lambda x: torch.from_numpy(x).cuda()
+    for groups in ([[4]], [[4], [5000]]):         # one launch, and the passes
+        plan = Plan(groups)
+        lp, kref = np.full(plan.E, -1.0, np.float32), np.full(plan.E, -1.0, np.float32)
+        kref[1] = 120.0                            # exp(121) passes fp32
+        tiles = _tiles(plan, np.ones(plan.E, np.int32), 0, 0, 0)
+        for reduce in range(3):
+            out, _ = _policy_run(tiles, plan, _policy_params(dict(kl=3, reduce=reduce, kl_coef=0.0, loss_scale=1.0)),
+                                 dev(lp), dev(lp), dev(kref), None, dev(np.full(plan.R, 2.0, np.float32)), None, extra=0)
+            n = 1 if reduce == 2 else 4
+            assert out["grad"][:4].tolist() == [-2.0 / n] * 4
+            assert out["loss"].tolist() == [-2.0 * (plan.tile_off[k + 1] - plan.tile_off[k] if reduce == 2 else 1)
+                                            for k in range(plan.K)]
+            assert out["means"][0, 1].item() == math.inf
+
+
+def test_calls_without_gradients():
+    """Values alone: the same bits as beside gradients, in every path by the run's size."""
+    import paper_2606_19989_amd as odb
+    torch = _torch()
+    for groups in ([[5, 9, 3]], [[700] * 9, [650] * 8], [[30] * 400, [7] * 300]):
+        plan = Plan(groups)
+        log(f"without gradients: {plan.E} elements")
+        rng = np.random.default_rng(5)
+        y = plan.labels(rng, 0.3)
+        on = plan.counted(y, 1)
+        lp, old, kref, H = (torch.from_numpy(np.where(on, v, 0).astype(np.float32)).cuda() for v in
+                            _inputs(plan, rng, on))
+        adv = torch.from_numpy(rng.standard_normal(plan.R).astype(np.float32)).cuda()
+        tiles = _tiles(plan, y, 1, 0, 0)
+        ws = torch.empty(odb.odb_loss_workspace_size(tiles, plan.R), dtype=torch.uint8, device="cuda")
+        for reduce in range(3):
+            p = _policy_params(dict(kl=3, reduce=reduce, entropy_coef=0.1))
+            want, _ = _policy_run(tiles, plan, p, lp, old, kref, H, adv, None, extra=0)
+            for with_grad in (False, True):           # entropies without their gradient
+                got = [torch.empty_like(want[k]) for k in ("loss", "means", "counts", "grad")]
+                odb.odb_policy_loss(tiles, odb.PolicyParams(**p), lp, adv, *got[:3], ws, old_logprob=old, ref_logprob=kref,
+                                    entropy=H, grad_logprob=got[3] if with_grad else None)
+                for k, v in zip(("loss", "means", "counts", "grad")[:4 if with_grad else 3], got):
+                    assert torch.equal(v, want[k]), (reduce, k)
+        at = rng.permutation(plan.R)[:plan.R // 2 * 2]
+        pair = np.zeros(plan.R, np.int32)
+        pair[at[0::2]], pair[at[1::2]] = at[1::2] + 1, -(at[0::2] + 1)
+        pair = torch.from_numpy(pair).cuda()
+        for ids in (None, torch.arange(plan.R, dtype=torch.int32, device="cuda")):
+            p = dict(kind=0, normalize=0, beta=0.2, margin=0.0, label_smoothing=0.0, loss_scale=1.0)
+            want, _ = _preference_run(tiles, plan, p, lp, kref, ids, pair, 0, 0)
+            got = [torch.empty_like(want[k]) for k in ("loss", "row_loss", "reward", "counts")]
+            odb.odb_preference_loss(tiles, odb.PreferenceParams(**p), lp, pair, *got, ws, ref_logprob=kref, row_ids=ids)
+            for k, v in zip(("loss", "row_loss", "reward", "counts"), got):
+                assert torch.equal(v, want[k]), k
+
+
+@pytest.mark.parametrize("elems", [0, 3000, 40_000])
+def test_many_idle_slots(elems):
+    """300,000 slots, nearly all of them idle: before, between and behind those with rows."""
+    torch = _torch()
+    log(f"idle slots, {elems} elements")
+    rng = np.random.default_rng(elems)
+    lens = []
+    while sum(lens) < elems:
+        lens.append(int(rng.integers(1, 120)))
+    groups = [[] for _ in range(300_000)]
+    for l, k in zip(lens, sorted(rng.choice(np.arange(50, 299_000), len(lens), replace=False))):
+        groups[k] = [l, l]
+    plan = Plan(groups)
+    y = plan.labels(rng, 0.3)
+    on = plan.counted(y, 0)
+    lp, old, kref, _ = (np.where(on, v, 0).astype(np.float32) for v in _inputs(plan, rng, on))
+    adv = rng.standard_normal(plan.R).astype(np.float32)
+    tiles = _tiles(plan, y, 0, 0, 0)
+    dev = lambda x: torch.from_numpy(np.ascontiguousarray(x)).cuda()
+    for reduce in range(3):
+        p = _policy_params(dict(kl=3, reduce=reduce))
+        want = ref.policy_loss(plan, y, 0, p, lp, old, kref, None, adv, None)
+        out, status = _policy_run(tiles, plan, p, dev(lp), dev(old), dev(kref), None, dev(adv), None, extra=0)
+        assert int(status.item()) == 0
+        assert np.array_equal(out["counts"].cpu().numpy(), want["counts"])
+        # the bound of test_policy_loss for ratios of at most exp(10)
+        C = 100 * U
+        mag = p["loss_scale"] * (want["mags"][:, 0] + p["kl_coef"] * want["mags"][:, 1])
+        assert np.all(np.abs(out["loss"].double().cpu().numpy() - want["loss"]) <= C * mag + 2 * U * np.abs(want["loss"]))
+        assert np.all(np.abs(out["grad"].double().cpu().numpy() - want["grad"]) <= 2 * C * want["grad_mag"])
+    pair = np.zeros(plan.R, np.int32)
+    pair[0::2], pair[1::2] = np.arange(1, plan.R, 2) + 1, -(np.arange(0, plan.R, 2) + 1)
+    p = dict(kind=0, normalize=0, beta=0.2, margin=0.0, label_smoothing=0.0, loss_scale=1.0)
+    for ids in (None, np.arange(plan.R, dtype=np.int32)):
+        want = ref.preference_loss(plan, y, 0, p, lp, kref, ids, pair)
+        out, status = _preference_run(tiles, plan, p, dev(lp), dev(kref), None if ids is None else dev(ids), dev(pair), 0, 0)
+        assert int(status.item()) == 0
+        _check_preference(out, want, plan, p, lp, kref, on)
+
+
 def test_bad_pairs_are_reported_and_do_not_count():
     torch = _torch()
     plan = Plan([[3, 4], [5, 6]])
@@ -635,7 +782,7 @@ def test_contradicting_tiles_are_reported():
         assert int(status.item()) != 0, (field, at)
 
 
-@pytest.mark.parametrize("elems", [60_000, 9_000_000, 34_000_000])
+@pytest.mark.parametrize("elems", [60_000, 3_000_000, 6_000_000, 9_000_000, 34_000_000])
 def test_large_runs(elems):
     """Runs of many tiles whose rows divide, or nearly divide, every step of the kernels, and whose
     tiles start at any element; each size takes another length of chunk."""

@@ -63,7 +63,7 @@ def _tiles(**kw):
 
 
 BAD_TILES = [dict(num_slots=-1), dict(num_slots=1 << 31), dict(num_rows=-1), dict(num_rows=1 << 31),
-             dict(num_elems=-1), dict(num_elems=(1 << 37) + 1), dict(num_elems=(1 << 63) - 1), dict(shift=2),
+             dict(num_elems=-1), dict(num_elems=(1 << 36) + 1), dict(num_elems=(1 << 63) - 1), dict(shift=2),
              dict(shift=-1), dict(reserved0=1)]
 BAD_ARRAYS = [dict(d_slot_rows=None), dict(d_slot_maxlen=None), dict(d_slot_row_off=None), dict(d_slot_tile_off=None),
               dict(d_labels=None)]
@@ -96,7 +96,7 @@ def test_loss_workspace():
     assert lib.odb_loss_workspace_size(None, 0) == 0
     assert size(-1) == 0 and size(1 << 31) == 0
     assert 0 < size() <= size(100) and size(10 ** 6) >= size() + 4 * 10 ** 6 - 4096
-    assert size(num_elems=1 << 37) > (1 << 34)
+    assert size(num_elems=1 << 36) > (1 << 33)
     need = size()
     for call, n in ((_policy, need), (_preference, size(9))):
         assert call(ws=None) == odb.ODB_E_INVALID_ARG
