@@ -692,7 +692,8 @@ typedef struct odb_preference_params {
  *   d_status          [1] device, or NULL: set to a nonzero value if a slot's arrays contradict
  *                     each other, an id lies outside [0, num_ids), or a row's id and the id it
  *                     is paired with do not name each other (such a row has no pair); never
- *                     cleared here
+ *                     cleared here.  The rows of a contradicting slot, and the pairs they are
+ *                     in, have values without meaning
  *   d_ws / ws_bytes   odb_loss_workspace_size(t, num_ids if d_row_ids else 0) bytes, 256-B
  *                     aligned; calls in flight at once need workspaces of their own
  *

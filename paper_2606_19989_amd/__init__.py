@@ -474,8 +474,20 @@ def _array(t, dtype, least: int, name: str, current: int):
     return t.data_ptr()
 
 
+def _tile_array(t, dtype, x, name: str, current: int, each: int = 1):
+    """The same for an array parallel to the tile of the logits: flat, or of the tile's shape."""
+    n = x.rows * x.cols * each
+    if t is not None and t.numel() != n and t.dim() > 1:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} beside a tile of {x.rows} x {x.cols}")
+    return _array(t, dtype, n, name, current)
+
+
 def _loss_stream(torch, stream, current):
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(current)
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(current)
+    if stream.device_index != current:
+        raise ValueError(f"the stream is on cuda:{stream.device_index}, the current device is cuda:{current}")
+    return stream.cuda_stream
 
 
 def _logits(x, kinds, shift, scale, current, name="logits"):
@@ -501,10 +513,10 @@ def odb_token_logprobs(logits, labels, logprob, stats=None, entropy=None, status
     torch, f32, _, i32, _, kinds = _torch_types()
     cur = _current(torch)
     x = _logits(logits, kinds, shift, scale, cur)
-    n = x.rows * x.cols
-    _check(load().odb_token_logprobs(ctypes.byref(x), _array(labels, i32, n, "labels", cur),
-                                     _array(logprob, f32, n, "logprob", cur), _array(stats, f32, 2 * n, "stats", cur),
-                                     _array(entropy, f32, n, "entropy", cur), _array(status, i32, 1, "status", cur),
+    a = _tile_array
+    _check(load().odb_token_logprobs(ctypes.byref(x), a(labels, i32, x, "labels", cur),
+                                     a(logprob, f32, x, "logprob", cur), a(stats, f32, x, "stats", cur, 2),
+                                     a(entropy, f32, x, "entropy", cur), _array(status, i32, 1, "status", cur),
                                      _loss_stream(torch, stream, cur)))
 
 
@@ -518,12 +530,12 @@ def odb_token_logprobs_backward(logits, labels, stats, grad_logprob, grad_logits
     g = _logits(grad_logits, kinds, shift, scale, cur, "grad_logits")
     if (g.dtype, g.rows, g.cols, g.vocab) != (x.dtype, x.rows, x.cols, x.vocab):
         raise ValueError("grad_logits must have the shape and type of the logits")
-    n = x.rows * x.cols
-    _check(load().odb_token_logprobs_backward(ctypes.byref(x), _array(labels, i32, n, "labels", cur),
-                                              _array(stats, f32, 2 * n, "stats", cur),
-                                              _array(grad_logprob, f32, n, "grad_logprob", cur),
-                                              _array(entropy, f32, n, "entropy", cur),
-                                              _array(grad_entropy, f32, n, "grad_entropy", cur), g.d_logits,
+    a = _tile_array
+    _check(load().odb_token_logprobs_backward(ctypes.byref(x), a(labels, i32, x, "labels", cur),
+                                              a(stats, f32, x, "stats", cur, 2),
+                                              a(grad_logprob, f32, x, "grad_logprob", cur),
+                                              a(entropy, f32, x, "entropy", cur),
+                                              a(grad_entropy, f32, x, "grad_entropy", cur), g.d_logits,
                                               g.row_stride, g.col_stride, _array(status, i32, 1, "status", cur),
                                               _loss_stream(torch, stream, cur)))
 
@@ -605,10 +617,13 @@ def odb_preference_loss(tiles, params, logprob, pair, loss, row_loss, row_reward
 
 
 class _PlanLosses:
-    """Losses over the tiles of a pipeline's plan.  Output buffers are kept and reused (views of
-    them are returned), so a call on another stream never writes freed memory; a policy and a
-    preference loss have buffers of their own.  Inputs are checked on the host; what the device
-    finds wrong with them is collected until :meth:`check_losses`."""
+    """Losses over the tiles of a pipeline's plan.  Output buffers and workspaces are kept and
+    reused, one set for policy and one for preference losses, and views of them are returned: a
+    call overwrites what the last one of its kind returned, and two of one kind must not be under
+    way at once.  A call that needs larger ones than any before it waits for the device and
+    replaces them, so it cannot be captured, and a graph captured before it is no longer valid.
+    Inputs are checked on the host; what the device finds wrong with them is collected until
+    :meth:`check_losses`."""
 
     _loss_buffers = None
 
@@ -630,6 +645,8 @@ class _PlanLosses:
             if self.outputs is None:
                 raise ValueError("collate first, or pass labels")
             labels = self.outputs[1]
+        if labels.numel() < e[1]:
+            raise ValueError(f"labels: {labels.numel()} elements, the plan's tiles have {int(self.info['padded_elems'])}")
         return Tiles(self.slot_rows[a:b], self.slot_maxlen[a:b], self.slot_row_off[a:b + 1],
                      self.slot_tile_off[a:b + 1], labels.reshape(-1)[e[0]:e[1]], r[1] - r[0], shift, slice(a, b),
                      slice(*r), slice(*e))
@@ -640,13 +657,14 @@ class _PlanLosses:
         if self._loss_buffers is None:
             self._loss_buffers = {"status": torch.zeros(1, dtype=torch.int32, device=self.device)}
             _sync_current(self.device)
-        grown = False
-        for name, (n, dtype) in sizes.items():
-            t = self._loss_buffers.get((kind, name))
-            if t is None or t.numel() < n:
+        small = [name for name, (n, _) in sizes.items()
+                 if (kind, name) not in self._loss_buffers or self._loss_buffers[kind, name].numel() < n]
+        if small:
+            if any((kind, name) in self._loss_buffers for name in small):
+                torch.cuda.synchronize(self.device)     # a call on any stream may still use the old ones
+            for name in small:
+                n, dtype = sizes[name]
                 self._loss_buffers[kind, name] = torch.empty(max(n, 1), dtype=getattr(torch, dtype), device=self.device)
-                grown = True
-        if grown:
             # buffers may be used on another stream than the one they were allocated on
             _sync_current(self.device)
         return [self._loss_buffers[kind, name][:n] for name, (n, _) in sizes.items()], self._loss_buffers["status"]

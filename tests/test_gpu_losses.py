@@ -979,6 +979,19 @@ def test_binding_checks_types_and_sizes():
         odb.odb_token_logprobs_backward(s["z"], s["y"], s["st"], s["g"], s["dz"][:, :, :40])
     with pytest.raises(ValueError):
         odb.odb_token_logprobs_backward(s["z"], s["y"], s["st"], s["g"], s["dz"].float())
+    for wide in (torch.zeros(4, 10, dtype=torch.int32, device="cuda"), torch.zeros(5, 9, dtype=torch.int32, device="cuda")):
+        with pytest.raises(ValueError, match="labels"):           # another tile's
+            odb.odb_token_logprobs(s["z"], wide, s["lp"])
+    odb.odb_token_logprobs(s["z"], torch.zeros(40, dtype=torch.int32, device="cuda"), s["lp"])    # flat and longer
+
+    class Elsewhere:
+        cuda_stream, device_index = 0, 1
+    for call in (lambda: odb.odb_token_logprobs(s["z"], s["y"], s["lp"], stream=Elsewhere),
+                 lambda: odb.odb_policy_loss(s["tiles"], s["params"], s["lp"], s["adv"], s["loss"], s["means"],
+                                             s["counts"], s["ws"], entropy=s["H"], ref_logprob=s["ref"],
+                                             stream=Elsewhere)):
+        with pytest.raises(ValueError, match="stream"):
+            call()
 
 
 # ------------------------------------------------------------------------- the whole chain
@@ -1142,4 +1155,34 @@ def test_check_losses_raises_once():
     with pytest.raises(odb.OdbError) as e:
         pipe.check_losses()
     assert e.value.status == odb.ODB_E_INVALID_DATA
+    pipe.check_losses()
+
+
+def test_pipeline_buffers_grow_behind_another_stream():
+    """A larger run's call waits for one under way on another stream before it replaces its buffers."""
+    import paper_2606_19989_amd as odb
+    torch = _torch()
+    rng = np.random.default_rng(79)
+    w = synth.window_from_ranks("loss_grow", [rng.integers(200, 600, 3000)], 40_000)
+    tok_off, toks, ident = synth.device_tensors(w, "cuda")
+    pipe = odb.Pipeline(odb.DeviceWindow(w.rank_off, tok_off, toks, ident, w.num_identities), w.budget)
+    pipe.form()
+    pipe.align()
+    pipe.collate()
+    whole, part = pipe.tiles(), pipe.tiles(first=0, count=pipe.num_slots // 2)
+    with pytest.raises(ValueError, match="labels"):
+        pipe.tiles(pipe.outputs[1][:whole.num_elems - 1])
+    gen = torch.Generator("cuda").manual_seed(79)
+    lp = -torch.rand(whole.num_elems, generator=gen, device="cuda")
+    adv = torch.randn(whole.num_rows, generator=gen, device="cuda")
+    params = odb.PolicyParams(kl=0, reduce=1)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    a = pipe.policy_loss(part, lp[part.elems], adv[part.rows], params, stream=side)
+    b = pipe.policy_loss(whole, lp, adv, params)
+    junk = torch.full((whole.num_elems,), -7.0, device="cuda")     # takes the memory that came free
+    torch.cuda.synchronize()
+    K = part.num_slots
+    assert torch.equal(a[0], b[0][:K]) and torch.equal(a[2], b[2][:K])
+    assert torch.equal(a[3], b[3][:part.num_elems]) and bool((junk == -7.0).all())
     pipe.check_losses()
