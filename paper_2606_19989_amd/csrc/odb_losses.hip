@@ -19,16 +19,24 @@ namespace odb {
 
 namespace {
 
-constexpr int kMaxChunk = 8192;                // elements of a chunk, at most
-constexpr int kOneChunk = 4096;                // elements of a run that one block takes
-constexpr int kOneSlots = 4096;                // and its slots: an empty one, too, has its numbers to write
+constexpr int kMinChunk = 1024, kMaxChunk = 8192;    // elements of a chunk
+// Runs of few elements go through one launch of one block, whose time grows with each 1,024 elements where
+// the passes' does not.  us in a graph, one block / passes:
+//   elements    policy, token mean   policy, row mean    preference, by id   preference, by row
+//   300          7.1 / 11.3           7.5 / 12.5         10.7 / 11.7          8.9 / 9.8
+//   1,000        7.3 / 11.2           7.6 / 13.1         11.7 / 11.6         12.5 / 9.8
+//   2,000        9.3 / 12.1           9.9 / 14.6         12.5 / 11.5         13.2 / 10.0
+//   4,000       13.2 / 12.3          14.2 / 14.7         13.4 / 11.7         14.0 / 10.4
+// With 1,024 threads: 12.6 / 13.0 (policy) at 4,000 elements, but 16.5 at 8,192, where the passes take 12.6.
+constexpr int kOnePolicy = 4096;
+constexpr int kOnePairs = 512;
+static_assert(kOnePairs <= kMinChunk);
+constexpr int kOneSlots = 4096;     // and few slots: an empty one, too, has its numbers to write
 constexpr int kWaves = kBlock / kWave;
 static_assert(kWaves == 4, "a wave takes a quarter of a chunk");
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLog2eLow = 1.92596299112661746887e-8f;   // log2 e - kLog2e
 constexpr float kLn2 = 0.69314718055994530942f;
-
-constexpr int32_t kIgnore = ODB_LABEL_IGNORE;
 
 typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef int int4u __attribute__((ext_vector_type(4), aligned(4)));
@@ -74,10 +82,8 @@ constexpr int64_t kMaxElems = (int64_t)1 << 36;    // 2^23 chunks: a grid's thre
 //   2^23         93 /  67 /  56 /  53 /  63    79 /  57 /  53 /  53 /  61
 //   2^25        310 / 208 / 155 / 138 / 145   244 / 158 / 130 / 127 / 131
 //   2^28       2469 /1538 /1049 / 918 / 968  2007 /1294 /1076 / 979 / 984
-// Up to 4,096 elements one block takes the run in one launch: 7 us, where the passes take 12.
 int32_t chunk_for(int64_t elems) {
-    if (elems <= kOneChunk) return kOneChunk;
-    int32_t chunk = 1024;
+    int32_t chunk = kMinChunk;
     while (chunk < kMaxChunk && elems >= chunk * (int64_t)2048) chunk *= 2;
     return chunk;
 }
@@ -189,17 +195,18 @@ __device__ __forceinline__ T block_total(T v) {
     return sum;
 }
 
-// Four values of an array from position o of a chunk on.  SAFE, for where they may end behind the array,
-// whose last four are at `last`: each is read on its own then, and the others are `fill`.  Otherwise a
-// position past `last` reads that one, so that loads of many groups go out without a branch between them.
+// Four values of an array from position o of a chunk on; what lies behind the array, whose last four are at
+// `last`, holds any of its values.  SAFE, for where a group may end behind it: each value is read on its own,
+// the last one for those behind.  Otherwise a position past `last` reads that one.  Either way there is no
+// branch, so that loads of many groups go out together.
 // What is read here is read once: past the caches' usual order, 67 M elements in 2,048 tiles take 266 us
 // instead of 280 (policy) and 246 instead of 300 (preference).
 template <typename V4, bool SAFE, typename T>
-__device__ __forceinline__ V4 load4(const T* p, int o, int last, T fill) {
+__device__ __forceinline__ V4 load4(const T* p, int o, int last) {
     if (SAFE) {
         V4 v;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = o + j < last + 4 ? p[o + j] : fill;
+        for (int j = 0; j < 4; ++j) v[j] = p[o + j < last + 3 ? o + j : last + 3];
         return v;
     }
     const uint32_t at = 4u * (uint32_t)(o < last ? o : last);    // one 32-bit offset to the chunk's address
@@ -329,12 +336,12 @@ __global__ void __launch_bounds__(kBlock) policy_count_kernel(PolicyArgs A) {
             p.advance(&q);
         };
         if (at_end(p.o1, last)) {
-            while (q.o < p.o1) take(load4<int4u, true>(labels, q.o, last, kIgnore));
+            while (q.o < p.o1) take(load4<int4u, true>(labels, q.o, last));
         } else {
             for (int o = p.o0 & ~3; o < p.o1; o += kAhead * p.ahead) {     // uniform
                 int4u y[kAhead];
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) y[i] = load4<int4u, false>(labels, q.o + i * p.ahead, last, kIgnore);
+                for (int i = 0; i < kAhead; ++i) y[i] = load4<int4u, false>(labels, q.o + i * p.ahead, last);
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) take(y[i]);
             }
@@ -441,12 +448,12 @@ __device__ __forceinline__ PolicyLoads policy_load(const PolicyArgs& A, const Po
     PolicyLoads L;
     L.on = on;
     const int o = on ? q.o : 0;
-    L.lp = load4<float4u, SAFE>(C.logprob, o, C.last, 0.0f);
-    L.old = load4<float4u, SAFE>(C.old, o, C.last, 0.0f);
-    if (KL != ODB_KL_NONE) L.ref = load4<float4u, SAFE>(C.ref, o, C.last, 0.0f);
-    if (ENT) L.H = load4<float4u, SAFE>(C.entropy, o, C.last, 0.0f);
+    L.lp = load4<float4u, SAFE>(C.logprob, o, C.last);
+    L.old = load4<float4u, SAFE>(C.old, o, C.last);
+    if (KL != ODB_KL_NONE) L.ref = load4<float4u, SAFE>(C.ref, o, C.last);
+    if (ENT) L.H = load4<float4u, SAFE>(C.entropy, o, C.last);
     if (A.token_advantage) {
-        L.adv = load4<float4u, SAFE>(C.advantage, o, C.last, 0.0f);
+        L.adv = load4<float4u, SAFE>(C.advantage, o, C.last);
     } else {
         L.adv[0] = C.advantage[on ? q.row : row_a];
         L.adv[1] = L.adv[2] = L.adv[3] = L.adv[0];
@@ -706,13 +713,13 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
         PolicySums S;
         if (at_end(p.o1, C.last)) {
             auto from_labels = [&](const Group& q) {
-                return count_mask(q, load4<int4u, true>(t.d_labels + c0, q.o, C.last, kIgnore), p.maxlen, t.shift);
+                return count_mask(q, load4<int4u, true>(t.d_labels + c0, q.o, C.last), p.maxlen, t.shift);
             };
             if (LABELS) policy_span<KL, ROWS, ENT, true>(A, C, p, from_labels, weight, S);
             else policy_span<KL, ROWS, ENT, true>(A, C, p, from_bits, weight, S);
         } else {
             auto from_labels = [&](const Group& q) {
-                return count_mask(q, load4<int4u, false>(t.d_labels + c0, q.o, C.last, kIgnore), p.maxlen, t.shift);
+                return count_mask(q, load4<int4u, false>(t.d_labels + c0, q.o, C.last), p.maxlen, t.shift);
             };
             if (LABELS) policy_span<KL, ROWS, ENT, false>(A, C, p, from_labels, weight, S);
             else policy_span<KL, ROWS, ENT, false>(A, C, p, from_bits, weight, S);
@@ -722,11 +729,11 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
     });
 }
 
-// A run of one chunk, in one launch of one block: 6 us for 256 elements where the passes take 12.
+// A run of few elements, in one launch of one block.
 template <int KL>
 __global__ void __launch_bounds__(kBlock) policy_one_kernel(PolicyArgs A, int reduce) {
-    __shared__ uint8_t s_nibble[kOneChunk / 4];
-    __shared__ int s_rows[kOneChunk];
+    __shared__ uint8_t s_nibble[kOnePolicy / 4];
+    __shared__ int s_rows[kOnePolicy];
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int64_t total = run_elems(t, e_base), none[3] = {0, 0, 0};
@@ -745,7 +752,7 @@ __global__ void __launch_bounds__(kBlock) policy_one_kernel(PolicyArgs A, int re
         __syncthreads();
         int count = 0;
         for (Group q = p.first((int)threadIdx.x); q.o < p.o1; p.advance(&q)) {
-            const uint32_t on = count_mask(q, load4<int4u, true>(t.d_labels, q.o, C.last, kIgnore), p.maxlen, t.shift);
+            const uint32_t on = count_mask(q, load4<int4u, true>(t.d_labels, q.o, C.last), p.maxlen, t.shift);
             s_nibble[q.o / 4] = (uint8_t)on;
             count += __builtin_popcount(on);
             if (reduce == ODB_REDUCE_ROW_MEAN) add_to_rows(s_rows, q, on, p.maxlen, 0);
@@ -890,9 +897,9 @@ __device__ __forceinline__ void long_rows(const PairArgs& A, const SlotView& s, 
 #pragma unroll
         for (int i = 0; i < kRowAhead; ++i) {
             const int at = o + 4 * (kWave * i + lane);
-            y[i] = load4<int4u, SAFE>(labels, at, last, kIgnore);
-            lp[i] = load4<float4u, SAFE>(logprob, at, last, 0.0f);
-            if (REF) rf[i] = load4<float4u, SAFE>(ref, at, last, 0.0f);
+            y[i] = load4<int4u, SAFE>(labels, at, last);
+            lp[i] = load4<float4u, SAFE>(logprob, at, last);
+            if (REF) rf[i] = load4<float4u, SAFE>(ref, at, last);
         }
 #pragma unroll
         for (int i = 0; i < kRowAhead; ++i) {
@@ -953,13 +960,13 @@ __device__ __forceinline__ void short_rows(const PairArgs& A, const SlotView& s,
                 int4u y;
                 float4u p, q = {0, 0, 0, 0};
                 if (o <= last) {
-                    y = load4<int4u, false>(A.t.d_labels + c0, o, last, kIgnore);
-                    p = load4<float4u, false>(A.logprob + c0, o, last, 0.0f);
-                    if (REF) q = load4<float4u, false>(A.ref + c0, o, last, 0.0f);
+                    y = load4<int4u, false>(A.t.d_labels + c0, o, last);
+                    p = load4<float4u, false>(A.logprob + c0, o, last);
+                    if (REF) q = load4<float4u, false>(A.ref + c0, o, last);
                 } else {
-                    y = load4<int4u, true>(A.t.d_labels + c0, o, last, kIgnore);
-                    p = load4<float4u, true>(A.logprob + c0, o, last, 0.0f);
-                    if (REF) q = load4<float4u, true>(A.ref + c0, o, last, 0.0f);
+                    y = load4<int4u, true>(A.t.d_labels + c0, o, last);
+                    p = load4<float4u, true>(A.logprob + c0, o, last);
+                    if (REF) q = load4<float4u, true>(A.ref + c0, o, last);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -1234,10 +1241,10 @@ __global__ void no_pairs_kernel(PairArgs A) {
     A.counts[0] = A.counts[1] = 0;
 }
 
-// A run of one chunk, in one launch of one block.
+// A run of few elements, which are one chunk, in one launch of one block.
 template <bool REF>
 __global__ void __launch_bounds__(kBlock) pairs_one_kernel(PairArgs A) {
-    __shared__ uint32_t s_bits[kOneChunk / 32];
+    __shared__ uint32_t s_bits[kMinChunk / 32];
     if (A.row_of) {
         clear_rows(A);
         __threadfence();     // before the atomics on the same entries
@@ -1340,7 +1347,7 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     a.dual = (float)p->dual_clip;
     a.token_advantage = p->token_advantage;
     const dim3 grid((unsigned)L.chunks), block(kBlock);     // at most 2^23 blocks
-    if (L.chunks <= 1 && t->num_slots <= kOneSlots) {
+    if (t->num_elems <= kOnePolicy && t->num_slots <= kOneSlots) {
         hipLaunchKernelGGL(policy_one_kernels[p->kl], dim3(1), block, 0, s, a, (int)p->reduce);
         ODB_LAUNCHED();
         return ODB_OK;
@@ -1424,7 +1431,7 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
         ODB_LAUNCHED();
         return ODB_OK;
     }
-    if (L.chunks <= 1 && t->num_slots <= kOneSlots) {
+    if (t->num_elems <= kOnePairs && t->num_slots <= kOneSlots) {
         hipLaunchKernelGGL(d_ref_logprob ? pairs_one_kernel<true> : pairs_one_kernel<false>, dim3(1), block, 0, s, a);
         ODB_LAUNCHED();
         return ODB_OK;
