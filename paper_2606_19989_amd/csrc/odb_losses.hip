@@ -471,7 +471,7 @@ __device__ __forceinline__ PolicyLoads policy_load(const PolicyArgs& A, const Po
 // A group's part of the sums, and its gradients.  weight(row, &f, &gs) gives the weight of a row's
 // token in the slot's mean and the factor of its gradient (ROWS: they differ from row to row).  What
 // does not count has its inputs replaced by 0, which makes all but the ratio and the linear KL term's
-// slope 0.  Within a group the sums are formed in fp32.  Four tokens go through without a branch but
+// slope 0.  Within a group the sums are formed in fp32, but for the policy terms of rows' means.  Four tokens go through without a branch but
 // the one of the rare cases.
 template <int KL, bool ROWS, bool ENT, typename Weight>
 __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyChunk& C, Group q, const PolicyLoads& L,
@@ -510,14 +510,16 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
                 if (KL == ODB_KL_EXP && fabsf(x[j]) >= kSeries) kl[j] = less_line_far(-x[j]);
             }
         }
-        float f[4], gs[4];
+        double f[4];
+        float gs[4];
         if (!ROWS) {
             weight(0, &f[0], &gs[0]);
 #pragma unroll
             for (int j = 1; j < 4; ++j) gs[j] = gs[0];
         } else {
             Group r = q;
-            float w = 0.0f, k = 0.0f;
+            double w = 0.0;
+            float k = 0.0f;
             int have = -1;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -537,7 +539,8 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
             const float ratio = exp_near(d[j]);
             float bound = over[j] ? (pos ? A.high : A.dual) : ratio;
             bound = under[j] ? A.low : bound;
-            const float policy = adv[j] == 0.0f ? 0.0f : -bound * adv[j];   // an overflowing ratio must not make it NaN
+            bound = adv[j] == 0.0f ? 0.0f : bound;   // an overflowing ratio must not make the term NaN
+            const float policy = -bound * adv[j];
             const float slope = over[j] || under[j] ? 0.0f : policy;
             float kl_slope = 0.0f;
             if (KL == ODB_KL_LINEAR) {
@@ -551,8 +554,10 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
             } else {
                 kl[j] = 0.0f;
             }
-            const float w = ROWS ? f[j] : 1.0f;
-            sum[0] = fmaf(w, policy, sum[0]);
+            // terms of both signs, whose sum may be far smaller than they are: the weights must not be rounded
+            if (ROWS) S.sum[0] = fma(f[j], (double)policy, S.sum[0]);
+            else sum[0] += policy;
+            const float w = ROWS ? (float)f[j] : 1.0f;
             if (KL != ODB_KL_NONE) sum[1] = fmaf(w, kl[j], sum[1]);
             if (ENT) sum[2] = fmaf(w, live ? L.H[j] : 0.0f, sum[2]);
             sum[3] = fmaf(w, live ? ratio : 0.0f, sum[3]);
@@ -563,7 +568,7 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
             if (ENT) ge[j] = live ? -C.entropy_coef * gs[j] : 0.0f;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = ROWS ? 1 : 0; j < 4; ++j)
             if ((KL != ODB_KL_NONE || j != 1) && (ENT || j != 2)) S.sum[j] += sum[j];
         S.counted += __builtin_popcount(L.on);
     }
@@ -698,13 +703,13 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
             __syncthreads();
         }
         const float factor = (float)(scale * same);
-        auto weight = [&](int row, float* f, float* gs) {
+        auto weight = [&](int row, double* f, float* gs) {
             if (ROWS) {
                 const double w = lds ? s_weight[row - p.row_a] : row_weight(row);
-                *f = (float)w;
+                *f = w;
                 *gs = (float)(scale * w);
             } else {
-                *f = 1.0f;
+                *f = 1.0;
                 *gs = factor;
             }
         };
@@ -765,9 +770,9 @@ __global__ void __launch_bounds__(kBlock) policy_one_kernel(PolicyArgs A, int re
         count = block_total(count);
         const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
         const double same = reduce == ODB_REDUCE_SUM ? 1.0 : count > 0 ? 1.0 / count : 0.0;
-        auto weight = [&](int row, float* f, float* gs) {
+        auto weight = [&](int row, double* f, float* gs) {
             const double w = reduce == ODB_REDUCE_ROW_MEAN ? 1.0 / ((double)s_rows[row] * count) : same;
-            *f = (float)w;
+            *f = w;
             *gs = (float)(scale * w);
         };
         PolicySums S;

@@ -655,6 +655,31 @@ def test_watched_kl_term_may_overflow():
             assert out["means"][0, 1].item() == math.inf
 
 
+def test_policy_terms_that_nearly_cancel():
+    """Ratios of 1 and advantages of few bits, so that every term is exact: what is left of terms a million
+    times larger is rounded once."""
+    torch = _torch()
+    dev = lambda x: torch.from_numpy(x).cuda()
+    rng = np.random.default_rng(61)
+    for lens in ([3, 5, 7, 11], [int(v) for v in rng.integers(1, 90, 40)], [int(v) for v in rng.integers(100, 900, 40)]):
+        plan = Plan([lens])
+        y = plan.labels(rng)
+        on = plan.counted(y, 0)
+        lp = -rng.random(plan.E).astype(np.float32)
+        adv = (rng.integers(-4096, 4097, plan.R) / 1024.0).astype(np.float32)
+        count = np.array([on[plan.row_of == r].sum() for r in range(plan.R)])
+        for reduce, weight in ((0, count / count.sum()), (1, np.full(plan.R, 1 / plan.R)), (2, count.astype(np.float64))):
+            # the last row's advantage takes back the others', up to its own step
+            adv[-1] = np.float32(np.round(-(adv[:-1].astype(np.float64) * weight[:-1]).sum() / weight[-1] * 1024) / 1024)
+            tiles = _tiles(plan, y, 0, 0, 0)
+            out, _ = _policy_run(tiles, plan, _policy_params(dict(kl=0, reduce=reduce, loss_scale=1.0, clip_low=0.5,
+                                                                  clip_high=0.5)), dev(lp), dev(lp), None, None,
+                                 dev(adv), None, extra=0)
+            want = -(adv.astype(np.float64) * weight).sum()
+            lost = 1e-15 * (np.abs(adv) * weight).sum() * plan.E
+            assert abs(float(out["loss"]) - want) <= U * abs(want) + lost, (plan.E, reduce)
+
+
 def test_calls_without_gradients():
     """Values alone: the same bits as beside gradients, in every path by the run's size."""
     import paper_2606_19989_amd as odb
