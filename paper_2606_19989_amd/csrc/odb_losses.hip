@@ -640,13 +640,46 @@ __device__ __forceinline__ void policy_span(const PolicyArgs& A, const PolicyChu
     }
 }
 
-// Counted tokens of a row, over the chunks it touches.
-__device__ __forceinline__ int row_tokens(const PolicyArgs& A, const SlotView& s, int64_t row) {
-    const int64_t start = s.lo + row * s.maxlen;
+// The chunks that a row touches.
+struct RowChunks {
+    int64_t first, last;
+
+    __device__ __forceinline__ RowChunks(const PolicyArgs& A, const SlotView& s, int64_t row) {
+        const int64_t start = s.lo + row * s.maxlen;
+        first = start >> A.chunk_log2;
+        last = (start + s.maxlen - 1) >> A.chunk_log2;
+    }
+};
+
+// Chunks of a row from which on the wave counts it, and not a lane: with a lane alone the mean over two rows of
+// 131,072 tokens took 39 us, 17 now; with the wave for all of them rows of 480 in one tile take 15.8, not 14.7.
+constexpr int kLongRow = 8;
+
+// Counted tokens of a row, over the chunks it touches, by a lane.
+__device__ __forceinline__ double row_tokens(const PolicyArgs& A, const SlotView& s, int64_t row) {
+    const RowChunks c(A, s, row);
     int n = 0;
-    const int64_t last = (start + s.maxlen - 1) >> A.chunk_log2;
-    for (int64_t b = start >> A.chunk_log2; b <= last; ++b) n += A.row_count[b + s.row0 + row];
+    for (int64_t b = c.first; b <= c.last; ++b) n += A.row_count[b + s.row0 + row];
     return n;
+}
+
+// The same by the wave; every lane must be active.
+__device__ __forceinline__ double long_row_tokens(const PolicyArgs& A, const SlotView& s, int64_t row,
+                                                  const RowChunks& c) {
+    double n = 0;
+#pragma unroll 4
+    for (int64_t b = c.first + (threadIdx.x & (kWave - 1)); b <= c.last; b += kWave) n += A.row_count[b + s.row0 + row];
+    return wave_total(n);
+}
+
+// Whether a row has any, by a lane: found in its first chunks, unless all of the row before is a prompt.
+__device__ __forceinline__ bool row_counts(const PolicyArgs& A, const SlotView& s, int64_t row) {
+    const RowChunks c(A, s, row);
+    for (int64_t b = c.first; b <= c.last; b += 2) {
+        const int64_t next = b < c.last ? b + 1 : b;
+        if (A.row_count[b + s.row0 + row] | A.row_count[next + s.row0 + row]) return true;
+    }
+    return false;
 }
 
 // Sum over a slot's chunks, one a lane, of f(chunk): a whole number that may pass 2^31.
@@ -686,7 +719,7 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
                 int n = A.slot_count[j + k];
                 if (end < s.hi && (end - s.lo) % s.maxlen) {
                     const int64_t row = (end - s.lo) / s.maxlen;
-                    if (s.lo + row * s.maxlen >= j * A.chunk) n += row_tokens(A, s, row) > 0;
+                    if (s.lo + row * s.maxlen >= j * A.chunk) n += row_counts(A, s, row);
                 }
                 return n;
             });
@@ -694,18 +727,27 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
             const double n = slot_total(A, s, [&](int64_t j) { return A.slot_count[j + k]; });
             same = n > 0 ? 1.0 / n : 0.0;
         }
-        auto row_weight = [&](int row) {
-            const int n = row_tokens(A, s, row);
-            return n > 0 ? 1.0 / ((double)n * rows) : 0.0;
+        auto of_count = [&](double n) { return n > 0 ? 1.0 / (n * rows) : 0.0; };
+        // of the rows here only the first and the last may be long; below 0: not
+        double w_first = -1.0, w_last = -1.0;
+        if (ROWS) {
+            const RowChunks first(A, s, p.row_a), last(A, s, p.row_a + here - 1);
+            if (first.last - first.first >= kLongRow) w_first = of_count(long_row_tokens(A, s, p.row_a, first));
+            if (here > 1 && last.last - last.first >= kLongRow)
+                w_last = of_count(long_row_tokens(A, s, p.row_a + here - 1, last));
+        }
+        auto row_weight = [&](int i) {
+            const double w = i == 0 ? w_first : i == here - 1 ? w_last : -1.0;
+            return w >= 0.0 ? w : of_count(row_tokens(A, s, p.row_a + i));
         };
         if (lds) {
-            for (int i = threadIdx.x; i < here; i += kBlock) s_weight[i] = row_weight(p.row_a + i);
+            for (int i = threadIdx.x; i < here; i += kBlock) s_weight[i] = row_weight(i);
             __syncthreads();
         }
         const float factor = (float)(scale * same);
         auto weight = [&](int row, double* f, float* gs) {
             if (ROWS) {
-                const double w = lds ? s_weight[row - p.row_a] : row_weight(row);
+                const double w = lds ? s_weight[row - p.row_a] : row_weight(row - p.row_a);
                 *f = w;
                 *gs = (float)(scale * w);
             } else {
@@ -1055,14 +1097,54 @@ __device__ __forceinline__ void clear_rows(const PairArgs& A) {
 
 __global__ void __launch_bounds__(kBlock) clear_rows_kernel(PairArgs A) { clear_rows(A); }
 
-// A row's log ratio from its record; nothing is read outside its partials whatever that holds.
-__device__ __forceinline__ double log_ratio(const PairArgs& A, int64_t row, const RowInfo& f, int* count) {
-    int n = f.count;
-    double s = f.sum;
-    if (f.parts > 1 && f.first >= 0 && (int64_t)f.first + f.parts <= kWaves * A.chunks) {
-        for (int64_t b = f.first; b < (int64_t)f.first + f.parts; ++b) {
-            n += A.row_count[b + row];
-            s += A.row_sum[b + row];
+// A lane's row's log ratio from its record (if `live`); nothing is read outside the partials whatever that
+// holds.  Every lane of the wave must be active.  A lane reads its row's parts 4 at a time, or the wave those
+// of its long rows one row after the other, 64 parts at a time: whichever takes fewer waits.  (Two rows of
+// 131,072 tokens: 12 us a call by the wave, 91 with a lane reading one part at a time; 100 rows of 40,000: 37
+// by the lanes, 94 by the wave.)
+constexpr int kLaneParts = 16;
+
+__device__ __forceinline__ double log_ratio(const PairArgs& A, int64_t row, const RowInfo& f, bool live, int* count) {
+    constexpr int kLoads = 4;
+    const int lane = threadIdx.x & (kWave - 1);
+    const bool joined = live && f.parts > 1 && f.first >= 0 && (int64_t)f.first + f.parts <= kWaves * A.chunks;
+    int n = live ? f.count : 0;
+    double s = live ? f.sum : 0.0;
+    uint64_t many = __ballot(joined && f.parts > kLaneParts);
+    if (!__any(joined && f.parts >= kLaneParts * __builtin_popcountll(many))) many = 0;
+    if (joined && !(many >> lane & 1)) {
+        for (int b = 0; b < f.parts; b += kLoads) {
+            int c[kLoads];
+            double v[kLoads];
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int64_t at = f.first + row + (b + i < f.parts ? b + i : f.parts - 1);
+                c[i] = A.row_count[at];
+                v[i] = A.row_sum[at];
+            }
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                n += b + i < f.parts ? c[i] : 0;
+                s += b + i < f.parts ? v[i] : 0.0;
+            }
+        }
+    }
+    for (; many; many &= many - 1) {
+        const int of = __builtin_ctzll(many);
+        const int parts = __builtin_amdgcn_readlane(f.parts, of);
+        const int64_t first = __shfl(f.first + row, of, kWave);
+        int m = 0;
+        double t = 0.0;
+#pragma unroll 4
+        for (int b = lane; b < parts; b += kWave) {
+            m += A.row_count[first + b];
+            t += A.row_sum[first + b];
+        }
+        m = wave_total(m);
+        t = wave_total(t);
+        if (lane == of) {
+            n += m;
+            s += t;
         }
     }
     *count = n;
@@ -1104,22 +1186,27 @@ struct PairSums {
     int pairs = 0, right = 0;
 };
 
-// A row's loss (at the chosen row of a pair) and reward, if `out`, and the factor of its tokens' gradients.
+// Of a lane's row, if it is below `rows`: its loss (at the chosen row of a pair) and reward, if `out`, and the
+// factor of its tokens' gradients.  Every lane of the wave must be active.
 __device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64_t rows, bool out, PairSums* sums) {
-    int n, m;
-    const RowInfo mine = A.row_info[row];
-    bool chosen;
-    int64_t j = partner_row(A, row, rows, &chosen);
-    const RowInfo its = A.row_info[j >= 0 ? j : row];
-    // an id's entry is believed only if the row that it names has the id
-    if (j >= 0 && A.row_of) {
-        const int64_t v = A.pair[A.row_ids[row]];
-        if (A.row_ids[j] != (v < 0 ? -v : v) - 1) j = -1;
+    const bool live = row < rows;
+    RowInfo mine{}, its{};
+    bool chosen = false;
+    int64_t j = -1;
+    if (live) {
+        mine = A.row_info[row];
+        j = partner_row(A, row, rows, &chosen);
+        its = A.row_info[j >= 0 ? j : row];
+        // an id's entry is believed only if the row that it names has the id
+        if (j >= 0 && A.row_of) {
+            const int64_t v = A.pair[A.row_ids[row]];
+            if (A.row_ids[j] != (v < 0 ? -v : v) - 1) j = -1;
+        }
     }
-    const double S = log_ratio(A, row, mine, &n);
+    int n, m;
+    const double S = log_ratio(A, row, mine, live, &n), T = log_ratio(A, j, its, j >= 0, &m);
     double c = 0.0, loss = 0.0;
     if (j >= 0) {
-        const double T = log_ratio(A, j, its, &m);
         const double h = A.beta * (chosen ? S - T : T - S) - A.margin;
         double dh;
         if (A.kind == ODB_PREFERENCE_SIGMOID) {
@@ -1145,7 +1232,7 @@ __device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64
         sums->pairs += chosen;
         sums->right += chosen && S > T;
     }
-    if (out) {
+    if (out && live) {
         A.row_loss[row] = (float)loss;
         A.row_reward[row] = (float)(A.beta * S);
     }
@@ -1157,7 +1244,8 @@ __global__ void __launch_bounds__(kBlock) pairs_kernel(PairArgs A) {
     const int64_t rows = run_rows(t, t.d_slot_row_off[0]);
     const int64_t row = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     PairSums sums;
-    if (row < rows) A.coef[row] = pair_row(A, row, rows, true, &sums);
+    const double c = pair_row(A, row, rows, true, &sums);
+    if (row < rows) A.coef[row] = c;
     PairPart p;
     p.loss = block_total(sums.loss);
     p.pairs = block_total(sums.pairs);
@@ -1226,7 +1314,7 @@ __global__ void __launch_bounds__(kBlock) pairs_grad_kernel(PairArgs A, int64_t 
     pairs_grad(A, A.coef, s_bits);
 }
 
-constexpr int64_t kFewChunks = 1024;
+constexpr int64_t kFewChunks = 256;
 
 // The same for runs of at most kBlock rows: every block forms all their factors, which costs it what
 // waiting for a kernel that does would, and the first one leaves the rows' numbers.
@@ -1235,7 +1323,7 @@ __global__ void __launch_bounds__(kBlock) few_rows_kernel(PairArgs A) {
     __shared__ uint32_t s_bits[kMaxChunk / 32];
     const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
     PairSums sums;
-    s_coef[threadIdx.x] = threadIdx.x < rows ? pair_row(A, threadIdx.x, rows, blockIdx.x == 0, &sums) : 0.0;
+    s_coef[threadIdx.x] = pair_row(A, threadIdx.x, rows, blockIdx.x == 0, &sums);
     if (blockIdx.x == 0) leave_totals(A, sums.loss, sums.pairs, sums.right);
     __syncthreads();
     pairs_grad(A, s_coef, s_bits);
@@ -1259,7 +1347,11 @@ __global__ void __launch_bounds__(kBlock) pairs_one_kernel(PairArgs A) {
     __syncthreads();
     const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
     PairSums sums;
-    for (int64_t row = threadIdx.x; row < rows; row += kBlock) A.coef[row] = pair_row(A, row, rows, true, &sums);
+    for (int64_t first = 0; first < rows; first += kBlock) {     // uniform
+        const int64_t row = first + threadIdx.x;
+        const double c = pair_row(A, row, rows, true, &sums);
+        if (row < rows) A.coef[row] = c;
+    }
     leave_totals(A, sums.loss, sums.pairs, sums.right);
     __syncthreads();
     pairs_grad(A, A.coef, s_bits);

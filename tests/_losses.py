@@ -253,6 +253,8 @@ def preference_loss_torch(m, labels, shift, p, lp, ref, row_ids, pair):
     on = (labels != IGNORE) & (m.col >= shift)
     zero = torch.zeros((), dtype=torch.float64, device=on.device)
     S = m.sum(torch.where(on, lp.double() - ref.double(), zero), m.by_row)
+    n = m.sum(on, m.by_row).clamp(min=1) if p["normalize"] else torch.ones_like(S)
+    S = S / n
     row_of = torch.empty_like(row_ids).long()
     row_of[row_ids.long()] = torch.arange(row_ids.numel(), device=on.device)
     a = torch.nonzero(pair > 0)[:, 0]
@@ -262,5 +264,6 @@ def preference_loss_torch(m, labels, shift, p, lp, ref, row_ids, pair):
     loss[c] = p["loss_scale"] * torch.nn.functional.softplus(-h)
     coef[c] = -p["loss_scale"] * p["beta"] * torch.sigmoid(-h)
     coef[r] = -coef[c]
+    coef = coef / n
     return dict(loss=loss.sum(), row_loss=loss, reward=p["beta"] * S, grad=torch.where(on, coef[m.row], zero),
                 counts=torch.stack([torch.tensor(a.numel(), device=on.device), (S[c] > S[r]).sum()]))

@@ -866,6 +866,56 @@ def test_large_runs(elems):
     assert near(out["grad"], want["grad"]) and near(out["loss"], want["loss"].reshape(1))
 
 
+LONG_ROWS = {"two": [[65_536, 131_072]], "beside_short": [[3, 40_000], [70_001, 5, 70_000, 69_999], [20], [30_000]],
+             "many": [[40_000 + 7 * i for i in range(40)], [5] * 30, [9_000] * 20], "one": [[400_000]]}
+
+
+@pytest.mark.parametrize("name", list(LONG_ROWS))
+def test_long_rows(name):
+    """Rows over many chunks, prompts that fill whole chunks, and a row in which nothing counts."""
+    torch = _torch()
+    plan = Plan(LONG_ROWS[name], base=(5, 77))
+    log(f"long rows {name}: {plan.R} rows, {plan.E} elements")
+    rng = np.random.default_rng(83)
+    y_host = plan.labels(rng, 0.9)
+    y_host[plan.row_of == plan.R - 1] = IGNORE if plan.R > 1 else 1
+    tiles = _tiles(plan, y_host, 0, 0, 0)
+    y = tiles.labels
+    maps = ref.Maps(plan, "cuda")
+    gen = torch.Generator("cuda").manual_seed(83)
+    r = lambda n, sd: torch.randn(n, generator=gen, device="cuda") * sd
+    lp = -r(plan.E, 2).abs()
+    old, kref, adv = lp + r(plan.E, 0.2), lp + r(plan.E, 0.4), r(plan.R, 1)
+    for reduce in range(3):
+        p = _policy_params(dict(kl=3, reduce=reduce))
+        out, status = _policy_run(tiles, plan, p, lp, old, kref, None, adv, None, extra=0)
+        assert int(status.item()) == 0
+        want = ref.policy_loss_torch(maps, y, 0, p, lp, old, kref, adv)
+        assert torch.equal(out["counts"], want["counts"])
+        C = (80 + 2 * 2) * U        # as in test_large_runs
+        mag = p["loss_scale"] * (want["mags"][:, 0] + p["kl_coef"] * want["mags"][:, 1])
+        assert torch.all((out["loss"].double() - want["loss"]).abs() <= C * mag + 2 * U * want["loss"].abs())
+        assert torch.all((out["grad"].double() - want["grad"]).abs() <= 2 * C * want["grad_mag"])
+    ids = torch.randperm(plan.R, generator=gen, device="cuda").int()
+    pair = torch.zeros(plan.R, dtype=torch.int32, device="cuda")
+    at = torch.randperm(plan.R, generator=gen, device="cuda")
+    a, b = at[0:plan.R // 2 * 2:2], at[1:plan.R // 2 * 2:2]
+    pair[a], pair[b] = (b + 1).int(), -(a + 1).int()
+    for normalize, beta in ((0, 1e-4), (1, 2.0)):
+        p = dict(kind=0, normalize=normalize, beta=beta, margin=0.0, label_smoothing=0.0, loss_scale=0.125)
+        out, status = _preference_run(tiles, plan, p, lp, kref, ids, pair, 0, 0)
+        assert int(status.item()) == 0
+        want = ref.preference_loss_torch(maps, y, 0, p, lp, kref, ids, pair)
+        # 64-bit sums of at most 400,000 terms of size 10, times a factor of at most 2, rounded once
+        near = lambda x, w: torch.all((x.double() - w).abs() <= 1.01 * U * w.abs() + 1e-9)
+        assert torch.equal(out["counts"], want["counts"])
+        assert near(out["row_loss"], want["row_loss"]) and near(out["reward"], want["reward"])
+        assert near(out["grad"], want["grad"]) and near(out["loss"], want["loss"].reshape(1))
+        again, _ = _preference_run(tiles, plan, p, lp, kref, ids, pair, 0, 0)
+        for key, v in out.items():
+            assert torch.equal(v, again[key]), key
+
+
 def test_tiles_past_32_bits():
     """More than 2^31 elements in one slot of two rows: positions, the mean and the last elements."""
     import paper_2606_19989_amd as odb
