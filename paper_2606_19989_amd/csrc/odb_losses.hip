@@ -199,7 +199,7 @@ __device__ __forceinline__ T block_total(T v) {
 // `last`, holds any of its values.  SAFE, for where a group may end behind it: each value is read on its own,
 // the last one for those behind.  Otherwise a position past `last` reads that one.  Either way there is no
 // branch, so that loads of many groups go out together.
-// What is read here is read once: past the caches' usual order, 67 M elements in 2,048 tiles take 266 us
+// What is read here is read once: past the caches' usual order, 67 M elements in 2,080 tiles take 266 us
 // instead of 280 (policy) and 246 instead of 300 (preference).
 template <typename V4, bool SAFE, typename T>
 __device__ __forceinline__ V4 load4(const T* p, int o, int last) {
@@ -301,7 +301,7 @@ __device__ __forceinline__ void add_to_rows(int* s_rows, Group q, uint32_t on, i
 
 // First pass of a mean: the bits, and per chunk and slot the counted tokens, or (ROWS) per chunk and
 // row the counted tokens and per chunk and slot the rows with any that lie wholly in the chunk.
-// Bound by the reads of the labels: 67 M elements in 2,048 tiles take 59 us (5.1 TB/s).
+// Bound by the reads of the labels: 67 M elements in 2,080 tiles take 59 us (5.1 TB/s).
 template <bool ROWS>
 __global__ void __launch_bounds__(kBlock) policy_count_kernel(PolicyArgs A) {
     __shared__ alignas(16) uint8_t s_nibble[kMaxChunk / 4];
@@ -693,7 +693,7 @@ __device__ __forceinline__ double slot_total(const PolicyArgs& A, const SlotView
 }
 
 // The loss and its gradient, the elements that count given by the bits (by the labels for a sum, which
-// needs no weights and so no pass before).  67 M elements in 2,048 tiles, the exponential KL term, 4/5 of them
+// needs no weights and so no pass before).  67 M elements in 2,080 tiles, the exponential KL term, 3/4 of them
 // counted: 193 us for 600 MB read and 270 MB written (4.5 TB/s).  Instructions (about 100 an element, a power
 // and the KL term's series among them) and memory take about as long; the waves of other chunks hide one
 // behind the other.  A variant of the kernel by KL term, reduction and entropies keeps the rest of the work
