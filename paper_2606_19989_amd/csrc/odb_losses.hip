@@ -283,8 +283,11 @@ struct PolicyArgs {
 // Groups of a thread whose loads are under way together.
 constexpr int kAhead = 4;
 
-// Rows of a slot that one block weighs in LDS.
-constexpr int kLdsRows = 4096;
+// Rows of a chunk that one block weighs in LDS; those of fewer elements than 8 may be more, and are weighed where
+// they are met.  us a call for room for 512 / 1,024 / 4,096, which leaves fewer blocks on a compute unit (mean
+// over rows, 67 M elements in rows of about 480): 330 / 330 / 351; 34 M in rows of 40: 204 / 198 / 213, of 5:
+// 250 / 234 / 242; one tile of 1,000,000 x 3: 71 / 68 / 67.
+constexpr int kLdsRows = 1024;
 
 // Adds a group's counted elements to its rows, the first of them `row0`.
 __device__ __forceinline__ void add_to_rows(int* s_rows, Group q, uint32_t on, int maxlen, int row0) {
