@@ -643,7 +643,8 @@ typedef struct odb_policy_params {
  *                     once (captured graphs too) need workspaces of their own
  *
  * A token that does not count contributes nothing, whatever its inputs hold, and has gradient 0;
- * a slot without counted tokens (an IDLE one among them) has loss, means and counts 0.  Elements
+ * a slot without counted tokens (an IDLE one among them) has loss, means and counts 0.  A KL
+ * term or an entropy whose coefficient is 0 is only reported, whatever its size.  Elements
  * behind the last slot are not written.  Sums run in 64 bits in a fixed order: results are the
  * same bit for bit from call to call.  Asynchronous.
  */

@@ -610,7 +610,8 @@ __device__ __forceinline__ void leave_slot(const PolicyArgs& A, int64_t k, const
                                            const int64_t clipped[3]) {
     const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
     const double kl = A.kl_coef != 0.0 ? A.kl_coef * sum[1] : 0.0;      // a term that is only watched may overflow
-    A.slot_loss[k] = counted > 0 ? (float)(scale * (sum[0] + kl - A.entropy_coef * sum[2])) : 0.0f;
+    const double bonus = A.entropy_coef != 0.0 ? A.entropy_coef * sum[2] : 0.0;
+    A.slot_loss[k] = counted > 0 ? (float)(scale * (sum[0] + kl - bonus)) : 0.0f;
     for (int i = 0; i < 4; ++i) A.slot_means[4 * k + i] = (float)sum[i];
     A.slot_counts[4 * k] = counted;
     for (int i = 0; i < 3; ++i) A.slot_counts[4 * k + 1 + i] = clipped[i];

@@ -653,6 +653,12 @@ def test_watched_kl_term_may_overflow():
             assert out["loss"].tolist() == [-2.0 * (plan.tile_off[k + 1] - plan.tile_off[k] if reduce == 2 else 1)
                                             for k in range(plan.K)]
             assert out["means"][0, 1].item() == math.inf
+            H = np.ones(plan.E, np.float32)
+            H[2] = np.inf
+            out, _ = _policy_run(tiles, plan, _policy_params(dict(kl=0, reduce=reduce, loss_scale=1.0)), dev(lp), dev(lp),
+                                 None, dev(H), dev(np.full(plan.R, 2.0, np.float32)), None, extra=0)
+            assert bool(torch.isfinite(out["loss"]).all()) and out["means"][0, 2].item() == math.inf
+            assert out["grad"][:4].tolist() == [-2.0 / n] * 4
 
 
 def test_policy_terms_that_nearly_cancel():
@@ -1261,3 +1267,48 @@ def test_pipeline_buffers_grow_behind_another_stream():
     assert torch.equal(a[0], b[0][:K]) and torch.equal(a[2], b[2][:K])
     assert torch.equal(a[3], b[3][:part.num_elems]) and bool((junk == -7.0).all())
     pipe.check_losses()
+
+
+def test_pipeline_losses_in_a_graph():
+    """Both losses of a plan captured together and replayed on new inputs, eager work of another pipeline between."""
+    import paper_2606_19989_amd as odb
+    torch = _torch()
+    rng = np.random.default_rng(89)
+    w = synth.window_from_ranks("loss_graph", [rng.integers(2, 300, 200), rng.integers(2, 300, 150)], 4000)
+    tok_off, toks, ident = synth.device_tensors(w, "cuda")
+
+    def make():
+        pipe = odb.Pipeline(odb.DeviceWindow(w.rank_off, tok_off, toks, ident, w.num_identities), w.budget)
+        pipe.form()
+        pipe.align()
+        pipe.collate()
+        return pipe, pipe.tiles()
+    (pipe, t), (plain, u) = make(), make()
+    pair = torch.zeros(w.n, dtype=torch.int32, device="cuda")
+    pair[0:300:2] = torch.arange(1, 300, 2, dtype=torch.int32, device="cuda") + 1
+    pair[1:300:2] = -(torch.arange(0, 300, 2, dtype=torch.int32, device="cuda") + 1)
+    params = odb.PolicyParams(kl=2, reduce=1, kl_coef=0.1)
+    gen = torch.Generator("cuda").manual_seed(89)
+    draw = lambda: [-torch.rand(t.num_elems, generator=gen, device="cuda") * 3 for _ in range(3)] + \
+        [torch.randn(t.num_rows, generator=gen, device="cuda")]
+    lp, old, kref, adv = draw()
+    call = lambda p, tiles, a: (p.policy_loss(tiles, a[0], a[3], params, a[1], a[2]) +
+                                p.preference_loss(tiles, a[0], pair, ref_logprob=a[2]))
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        call(pipe, t, (lp, old, kref, adv))
+    side.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        got = call(pipe, t, (lp, old, kref, adv))
+    for _ in range(4):
+        new = draw()
+        for a, b in zip((lp, old, kref, adv), new):
+            a.copy_(b)
+        want = call(plain, u, new)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert (a is None and b is None) or torch.equal(a, b)
+    pipe.check_losses()
+    plain.check_losses()
