@@ -482,7 +482,7 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
                                              int maxlen, const Weight& weight, PolicySums& S) {
     float g[4] = {0, 0, 0, 0}, ge[4] = {0, 0, 0, 0};
     if (__any(L.on != 0)) {
-        float d[4], x[4], adv[4], kl[4];
+        float d[4], x[4], adv[4], kl[4], kl_slope[4];
         bool over[4], under[4], rare = false;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -501,6 +501,7 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
             if (KL != ODB_KL_NONE) x[j] = lp - (live ? L.ref[j] : 0.0f);
             if (KL == ODB_KL_EXP) {
                 kl[j] = less_line_series(-x[j]);
+                kl_slope[j] = x[j] - kl[j];    // 1 - exp(-x)
                 rare |= fabsf(x[j]) >= kSeries;
             }
         }
@@ -511,7 +512,11 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
                 const double z = A.on_policy || !live ? 0.0 : (double)L.lp[j] - (double)L.old[j];
                 over[j] = z > (pos ? A.at_high : neg ? A.at_dual : HUGE_VAL);
                 under[j] = neg && z < A.at_low;
-                if (KL == ODB_KL_EXP && fabsf(x[j]) >= kSeries) kl[j] = less_line_far(-x[j]);
+                if (KL == ODB_KL_EXP && fabsf(x[j]) >= kSeries) {
+                    // the slope without x, beside which it would be lost: a reference of no probability has 1
+                    kl[j] = less_line_far(-x[j]);
+                    kl_slope[j] = 1.0f - exp_near(-x[j]);
+                }
             }
         }
         double f[4];
@@ -546,17 +551,14 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
             bound = adv[j] == 0.0f ? 0.0f : bound;   // an overflowing ratio must not make the term NaN
             const float policy = -bound * adv[j];
             const float slope = over[j] || under[j] ? 0.0f : policy;
-            float kl_slope = 0.0f;
             if (KL == ODB_KL_LINEAR) {
                 kl[j] = x[j];
-                kl_slope = live ? 1.0f : 0.0f;
+                kl_slope[j] = live ? 1.0f : 0.0f;
             } else if (KL == ODB_KL_SQUARE) {
                 kl[j] = 0.5f * x[j] * x[j];
-                kl_slope = x[j];
-            } else if (KL == ODB_KL_EXP) {
-                kl_slope = x[j] - kl[j];    // 1 - exp(-x)
-            } else {
-                kl[j] = 0.0f;
+                kl_slope[j] = x[j];
+            } else if (KL == ODB_KL_NONE) {
+                kl[j] = kl_slope[j] = 0.0f;
             }
             // terms of both signs, whose sum may be far smaller than they are: the weights must not be rounded
             if (ROWS) S.sum[0] = fma(f[j], (double)policy, S.sum[0]);
@@ -568,7 +570,7 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
             S.clipped[0] += under[j];
             S.clipped[1] += over[j] && pos;
             S.clipped[2] += over[j] && !pos;
-            g[j] = gs[j] * (C.kl_coef != 0.0f ? fmaf(C.kl_coef, kl_slope, slope) : slope);
+            g[j] = gs[j] * (C.kl_coef != 0.0f ? fmaf(C.kl_coef, kl_slope[j], slope) : slope);
             if (ENT) ge[j] = live ? -C.entropy_coef * gs[j] : 0.0f;
         }
 #pragma unroll
