@@ -698,9 +698,10 @@ typedef struct odb_preference_params {
  *   d_ws / ws_bytes   odb_loss_workspace_size(t, num_ids if d_row_ids else 0) bytes, 256-B
  *                     aligned; calls in flight at once need workspaces of their own
  *
- * A pair counts if both ids have a row here.  If an id has several rows (sampler padding), the
- * first of them is its row and the others have no pair.  Rows and elements behind the last slot
- * are not written.  Sums run in 64 bits in a fixed order.  Asynchronous.
+ * A log ratio that is NaN, or the same infinity on both sides, makes the pair's loss and gradients
+ * NaN in every kind.  A pair counts if both ids have a row here.  If an id has several rows
+ * (sampler padding), the first of them is its row and the others have no pair.  Rows and elements
+ * behind the last slot are not written.  Sums run in 64 bits in a fixed order.  Asynchronous.
  */
 int odb_preference_loss(const odb_tiles_t* t, const odb_preference_params_t* p, const float* d_logprob,
                         const float* d_ref_logprob, const int32_t* d_row_ids, int64_t num_ids, const int32_t* d_pair,

@@ -1234,8 +1234,9 @@ __device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64
                    (A.smoothing > 0.0 ? A.smoothing * (soft + (h > 0 ? h : 0.0)) : 0.0);
             dh = A.smoothing * up - (1.0 - A.smoothing) * down;
         } else if (A.kind == ODB_PREFERENCE_HINGE) {
-            loss = h < 1.0 ? 1.0 - h : 0.0;
-            dh = h < 1.0 ? -1.0 : 0.0;
+            // a NaN stays one: it is not below 1, and not at or above it either
+            loss = h >= 1.0 ? 0.0 : 1.0 - h;
+            dh = h >= 1.0 ? 0.0 : h < 1.0 ? -1.0 : h;
         } else {
             loss = (h - 0.5) / A.beta;
             dh = 2.0 * loss / A.beta;

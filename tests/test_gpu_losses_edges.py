@@ -53,3 +53,37 @@ def test_slope_of_far_kl_terms(groups):
         got = out["grad"].double().cpu().numpy()
         bad = ~(np.abs(got - w * slope) <= w * (bound + 2 * U * np.abs(slope)))
         assert not bad.any(), (reduce, x[bad][:8], got[bad][:8] / w[bad][:8], slope[bad][:8])
+
+
+# --------------------------------------------------------------------- preference loss
+@pytest.mark.parametrize("rows", [8, 40, 600], ids=["one", "few", "many"])
+@pytest.mark.parametrize("by_id", [False, True])
+@pytest.mark.parametrize("kind", range(3))
+def test_pairs_without_a_number(rows, by_id, kind):
+    """A NaN among a pair's log-probabilities, or no probability on either side: the pair's loss and gradients
+    are NaN, and the total's; the other pairs keep theirs."""
+    torch = _torch()
+    plan = Plan([[40] * rows])
+    y = np.ones(plan.E, np.int32)
+    rng = np.random.default_rng(rows)
+    pair = np.zeros(plan.R, np.int32)
+    pair[0::2], pair[1::2] = np.arange(1, plan.R, 2) + 1, -(np.arange(0, plan.R, 2) + 1)
+    p = dict(kind=kind, normalize=0, beta=0.1, margin=0.1, label_smoothing=0.0, loss_scale=1.0)
+    tiles = _tiles(plan, y, 0, 0, 0)
+    ids = _dev(np.arange(plan.R, dtype=np.int32)) if by_id else None
+    base = (-rng.random(plan.E)).astype(np.float32)
+    good, _ = _preference_run(tiles, plan, p, _dev(base), None, ids, _dev(pair), 0, 0)
+    for c, values in ((4, {4: math.nan}), (2, {3: math.nan}), (6, {6: -math.inf, 7: -math.inf})):
+        lp = base.copy()
+        for r, v in values.items():
+            lp[np.nonzero(plan.row_of == r)[0][17]] = v
+        out, status = _preference_run(tiles, plan, p, _dev(lp), None, ids, _dev(pair), 0, 0)
+        assert int(status.item()) == 0
+        assert math.isnan(out["loss"].item()), (c, kind)
+        assert out["counts"][0].item() == plan.R // 2
+        mine = np.isin(np.arange(plan.R), (c, c + 1))
+        row_loss, grad = out["row_loss"].cpu().numpy(), out["grad"].cpu().numpy()
+        assert math.isnan(row_loss[c]) and row_loss[c + 1] == 0
+        assert np.array_equal(row_loss[~mine], good["row_loss"].cpu().numpy()[~mine])
+        at = mine[plan.row_of]
+        assert np.isnan(grad[at]).all() and np.array_equal(grad[~at], good["grad"].cpu().numpy()[~at])
