@@ -645,8 +645,9 @@ typedef struct odb_policy_params {
  * A token that does not count contributes nothing, whatever its inputs hold, and has gradient 0;
  * a slot without counted tokens (an IDLE one among them) has loss, means and counts 0.  A KL
  * term or an entropy whose coefficient is 0 is only reported, whatever its size.  Elements
- * behind the last slot are not written.  Sums run in 64 bits in a fixed order: results are the
- * same bit for bit from call to call.  Asynchronous.
+ * behind the last slot are not written.  A token's terms and slopes are formed in 32 bits, weights
+ * and sums in 64, in a fixed order: results are the same bit for bit from call to call.  A gradient
+ * is the slope times its factor (loss_scale, slot and token weight) rounded to 32 bits.  Asynchronous.
  */
 int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* p, const float* d_logprob,
                     const float* d_old_logprob, const float* d_ref_logprob, const float* d_entropy,

@@ -55,6 +55,75 @@ def test_slope_of_far_kl_terms(groups):
         assert not bad.any(), (reduce, x[bad][:8], got[bad][:8] / w[bad][:8], slope[bad][:8])
 
 
+@SIZES
+@pytest.mark.parametrize("reduce", range(3))
+def test_terms_of_both_signs_in_one_group(groups, reduce):
+    """Advantages per token whose large ones cancel, side by side: the small ones are what is left."""
+    plan = Plan(groups)
+    adv = np.resize(np.array([2.0 ** 24, 1, -2.0 ** 24, 1], np.float32), plan.E)
+    n = (plan.tile_off[1:] - plan.tile_off[:-1])
+    slot = plan.slot_of_row[plan.row_of]
+    lp = np.full(plan.E, -1.0, np.float32)
+    tiles = _tiles(plan, np.ones(plan.E, np.int32), 0, 0, 0)
+    p = _policy_params(dict(kl=0, reduce=reduce, token_advantage=1, loss_scale=1.0))
+    out, status = _policy_run(tiles, plan, p, _dev(lp), _dev(lp), None, None, _dev(adv), None, extra=0)
+    assert int(status.item()) == 0
+    total = -np.bincount(slot, weights=adv.astype(np.float64), minlength=plan.K)
+    mags = np.bincount(slot, weights=np.abs(adv).astype(np.float64), minlength=plan.K)
+    w = 1.0 / n if reduce < 2 else np.ones(plan.K)
+    # weights and sums of 64 bits, each step at most 2^-53 of the sum of magnitudes, one rounding to fp32
+    lost = 2.0 ** -52 * w * mags * (2 + n)
+    assert np.all(np.abs(out["loss"].double().cpu().numpy() - w * total) <= U * np.abs(w * total) + lost)
+    assert np.all(np.abs(out["means"][:, 0].double().cpu().numpy() - w * total) <= U * np.abs(w * total) + lost)
+
+
+def test_linear_kl_terms_that_nearly_cancel():
+    """Log ratios of few bits, so that every term is exact: what is left of terms a million times larger is
+    rounded once, in every reduction."""
+    rng = np.random.default_rng(67)
+    for lens in ([3, 5, 7, 11], [int(v) for v in rng.integers(1, 90, 40)], [int(v) for v in rng.integers(100, 900, 40)]):
+        plan = Plan([lens])
+        y = plan.labels(rng)
+        on = plan.counted(y, 0)
+        x = rng.integers(-4096, 4097, plan.R) / 1024.0
+        count = np.array([on[plan.row_of == r].sum() for r in range(plan.R)])
+        for reduce, weight in ((0, count / count.sum()), (1, np.full(plan.R, 1 / plan.R)), (2, count.astype(np.float64))):
+            # the last row's log ratio takes back the others', up to its own step
+            x[-1] = np.round(-(x[:-1] * weight[:-1]).sum() / weight[-1] * 1024) / 1024
+            kref = np.where(on, -x[plan.row_of], 0).astype(np.float32)
+            tiles = _tiles(plan, y, 0, 0, 0)
+            p = _policy_params(dict(kl=1, reduce=reduce, kl_coef=1.0, loss_scale=1.0))
+            zero = np.zeros(plan.E, np.float32)
+            out, _ = _policy_run(tiles, plan, p, _dev(zero), None, _dev(kref), None, _dev(np.zeros(plan.R, np.float32)),
+                                 None, extra=0)
+            want = (x * weight).sum()
+            lost = 1e-15 * (np.abs(x) * weight).sum() * plan.E
+            assert abs(float(out["loss"]) - want) <= U * abs(want) + lost, (plan.E, reduce, float(out["loss"]), want)
+            assert abs(float(out["means"][0, 1]) - want) <= U * abs(want) + lost, (plan.E, reduce)
+
+
+@SIZES
+@pytest.mark.parametrize("reduce", [0, 1])
+def test_means_of_terms_near_the_largest(groups, reduce):
+    """KL terms, ratios and entropies of up to 2e38 have a mean."""
+    plan = Plan(groups)
+    n = plan.tile_off[1:] - plan.tile_off[:-1]
+    slot = plan.slot_of_row[plan.row_of]
+    d = np.resize(np.array([88.0, 87.5, 88.2, 88.0, 87.9], np.float32), plan.E)
+    lp = np.zeros(plan.E, np.float32)
+    H = np.full(plan.E, 2e38, np.float32)
+    tiles = _tiles(plan, np.ones(plan.E, np.int32), 0, 0, 0)
+    p = _policy_params(dict(kl=3, reduce=reduce, kl_coef=0.0, loss_scale=1.0, clip_high=math.inf))
+    out, _ = _policy_run(tiles, plan, p, _dev(lp), _dev(-d), _dev(d), _dev(H), _dev(np.zeros(plan.R, np.float32)), None,
+                         extra=0)
+    mean = lambda v: np.bincount(slot, weights=v, minlength=plan.K) / n
+    want = np.stack([mean(np.exp(d.astype(np.float64)) - 1 - d), mean(H.astype(np.float64)),
+                     mean(np.exp(d.astype(np.float64)))], 1)
+    got = out["means"][:, 1:].double().cpu().numpy()
+    # the power of an argument that is exact: 8 roundings, a few for the sums
+    assert np.all(np.abs(got - want) <= 16 * U * want), (got, want)
+
+
 # --------------------------------------------------------------------- preference loss
 @pytest.mark.parametrize("rows", [8, 40, 600], ids=["one", "few", "many"])
 @pytest.mark.parametrize("by_id", [False, True])
