@@ -569,7 +569,9 @@ __device__ __forceinline__ void policy_group(const PolicyArgs& A, const PolicyCh
             S.clipped[0] += under[j];
             S.clipped[1] += over[j] && pos;
             S.clipped[2] += over[j] && !pos;
-            g[j] = gs[j] * (C.kl_coef != 0.0f ? fmaf(C.kl_coef, kl_slope[j], slope) : slope);
+            // 0 where nothing counts, also times a factor that is not finite
+            const float total = C.kl_coef != 0.0f ? fmaf(C.kl_coef, kl_slope[j], slope) : slope;
+            g[j] = live ? gs[j] * total : 0.0f;
             if (ENT) ge[j] = live ? -C.entropy_coef * gs[j] : 0.0f;
         }
         S.counted += __builtin_popcount(L.on);

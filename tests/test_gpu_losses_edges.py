@@ -124,6 +124,28 @@ def test_means_of_terms_near_the_largest(groups, reduce):
     assert np.all(np.abs(got - want) <= 16 * U * want), (got, want)
 
 
+@SIZES
+@pytest.mark.parametrize("reduce", range(3))
+def test_tokens_that_do_not_count_beside_weights_that_are_not_finite(groups, reduce):
+    rng = np.random.default_rng(3)
+    plan = Plan(groups)
+    y = plan.labels(rng, 0.6)
+    on = plan.counted(y, 1)
+    assert on.any() and not on.all()
+    lp = np.where(on, -1.0, np.nan).astype(np.float32)
+    H = np.where(on, 1.0, np.nan).astype(np.float32)
+    adv = np.ones(plan.R, np.float32)
+    tiles = _tiles(plan, y, 1, 0, 0)
+    for kl in range(4):
+        p = _policy_params(dict(kl=kl, reduce=reduce, kl_coef=0.5, entropy_coef=0.1, loss_scale=1e30))
+        for w in (math.inf, math.nan, 1e30):
+            out, _ = _policy_run(tiles, plan, p, _dev(lp), None, _dev(lp) if kl else None, _dev(H), _dev(adv),
+                                 _dev(np.full(plan.K, w)), extra=0)
+            for k in ("grad", "grad_ent"):
+                assert np.all(out[k].cpu().numpy()[~on] == 0), (kl, w, k)
+                assert not np.isfinite(out[k].cpu().numpy()[on]).any(), (kl, w, k)
+
+
 # --------------------------------------------------------------------- preference loss
 @pytest.mark.parametrize("rows", [8, 40, 600], ids=["one", "few", "many"])
 @pytest.mark.parametrize("by_id", [False, True])
