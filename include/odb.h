@@ -609,9 +609,9 @@ typedef struct odb_policy_params {
     double  clip_low;            /* e_l in [0, 1] (1: no lower clip)                           */
     double  clip_high;           /* e_h >= 0 (infinite: no upper clip)                         */
     double  dual_clip;           /* bound c > 1 on the ratio where A < 0, or 0 (none)          */
-    double  kl_coef;
+    double  kl_coef;             /* both finite in fp32                                        */
     double  entropy_coef;
-    double  loss_scale;          /* factor of every slot's loss (W in Eq. 2's scaling)         */
+    double  loss_scale;          /* finite; factor of every slot's loss (W in Eq. 2's scaling) */
 } odb_policy_params_t;
 
 /*

@@ -1416,8 +1416,9 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     if (!(p->clip_high >= 0.0)) return set_error(ODB_E_INVALID_ARG, "clip_high must be >= 0");
     if (!(p->dual_clip == 0.0 || (p->dual_clip > 1.0 && std::isfinite(p->dual_clip))))
         return set_error(ODB_E_INVALID_ARG, "dual_clip must be 0 or finite and > 1");
-    if (!std::isfinite(p->kl_coef) || !std::isfinite(p->entropy_coef) || !std::isfinite(p->loss_scale))
-        return set_error(ODB_E_INVALID_ARG, "kl_coef, entropy_coef and loss_scale must be finite");
+    // the gradients' coefficients are rounded to fp32
+    if (!std::isfinite((float)p->kl_coef) || !std::isfinite((float)p->entropy_coef) || !std::isfinite(p->loss_scale))
+        return set_error(ODB_E_INVALID_ARG, "kl_coef and entropy_coef must be finite in fp32, loss_scale finite");
     if (t->num_elems > 0 && !d_entropy && (p->entropy_coef != 0.0 || d_grad_entropy))
         return set_error(ODB_E_INVALID_ARG, "an entropy term needs d_entropy");
     if (t->num_slots == 0) return ODB_OK;

@@ -120,6 +120,12 @@ def test_policy_arguments_refused():
     assert lib.odb_policy_loss(byref(_tiles()), None, *[P] * 11, None, P, 1 << 40, None) == odb.ODB_E_INVALID_ARG
 
 
+def test_policy_coefficients_beyond_fp32_refused():
+    for big in (1e39, -1e39, 3.4028236e38):     # the last one rounds to infinity
+        assert _policy(p=odb.PolicyParams(kl=3, kl_coef=big)) == odb.ODB_E_INVALID_ARG, big
+        assert _policy(p=odb.PolicyParams(kl=3, entropy_coef=big), ent=P) == odb.ODB_E_INVALID_ARG, big
+
+
 def test_preference_arguments_refused():
     for bad in (dict(kind=3), dict(kind=-1), dict(normalize=2), dict(beta=0.0), dict(beta=-1.0), dict(beta=math.nan),
                 dict(beta=math.inf), dict(margin=math.nan), dict(loss_scale=math.inf), dict(label_smoothing=-0.1),
