@@ -637,8 +637,11 @@ typedef struct odb_policy_params {
  *   d_grad_logprob    [num_elems] out, or NULL
  *   d_grad_entropy    [num_elems] out, or NULL (needs d_entropy)
  *   d_status          [1] device, or NULL: set to a nonzero value if a slot's arrays contradict
- *                     each other or leave the arrays' lengths (such a slot counts nothing and its
- *                     gradients are not written); never cleared here
+ *                     each other or leave the arrays' lengths; never cleared here.  A slot whose
+ *                     rows or maxlen do not fit its offsets counts nothing and its gradients are
+ *                     not written; the others are as without it.  Where a slot's offsets fall or
+ *                     leave the arrays, any slot may count nothing instead of what it holds, and
+ *                     no gradient has a meaning
  *   d_ws / ws_bytes   odb_loss_workspace_size(t, 0) bytes, 256-B aligned; calls in flight at
  *                     once (captured graphs too) need workspaces of their own
  *
@@ -694,8 +697,10 @@ typedef struct odb_preference_params {
  *   d_status          [1] device, or NULL: set to a nonzero value if a slot's arrays contradict
  *                     each other, an id lies outside [0, num_ids), or a row's id and the id it
  *                     is paired with do not name each other (such a row has no pair); never
- *                     cleared here.  The rows of a contradicting slot, and the pairs they are
- *                     in, have values without meaning
+ *                     cleared here.  The rows of a slot whose rows or maxlen do not fit its
+ *                     offsets have no pair and a reward of 0, and their gradients are not
+ *                     written.  Where a slot's offsets fall or leave the arrays, d_loss, d_counts
+ *                     and the rows' numbers are 0 and no gradient has a meaning
  *   d_ws / ws_bytes   odb_loss_workspace_size(t, num_ids if d_row_ids else 0) bytes, 256-B
  *                     aligned; calls in flight at once need workspaces of their own
  *

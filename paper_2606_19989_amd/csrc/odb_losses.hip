@@ -41,6 +41,8 @@ constexpr float kLn2 = 0.69314718055994530942f;
 typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef int int4u __attribute__((ext_vector_type(4), aligned(4)));
 
+constexpr int kCheckBlocks = 256;   // blocks of a pass that look over the slots, at most
+
 // ------------------------------------------------------------------ workspace
 struct SlotPart {
     double sum[4];      // policy, KL, entropy, ratio
@@ -49,7 +51,7 @@ struct SlotPart {
 };
 
 // A row's sum and count where it lies in one part (a wave's quarter of a chunk), otherwise the parts
-// that it touches, whose partials hold them.
+// that it touches, whose partials hold them.  No parts: a row of a contradicting slot.
 struct RowInfo {
     double sum;
     int32_t count;
@@ -63,7 +65,7 @@ struct PairPart {
 };
 
 struct LossLayout {
-    size_t bits, chunk_slot, slot_count, slot_part, row_sum, row_count, row_info, coef, pair_part, row_of;
+    size_t bits, chunk_slot, slot_count, slot_part, row_sum, row_count, row_info, coef, pair_part, disorder, row_of;
     size_t total;
     int64_t chunks;
     int32_t chunk;
@@ -120,6 +122,7 @@ LossLayout loss_layout(const odb_tiles_t* t, int64_t num_ids) {
     L.row_info = take((int64_t)sizeof(RowInfo) * R);
     L.coef = take(8 * R);
     L.pair_part = take((int64_t)sizeof(PairPart) * (R / kBlock + 1));
+    L.disorder = take(4 * kCheckBlocks * kWaves);
     L.row_of = take(4 * num_ids);
     L.total = o;
     return L;
@@ -134,7 +137,38 @@ int check_loss_workspace(const LossLayout& L, const void* d_ws, size_t ws_bytes)
     return ODB_OK;
 }
 
+// Blocks that look over K slots.
+int64_t check_blocks(int64_t K) { return std::min((K + kBlock - 1) / kBlock, (int64_t)kCheckBlocks); }
+
 // ------------------------------------------------------------------ shared by the passes
+// The first `blocks` blocks of a pass look over the run's slots: f(k, slot) for every one, called by whole waves
+// (`real`: the lane has a slot).  A wave of them leaves a word: is one of its slots not ordered?  Then the passes'
+// partials mean nothing, and who takes the sums has them as 0.
+template <typename F>
+__device__ __forceinline__ void check_slots(const odb_tiles_t& t, int64_t e_base, int64_t r_base, uint32_t* disorder,
+                                            int64_t blocks, const F& f) {
+    const int64_t b = blockIdx.x;
+    if (b >= blocks) return;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    uint32_t found = 0;
+    for (int64_t first = b * kBlock + wave * kWave; first < t.num_slots; first += blocks * kBlock) {   // uniform
+        const int64_t k = first + lane;
+        const bool real = k < t.num_slots;
+        const SlotView s = slot_view(t, real ? k : first, e_base, r_base);
+        found |= !s.ordered;
+        f(real, s);
+    }
+    found = __any(found);
+    if (lane == 0) disorder[b * kWaves + wave] = found;
+}
+
+// Whether one of those words is set; every lane of the wave must be active.
+__device__ __forceinline__ bool slots_disordered(const uint32_t* disorder, int64_t blocks) {
+    uint32_t found = 0;
+    for (int64_t i = threadIdx.x & (kWave - 1); i < blocks * kWaves; i += kWave) found |= disorder[i];
+    return __any(found);
+}
+
 // Last slot from `from` on that starts at or before element e, 64 probes a step (one a lane; every lane of
 // the wave must be active): two loads one after the other for up to 4,096 slots, where halving the range
 // takes twelve.
@@ -271,8 +305,9 @@ struct PolicyArgs {
     int32_t* slot_count;        // counted tokens (token mean) or complete rows with any (row mean)
     SlotPart* slot_part;
     int32_t* row_count;
+    uint32_t* disorder;
     int32_t* status;
-    int64_t chunks;
+    int64_t chunks, check_blocks;
     double at_low, at_high, at_dual;    // ln(1 - e_l), ln(1 + e_h), ln c
     double kl_coef, entropy_coef, loss_scale;
     float low, high, dual;              // 1 - e_l, 1 + e_h, c
@@ -311,6 +346,7 @@ __global__ void __launch_bounds__(kBlock) policy_count_kernel(PolicyArgs A) {
     __shared__ int s_rows[ROWS ? kLdsRows : 1];
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
+    check_slots(t, e_base, r_base, A.disorder, A.check_blocks, [](bool, const SlotView&) {});
     const int64_t total = run_elems(t, e_base);
     const int64_t b = blockIdx.x, c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
     if (c0 >= c1) return;
@@ -709,6 +745,7 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
     __shared__ uint32_t s_bits[LABELS ? 1 : kMaxChunk / 32];
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
+    if (LABELS) check_slots(t, e_base, r_base, A.disorder, A.check_blocks, [](bool, const SlotView&) {});
     const int64_t total = run_elems(t, e_base);
     const int64_t b = blockIdx.x, c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
     if (c0 >= c1) return;
@@ -785,22 +822,23 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
     });
 }
 
-// A run of few elements, in one launch of one block.
+// A run of few elements, in one launch of one block.  A slot that the walk misses for offsets out of order keeps
+// the zeros written first.
 template <int KL>
 __global__ void __launch_bounds__(kBlock) policy_one_kernel(PolicyArgs A, int reduce) {
     __shared__ uint8_t s_nibble[kOnePolicy / 4];
     __shared__ int s_rows[kOnePolicy];
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
-    const int64_t total = run_elems(t, e_base), none[3] = {0, 0, 0};
+    const int64_t none[3] = {0, 0, 0};
     const double nothing[4] = {0, 0, 0, 0};
     for (int64_t k = threadIdx.x; k < t.num_slots; k += kBlock) {
         leave_slot(A, k, nothing, 0, none);
         if (A.status && !slot_view(t, k, e_base, r_base).ok) *A.status = kErrTiles;
     }
     __syncthreads();
-    if (total == 0) return;
-    each_slot(t, e_base, r_base, first_slot(t, e_base, 0), 0, total,
+    if (t.num_elems == 0) return;
+    each_slot(t, e_base, r_base, first_slot(t, e_base, 0), 0, t.num_elems,
               [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
         const Span p(s, a0, a1, 0, kBlock);
         const PolicyChunk C = policy_chunk(A, s, 0);
@@ -855,6 +893,7 @@ __global__ void __launch_bounds__(kBlock) policy_slots_kernel(PolicyArgs A) {
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int lane = threadIdx.x & (kWave - 1);
+    const bool disordered = slots_disordered(A.disorder, A.check_blocks);
     for (int64_t k = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); k < t.num_slots;
          k += (int64_t)gridDim.x * kWaves) {
         const SlotView s = slot_view(t, k, e_base, r_base);
@@ -862,7 +901,7 @@ __global__ void __launch_bounds__(kBlock) policy_slots_kernel(PolicyArgs A) {
         double n = 0, clipped[3] = {0, 0, 0};     // whole numbers below 2^41
         if (!s.ok) {
             if (A.status && lane == 0) *A.status = kErrTiles;
-        } else if (s.hi > s.lo) {
+        } else if (s.hi > s.lo && !disordered) {
             for (int64_t j = (s.lo >> A.chunk_log2) + lane; j <= (s.hi - 1) >> A.chunk_log2; j += kWave) {
                 const SlotPart p = A.slot_part[j + k];
 #pragma unroll
@@ -899,6 +938,7 @@ struct PairArgs {
     double* coef;
     PairPart* part;
     uint32_t* bits;
+    uint32_t* disorder;
     int32_t* chunk_slot;
     float* loss;
     float* row_loss;
@@ -906,7 +946,7 @@ struct PairArgs {
     int64_t* counts;
     float* grad;
     int32_t* status;
-    int64_t chunks;
+    int64_t chunks, check_blocks;
     double beta, margin, smoothing, loss_scale;
     int32_t kind, chunk, quarter_log2;
     bool normalize;
@@ -1061,9 +1101,6 @@ __device__ __forceinline__ void row_sums(const PairArgs& A, uint32_t* s_bits) {
     // (uniform over the wave, which the compiler does not see by itself)
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int64_t b = blockIdx.x;
-    if (A.status)
-        for (int64_t k = b * kBlock + threadIdx.x; k < t.num_slots; k += (int64_t)gridDim.x * kBlock)
-            if (!slot_view(t, k, e_base, r_base).ok) *A.status = kErrTiles;
     if (A.row_of) {      // the ids' first rows, beside the tiles
         const int64_t rows = run_rows(t, r_base);
         for (int64_t i = b * kBlock + threadIdx.x; i < rows; i += (int64_t)gridDim.x * kBlock) {
@@ -1093,9 +1130,25 @@ __device__ __forceinline__ void row_sums(const PairArgs& A, uint32_t* s_bits) {
     for (int i = threadIdx.x; i < words; i += kBlock) A.bits[b * words + i] = s_bits[i];
 }
 
+// What the pass leaves of the slots.
+__device__ __forceinline__ void check_rows(const PairArgs& A) {
+    const int64_t e_base = A.t.d_slot_tile_off[0], r_base = A.t.d_slot_row_off[0];
+    check_slots(A.t, e_base, r_base, A.disorder, A.check_blocks, [&](bool real, const SlotView& s) {
+        if (real && !s.ok && A.status) *A.status = kErrTiles;
+        // rows that the walk passes over
+        for (uint64_t bad = __ballot(real && !s.ok && s.ordered); bad; bad &= bad - 1) {
+            const int of = __builtin_ctzll(bad);
+            const int64_t row1 = __shfl(s.row1, of, kWave);
+            for (int64_t i = __shfl(s.row0, of, kWave) + (threadIdx.x & (kWave - 1)); i < row1; i += kWave)
+                A.row_info[i] = RowInfo{};
+        }
+    });
+}
+
 template <bool REF>
 __global__ void __launch_bounds__(kBlock) row_sums_kernel(PairArgs A) {
     __shared__ uint32_t s_bits[kMaxChunk / 32];
+    check_rows(A);
     row_sums<REF>(A, s_bits);
 }
 
@@ -1201,9 +1254,10 @@ struct PairSums {
 };
 
 // Of a lane's row, if it is below `rows`: its loss (at the chosen row of a pair) and reward, if `out`, and the
-// factor of its tokens' gradients.  Every lane of the wave must be active.
-__device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64_t rows, bool out, PairSums* sums) {
-    const bool live = row < rows;
+// factor of its tokens' gradients; all 0 if slots are out of order.  Every lane of the wave must be active.
+__device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64_t rows, bool disordered, bool out,
+                                           PairSums* sums) {
+    const bool live = row < rows && !disordered;
     RowInfo mine{}, its{};
     bool chosen = false;
     int64_t j = -1;
@@ -1211,6 +1265,7 @@ __device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64
         mine = A.row_info[row];
         j = partner_row(A, row, rows, &chosen);
         its = A.row_info[j >= 0 ? j : row];
+        if (mine.parts == 0 || its.parts == 0) j = -1;
         // an id's entry is believed only if the row that it names has the id
         if (j >= 0 && A.row_of) {
             const int64_t v = A.pair[A.row_ids[row]];
@@ -1247,7 +1302,7 @@ __device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64
         sums->pairs += chosen;
         sums->right += chosen && S > T;
     }
-    if (out && live) {
+    if (out && row < rows) {
         A.row_loss[row] = (float)loss;
         A.row_reward[row] = (float)(A.beta * S);
     }
@@ -1261,7 +1316,7 @@ __global__ void __launch_bounds__(kBlock) pairs_kernel(PairArgs A) {
     const int64_t rows = run_rows(t, t.d_slot_row_off[0]);
     const int64_t row = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     PairSums sums;
-    const double c = pair_row(A, row, rows, true, &sums);
+    const double c = pair_row(A, row, rows, slots_disordered(A.disorder, A.check_blocks), true, &sums);
     if (row < rows) A.coef[row] = c;
     PairPart p;
     p.loss = block_total(sums.loss);
@@ -1343,7 +1398,8 @@ __global__ void __launch_bounds__(kBlock) few_rows_kernel(PairArgs A) {
     __shared__ uint32_t s_bits[kMaxChunk / 32];
     const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
     PairSums sums;
-    s_coef[threadIdx.x] = pair_row(A, threadIdx.x, rows, blockIdx.x == 0, &sums);
+    s_coef[threadIdx.x] = pair_row(A, threadIdx.x, rows, slots_disordered(A.disorder, A.check_blocks), blockIdx.x == 0,
+                                   &sums);
     if (blockIdx.x == 0) leave_totals(A, sums.loss, sums.pairs, sums.right);
     __syncthreads();
     pairs_grad(A, s_coef, s_bits);
@@ -1363,13 +1419,15 @@ __global__ void __launch_bounds__(kBlock) pairs_one_kernel(PairArgs A) {
         __threadfence();     // before the atomics on the same entries
         __syncthreads();
     }
+    check_rows(A);
     row_sums<REF>(A, s_bits);
     __syncthreads();
     const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
+    const bool disordered = slots_disordered(A.disorder, A.check_blocks);
     PairSums sums;
     for (int64_t first = 0; first < rows; first += kBlock) {     // uniform
         const int64_t row = first + threadIdx.x;
-        const double c = pair_row(A, row, rows, true, &sums);
+        const double c = pair_row(A, row, rows, disordered, true, &sums);
         if (row < rows) A.coef[row] = c;
     }
     leave_totals(A, sums.loss, sums.pairs, sums.right);
@@ -1450,8 +1508,10 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     a.slot_count = ws_at<int32_t>(d_ws, L.slot_count);
     a.slot_part = ws_at<SlotPart>(d_ws, L.slot_part);
     a.row_count = ws_at<int32_t>(d_ws, L.row_count);
+    a.disorder = ws_at<uint32_t>(d_ws, L.disorder);
     a.status = d_status;
     a.chunks = L.chunks;
+    a.check_blocks = L.chunks > 0 ? check_blocks(t->num_slots) : 0;
     a.chunk = L.chunk;
     a.chunk_log2 = __builtin_ctz((unsigned)L.chunk);
     a.at_low = std::log1p(-p->clip_low);
@@ -1464,7 +1524,8 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     a.high = (float)(1.0 + p->clip_high);
     a.dual = (float)p->dual_clip;
     a.token_advantage = p->token_advantage;
-    const dim3 grid((unsigned)L.chunks), block(kBlock);     // at most 2^23 blocks
+    // at most 2^23 blocks; in the first pass those behind the chunks only look over slots
+    const dim3 grid((unsigned)L.chunks), first((unsigned)std::max(L.chunks, a.check_blocks)), block(kBlock);
     if (t->num_elems <= kOnePolicy && t->num_slots <= kOneSlots) {
         hipLaunchKernelGGL(policy_one_kernels[p->kl], dim3(1), block, 0, s, a, (int)p->reduce);
         ODB_LAUNCHED();
@@ -1472,11 +1533,12 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     }
     if (L.chunks > 0 && p->reduce != ODB_REDUCE_SUM) {
         hipLaunchKernelGGL(p->reduce == ODB_REDUCE_ROW_MEAN ? policy_count_kernel<true> : policy_count_kernel<false>,
-                           grid, block, 0, s, a);
+                           first, block, 0, s, a);
         ODB_LAUNCHED();
     }
     if (L.chunks > 0) {
-        hipLaunchKernelGGL(policy_kernels[p->kl][d_entropy ? 1 : 0][p->reduce], grid, block, 0, s, a);
+        hipLaunchKernelGGL(policy_kernels[p->kl][d_entropy ? 1 : 0][p->reduce], p->reduce == ODB_REDUCE_SUM ? first : grid,
+                           block, 0, s, a);
         ODB_LAUNCHED();
     }
     hipLaunchKernelGGL(policy_slots_kernel, dim3(grid_for(t->num_slots, kWaves)), block, 0, s, a);
@@ -1533,8 +1595,10 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
     a.row_reward = d_row_reward;
     a.counts = d_counts;
     a.grad = d_grad_logprob;
+    a.disorder = ws_at<uint32_t>(d_ws, L.disorder);
     a.status = d_status;
     a.chunks = L.chunks;
+    a.check_blocks = check_blocks(t->num_slots);
     a.chunk = L.chunk;
     a.quarter_log2 = __builtin_ctz((unsigned)L.chunk) - 2;
     a.beta = p->beta;
@@ -1550,6 +1614,7 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
         return ODB_OK;
     }
     if (t->num_elems <= kOnePairs && t->num_slots <= kOneSlots) {
+        a.check_blocks = 1;
         hipLaunchKernelGGL(d_ref_logprob ? pairs_one_kernel<true> : pairs_one_kernel<false>, dim3(1), block, 0, s, a);
         ODB_LAUNCHED();
         return ODB_OK;
@@ -1560,7 +1625,7 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
         ODB_LAUNCHED();
     }
     // at most 2^23 blocks; those behind the chunks only look over the slots
-    const dim3 sums((unsigned)std::max(L.chunks, (t->num_slots + kOneSlots - 1) / kOneSlots));
+    const dim3 sums((unsigned)std::max(L.chunks, a.check_blocks));
     hipLaunchKernelGGL(d_ref_logprob ? row_sums_kernel<true> : row_sums_kernel<false>, sums, block, 0, s, a);
     ODB_LAUNCHED();
     // without gradients the first block is all that the last kernel has to do

@@ -14,10 +14,15 @@ namespace odb {
 // Slot k of a run: its elements [lo, hi) and its first row, counted from the run's first.
 struct SlotView {
     int64_t lo, hi;
-    int64_t row0;
+    int64_t row0, row1;
     int32_t rows, maxlen;
-    bool ok;    // the arrays agree and stay inside the run's lengths
+    bool ordered;    // its offsets do not fall and stay inside the run's lengths
+    bool ok;         // and its arrays agree
 };
+
+// If every slot is ordered, a slot's offsets are where the one before it ends: the walk below then meets
+// each ok slot whole, and no two slots share an element or a row.  If one is not, neither holds: the
+// search goes by offsets that fall, and the walk ends at one that leaves the run.
 
 // Differences of offsets that may hold anything.
 __host__ __device__ __forceinline__ int64_t offset_from(int64_t a, int64_t base) {
@@ -30,12 +35,13 @@ __host__ __device__ __forceinline__ SlotView slot_view(const odb_tiles_t& t, int
     s.lo = offset_from(t.d_slot_tile_off[k], e_base);
     s.hi = offset_from(t.d_slot_tile_off[k + 1], e_base);
     s.row0 = offset_from(t.d_slot_row_off[k], r_base);
-    const int64_t row1 = offset_from(t.d_slot_row_off[k + 1], r_base);
+    s.row1 = offset_from(t.d_slot_row_off[k + 1], r_base);
     s.rows = t.d_slot_rows[k];
     s.maxlen = t.d_slot_maxlen[k];
-    s.ok = s.rows >= 0 && s.maxlen >= 0 && (s.rows == 0) == (s.maxlen == 0) && 0 <= s.lo && s.lo <= s.hi &&
-           s.hi <= t.num_elems && 0 <= s.row0 && s.row0 <= row1 && row1 <= t.num_rows && row1 - s.row0 == s.rows &&
-           s.hi - s.lo == (int64_t)s.rows * s.maxlen;
+    s.ordered = 0 <= s.lo && s.lo <= s.hi && s.hi <= t.num_elems && 0 <= s.row0 && s.row0 <= s.row1 &&
+                s.row1 <= t.num_rows;
+    s.ok = s.ordered && s.rows >= 0 && s.maxlen >= 0 && (s.rows == 0) == (s.maxlen == 0) &&
+           s.row1 - s.row0 == s.rows && s.hi - s.lo == (int64_t)s.rows * s.maxlen;
     return s;
 }
 

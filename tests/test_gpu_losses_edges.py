@@ -178,3 +178,90 @@ def test_pairs_without_a_number(rows, by_id, kind):
         assert np.array_equal(row_loss[~mine], good["row_loss"].cpu().numpy()[~mine])
         at = mine[plan.row_of]
         assert np.isnan(grad[at]).all() and np.array_equal(grad[~at], good["grad"].cpu().numpy()[~at])
+
+
+# ------------------------------------------------------------------ arrays that contradict each other
+def _broken(plan, field, at, value):
+    bad = Plan([[1]])
+    for name in ("rows", "maxlen", "row_off", "tile_off"):
+        setattr(bad, name, getattr(plan, name).copy())
+    getattr(bad, field)[at] = value
+    bad.R, bad.E, bad.K = plan.R, plan.E, plan.K
+    return bad
+
+
+BROKEN = {
+    # name: (groups, offsets that fall or leave the arrays, slots whose rows do not fit their offsets)
+    "one": ([[4, 6], [9], [3, 3, 3]], [("tile_off", 3, 5), ("tile_off", 3, -2), ("tile_off", 1, 10 ** 9), ("row_off", 3, 0)],
+            [("rows", 1, 2), ("maxlen", 2, 4)]),
+    "passes": ([[70] * 10] * 12, [("tile_off", 2, 1 << 40), ("tile_off", 2, 9000), ("tile_off", 2, -1),
+                                  ("tile_off", 12, 700), ("tile_off", 12, -5), ("tile_off", 6, 0), ("row_off", 5, 0),
+                                  ("row_off", 12, 1000), ("row_off", 12, 3), ("row_off", 1, 1 << 40)],
+               [("rows", 3, 9), ("maxlen", 3, 71), ("rows", 0, -1), ("maxlen", 11, 0), ("rows", 11, 1 << 30)]),
+    "many": ([[9] * 10] * 700, [("tile_off", 600, 0), ("row_off", 699, 1 << 50)], [("rows", 600, 9), ("maxlen", 0, 8)]),
+}
+
+
+@pytest.mark.parametrize("name", list(BROKEN))
+def test_slots_that_contradict_each_other(name):
+    """Whatever the workspace held: beside a slot whose rows do not fit the others have their numbers; with
+    offsets out of order a slot has its numbers or none."""
+    torch = _torch()
+    groups, offsets, slots = BROKEN[name]
+    plan = Plan(groups)
+    rng = np.random.default_rng(7)
+    y = plan.labels(rng, 0.3)
+    on = plan.counted(y, 1)
+    lp = np.where(on, -rng.random(plan.E), 0).astype(np.float32)
+    old, kref = (np.where(on, lp + rng.normal(size=plan.E) * 0.1, 0).astype(np.float32) for _ in range(2))
+    adv = rng.standard_normal(plan.R).astype(np.float32)
+    pair = np.zeros(plan.R, np.int32)
+    at = rng.permutation(plan.R)[:plan.R // 2 * 2]
+    pair[at[0::2]], pair[at[1::2]] = at[1::2] + 1, -(at[0::2] + 1)
+    pp = dict(kind=0, normalize=0, beta=0.2, margin=0.0, label_smoothing=0.0, loss_scale=1.0)
+    slot_of = plan.slot_of_row[plan.row_of]
+    good = [_policy_run(_tiles(plan, y, 1, 0, 0), plan, _policy_params(dict(kl=3, reduce=r)), _dev(lp), _dev(old),
+                        _dev(kref), None, _dev(adv), None, extra=0)[0] for r in range(3)]
+    fair, _ = _preference_run(_tiles(plan, y, 1, 0, 0), plan, pp, _dev(lp), _dev(kref), None, _dev(pair), 0, 0)
+    for field, k, value in offsets + slots:
+        tiles = _tiles(_broken(plan, field, k, value), y, 1, 0, 0)
+        ordered = (field, k, value) in slots
+        left = [torch.full((1 << 20,), fill, dtype=torch.uint8, device="cuda") for fill in (0x3f, 0x01)]
+        for reduce in range(3):
+            for ws in left:
+                out, status = _policy_run(tiles, plan, _policy_params(dict(kl=3, reduce=reduce)), _dev(lp), _dev(old),
+                                          _dev(kref), None, _dev(adv), None, extra=0, ws=ws)
+                assert int(status.item()) != 0
+                for key in ("loss", "means", "counts"):
+                    got, want = out[key].cpu().numpy(), good[reduce][key].cpu().numpy()
+                    if ordered:
+                        want[k] = 0
+                        assert np.array_equal(got, want), (field, k, value, reduce, key)
+                    else:
+                        whole = np.array([np.array_equal(g, w) for g, w in zip(got, want)])
+                        none = np.array([not np.any(g) for g in got])
+                        assert np.all(whole | none), (field, k, value, reduce, key, got)
+                if ordered:
+                    other = slot_of != k
+                    assert np.array_equal(out["grad"].cpu().numpy()[other], good[reduce]["grad"].cpu().numpy()[other])
+        for ids in (None, _dev(np.arange(plan.R, dtype=np.int32))):
+            out, status = _preference_run(tiles, plan, pp, _dev(lp), _dev(kref), ids, _dev(pair), 0, 0, ws=left[0])
+            assert int(status.item()) != 0
+            got = {key: v.cpu().numpy() for key, v in out.items()}
+            if not ordered:
+                assert got["loss"][0] == 0 and not got["counts"].any()
+                # rows behind the last offset are behind the run
+                assert np.isin(got["row_loss"], (0, -3)).all() and np.isin(got["reward"], (0, -3)).all()
+                continue
+            lost = plan.slot_of_row == k
+            partner = np.abs(pair.astype(np.int64)) - 1
+            unpaired = lost | ((partner >= 0) & lost[partner])
+            want = np.where(unpaired, 0, fair["row_loss"].cpu().numpy())
+            assert np.array_equal(got["row_loss"], want)
+            assert np.array_equal(got["reward"], np.where(lost, 0, fair["reward"].cpu().numpy()))
+            assert got["counts"][0] == ((pair > 0) & ~unpaired).sum()
+            total = want.astype(np.float64).sum()
+            assert abs(got["loss"][0] - total) <= 2 * U * np.abs(want).sum()     # rows rounded once each, and the total
+            at = ~lost[plan.row_of]
+            grad = np.where(unpaired[plan.row_of], 0, fair["grad"].cpu().numpy())
+            assert np.array_equal(got["grad"][at], grad[at])

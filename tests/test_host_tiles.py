@@ -17,3 +17,13 @@ def test_chunk_walk_stays_inside_the_arrays(tmp_path):
     assert r.returncode == 0, r.stderr
     r = subprocess.run([exe], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0, (r.returncode, r.stdout)
+
+
+def test_sound_slots_are_met_whole_unless_offsets_are_out_of_order(tmp_path):
+    exe = str(tmp_path / "tile_order")
+    r = subprocess.run([build.HIPCC, "--offload-host-only", "-O1", "-std=c++17", "-Wall", "-Werror", "-I", build.CSRC,
+                        "-I", build.INCLUDE, "-x", "hip", os.path.join(HERE, "host", "tile_order.cpp"), "-o", exe],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0, (r.returncode, r.stdout)
