@@ -141,14 +141,14 @@ int check_loss_workspace(const LossLayout& L, const void* d_ws, size_t ws_bytes)
 int64_t check_blocks(int64_t K) { return std::min((K + kBlock - 1) / kBlock, (int64_t)kCheckBlocks); }
 
 // ------------------------------------------------------------------ shared by the passes
-// The first `blocks` blocks of a pass look over the run's slots: f(k, slot) for every one, called by whole waves
-// (`real`: the lane has a slot).  A wave of them leaves a word: is one of its slots not ordered?  Then the passes'
-// partials mean nothing, and who takes the sums has them as 0.
+// Blocks of the first pass behind those of the chunks look over the run's slots, beside them (in front of a
+// chunk the look took 0.3 us of a call): f(real, slot) for every one, called by whole waves (`real`: the lane has
+// a slot).  A wave of them leaves a word: is one of its slots not ordered?  Then the passes' partials mean
+// nothing, and who takes the sums has them as 0.
 template <typename F>
-__device__ __forceinline__ void check_slots(const odb_tiles_t& t, int64_t e_base, int64_t r_base, uint32_t* disorder,
-                                            int64_t blocks, const F& f) {
-    const int64_t b = blockIdx.x;
-    if (b >= blocks) return;
+__device__ __forceinline__ void check_slots(const odb_tiles_t& t, int64_t b, uint32_t* disorder, int64_t blocks,
+                                            const F& f) {
+    const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     uint32_t found = 0;
     for (int64_t first = b * kBlock + wave * kWave; first < t.num_slots; first += blocks * kBlock) {   // uniform
@@ -161,6 +161,10 @@ __device__ __forceinline__ void check_slots(const odb_tiles_t& t, int64_t e_base
     found = __any(found);
     if (lane == 0) disorder[b * kWaves + wave] = found;
 }
+
+struct NoVisit {
+    __device__ __forceinline__ void operator()(bool, const SlotView&) const {}
+};
 
 // Whether one of those words is set; every lane of the wave must be active.
 __device__ __forceinline__ bool slots_disordered(const uint32_t* disorder, int64_t blocks) {
@@ -345,8 +349,8 @@ __global__ void __launch_bounds__(kBlock) policy_count_kernel(PolicyArgs A) {
     __shared__ alignas(16) uint8_t s_nibble[kMaxChunk / 4];
     __shared__ int s_rows[ROWS ? kLdsRows : 1];
     const odb_tiles_t& t = A.t;
+    if (blockIdx.x >= A.chunks) return check_slots(t, blockIdx.x - A.chunks, A.disorder, A.check_blocks, NoVisit{});
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
-    check_slots(t, e_base, r_base, A.disorder, A.check_blocks, [](bool, const SlotView&) {});
     const int64_t total = run_elems(t, e_base);
     const int64_t b = blockIdx.x, c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
     if (c0 >= c1) return;
@@ -744,8 +748,9 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
     __shared__ double s_weight[ROWS ? kLdsRows : 1];
     __shared__ uint32_t s_bits[LABELS ? 1 : kMaxChunk / 32];
     const odb_tiles_t& t = A.t;
+    if (LABELS && blockIdx.x >= A.chunks)
+        return check_slots(t, blockIdx.x - A.chunks, A.disorder, A.check_blocks, NoVisit{});
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
-    if (LABELS) check_slots(t, e_base, r_base, A.disorder, A.check_blocks, [](bool, const SlotView&) {});
     const int64_t total = run_elems(t, e_base);
     const int64_t b = blockIdx.x, c0 = b * A.chunk, c1 = c0 + A.chunk < total ? c0 + A.chunk : total;
     if (c0 >= c1) return;
@@ -1131,9 +1136,8 @@ __device__ __forceinline__ void row_sums(const PairArgs& A, uint32_t* s_bits) {
 }
 
 // What the pass leaves of the slots.
-__device__ __forceinline__ void check_rows(const PairArgs& A) {
-    const int64_t e_base = A.t.d_slot_tile_off[0], r_base = A.t.d_slot_row_off[0];
-    check_slots(A.t, e_base, r_base, A.disorder, A.check_blocks, [&](bool real, const SlotView& s) {
+__device__ __forceinline__ void check_rows(const PairArgs& A, int64_t b) {
+    check_slots(A.t, b, A.disorder, A.check_blocks, [&](bool real, const SlotView& s) {
         if (real && !s.ok && A.status) *A.status = kErrTiles;
         // rows that the walk passes over
         for (uint64_t bad = __ballot(real && !s.ok && s.ordered); bad; bad &= bad - 1) {
@@ -1148,7 +1152,7 @@ __device__ __forceinline__ void check_rows(const PairArgs& A) {
 template <bool REF>
 __global__ void __launch_bounds__(kBlock) row_sums_kernel(PairArgs A) {
     __shared__ uint32_t s_bits[kMaxChunk / 32];
-    check_rows(A);
+    if (blockIdx.x >= A.chunks) check_rows(A, blockIdx.x - A.chunks);
     row_sums<REF>(A, s_bits);
 }
 
@@ -1419,7 +1423,7 @@ __global__ void __launch_bounds__(kBlock) pairs_one_kernel(PairArgs A) {
         __threadfence();     // before the atomics on the same entries
         __syncthreads();
     }
-    check_rows(A);
+    check_rows(A, 0);
     row_sums<REF>(A, s_bits);
     __syncthreads();
     const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
@@ -1524,8 +1528,8 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     a.high = (float)(1.0 + p->clip_high);
     a.dual = (float)p->dual_clip;
     a.token_advantage = p->token_advantage;
-    // at most 2^23 blocks; in the first pass those behind the chunks only look over slots
-    const dim3 grid((unsigned)L.chunks), first((unsigned)std::max(L.chunks, a.check_blocks)), block(kBlock);
+    // at most 2^23 blocks and, in the first pass, those that look over the slots
+    const dim3 grid((unsigned)L.chunks), first((unsigned)(L.chunks + a.check_blocks)), block(kBlock);
     if (t->num_elems <= kOnePolicy && t->num_slots <= kOneSlots) {
         hipLaunchKernelGGL(policy_one_kernels[p->kl], dim3(1), block, 0, s, a, (int)p->reduce);
         ODB_LAUNCHED();
@@ -1624,8 +1628,8 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
         hipLaunchKernelGGL(clear_rows_kernel, dim3(grid_for(parts, 1)), block, 0, s, a);
         ODB_LAUNCHED();
     }
-    // at most 2^23 blocks; those behind the chunks only look over the slots
-    const dim3 sums((unsigned)std::max(L.chunks, a.check_blocks));
+    // at most 2^23 blocks and those that look over the slots
+    const dim3 sums((unsigned)(L.chunks + a.check_blocks));
     hipLaunchKernelGGL(d_ref_logprob ? row_sums_kernel<true> : row_sums_kernel<false>, sums, block, 0, s, a);
     ODB_LAUNCHED();
     // without gradients the first block is all that the last kernel has to do
