@@ -7,9 +7,8 @@ import math
 import numpy as np
 import pytest
 
-import _losses as ref
-from _losses import U, Plan
-from test_gpu_losses import _pad, _policy_params, _policy_run, _preference_run, _tiles, _torch
+from _losses import IGNORE, U, Plan
+from test_gpu_losses import _policy_params, _policy_run, _preference_run, _tiles, _torch
 
 pytestmark = pytest.mark.gpu
 
@@ -265,3 +264,54 @@ def test_slots_that_contradict_each_other(name):
             at = ~lost[plan.row_of]
             grad = np.where(unpaired[plan.row_of], 0, fair["grad"].cpu().numpy())
             assert np.array_equal(got["grad"][at], grad[at])
+
+
+# ------------------------------------------------------------------------- slots of many chunks
+@pytest.mark.parametrize("reduce", range(3))
+def test_one_slot_of_very_many_chunks(reduce):
+    """2^28 elements in one slot: their numbers, in a time near that of as many in 256 slots (what each chunk
+    adds up must not grow with its slot)."""
+    import paper_2606_19989_amd as odb
+    torch = _torch()
+    E, L = 1 << 28, 512
+    i32, i64 = dict(dtype=torch.int32, device="cuda"), dict(dtype=torch.int64, device="cuda")
+    gen = torch.Generator("cuda").manual_seed(5)
+    y = torch.randint(-130, 200, (E,), generator=gen, **i32).clamp_(min=IGNORE)       # 1 in 11 does not count
+    y.view(-1, L)[::5] = IGNORE                                                        # rows in which nothing does
+    lp = torch.rand(E, generator=gen, device="cuda") - 1
+    grad = torch.empty(E, device="cuda")
+    adv = torch.randn(E // L, generator=gen, device="cuda")
+    on = (y != IGNORE).view(-1, L)
+    on[:, 0] = False
+    count = on.sum(1)
+    took = {}
+    for K in (256, 1):
+        rows = E // L // K
+        tiles = odb.Tiles(torch.full((K,), rows, **i32), torch.full((K,), L, **i32), torch.arange(K + 1, **i64) * rows,
+                          torch.arange(K + 1, **i64) * rows * L, y, E // L)
+        ws = torch.full((odb.odb_loss_workspace_size(tiles),), 0x7f, dtype=torch.uint8, device="cuda")
+        loss, means, counts = torch.empty(K, device="cuda"), torch.empty(K, 4, device="cuda"), torch.empty(K, 4, **i64)
+        call = lambda: odb.odb_policy_loss(tiles, odb.PolicyParams(reduce=reduce), lp, adv, loss, means, counts, ws,
+                                           grad_logprob=grad)
+        call()
+        n = count.view(K, rows).sum(1)
+        real = (count > 0).view(K, rows).sum(1)
+        w = {0: 1.0 / n.double()[:, None].expand(K, rows), 2: torch.ones(K, rows, device="cuda").double(),
+             1: 1.0 / (count.clamp(min=1).double().view(K, rows) * real[:, None])}[reduce]
+        terms = -adv.double().view(K, rows) * w * count.view(K, rows)
+        want, mag = terms.sum(1), terms.abs().sum(1)
+        assert torch.equal(counts[:, 0], n)
+        assert torch.all((loss.double() - want).abs() <= U * want.abs() + 1e-12 * mag)
+        g = (-adv.double() * w.reshape(-1))                 # two roundings: the factor, the product
+        assert torch.all((grad.view(-1, L)[:, 7].double() - g * on[:, 7]).abs() <= 2.01 * U * g.abs())
+        assert torch.all(grad.view(-1, L)[~on] == 0)
+        times = []
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            call()
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        took[K] = min(times)
+    assert took[1] < 2 * took[256], took        # 1.3; with a sum per chunk over its whole slot 4 to 6
