@@ -477,7 +477,8 @@ def _array(t, dtype, least: int, name: str, current: int):
 def _tile_array(t, dtype, x, name: str, current: int, each: int = 1):
     """The same for an array parallel to the tile of the logits: flat, or of the tile's shape."""
     n = x.rows * x.cols * each
-    if t is not None and t.numel() != n and t.dim() > 1:
+    # the first size tells [cols, rows] apart; [1, rows, cols] and [rows * cols, each] are as flat
+    if t is not None and t.dim() > 1 and (t.numel() != n or t.size(0) not in (x.rows, 1, x.rows * x.cols)):
         raise ValueError(f"{name}: shape {tuple(t.shape)} beside a tile of {x.rows} x {x.cols}")
     return _array(t, dtype, n, name, current)
 

@@ -157,6 +157,24 @@ def test_binding_refuses_host_tensors():
         odb.Tiles(torch.zeros(1, **i32), torch.zeros(1, **i32), torch.zeros(2, **i64), torch.zeros(2, **i64), y, 1)
 
 
+def test_binding_refuses_arrays_of_a_transposed_tile():
+    import types
+
+    import torch
+
+    tile, f32 = types.SimpleNamespace(rows=4, cols=9), torch.float32
+    array = lambda *shape, each=1: odb._tile_array(torch.zeros(*shape), f32, tile, "stats", -1, each)   # -1: the host
+    for shape in ((9, 4), (2, 18), (9, 4, 1), (5, 9)):
+        with pytest.raises(ValueError, match="stats"):
+            array(*shape)
+    with pytest.raises(ValueError, match="stats"):
+        array(9, 4, 2, each=2)
+    for shape in ((4, 9), (36,), (40,), (1, 36), (36, 1), (4, 9, 1), (4, 3, 3), (1, 4, 9)):
+        assert array(*shape)
+    for shape in ((4, 9, 2), (36, 2), (72,), (1, 72)):
+        assert array(*shape, each=2)
+
+
 # ------------------------------------------------------------ the references themselves
 def _difference(f, x, at, eps):
     up, down = x.copy(), x.copy()
