@@ -646,6 +646,8 @@ class _PlanLosses:
             if self.outputs is None:
                 raise ValueError("collate first, or pass labels")
             labels = self.outputs[1]
+        if not labels.is_contiguous():
+            raise ValueError("labels: expected a contiguous tensor")
         if labels.numel() < e[1]:
             raise ValueError(f"labels: {labels.numel()} elements, the plan's tiles have {int(self.info['padded_elems'])}")
         return Tiles(self.slot_rows[a:b], self.slot_maxlen[a:b], self.slot_row_off[a:b + 1],

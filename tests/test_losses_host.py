@@ -175,6 +175,17 @@ def test_binding_refuses_arrays_of_a_transposed_tile():
         assert array(*shape, each=2)
 
 
+def test_tiles_of_a_plan_refuse_labels_with_strides():
+    import torch
+
+    plan = odb._PlanLosses()
+    plan.torch, plan.outputs, plan.num_slots = torch, None, 2
+    plan.info = {"emitted_samples": 3, "padded_elems": 20}
+    # a copy of them would be made on the current stream and not on the loss's
+    with pytest.raises(ValueError, match="contiguous"):
+        plan.tiles(torch.zeros(5, 8, dtype=torch.int32)[:, ::2])
+
+
 # ------------------------------------------------------------ the references themselves
 def _difference(f, x, at, eps):
     up, down = x.copy(), x.copy()
