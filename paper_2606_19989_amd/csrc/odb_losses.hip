@@ -147,10 +147,10 @@ int check_loss_workspace(const LossLayout& L, const void* d_ws, size_t ws_bytes)
 int64_t check_blocks(int64_t K) { return std::min((K + kBlock - 1) / kBlock, (int64_t)kCheckBlocks); }
 
 // ------------------------------------------------------------------ shared by the passes
-// Blocks of the first pass behind those of the chunks look over the run's slots, beside them (in front of a
-// chunk the look took 0.3 us of a call): f(real, slot) for every one, called by whole waves (`real`: the lane has
-// a slot).  A wave of them leaves a word: is one of its slots not ordered?  Then the passes' partials mean
-// nothing, and who takes the sums has them as 0.
+// Block b of `blocks` looks over its part of the run's slots: f(real, slot) for every one, called by whole waves
+// (`real`: the lane has a slot).  A wave leaves a word: is one of its slots not ordered?  Then the passes' partials
+// mean nothing, and who takes the sums has them as 0.  Blocks of the first pass behind those of the chunks do it,
+// beside them (in front of a chunk it took 0.3 us of a call).
 template <typename F>
 __device__ __forceinline__ void check_slots(const odb_tiles_t& t, int64_t b, uint32_t* disorder, int64_t blocks,
                                             const F& f) {
@@ -1157,24 +1157,26 @@ __device__ __forceinline__ void row_sums(const PairArgs& A, uint32_t* s_bits) {
     for (int i = threadIdx.x; i < words; i += kBlock) A.bits[b * words + i] = s_bits[i];
 }
 
-// What the pass leaves of the slots.
-__device__ __forceinline__ void check_rows(const PairArgs& A, int64_t b) {
-    check_slots(A.t, b, A.disorder, A.check_blocks, [&](bool real, const SlotView& s) {
+// What a wave leaves of its lanes' slots: the status and the rows that the walk passes over.
+struct MarkRows {
+    const PairArgs& A;
+
+    __device__ __forceinline__ void operator()(bool real, const SlotView& s) const {
         if (real && !s.ok && A.status) *A.status = kErrTiles;
-        // rows that the walk passes over
         for (uint64_t bad = __ballot(real && !s.ok && s.ordered); bad; bad &= bad - 1) {
             const int of = __builtin_ctzll(bad);
             const int64_t row1 = __shfl(s.row1, of, kWave);
             for (int64_t i = __shfl(s.row0, of, kWave) + (threadIdx.x & (kWave - 1)); i < row1; i += kWave)
                 A.row_info[i] = RowInfo{};
         }
-    });
-}
+    }
+};
 
 template <bool REF>
 __global__ void __launch_bounds__(kBlock) row_sums_kernel(PairArgs A) {
     __shared__ uint32_t s_bits[kMaxChunk / 32];
-    if (blockIdx.x >= A.chunks) check_rows(A, blockIdx.x - A.chunks);
+    if (blockIdx.x >= A.chunks)
+        check_slots(A.t, blockIdx.x - A.chunks, A.disorder, A.check_blocks, MarkRows{A});
     row_sums<REF>(A, s_bits);
 }
 
@@ -1440,16 +1442,18 @@ __global__ void no_pairs_kernel(PairArgs A) {
 template <bool REF>
 __global__ void __launch_bounds__(kBlock) pairs_one_kernel(PairArgs A) {
     __shared__ uint32_t s_bits[kMinChunk / 32];
+    __shared__ uint32_t s_disorder[kWaves];
     if (A.row_of) {
         clear_rows(A);
         __threadfence();     // before the atomics on the same entries
         __syncthreads();
     }
-    check_rows(A, 0);
     row_sums<REF>(A, s_bits);
+    // behind the sums, which have the slots at hand
+    check_slots(A.t, 0, s_disorder, 1, MarkRows{A});
     __syncthreads();
+    const bool disordered = s_disorder[0] | s_disorder[1] | s_disorder[2] | s_disorder[3];
     const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
-    const bool disordered = slots_disordered(A.disorder, A.check_blocks);
     PairSums sums;
     for (int64_t first = 0; first < rows; first += kBlock) {     // uniform
         const int64_t row = first + threadIdx.x;
@@ -1646,7 +1650,6 @@ extern "C" int odb_preference_loss(const odb_tiles_t* t, const odb_preference_pa
         return ODB_OK;
     }
     if (t->num_elems <= kOnePairs && t->num_slots <= kOneSlots) {
-        a.check_blocks = 1;
         hipLaunchKernelGGL(d_ref_logprob ? pairs_one_kernel<true> : pairs_one_kernel<false>, dim3(1), block, 0, s, a);
         ODB_LAUNCHED();
         return ODB_OK;
