@@ -41,9 +41,10 @@ constexpr float kLn2 = 0.69314718055994530942f;
 typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef int int4u __attribute__((ext_vector_type(4), aligned(4)));
 
-// Chunks of a run from which on a launch of its own adds up what the chunks counted of every slot; below, each
-// block does for the slots it meets.  A slot of C chunks is added up C times then: 2^28 elements in one slot took
-// 3.0 ms and 2^30 42.5 (mean over tokens), with the launch 0.97 and 4.0; in slots of 2^20 0.74 and 2.9.
+// Chunks of a run from which on a launch of its own folds what the chunks counted of a slot into its first 64
+// chunks' counts, which is all that each block adds up then.  Without it a slot of C chunks is added up C times:
+// 2^28 elements in one slot took 3.0 ms and 2^30 42.5 (mean over tokens), with it 0.98 and 4.0; in slots of 2^20
+// 0.75 and 3.0.
 constexpr int64_t kManyChunks = 1 << 15;
 constexpr int kCheckBlocks = 256;   // blocks of a pass that look over the slots, at most
 
@@ -69,8 +70,7 @@ struct PairPart {
 };
 
 struct LossLayout {
-    size_t bits, chunk_slot, slot_count, slot_whole, slot_part, row_sum, row_count, row_info, coef, pair_part, disorder,
-        row_of;
+    size_t bits, chunk_slot, slot_count, slot_part, row_sum, row_count, row_info, coef, pair_part, disorder, row_of;
     size_t total;
     int64_t chunks;
     int32_t chunk;
@@ -121,7 +121,6 @@ LossLayout loss_layout(const odb_tiles_t* t, int64_t num_ids) {
     L.bits = take(L.chunks * (L.chunk / 8));
     L.chunk_slot = take(4 * L.chunks);
     L.slot_count = take(4 * (L.chunks + K));
-    L.slot_whole = take(L.chunks >= kManyChunks ? 8 * K : 0);
     L.slot_part = take((int64_t)sizeof(SlotPart) * (L.chunks + K));
     L.row_sum = take(8 * (kWaves * L.chunks + R));
     L.row_count = take(4 * (kWaves * L.chunks + R));
@@ -313,12 +312,12 @@ struct PolicyArgs {
     uint32_t* bits;
     int32_t* chunk_slot;        // first slot of every chunk, left by the first pass
     int32_t* slot_count;        // counted tokens (token mean) or complete rows with any (row mean)
-    double* slot_whole;         // of all the slot's chunks, for runs of many; else NULL
     SlotPart* slot_part;
     int32_t* row_count;
     uint32_t* disorder;
     int32_t* status;
     int64_t chunks, check_blocks;
+    int64_t counts;                     // chunks from a slot's first on that hold what all of them counted
     double at_low, at_high, at_dual;    // ln(1 - e_l), ln(1 + e_h), ln c
     double kl_coef, entropy_coef, loss_scale;
     float low, high, dual;              // 1 - e_l, 1 + e_h, c
@@ -734,36 +733,53 @@ __device__ __forceinline__ bool row_counts(const PolicyArgs& A, const SlotView& 
     return false;
 }
 
-// A slot's tokens, or (ROWS) rows with a token, that count: those of its chunks from `first` on, every `step`th;
-// a whole number that may pass 2^31.
+// What chunk j counted of a slot: tokens, or (ROWS) whole rows with any and the row that starts in it and goes on.
 template <bool ROWS>
-__device__ __forceinline__ double slot_counted(const PolicyArgs& A, const SlotView& s, int64_t k, int first, int step) {
-    double n = 0;
-    for (int64_t j = (s.lo >> A.chunk_log2) + first; j <= (s.hi - 1) >> A.chunk_log2; j += step) {
-        int c = A.slot_count[j + k];
-        if (ROWS) {
-            // whole rows of the chunk, and the one that starts in it and goes on
-            const int64_t end = (j + 1) * A.chunk;
-            if (end < s.hi && (end - s.lo) % s.maxlen) {
-                const int64_t row = (end - s.lo) / s.maxlen;
-                if (s.lo + row * s.maxlen >= j * A.chunk) c += row_counts(A, s, row);
-            }
+__device__ __forceinline__ int chunk_counted(const PolicyArgs& A, const SlotView& s, int64_t k, int64_t j) {
+    int n = A.slot_count[j + k];
+    if (ROWS) {
+        const int64_t end = (j + 1) * A.chunk;
+        if (end < s.hi && (end - s.lo) % s.maxlen) {
+            const int64_t row = (end - s.lo) / s.maxlen;
+            if (s.lo + row * s.maxlen >= j * A.chunk) n += row_counts(A, s, row);
         }
-        n += c;
     }
     return n;
 }
 
-// The same of every slot, a block a slot.
+// A slot's count from its chunks', one a lane, on every lane: a whole number that may pass 2^31.
 template <bool ROWS>
-__global__ void __launch_bounds__(kBlock) policy_whole_kernel(PolicyArgs A) {
+__device__ __forceinline__ double slot_counted(const PolicyArgs& A, const SlotView& s, int64_t k) {
+    const int64_t first = s.lo >> A.chunk_log2, end = ((s.hi - 1) >> A.chunk_log2) + 1;
+    const int64_t stop = end < first + A.counts ? end : first + A.counts;
+    const bool folded = A.counts == kWave;
+    double n = 0;
+    for (int64_t j = first + (threadIdx.x & (kWave - 1)); j < stop; j += kWave)
+        n += ROWS && !folded ? chunk_counted<true>(A, s, k, j) : A.slot_count[j + k];
+    return wave_total(n);
+}
+
+// Folds the counts of slots of more than 64 chunks, a block a slot: at most 2^17 chunks into one, 2^30 tokens.
+template <bool ROWS>
+__global__ void __launch_bounds__(kBlock) policy_fold_kernel(PolicyArgs A) {
+    __shared__ int s_count[kBlock];
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     for (int64_t k = blockIdx.x; k < t.num_slots; k += gridDim.x) {
         const SlotView s = slot_view(t, k, e_base, r_base);
         if (!s.ok || s.hi == s.lo) continue;     // uniform
-        const double n = block_total(slot_counted<ROWS>(A, s, k, (int)threadIdx.x, kBlock));
-        if (threadIdx.x == 0) A.slot_whole[k] = n;
+        const int64_t first = s.lo >> A.chunk_log2, last = (s.hi - 1) >> A.chunk_log2;
+        int n = 0;
+        for (int64_t j = first + threadIdx.x; j <= last; j += kBlock) n += chunk_counted<ROWS>(A, s, k, j);
+        s_count[threadIdx.x] = n;
+        __syncthreads();
+        if (threadIdx.x < kWave && first + threadIdx.x <= last) {
+            n = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) n += s_count[w * kWave + threadIdx.x];
+            A.slot_count[first + threadIdx.x + k] = n;
+        }
+        __syncthreads();
     }
 }
 
@@ -795,8 +811,7 @@ __global__ void __launch_bounds__(kBlock) policy_kernel(PolicyArgs A) {
         const int here = (int)((a1 - 1 - s.lo) / s.maxlen) - p.row_a + 1;
         const bool lds = ROWS && here <= kLdsRows;
         if (!LABELS) {
-            const double n = A.slot_whole ? A.slot_whole[k]
-                                          : wave_total(slot_counted<ROWS>(A, s, k, threadIdx.x & (kWave - 1), kWave));
+            const double n = slot_counted<ROWS>(A, s, k);
             if (ROWS) rows = n;
             else same = n > 0 ? 1.0 / n : 0.0;
         }
@@ -1536,13 +1551,13 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
     a.bits = ws_at<uint32_t>(d_ws, L.bits);
     a.chunk_slot = ws_at<int32_t>(d_ws, L.chunk_slot);
     a.slot_count = ws_at<int32_t>(d_ws, L.slot_count);
-    a.slot_whole = L.chunks >= kManyChunks ? ws_at<double>(d_ws, L.slot_whole) : nullptr;
     a.slot_part = ws_at<SlotPart>(d_ws, L.slot_part);
     a.row_count = ws_at<int32_t>(d_ws, L.row_count);
     a.disorder = ws_at<uint32_t>(d_ws, L.disorder);
     a.status = d_status;
     a.chunks = L.chunks;
     a.check_blocks = L.chunks > 0 ? check_blocks(t->num_slots) : 0;
+    a.counts = L.chunks >= kManyChunks ? kWave : kMaxElems;
     a.chunk = L.chunk;
     a.chunk_log2 = __builtin_ctz((unsigned)L.chunk);
     a.at_low = std::log1p(-p->clip_low);
@@ -1566,8 +1581,8 @@ extern "C" int odb_policy_loss(const odb_tiles_t* t, const odb_policy_params_t* 
         hipLaunchKernelGGL(p->reduce == ODB_REDUCE_ROW_MEAN ? policy_count_kernel<true> : policy_count_kernel<false>,
                            first, block, 0, s, a);
         ODB_LAUNCHED();
-        if (a.slot_whole) {
-            hipLaunchKernelGGL(p->reduce == ODB_REDUCE_ROW_MEAN ? policy_whole_kernel<true> : policy_whole_kernel<false>,
+        if (a.counts == kWave) {
+            hipLaunchKernelGGL(p->reduce == ODB_REDUCE_ROW_MEAN ? policy_fold_kernel<true> : policy_fold_kernel<false>,
                                dim3(grid_for(t->num_slots, 1)), block, 0, s, a);
             ODB_LAUNCHED();
         }
