@@ -528,8 +528,9 @@ typedef struct odb_logits {
  *               backward call takes; ln sum_v exp(a z_v) = a * largest + logsum.  8-byte aligned
  *   d_entropy   [rows * cols] out, or NULL
  *   d_status    [1] device, or NULL: set to a nonzero value if a label lies outside [0, V) and
- *               is not ODB_LABEL_IGNORE (that token does not count); never cleared here, so one
- *               word may collect the errors of many calls
+ *               is not ODB_LABEL_IGNORE (that token does not count here; the losses below, which
+ *               know no vocabulary, count every label but ODB_LABEL_IGNORE and take the 0 written
+ *               for it); never cleared here, so one word may collect the errors of many calls
  *
  * Logits of -inf and of a type's lowest value are masked vocabulary entries.  A token whose
  * logits are all -inf, or hold a NaN or +inf, gets NaN (no distribution); a label at -inf
@@ -577,7 +578,8 @@ typedef struct odb_tiles {
     const int64_t* d_slot_row_off;   /* [K+1]                                                  */
     const int64_t* d_slot_tile_off;  /* [K+1]                                                  */
     const int32_t* d_labels;         /* [num_elems]; a token (i, c) of a tile counts if c >= shift
-                                        and its label is not ODB_LABEL_IGNORE                  */
+                                        and its label is not ODB_LABEL_IGNORE, also one that
+                                        odb_token_logprobs has refused as outside [0, V)       */
     int32_t shift;                   /* as in odb_logits_t: 0 or 1                             */
     int32_t reserved0;               /* must be 0                                              */
 } odb_tiles_t;

@@ -9,10 +9,10 @@
 // Backward: p = exp(a (z - m)) exp(-logsum) needs no second pass, the forward call left both.
 //
 // Bound by the reads of the logits (and the writes of the gradient): 2 or 4 bytes against about
-// ten instructions a logit, of which the exponential is a quarter-rate one.  Measured: 8,176 positions
-// of 151,936 bf16 logits forward in 350 to 375 us (6.4 to 6.8 TB/s of reads), 4,088 of them backward in
+// ten instructions a logit, of which the exponential is a quarter-rate one.  Measured: 7,832 scored positions
+// of 151,936 bf16 logits forward in 350 to 375 us (6.4 to 6.8 TB/s of reads), 3,928 of 4,096 backward in
 // 440 to 450 us (5.5 TB/s, half reads and half writes; a copy reaches 5.0 to 5.2).  One position of 32,000:
-// 5.7 us, the label's load, one round of the logits' and the reduction one after the other.
+// 5.3 us, the label's load, one round of the logits' and the reduction one after the other.
 #include <cmath>
 
 #include "odb_internal.h"
@@ -32,8 +32,8 @@ typedef _Float16 fp16_t;
 // 16 bytes of logits: N values.  Rows of an odd vocabulary start at any element; global memory serves
 // 16-byte accesses at any address.  The forward call makes use of that, so that a row's sums run in the
 // same order wherever it lies.  The gradient is written in the alignment of its own rows: up to N - 1
-// elements one by one, then 16 bytes at a time (2,545 positions of 65,537 bf16 logits: 79 us, 120 us
-// without).
+// elements one by one, then 16 bytes at a time (2,545 positions of 65,537 bf16 logits, replayed in a graph:
+// 79 us, 120 us without).
 typedef unsigned u4a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned u4a4 __attribute__((ext_vector_type(4), aligned(4)));
 template <int ALIGN>
@@ -322,15 +322,24 @@ int check_tile(const odb_logits_t* x, const void* p, int64_t rs, int64_t cs, con
 
 // Threads of a position, by the bytes of its logits.  Too many leave the reduction and the label's load
 // in front of too little work, too few leave loads unissued.  us for about 600 MB of logits (N positions
-// of V), the last two lines for few positions; 2 x 600 MB for the gradient:
+// of V; 2 x 600 MB for the gradient), and in a graph for 32 positions:
 //   bytes of a row     forward 64 / 256 / 512 / 1,024 threads    backward 64 / 256 / 512 / 1,024
 //   4 KB               109 / 246 / 463 / 1320                    198 / 325 / 567 / 1049
 //   16 KB               95 / 122 / 189 /  412                    222 / 201 / 245 / 403
 //   32 KB               98 /  96 / 123 /  267                    219 / 212 / 195 / 284
 //   64 KB              103 /  98 / 110 /  207                    250 / 229 / 207 / 203
 //   128 KB             120 / 101 /  97 /  147                    283 / 263 / 249 / 215
-//   64 KB x 32        14.7 / 8.4 / 7.2 /  7.7                    14.3 / 6.9 / 6.1 / 5.8
-//   304 KB x 1          58 /  19 /  13 /   12                     53 /  17 /  12 /  11
+//   1 KB x 32          3.0 / 3.3 / 3.4 /  4.1                    3.0 / 3.0 / 2.9 / 2.9
+//   4 KB x 32          3.4 / 3.4 / 3.5 /  4.1                    3.4 / 3.0 / 2.9 / 2.9
+//   16 KB x 32         5.7 / 3.8 / 3.9 /  4.7                    5.7 / 3.6 / 3.3 / 3.7
+//   32 KB x 32         9.1 / 4.6 / 4.3 /  5.0                    9.0 / 4.4 / 3.8 / 3.9
+//   48 KB x 32        12.2 / 5.3 / 5.1 /  5.4                   12.0 / 5.1 / 4.7 / 4.3
+//   64 KB x 32        15.7 / 6.1 / 5.4 /  5.9                   15.2 / 6.1 / 5.0 / 4.7
+//   128 KB x 32       26.9 / 9.2 / 7.6 /  7.7                   27.8 / 9.2 / 7.5 / 6.9
+//   304 KB x 32         81 /  23 /  17 /   15                     61 /  18 /  14 /  12
+//   304 KB x 1          56 /  17 /  13 /   12                     55 /  17 /  13 /  12
+// One position's are within 0.6 us of 32's up to 128 KB; 512 positions of up to 8 KB take up to 1.5 us more with
+// 1,024 threads, with fewer 0.5.
 // Rows of 128 bytes, 4.7 M: 1,682 with a wave a row, 245 with 8 threads; of 512 bytes 461 and 106; of
 // 1 KB 240 and 99; of 2 KB 160, and 110 with 32.
 enum Group { kGroup8, kGroup32, kGroup64, kGroup256, kGroup512, kGroup1024 };

@@ -23,10 +23,10 @@ constexpr int kMinChunk = 1024, kMaxChunk = 8192;    // elements of a chunk
 // Runs of few elements go through one launch of one block, whose time grows with each 1,024 elements where
 // the passes' does not.  us in a graph, one block / passes:
 //   elements    policy, token mean   policy, row mean    preference, by id   preference, by row
-//   300          7.1 / 11.3           7.5 / 12.5         10.7 / 11.7          8.9 / 9.8
-//   1,000        7.3 / 11.2           7.6 / 13.1         11.7 / 11.6         12.5 / 9.8
-//   2,000        9.3 / 12.1           9.9 / 14.6         12.5 / 11.5         13.2 / 10.0
-//   4,000       13.2 / 12.3          14.2 / 14.7         13.4 / 11.7         14.0 / 10.4
+//   300          6.9 / 11.3           7.1 / 13.0         11.3 / 12.2          9.7 / 9.9
+//   1,000        7.5 / 11.6           7.7 / 13.3         15.1 / 12.5         13.3 / 10.0
+//   2,000        9.7 / 12.3          10.1 / 14.2         15.7 / 13.0         13.9 / 10.6
+//   4,000       13.7 / 12.3          14.5 / 14.7         16.3 / 13.1         14.6 / 10.6
 // With 1,024 threads: 12.6 / 13.0 (policy) at 4,000 elements, but 16.5 at 8,192, where the passes take 12.6.
 constexpr int kOnePolicy = 4096;
 constexpr int kOnePairs = 512;
@@ -81,14 +81,14 @@ constexpr int64_t kMaxElems = (int64_t)1 << 36;    // 2^23 chunks: a grid's thre
 // Elements of a chunk, a power of two: as many chunks as keep the chip busy (it holds 2,048 blocks of 256
 // threads), but not more, since each costs a search for its first slot and a reduction.  us of a whole call
 // with chunks of 1,024 / 2,048 / 4,096 / 8,192 / 16,384, tiles of up to 32,768 tokens:
-//   elements    policy, mean over tokens      preference, rows of about 480
-//   2^17         13 /  13 /  16 /  21 /  32    15 /  16 /  17 /  20 /  25
-//   2^20         25 /  22 /  23 /  28 /  44    25 /  23 /  25 /  33 /  38
-//   2^21         39 /  30 /  29 /  35 /  48    36 /  28 /  30 /  41 /  45
-//   2^22         57 /  45 /  38 /  41 /  53    51 /  39 /  40 /  50 /  54
-//   2^23         93 /  67 /  56 /  53 /  63    79 /  57 /  53 /  53 /  61
-//   2^25        310 / 208 / 155 / 138 / 145   244 / 158 / 130 / 127 / 131
-//   2^28       2469 /1538 /1049 / 918 / 968  2007 /1294 /1076 / 979 / 984
+//   elements    policy, mean over tokens      preference by row, rows of about 480
+//   2^17         18 /  19 /  21 /  28 /  38    16 /  16 /  18 /  23 /  32
+//   2^20         25 /  23 /  24 /  29 /  40    21 /  20 /  21 /  25 /  36
+//   2^21         39 /  32 /  30 /  36 /  50    32 /  26 /  27 /  31 /  41
+//   2^22         60 /  47 /  40 /  42 /  55    46 /  36 /  32 /  37 /  49
+//   2^23         99 /  72 /  59 /  54 /  63    75 /  52 /  46 /  48 /  58
+//   2^25        317 / 220 / 162 / 150 / 150   244 / 154 / 123 / 117 / 124
+//   2^28       2527 /1598 /1102 / 946 / 957  2027 /1274 /1036 / 934 / 941
 int32_t chunk_for(int64_t elems) {
     int32_t chunk = kMinChunk;
     while (chunk < kMaxChunk && elems >= chunk * (int64_t)2048) chunk *= 2;
@@ -242,8 +242,8 @@ __device__ __forceinline__ T block_total(T v) {
 // `last`, holds any of its values.  SAFE, for where a group may end behind it: each value is read on its own,
 // the last one for those behind.  Otherwise a position past `last` reads that one.  Either way there is no
 // branch, so that loads of many groups go out together.
-// What is read here is read once: past the caches' usual order, 67 M elements in 2,080 tiles take 266 us
-// instead of 280 (policy) and 246 instead of 300 (preference).
+// What is read here is read once: past the caches' usual order, 67 M elements in 2,080 tiles take 260 us
+// instead of 268 (policy) and 222 instead of 283 (preference).
 template <typename V4, bool SAFE, typename T>
 __device__ __forceinline__ V4 load4(const T* p, int o, int last) {
     if (SAFE) {
@@ -330,8 +330,8 @@ constexpr int kAhead = 4;
 
 // Rows of a chunk that one block weighs in LDS; those of fewer elements than 8 may be more, and are weighed where
 // they are met.  us a call for room for 512 / 1,024 / 4,096, which leaves fewer blocks on a compute unit (mean
-// over rows, 67 M elements in rows of about 480): 330 / 330 / 351; 34 M in rows of 40: 204 / 198 / 213, of 5:
-// 250 / 234 / 242; one tile of 1,000,000 x 3: 71 / 68 / 67.
+// over rows, 67 M elements in rows of about 480): 319 / 319 / 344; 34 M in rows of 40: 208 / 204 / 214, of 5:
+// 262 / 239 / 248; one tile of 1,000,000 x 3: 71 / 70 / 68.
 constexpr int kLdsRows = 1024;
 
 // Adds a group's counted elements to its rows, the first of them `row0`.
@@ -703,7 +703,7 @@ struct RowChunks {
 };
 
 // Chunks of a row from which on the wave counts it, and not a lane: with a lane alone the mean over two rows of
-// 131,072 tokens took 39 us, 17 now; with the wave for all of them rows of 480 in one tile take 15.8, not 14.7.
+// 131,072 tokens takes 26 us, not 17.5; with the wave for all of them rows of 480 in one tile take 15.5, not 14.6.
 constexpr int kLongRow = 8;
 
 // Counted tokens of a row, over the chunks it touches, by a lane.
@@ -785,7 +785,7 @@ __global__ void __launch_bounds__(kBlock) policy_fold_kernel(PolicyArgs A) {
 
 // The loss and its gradient, the elements that count given by the bits (by the labels for a sum, which
 // needs no weights and so no pass before).  67 M elements in 2,080 tiles, the exponential KL term, 3/4 of them
-// counted: 193 us for 600 MB read and 270 MB written (4.5 TB/s).  Instructions (about 100 an element, a power
+// counted: 203 us for 603 MB read and 270 MB written (4.3 TB/s).  Instructions (about 100 an element, a power
 // and the KL term's series among them) and memory take about as long; the waves of other chunks hide one
 // behind the other.  A variant of the kernel by KL term, reduction and entropies keeps the rest of the work
 // and its registers out of it.
@@ -1133,7 +1133,7 @@ __device__ __forceinline__ void short_rows(const PairArgs& A, const SlotView& s,
 // First pass: the bits, and per quarter of a chunk and row how many tokens count and the sum over
 // them.  A wave takes a quarter.  Rows of more than 64 elements are summed across the wave as its 256
 // elements at a time come in and are left where they end.  Bound by the reads: 67 M elements of labels and two
-// log-probabilities, rows of about 480 with prompts, 155 us for 821 MB (5.3 TB/s).
+// log-probabilities, rows of about 480 with prompts, 156 us for 821 MB (5.3 TB/s).
 template <bool REF>
 __device__ __forceinline__ void row_sums(const PairArgs& A, uint32_t* s_bits) {
     const odb_tiles_t& t = A.t;
@@ -1415,7 +1415,7 @@ __device__ __forceinline__ void pairs_grad(const PairArgs& A, const double* coef
 }
 
 // Gradients of the tiles; the first block also sums what the pairs left.  Bound by the writes: 67 M elements
-// take 46 us for 269 MB (5.8 TB/s).
+// take 48 us for 269 MB (5.6 TB/s).
 __global__ void __launch_bounds__(kBlock) pairs_grad_kernel(PairArgs A, int64_t parts) {
     __shared__ uint32_t s_bits[kMaxChunk / 32];
     if (blockIdx.x == 0) {
@@ -1432,8 +1432,8 @@ __global__ void __launch_bounds__(kBlock) pairs_grad_kernel(PairArgs A, int64_t 
 
 // Runs of at most kBlock rows and kFewChunks chunks: every block forms the factors of all rows instead of
 // waiting for a kernel that does, and the first one leaves the rows' numbers.  us a call, this / the two
-// kernels: 64 rows of 480 tokens (30 chunks) 9.6 / 11.1, 256 of 1,000 (250) 11.0 / 12.2, 256 of 2,000 (500)
-// 15.2 / 13.9, 256 of 32,768 (1,024) 69 / 38.
+// kernels: 64 rows of 480 tokens (30 chunks) 10.4 / 12.0, 256 of 1,000 (250) 11.2 / 12.7, 256 of 2,000 (500)
+// 14.3 / 14.3, 256 of 32,768 (1,024) 60 / 39.
 constexpr int64_t kFewChunks = 256;
 
 __global__ void __launch_bounds__(kBlock) few_rows_kernel(PairArgs A) {
