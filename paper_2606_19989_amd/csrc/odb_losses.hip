@@ -785,7 +785,7 @@ __global__ void __launch_bounds__(kBlock) policy_fold_kernel(PolicyArgs A) {
 
 // The loss and its gradient, the elements that count given by the bits (by the labels for a sum, which
 // needs no weights and so no pass before).  67 M elements in 2,080 tiles, the exponential KL term, 3/4 of them
-// counted: 203 us for 603 MB read and 270 MB written (4.3 TB/s).  Instructions (about 100 an element, a power
+// counted: 201 us for 603 MB read and 270 MB written (4.3 TB/s).  Instructions (about 100 an element, a power
 // and the KL term's series among them) and memory take about as long; the waves of other chunks hide one
 // behind the other.  A variant of the kernel by KL term, reduction and entropies keeps the rest of the work
 // and its registers out of it.
@@ -1133,7 +1133,7 @@ __device__ __forceinline__ void short_rows(const PairArgs& A, const SlotView& s,
 // First pass: the bits, and per quarter of a chunk and row how many tokens count and the sum over
 // them.  A wave takes a quarter.  Rows of more than 64 elements are summed across the wave as its 256
 // elements at a time come in and are left where they end.  Bound by the reads: 67 M elements of labels and two
-// log-probabilities, rows of about 480 with prompts, 156 us for 821 MB (5.3 TB/s).
+// log-probabilities, rows of about 480 with prompts, 157 us for 821 MB (5.3 TB/s).
 template <bool REF>
 __device__ __forceinline__ void row_sums(const PairArgs& A, uint32_t* s_bits) {
     const odb_tiles_t& t = A.t;
@@ -1415,7 +1415,7 @@ __device__ __forceinline__ void pairs_grad(const PairArgs& A, const double* coef
 }
 
 // Gradients of the tiles; the first block also sums what the pairs left.  Bound by the writes: 67 M elements
-// take 48 us for 269 MB (5.6 TB/s).
+// take 47 us for 269 MB (5.7 TB/s).
 __global__ void __launch_bounds__(kBlock) pairs_grad_kernel(PairArgs A, int64_t parts) {
     __shared__ uint32_t s_bits[kMaxChunk / 32];
     if (blockIdx.x == 0) {
