@@ -171,11 +171,13 @@ struct NoVisit {
     __device__ __forceinline__ void operator()(bool, const SlotView&) const {}
 };
 
-// Whether one of those words is set; every lane of the wave must be active.
-__device__ __forceinline__ bool slots_disordered(const uint32_t* disorder, int64_t blocks) {
-    uint32_t found = 0;
-    for (int64_t i = threadIdx.x & (kWave - 1); i < blocks * kWaves; i += kWave) found |= disorder[i];
-    return __any(found);
+// A lane's part of those words, of which one that is set is asked for with __any: late, when other loads have
+// been waited for as well.
+__device__ __forceinline__ uint32_t disorder_words(const uint32_t* disorder, int64_t blocks) {
+    const int lane = threadIdx.x & (kWave - 1), words = (int)blocks * kWaves;
+    uint32_t found = lane < words ? disorder[lane] : 0;
+    for (int i = lane + kWave; i < words; i += kWave) found |= disorder[i];    // more than 4,096 slots
+    return found;
 }
 
 // Last slot from `from` on that starts at or before element e, 64 probes a step (one a lane; every lane of
@@ -935,7 +937,7 @@ __global__ void __launch_bounds__(kBlock) policy_slots_kernel(PolicyArgs A) {
     const odb_tiles_t& t = A.t;
     const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
     const int lane = threadIdx.x & (kWave - 1);
-    const bool disordered = slots_disordered(A.disorder, A.check_blocks);
+    const uint32_t disorder = disorder_words(A.disorder, A.check_blocks);
     for (int64_t k = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); k < t.num_slots;
          k += (int64_t)gridDim.x * kWaves) {
         const SlotView s = slot_view(t, k, e_base, r_base);
@@ -943,7 +945,7 @@ __global__ void __launch_bounds__(kBlock) policy_slots_kernel(PolicyArgs A) {
         double n = 0, clipped[3] = {0, 0, 0};     // whole numbers below 2^41
         if (!s.ok) {
             if (A.status && lane == 0) *A.status = kErrTiles;
-        } else if (s.hi > s.lo && !disordered) {
+        } else if (s.hi > s.lo) {
             for (int64_t j = (s.lo >> A.chunk_log2) + lane; j <= (s.hi - 1) >> A.chunk_log2; j += kWave) {
                 const SlotPart p = A.slot_part[j + k];
 #pragma unroll
@@ -958,6 +960,7 @@ __global__ void __launch_bounds__(kBlock) policy_slots_kernel(PolicyArgs A) {
 #pragma unroll
         for (int i = 0; i < 3; ++i) clipped[i] = wave_total(clipped[i]);
         n = wave_total(n);
+        if (__any(disorder)) n = sum[0] = sum[1] = sum[2] = sum[3] = clipped[0] = clipped[1] = clipped[2] = 0.0;
         if (lane == 0) {
             const int64_t c[3] = {(int64_t)clipped[0], (int64_t)clipped[1], (int64_t)clipped[2]};
             leave_slot(A, k, sum, (int64_t)n, c);
@@ -1297,10 +1300,11 @@ struct PairSums {
 };
 
 // Of a lane's row, if it is below `rows`: its loss (at the chosen row of a pair) and reward, if `out`, and the
-// factor of its tokens' gradients; all 0 if slots are out of order.  Every lane of the wave must be active.
-__device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64_t rows, bool disordered, bool out,
+// factor of its tokens' gradients; all 0 if slots are out of order (a word of `disorder` is set: the records may
+// hold anything).  Every lane of the wave must be active.
+__device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64_t rows, uint32_t disorder, bool out,
                                            PairSums* sums) {
-    const bool live = row < rows && !disordered;
+    const bool live = row < rows;
     RowInfo mine{}, its{};
     bool chosen = false;
     int64_t j = -1;
@@ -1315,8 +1319,10 @@ __device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64
             if (A.row_ids[j] != (v < 0 ? -v : v) - 1) j = -1;
         }
     }
+    const bool sound = !__any(disorder);
+    if (!sound) j = -1;
     int n, m;
-    const double S = log_ratio(A, row, mine, live, &n), T = log_ratio(A, j, its, j >= 0, &m);
+    const double S = log_ratio(A, row, mine, live && sound, &n), T = log_ratio(A, j, its, j >= 0, &m);
     double c = 0.0, loss = 0.0;
     if (j >= 0) {
         const double h = A.beta * (chosen ? S - T : T - S) - A.margin;
@@ -1345,7 +1351,7 @@ __device__ __forceinline__ double pair_row(const PairArgs& A, int64_t row, int64
         sums->pairs += chosen;
         sums->right += chosen && S > T;
     }
-    if (out && row < rows) {
+    if (out && live) {
         A.row_loss[row] = (float)loss;
         A.row_reward[row] = (float)(A.beta * S);
     }
@@ -1359,7 +1365,7 @@ __global__ void __launch_bounds__(kBlock) pairs_kernel(PairArgs A) {
     const int64_t rows = run_rows(t, t.d_slot_row_off[0]);
     const int64_t row = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     PairSums sums;
-    const double c = pair_row(A, row, rows, slots_disordered(A.disorder, A.check_blocks), true, &sums);
+    const double c = pair_row(A, row, rows, disorder_words(A.disorder, A.check_blocks), true, &sums);
     if (row < rows) A.coef[row] = c;
     PairPart p;
     p.loss = block_total(sums.loss);
@@ -1441,7 +1447,7 @@ __global__ void __launch_bounds__(kBlock) few_rows_kernel(PairArgs A) {
     __shared__ uint32_t s_bits[kMaxChunk / 32];
     const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
     PairSums sums;
-    s_coef[threadIdx.x] = pair_row(A, threadIdx.x, rows, slots_disordered(A.disorder, A.check_blocks), blockIdx.x == 0,
+    s_coef[threadIdx.x] = pair_row(A, threadIdx.x, rows, disorder_words(A.disorder, A.check_blocks), blockIdx.x == 0,
                                    &sums);
     if (blockIdx.x == 0) leave_totals(A, sums.loss, sums.pairs, sums.right);
     __syncthreads();
@@ -1467,12 +1473,12 @@ __global__ void __launch_bounds__(kBlock) pairs_one_kernel(PairArgs A) {
     // behind the sums, which have the slots at hand
     check_slots(A.t, 0, s_disorder, 1, MarkRows{A});
     __syncthreads();
-    const bool disordered = s_disorder[0] | s_disorder[1] | s_disorder[2] | s_disorder[3];
+    const uint32_t disorder = s_disorder[0] | s_disorder[1] | s_disorder[2] | s_disorder[3];
     const int64_t rows = run_rows(A.t, A.t.d_slot_row_off[0]);
     PairSums sums;
     for (int64_t first = 0; first < rows; first += kBlock) {     // uniform
         const int64_t row = first + threadIdx.x;
-        const double c = pair_row(A, row, rows, disordered, true, &sums);
+        const double c = pair_row(A, row, rows, disorder, true, &sums);
         if (row < rows) A.coef[row] = c;
     }
     leave_totals(A, sums.loss, sums.pairs, sums.right);
