@@ -476,11 +476,18 @@ def _array(t, dtype, least: int, name: str, current: int):
 
 def _tile_array(t, dtype, x, name: str, current: int, each: int = 1):
     """The same for an array parallel to the tile of the logits: flat, or of the tile's shape."""
-    n = x.rows * x.cols * each
-    # the first size tells [cols, rows] apart; [1, rows, cols] and [rows * cols, each] are as flat
-    if t is not None and t.dim() > 1 and (t.numel() != n or t.size(0) not in (x.rows, 1, x.rows * x.cols)):
-        raise ValueError(f"{name}: shape {tuple(t.shape)} beside a tile of {x.rows} x {x.cols}")
-    return _array(t, dtype, n, name, current)
+    if t is None:
+        return None
+    rows, cols = x.rows, x.cols
+    if t.shape != ((rows, cols) if each == 1 else (rows, cols, each)):    # one comparison where the shape is the tile's
+        n = rows * cols * each
+        # the first size tells [cols, rows] apart; [1, rows, cols] and [rows * cols, each] are as flat
+        if t.dim() > 1 and (t.numel() != n or t.size(0) not in (rows, 1, rows * cols)):
+            raise ValueError(f"{name}: shape {tuple(t.shape)} beside a tile of {rows} x {cols}")
+        return _array(t, dtype, n, name, current)
+    if t.dtype is not dtype or t.get_device() != current or not t.is_contiguous():
+        _refuse(t, dtype, 0, name, current)
+    return t.data_ptr()
 
 
 def _loss_stream(torch, stream, current):
