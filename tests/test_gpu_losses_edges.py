@@ -264,6 +264,15 @@ def test_slots_that_contradict_each_other(name):
             at = ~lost[plan.row_of]
             grad = np.where(unpaired[plan.row_of], 0, fair["grad"].cpu().numpy())
             assert np.array_equal(got["grad"][at], grad[at])
+        # nothing stays behind in the workspace
+        tiles = _tiles(plan, y, 1, 0, 0)
+        for reduce in range(3):
+            out, status = _policy_run(tiles, plan, _policy_params(dict(kl=3, reduce=reduce)), _dev(lp), _dev(old),
+                                      _dev(kref), None, _dev(adv), None, extra=0, ws=left[0])
+            assert int(status.item()) == 0
+            assert all(v is None or torch.equal(v, good[reduce][key]) for key, v in out.items()), (field, k, value)
+        out, status = _preference_run(tiles, plan, pp, _dev(lp), _dev(kref), None, _dev(pair), 0, 0, ws=left[0])
+        assert int(status.item()) == 0 and all(torch.equal(v, fair[key]) for key, v in out.items()), (field, k, value)
 
 
 # ------------------------------------------------------------------------- slots of many chunks
