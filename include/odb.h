@@ -20,6 +20,8 @@
  *
  *   odb_token_logprobs           log-probabilities of a tile's labels from its logits
  *   odb_token_logprobs_backward  their gradient with respect to the logits
+ *   odb_token_list_logprobs      log-probabilities of a list of tokens at every position
+ *   odb_token_list_logprobs_backward  their gradient with respect to the logits
  *   odb_policy_loss              clipped policy loss with a KL term, weighted per slot, and its
  *                                gradient with respect to the log-probabilities
  *   odb_preference_loss          loss over pairs of rows (paired log ratios) and its gradient
@@ -561,6 +563,52 @@ int odb_token_logprobs_backward(const odb_logits_t* x, const int32_t* d_labels, 
                                 const float* d_grad_logprob, const float* d_entropy, const float* d_grad_entropy,
                                 void* d_grad_logits, int64_t grad_row_stride, int64_t grad_col_stride,
                                 int32_t* d_status, void* stream);
+
+/* Entries of a position's list of tokens, at most. */
+#define ODB_LIST_MAX 128
+
+/*
+ * Log-probabilities of a list of k tokens at every position of a tile.  With z the logits that score
+ * token (i, c), largest and logsum as above and id_j = ids(i, c, j):
+ *   list_logprob_j = a (z_{id_j} - largest) - logsum
+ * A token counts as above, or, without labels, if c >= shift.  An entry whose id is ODB_LABEL_IGNORE is
+ * none: its output is 0.  So is every output of a token that does not count, whose logits and ids are not
+ * read.  A list may name a token more than once (the label among them, say).
+ *
+ *   d_labels        [rows * cols] int32, or NULL
+ *   k               entries of a list, 1 <= k <= ODB_LIST_MAX
+ *   d_ids           [rows * cols * k] int32
+ *   d_list_logprob  [rows * cols * k] out
+ *   d_stats         [rows * cols * 2] out, or NULL: as above, for the backward call.  8-byte aligned
+ *   d_status        [1] device, or NULL: set to a nonzero value if a label or an id of a counted token lies
+ *                   outside [0, V) and is not ODB_LABEL_IGNORE (that token does not count, that entry is
+ *                   none); never cleared here
+ *
+ * Masked vocabulary entries and logits without a distribution as above.  Asynchronous (one kernel); needs
+ * no workspace.
+ */
+int odb_token_list_logprobs(const odb_logits_t* x, const int32_t* d_labels, int32_t k, const int32_t* d_ids,
+                            float* d_list_logprob, float* d_stats, int32_t* d_status, void* stream);
+
+/*
+ * Gradient of the above: with g_j the gradients of a token's list,
+ *   d z_v = a (sum_{j: id_j = v} g_j - p_v sum_j g_j).
+ *
+ *   x, d_labels, k,    as in the forward call
+ *   d_ids
+ *   d_stats            [rows * cols * 2] as the forward call, odb_token_logprobs or
+ *                      odb_token_top_logprobs wrote them for these logits and this scale
+ *   d_grad_list        [rows * cols * k]; read only where the token counts and the entry is one
+ *   d_grad_logits,     as in odb_token_logprobs_backward: in place or memory that does not overlap
+ *   grad strides
+ *   d_status           as in the forward call
+ *
+ * Where all of a token's g_j are 0 its gradient is 0.  Sums run in 32 bits, in the list's order.
+ * Asynchronous (one kernel); needs no workspace.
+ */
+int odb_token_list_logprobs_backward(const odb_logits_t* x, const int32_t* d_labels, int32_t k, const int32_t* d_ids,
+                                     const float* d_stats, const float* d_grad_list, void* d_grad_logits,
+                                     int64_t grad_row_stride, int64_t grad_col_stride, int32_t* d_status, void* stream);
 
 /*
  * A run of a plan's slots and their labels.  The slot arrays are the plan's (odb_align_groups,

@@ -35,6 +35,7 @@ ODB_MODE_NONJOIN_QUOTA = 1
 ODB_STOP_DRAINED, ODB_STOP_QUOTA, ODB_STOP_RANK_FINISHED = 0, 1, 2
 ODB_WEIGHT_SAMPLE, ODB_WEIGHT_TOKEN_APPROX, ODB_WEIGHT_TOKEN_EXACT = 0, 1, 2
 ODB_LABEL_IGNORE = -100
+ODB_LIST_MAX = 128
 ODB_FLOAT32, ODB_BFLOAT16, ODB_FLOAT16 = 0, 1, 2
 ODB_KL_NONE, ODB_KL_LINEAR, ODB_KL_SQUARE, ODB_KL_EXP = 0, 1, 2, 3
 ODB_REDUCE_TOKEN_MEAN, ODB_REDUCE_ROW_MEAN, ODB_REDUCE_SUM = 0, 1, 2
@@ -45,7 +46,7 @@ EXPORTED = [
     "odb_align_groups", "odb_collate", "odb_collate_status", "odb_check_coverage", "odb_loss_weights",
     "odb_length_sketch", "odb_stream_workspace_size", "odb_stream_plan", "odb_collate_static",
     "odb_token_logprobs", "odb_token_logprobs_backward", "odb_loss_workspace_size", "odb_policy_loss",
-    "odb_preference_loss",
+    "odb_preference_loss", "odb_token_list_logprobs", "odb_token_list_logprobs_backward",
 ]
 ODB_COLLATE_STATIC_MAX_ROWS = 2097152
 
@@ -276,6 +277,10 @@ def load():
         lib.odb_token_logprobs.argtypes = [ctypes.POINTER(Logits), P, P, P, P, P, P]
         lib.odb_token_logprobs_backward.restype = ctypes.c_int
         lib.odb_token_logprobs_backward.argtypes = [ctypes.POINTER(Logits), P, P, P, P, P, P, I64, I64, P, P]
+        lib.odb_token_list_logprobs.restype = ctypes.c_int
+        lib.odb_token_list_logprobs.argtypes = [ctypes.POINTER(Logits), P, I32, P, P, P, P, P]
+        lib.odb_token_list_logprobs_backward.restype = ctypes.c_int
+        lib.odb_token_list_logprobs_backward.argtypes = [ctypes.POINTER(Logits), P, I32, P, P, P, P, I64, I64, P, P]
         lib.odb_loss_workspace_size.restype = SZ
         lib.odb_loss_workspace_size.argtypes = [T, I64]
         lib.odb_policy_loss.restype = ctypes.c_int
@@ -546,6 +551,47 @@ def odb_token_logprobs_backward(logits, labels, stats, grad_logprob, grad_logits
                                               a(grad_entropy, f32, x, "grad_entropy", cur), g.d_logits,
                                               g.row_stride, g.col_stride, _array(status, i32, 1, "status", cur),
                                               _loss_stream(torch, stream, cur)))
+
+
+def _list_length(t, x, name: str) -> int:
+    """Entries of the lists of an array [rows, cols, k] beside a tile."""
+    if t.dim() != 3 or t.size(0) != x.rows or t.size(1) != x.cols:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{x.rows}, {x.cols}, k]")
+    return t.size(2)
+
+
+def odb_token_list_logprobs(logits, ids, list_logprob, labels=None, stats=None, status=None, shift=1, scale=1.0,
+                            stream=None):
+    """Log-probabilities of the tokens ``ids`` (int32, [rows, cols, k]) at every position of a tile, from its
+    logits [rows, cols, vocab]; ``ODB_LABEL_IGNORE`` is no entry.  ``labels`` says which tokens count (default:
+    all); ``stats`` (float32, [rows, cols, 2]) is what the backward call takes."""
+    torch, f32, _, i32, _, kinds = _torch_types()
+    cur = _current(torch)
+    x = _logits(logits, kinds, shift, scale, cur)
+    k, a = _list_length(ids, x, "ids"), _tile_array
+    _check(load().odb_token_list_logprobs(ctypes.byref(x), a(labels, i32, x, "labels", cur), k,
+                                          a(ids, i32, x, "ids", cur, k),
+                                          a(list_logprob, f32, x, "list_logprob", cur, k),
+                                          a(stats, f32, x, "stats", cur, 2), _array(status, i32, 1, "status", cur),
+                                          _loss_stream(torch, stream, cur)))
+
+
+def odb_token_list_logprobs_backward(logits, ids, stats, grad_list, grad_logits, labels=None, status=None, shift=1,
+                                     scale=1.0, stream=None):
+    """Gradient of :func:`odb_token_list_logprobs` with respect to the logits, written to ``grad_logits`` (the
+    logits' shape and type; may be the logits themselves)."""
+    torch, f32, _, i32, _, kinds = _torch_types()
+    cur = _current(torch)
+    x = _logits(logits, kinds, shift, scale, cur)
+    g = _logits(grad_logits, kinds, shift, scale, cur, "grad_logits")
+    if (g.dtype, g.rows, g.cols, g.vocab) != (x.dtype, x.rows, x.cols, x.vocab):
+        raise ValueError("grad_logits must have the shape and type of the logits")
+    k, a = _list_length(ids, x, "ids"), _tile_array
+    _check(load().odb_token_list_logprobs_backward(ctypes.byref(x), a(labels, i32, x, "labels", cur), k,
+                                                   a(ids, i32, x, "ids", cur, k), a(stats, f32, x, "stats", cur, 2),
+                                                   a(grad_list, f32, x, "grad_list", cur, k), g.d_logits, g.row_stride,
+                                                   g.col_stride, _array(status, i32, 1, "status", cur),
+                                                   _loss_stream(torch, stream, cur)))
 
 
 class Tiles:

@@ -1,0 +1,75 @@
+"""The operators over lists of tokens without a GPU: what the library and the binding refuse before any launch."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import _lists as ref
+import paper_2606_19989_amd as odb
+from test_losses_host import BAD_LOGITS, P, _logits
+
+byref = ctypes.byref
+BAD = odb.ODB_E_INVALID_ARG
+
+
+def _list(x=None, labels=P, k=4, ids=P, out=P, stats=P):
+    return odb.load().odb_token_list_logprobs(byref(_logits() if x is None else x), labels, k, ids, out, stats, None, None)
+
+
+def _list_back(x=None, labels=P, k=4, ids=P, stats=P, g=P, out=P + 4096, rs=30, cs=10):
+    return odb.load().odb_token_list_logprobs_backward(byref(_logits() if x is None else x), labels, k, ids, stats, g,
+                                                       out, rs, cs, None, None)
+
+
+@pytest.mark.parametrize("bad", BAD_LOGITS, ids=str)
+def test_logits_refused(bad):
+    assert _list(_logits(**bad)) == BAD and odb.load().odb_last_error_message() != b""
+    assert _list_back(_logits(**bad)) == BAD
+
+
+def test_list_arguments_refused():
+    assert odb.load().odb_token_list_logprobs(None, P, 4, P, P, P, None, None) == BAD
+    assert odb.load().odb_token_list_logprobs_backward(None, P, 4, P, P, P, P, 30, 10, None, None) == BAD
+    for bad in (dict(k=0), dict(k=-1), dict(k=odb.ODB_LIST_MAX + 1), dict(ids=None), dict(out=None), dict(stats=P + 4)):
+        assert _list(**bad) == BAD, bad
+    for bad in (dict(k=0), dict(k=odb.ODB_LIST_MAX + 1), dict(ids=None), dict(stats=None), dict(stats=P + 4),
+                dict(g=None), dict(out=None), dict(out=P + 1), dict(rs=-1), dict(cs=-1), dict(cs=9), dict(rs=29),
+                dict(rs=10, cs=10), dict(rs=0), dict(out=P, rs=40), dict(out=P, rs=40, cs=12)):
+        assert _list_back(**bad) == BAD, bad
+    for shape in (dict(rows=0), dict(cols=0)):    # nothing to do
+        x0 = _logits(d_logits=None, **shape)
+        assert _list(x0, None, 4, None, None, None) == odb.ODB_OK
+        assert _list_back(x0, None, 4, None, None, None, None) == odb.ODB_OK
+        assert _list(x0, None, 0, None, None, None) == BAD
+
+
+def test_binding_refuses_other_shapes():
+    import torch
+
+    z = torch.zeros(2, 3, 10)
+    ids = torch.zeros(2, 3, 4, dtype=torch.int32)
+    out = torch.zeros(2, 3, 4)
+    for bad in (ids[0], ids[:1], ids[:, :2], ids.view(6, 4), ids.long()):
+        with pytest.raises(ValueError):
+            odb.odb_token_list_logprobs(z, bad, out)
+    with pytest.raises(ValueError):        # host tensors
+        odb.odb_token_list_logprobs(z, ids, out)
+    with pytest.raises(ValueError):
+        odb.odb_token_list_logprobs_backward(z, ids, torch.zeros(2, 3, 2), out, torch.zeros(2, 3, 11))
+
+
+def test_reference_gradient_is_the_slope():
+    rng = np.random.default_rng(3)
+    z = rng.standard_normal((2, 3, 9))
+    y = rng.integers(0, 9, (2, 3)).astype(np.int32)
+    y[0, 1] = -100
+    ids = rng.integers(0, 9, (2, 3, 4)).astype(np.int32)
+    ids[1, 2, 1] = -100
+    g = rng.standard_normal((2, 3, 4))
+    value = lambda x: float((ref.list_logprobs(x, y, ids, 1, 1.3)[0] * g).sum())
+    grad = ref.list_logprobs_grad(z, y, ids, 1, 1.3, g)
+    for at in np.ndindex(z.shape):
+        up, down = z.copy(), z.copy()
+        up[at] += 1e-5
+        down[at] -= 1e-5
+        assert abs((value(up) - value(down)) / 2e-5 - grad[at]) < 1e-7
