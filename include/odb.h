@@ -20,6 +20,7 @@
  *
  *   odb_token_logprobs           log-probabilities of a tile's labels from its logits
  *   odb_token_logprobs_backward  their gradient with respect to the logits
+ *   odb_token_top_logprobs       the most probable tokens at every position, with their log-probabilities
  *   odb_token_list_logprobs      log-probabilities of a list of tokens at every position
  *   odb_token_list_logprobs_backward  their gradient with respect to the logits
  *   odb_policy_loss              clipped policy loss with a KL term, weighted per slot, and its
@@ -566,6 +567,37 @@ int odb_token_logprobs_backward(const odb_logits_t* x, const int32_t* d_labels, 
 
 /* Entries of a position's list of tokens, at most. */
 #define ODB_LIST_MAX 128
+
+/* Bytes of device workspace odb_token_top_logprobs needs: a function of the type, the shape and k alone.
+ * 0 on bad arguments. */
+size_t odb_token_top_workspace_size(const odb_logits_t* x, int32_t k);
+
+/*
+ * The k most probable tokens at every position of a tile, the likeliest first and of equally likely ones
+ * the lowest id first, with their log-probabilities; beside them what odb_token_logprobs gives and the
+ * label's rank (0: the likeliest): the number of tokens that come before it in that order.  What a server
+ * returns beside a token, and what of a teacher's answer a student is trained on.
+ *
+ *   d_labels       [rows * cols] int32, or NULL: then every token with c >= shift counts
+ *   k              1 <= k <= ODB_LIST_MAX; may pass V
+ *   d_top_ids      [rows * cols * k] int32 out
+ *   d_top_logprob  [rows * cols * k] out
+ *   d_logprob      [rows * cols] out, or NULL (needs d_labels)
+ *   d_rank         [rows * cols] int32 out, or NULL (needs d_labels)
+ *   d_stats        [rows * cols * 2] out, or NULL: as odb_token_logprobs.  8-byte aligned
+ *   d_entropy      [rows * cols] out, or NULL
+ *   d_status       as odb_token_logprobs
+ *   d_ws/ws_bytes  odb_token_top_workspace_size bytes, 256-byte aligned; calls in flight at once (captured
+ *                  graphs too) need workspaces of their own
+ *
+ * A logit of -inf is no alternative.  Entries that a position does not have, and all of a token that does
+ * not count, have id ODB_LABEL_IGNORE and log-probability -inf (no entries for the calls that take lists);
+ * such a token's rank is -1 and its other outputs are 0.  A token whose logits have no distribution (all
+ * -inf, a NaN, +inf) has no ids, rank -1, and NaN elsewhere.  Asynchronous.
+ */
+int odb_token_top_logprobs(const odb_logits_t* x, const int32_t* d_labels, int32_t k, int32_t* d_top_ids,
+                           float* d_top_logprob, float* d_logprob, int32_t* d_rank, float* d_stats, float* d_entropy,
+                           int32_t* d_status, void* d_ws, size_t ws_bytes, void* stream);
 
 /*
  * Log-probabilities of a list of k tokens at every position of a tile.  With z the logits that score

@@ -47,6 +47,7 @@ EXPORTED = [
     "odb_length_sketch", "odb_stream_workspace_size", "odb_stream_plan", "odb_collate_static",
     "odb_token_logprobs", "odb_token_logprobs_backward", "odb_loss_workspace_size", "odb_policy_loss",
     "odb_preference_loss", "odb_token_list_logprobs", "odb_token_list_logprobs_backward",
+    "odb_token_top_workspace_size", "odb_token_top_logprobs",
 ]
 ODB_COLLATE_STATIC_MAX_ROWS = 2097152
 
@@ -277,6 +278,10 @@ def load():
         lib.odb_token_logprobs.argtypes = [ctypes.POINTER(Logits), P, P, P, P, P, P]
         lib.odb_token_logprobs_backward.restype = ctypes.c_int
         lib.odb_token_logprobs_backward.argtypes = [ctypes.POINTER(Logits), P, P, P, P, P, P, I64, I64, P, P]
+        lib.odb_token_top_workspace_size.restype = SZ
+        lib.odb_token_top_workspace_size.argtypes = [ctypes.POINTER(Logits), I32]
+        lib.odb_token_top_logprobs.restype = ctypes.c_int
+        lib.odb_token_top_logprobs.argtypes = [ctypes.POINTER(Logits), P, I32, P, P, P, P, P, P, P, P, SZ, P]
         lib.odb_token_list_logprobs.restype = ctypes.c_int
         lib.odb_token_list_logprobs.argtypes = [ctypes.POINTER(Logits), P, I32, P, P, P, P, P]
         lib.odb_token_list_logprobs_backward.restype = ctypes.c_int
@@ -558,6 +563,33 @@ def _list_length(t, x, name: str) -> int:
     if t.dim() != 3 or t.size(0) != x.rows or t.size(1) != x.cols:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{x.rows}, {x.cols}, k]")
     return t.size(2)
+
+
+def odb_token_top_workspace_size(logits, k: int) -> int:
+    """Bytes of workspace for the ``k`` likeliest tokens of logits [rows, cols, vocab]."""
+    torch, _, _, _, _, kinds = _torch_types()
+    v = load().odb_token_top_workspace_size(ctypes.byref(_logits(logits, kinds, 0, 1.0, _current(torch))), int(k))
+    if v == 0:
+        _check(ODB_E_INVALID_ARG)
+    return int(v)
+
+
+def odb_token_top_logprobs(logits, top_ids, top_logprob, ws, labels=None, logprob=None, rank=None, stats=None,
+                           entropy=None, status=None, shift=1, scale=1.0, stream=None):
+    """The likeliest tokens at every position of a tile: ``top_ids`` (int32) and ``top_logprob`` (float32), both
+    [rows, cols, k], from its logits [rows, cols, vocab].  ``labels`` says which tokens count (default: all) and
+    is what ``logprob`` and ``rank`` are of."""
+    torch, f32, _, i32, _, kinds = _torch_types()
+    cur = _current(torch)
+    x = _logits(logits, kinds, shift, scale, cur)
+    k, a = _list_length(top_ids, x, "top_ids"), _tile_array
+    _check(load().odb_token_top_logprobs(ctypes.byref(x), a(labels, i32, x, "labels", cur), k,
+                                         a(top_ids, i32, x, "top_ids", cur, k),
+                                         a(top_logprob, f32, x, "top_logprob", cur, k),
+                                         a(logprob, f32, x, "logprob", cur), a(rank, i32, x, "rank", cur),
+                                         a(stats, f32, x, "stats", cur, 2), a(entropy, f32, x, "entropy", cur),
+                                         _array(status, i32, 1, "status", cur), _array(ws, ws.dtype, 0, "ws", cur),
+                                         ws.numel() * ws.element_size(), _loss_stream(torch, stream, cur)))
 
 
 def odb_token_list_logprobs(logits, ids, list_logprob, labels=None, stats=None, status=None, shift=1, scale=1.0,

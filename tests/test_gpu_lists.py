@@ -252,3 +252,188 @@ def test_gradient_against_differences():
         # the third derivative is below 6 * 1.5^3 * sum |g|; values of 18 entries of about 5 are right to U each
         most = float(g.abs().sum())
         assert abs(slope - float(back[0, c, v])) <= h * h * 1.5 ** 3 * most + 16 * U * 6 * most / h
+
+
+# ------------------------------------------------------------------ the likeliest tokens
+def _top(zd, k, y=None, shift=0, scale=1.0, rank=True, entropy=True, status=None, stream=None):
+    import paper_2606_19989_amd as odb
+    torch = _torch()
+    rows, cols, _ = zd.shape
+    full = lambda *n, t=torch.float32: torch.full((rows, cols, *n), 7, dtype=t, device="cuda")
+    o = {"ids": full(k, t=torch.int32), "top": full(k), "stats": full(2), "entropy": full() if entropy else None,
+         "logprob": None if y is None else full(), "rank": full(t=torch.int32) if y is not None and rank else None}
+    ws = torch.empty(odb.odb_token_top_workspace_size(zd, k), dtype=torch.uint8, device="cuda")
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+    odb.odb_token_top_logprobs(zd, o["ids"], o["top"], ws, labels=y, logprob=o["logprob"], rank=o["rank"],
+                               stats=o["stats"], entropy=o["entropy"], status=status, shift=shift, scale=scale,
+                               stream=stream)
+    torch.cuda.synchronize()
+    return {n: None if v is None else v.cpu().numpy().astype(np.float64 if v.is_floating_point() else np.int64)
+            for n, v in o.items()}
+
+
+def _check_top(o, z64, y, on, k, shift, scale, elt):
+    V = z64.shape[2]
+    assert np.all(o["ids"][~on] == IGNORE) and np.all(o["top"][~on] == -math.inf) and np.all(o["stats"][~on] == 0)
+    for n, none in (("logprob", 0), ("entropy", 0), ("rank", -1)):
+        if o[n] is not None:
+            assert np.all(o[n][~on] == none), n
+    for i, c in zip(*np.nonzero(on)):
+        row = z64[i, c - shift]
+        want = ref.top(row, k)
+        got = o["ids"][i, c]
+        assert np.array_equal(got[:want.size], want), (i, c, got, want)
+        assert np.all(got[want.size:] == IGNORE) and np.all(o["top"][i, c][want.size:] == -math.inf)
+        m, x, e, s = ref._softmax(row, scale)
+        L = math.log(s)
+        x2 = ref.spread(row, scale)
+        lse = ref.sum_bounds(V, elt, x2, L)
+        assert o["stats"][i, c, 0] == m and abs(o["stats"][i, c, 1] - L) <= lse
+
+        def near(got, x):
+            low = x < -3e38        # fp32's lowest times a scale: either side of the largest number
+            assert np.all(got[low] < -3e38)
+            g, x = got[~low], x[~low]
+            assert np.all(np.abs(g - (x - L)) <= lse + U * (3 * np.abs(x) + 2 * (np.abs(x) + abs(L))))
+
+        near(o["top"][i, c][:want.size], x[want])
+        if y is not None:
+            near(o["logprob"][i, c][None], x[y[i, c]][None])
+            if o["rank"] is not None:
+                assert o["rank"][i, c] == ref.rank(row, y[i, c]), (i, c)
+        if o["entropy"] is not None:
+            p = e / s
+            H = L - np.sum(np.where(p > 0, p * np.where(p > 0, x, 0.0), 0.0))
+            assert abs(o["entropy"][i, c] - H) <= lse + 2 * lse * (x2 + 1) + U * (8 * x2 * x2 + 4 * abs(L) + 2 * abs(H))
+
+
+TOP_CASES = [
+    # rows, cols, V, dtype, shift, scale, pad, k, labels, entropy
+    (1, 1, 1, "fp32", 0, 1.0, 0, 1, False, True), (1, 1, 1, "bf16", 0, 1.0, 0, 128, True, False),
+    (1, 1, 7, "bf16", 0, 1.0, 0, 5, True, True), (2, 1, 64, "fp16", 0, 1.0, 0, 64, False, True),
+    (3, 5, 63, "bf16", 1, 1.0, 0, 128, True, True), (2, 9, 257, "fp16", 1, 0.5, 3, 17, False, False),
+    (4, 33, 129, "fp32", 1, 2.0, 1, 20, True, True), (3, 17, 1000, "fp16", 1, 1.0, 0, 1, True, True),
+    (2, 8, 2047, "bf16", 0, 1.25, 0, 2, True, False), (2, 8, 2049, "fp32", 1, 1.0, 0, 64, True, True),
+    (2, 4, 8191, "fp16", 1, 1.0, 0, 33, True, True), (1, 5, 8193, "bf16", 0, 0.75, 0, 100, False, True),
+    (2, 3, 32000, "fp32", 1, 1.0, 0, 20, True, False), (2, 4, 50021, "bf16", 1, 1.5, 11, 128, True, True),
+    (1, 3, 151936, "bf16", 1, 1.0, 0, 64, True, True), (1, 2, 200003, "fp32", 0, 1.0, 1, 5, False, True),
+    (300, 3, 5, "bf16", 1, 1.0, 0, 4, True, True), (300, 3, 100, "fp32", 1, 1.0, 0, 64, True, True),
+    (600, 2, 515, "bf16", 1, 0.8, 1, 20, True, False), (300, 2, 2049, "fp16", 0, 1.0, 0, 64, True, True),
+    (270, 2, 5003, "bf16", 0, 1.0, 3, 50, True, True), (300, 2, 4001, "fp32", 1, 1.0, 3, 7, False, False),
+    (300, 2, 4001, "bf16", 1, 1.0, 0, 65, True, True),
+]
+
+
+@pytest.mark.parametrize("case", TOP_CASES, ids=str)
+def test_top_logprobs(case):
+    rows, cols, V, dtype, shift, scale, pad, k, labels, entropy = case
+    log(f"top logprobs {case}")
+    torch = _torch()
+    rng = np.random.default_rng(rows * 1000 + cols * 10 + V + k)
+    zd, z64, y, on, _ = _tile(rng, rows, cols, V, dtype, shift, pad, labels)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    o = _top(zd, k, _dev(y), shift, scale, entropy=entropy, status=status)
+    assert int(status.item()) == 0
+    _check_top(o, z64, y, on, k, shift, scale, 4 if dtype == "fp32" else 2)
+    # without the rank's count the same
+    if labels:
+        p = _top(zd, k, _dev(y), shift, scale, rank=False, entropy=entropy)
+        assert all(np.array_equal(o[n], p[n]) for n in ("ids", "top", "logprob", "stats"))
+
+
+def _hard_rows(V, rng):
+    """Rows that pass few bounds or many: by name."""
+    base = rng.standard_normal(V).astype(np.float32) * 2.5
+    up = np.sort(base)
+    far = base.copy()
+    far[:V // 2] = -300.0
+    low = np.full(V, np.finfo(np.float32).min, np.float32)
+    low[V // 3::97] = rng.standard_normal(low[V // 3::97].size)
+    most = np.full(V, -math.inf, np.float32)
+    most[[V - 1, V // 2, 3]] = [1.0, 1.0, -2.0]
+    steps = np.round(base)
+    saw = (np.arange(V) % 17).astype(np.float32)
+    signs = np.where(np.arange(V) % 3 == 0, -0.0, 0.0).astype(np.float32)
+    last = np.where(np.arange(V) < V - V // 50, 0.0, 1.0).astype(np.float32)
+    return {"ascending": up, "descending": up[::-1].copy(), "equal": np.zeros(V, np.float32), "half far below": far,
+            "lowest": np.full(V, np.finfo(np.float32).min, np.float32), "mostly lowest": low, "three finite": most,
+            "whole numbers": steps, "saw": saw, "zeros of both signs": signs, "the last are ahead": last,
+            "two values": np.where(rng.random(V) < 0.5, 1.0, 2.0).astype(np.float32),
+            "huge": np.where(rng.random(V) < 0.3, 3e38, -3e38).astype(np.float32),
+            "tiny": (rng.standard_normal(V) * 1e-40).astype(np.float32)}
+
+
+@pytest.mark.parametrize("copies", [1, 40])
+@pytest.mark.parametrize("V,dtype", [(1500, "fp32"), (4096, "bf16"), (7001, "fp16"), (40007, "fp32"), (152001, "bf16")])
+def test_top_of_hard_rows(V, dtype, copies):
+    """Ties, rows in order, masks of the type's lowest value, a first part far below the rest: with few and with
+    many positions (lanes of a wave, of a block)."""
+    torch = _torch()
+    if copies > 1 and V > 8000:
+        copies = 3
+    log(f"top of hard rows {V} {dtype} x {copies}")
+    rows = _hard_rows(V, np.random.default_rng(V))
+    names = list(rows)
+    z = torch.from_numpy(np.stack([rows[n] for n in names]))
+    if dtype != "fp32":
+        z = z.clamp(min=torch.finfo(_types()[dtype]).min, max=torch.finfo(_types()[dtype]).max)
+        z[names.index("three finite")][z[names.index("three finite")] < -1e4] = -math.inf
+    z = z.to(_types()[dtype])
+    z64 = z.double().numpy()[:, None]
+    zd = z.cuda()[:, None].repeat(copies, 1, 1)
+    rng = np.random.default_rng(1)
+    y = rng.integers(0, V, (len(names), 1)).astype(np.int32)
+    y[names.index("three finite")] = V // 2
+    on = np.ones((len(names), 1), bool)
+    for k in (1, 20, 64, 128):
+        o = _top(zd, k, _dev(np.tile(y, (copies, 1))))
+        for at in {0, copies - 1}:
+            part = {n: v[at * len(names):(at + 1) * len(names)] for n, v in o.items()}
+            for i, name in enumerate(names):
+                log(f"  k {k}: {name}")
+                one = {n: v[i:i + 1] for n, v in part.items()}
+                one["entropy"] = None if name == "huge" else one["entropy"]
+                _check_top(one, z64[i:i + 1], y[i:i + 1], on[i:i + 1], k, 0, 1.0, 4 if dtype == "fp32" else 2)
+
+
+@pytest.mark.parametrize("bad", ["nan", "inf", "all -inf"])
+@pytest.mark.parametrize("V", [100, 30000])
+def test_top_without_a_distribution(bad, V):
+    torch = _torch()
+    z = torch.randn(3, 1, V, device="cuda", dtype=torch.bfloat16)
+    if bad == "all -inf":
+        z[1] = -math.inf
+    else:
+        z[1, 0, V - 7] = float(bad)
+    y = torch.tensor([[1], [2], [3]], dtype=torch.int32, device="cuda")
+    o = _top(z, 6, y)
+    assert np.all(o["ids"][1] == IGNORE) and o["rank"][1, 0] == -1
+    for n in ("top", "logprob", "entropy"):
+        assert np.all(np.isnan(o[n][1])), n
+        assert np.all(np.isfinite(o[n][[0, 2]])), n
+
+
+def test_top_of_labels_outside_the_vocabulary():
+    torch = _torch()
+    z = torch.randn(1, 3, 100, device="cuda")
+    y = torch.tensor([[100, -5, 4]], dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    o = _top(z, 3, y, status=status)
+    assert int(status.item()) != 0
+    assert np.all(o["ids"][0, :2] == IGNORE) and np.all(o["rank"][0, :2] == -1) and np.all(o["ids"][0, 2] >= 0)
+
+
+def test_top_with_strides_of_rows_and_columns():
+    """A tile that lies transposed, and one row broadcast over all."""
+    torch = _torch()
+    z = torch.randn(5, 7, 3001, device="cuda", dtype=torch.float16)
+    want = _top(z, 9, shift=1)
+    turned = z.transpose(0, 1).contiguous().transpose(0, 1)
+    assert turned.stride(0) < turned.stride(1)
+    got = _top(turned, 9, shift=1)
+    assert all(np.array_equal(want[n], got[n]) for n in ("ids", "top", "stats", "entropy"))
+    one = z[2:3].expand(5, 7, 3001)
+    got = _top(one, 9, shift=1)
+    for n in ("ids", "top"):
+        assert np.array_equal(got[n], np.tile(want[n][2:3], (5, 1, 1))), n

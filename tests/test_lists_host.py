@@ -73,3 +73,52 @@ def test_reference_gradient_is_the_slope():
         up[at] += 1e-5
         down[at] -= 1e-5
         assert abs((value(up) - value(down)) / 2e-5 - grad[at]) < 1e-7
+
+
+def _top(x=None, labels=P, k=4, ids=P, top=P, logprob=P, rank=P, stats=P, entropy=P, ws=P, ws_bytes=1 << 40):
+    return odb.load().odb_token_top_logprobs(byref(_logits() if x is None else x), labels, k, ids, top, logprob, rank,
+                                             stats, entropy, None, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("bad", BAD_LOGITS, ids=str)
+def test_top_logits_refused(bad):
+    assert _top(_logits(**bad)) == BAD and odb.load().odb_last_error_message() != b""
+
+
+def test_top_arguments_refused():
+    lib = odb.load()
+    assert lib.odb_token_top_logprobs(None, P, 4, P, P, P, P, P, P, None, P, 1 << 40, None) == BAD
+    for bad in (dict(k=0), dict(k=-3), dict(k=odb.ODB_LIST_MAX + 1), dict(ids=None), dict(top=None), dict(stats=P + 4),
+                dict(labels=None), dict(labels=None, rank=None), dict(labels=None, logprob=None), dict(ws=None),
+                dict(ws=P + 128)):
+        assert _top(**bad) == BAD, bad
+    x = _logits()
+    size = lib.odb_token_top_workspace_size(byref(x), 4)
+    assert size > 0
+    assert _top(ws_bytes=size - 1) == odb.ODB_E_WORKSPACE
+    for shape in (dict(rows=0), dict(cols=0)):
+        x0 = _logits(d_logits=None, **shape)
+        assert _top(x0, None, 4, None, None, None, None, None, None, None, 0) == odb.ODB_OK
+    assert lib.odb_token_top_workspace_size(None, 4) == 0
+    for k in (0, odb.ODB_LIST_MAX + 1):
+        assert lib.odb_token_top_workspace_size(byref(x), k) == 0
+    for bad in (dict(dtype=3), dict(vocab=0), dict(rows=-1), dict(rows=1 << 16, cols=1 << 15)):
+        assert lib.odb_token_top_workspace_size(byref(_logits(**bad)), 4) == 0
+
+
+def test_top_binding_refuses():
+    import torch
+
+    z = torch.zeros(2, 3, 10)
+    ids, top = torch.zeros(2, 3, 4, dtype=torch.int32), torch.zeros(2, 3, 4)
+    ws = torch.zeros(256, dtype=torch.uint8)
+    with pytest.raises(ValueError):        # host tensors
+        odb.odb_token_top_logprobs(z, ids, top, ws)
+    with pytest.raises(ValueError):
+        odb.odb_token_top_logprobs(z, ids[0], top, ws)
+
+
+def test_reference_of_ties():
+    row = np.array([1.0, 3.0, -np.inf, 3.0, 1.0, 0.0])
+    assert ref.top(row, 4).tolist() == [1, 3, 0, 4] and ref.top(row, 9).tolist() == [1, 3, 0, 4, 5]
+    assert [ref.rank(row, y) for y in range(6)] == [2, 0, 5, 1, 3, 4]
