@@ -16,9 +16,24 @@ namespace odb {
 namespace {
 
 typedef unsigned long long u64;
+#ifndef ODB_TOP_G
+#define ODB_TOP_G 256
+#endif
+#ifndef ODB_TOP_WAVES
+#define ODB_TOP_WAVES 4
+#endif
 
 constexpr int kBins = 256;      // of a digit
 constexpr float kNone = -HUGE_VALF;
+
+template <typename T>
+__device__ __forceinline__ float lowest_of();
+template <>
+__device__ __forceinline__ float lowest_of<float>() { return kLowest; }
+template <>
+__device__ __forceinline__ float lowest_of<bf16_t>() { return -3.38953138925153547590470800371487867e38f; }
+template <>
+__device__ __forceinline__ float lowest_of<fp16_t>() { return -65504.0f; }
 
 // Logits to whole numbers of the same order; -0 is 0.
 __device__ __forceinline__ uint32_t ordered(float f) {
@@ -45,20 +60,31 @@ struct TopArgs {
     int32_t k;
 };
 
-// A group's LDS.  Enough candidates for k = 128 and a step of one load of (at most 256) threads.
+// A group's LDS.
 template <int G>
 struct Room {
-    static constexpr int kLanes = G < 256 ? G : 256;        // threads that load in a step
-    static constexpr int kHold = ODB_LIST_MAX + kLanes * 8;
-    static constexpr int kFew = G < 256 ? 128 : 256;        // candidates that are ordered by counting
-    u64 key[kHold];
+    static constexpr int kWaves = G / kWave;
+    static constexpr int kLanes = G < 256 ? G : 256;                // threads that load in a step of the second way
+    static constexpr int kHits = G < 256 ? 192 : 1024;
+    static constexpr int kKeys = G < 256 ? 256 : 512;               // all multiples of 8
+    static constexpr int kFew = G < 256 ? 128 : 256;                // candidates that are ordered by counting
+    static constexpr int kHold = kHits * 20 / 8 + kKeys;            // the second way's candidates
+    static_assert(kHold >= ODB_LIST_MAX + kLanes * 8 && kHold % 8 == 0, "k of them and a step's");
+    union {
+        struct {
+            uint4 hit[kHits];           // groups of 16 bytes with a candidate in them
+            uint32_t hit_at[kHits];     // their first columns
+            u64 key[kKeys];             // candidates
+        };
+        u64 hold[kHold];
+    };
     u64 few[kFew];
     u64 top[ODB_LIST_MAX];
     uint32_t bins[kBins];
-    uint32_t bound[(G + kWave - 1) / kWave];
-    Acc acc[(G + kWave - 1) / kWave];
+    uint32_t bound[kWaves];
+    Acc acc[kWaves];
     u64 differ;
-    uint32_t count, few_count, ahead;
+    uint32_t hits, count, few_count, ahead;
 };
 
 // The largest whole number with its low 16 bits 0 that `kth` of the wave's lanes reach.
@@ -72,26 +98,19 @@ __device__ __forceinline__ uint32_t wave_kth(uint32_t o, int kth) {
     return r;
 }
 
+// The k largest of a list's n keys, ordered, to s.top; fewer if n < k.  The list has room for n rounded up to
+// eight.  The group has met before, and meets at the end.
 template <int G>
-__device__ __forceinline__ void keep(Room<G>& s, u64 key) {
-    const uint32_t at = atomicAdd(&s.count, 1u);
-    if (at < Room<G>::kHold) s.key[at] = key;
-}
-
-// The k largest of the n candidates (n <= kHold), ordered, to s.top; fewer if n < k.  The group has met
-// before, and meets at the end.
-template <int G>
-__device__ void pick(Room<G>& s, int n, int k) {
+__device__ __forceinline__ void pick(Room<G>& s, u64* list, int n, int k) {
     constexpr int kFew = Room<G>::kFew;
     const int t = threadIdx.x & (G - 1), lane = threadIdx.x & (kWave - 1);
-    const u64* list = s.key;
     if (n > kFew) {
         // digits of 8 bits from the highest bit that differs
         if (t == 0) s.differ = 0;
         group_sync<G>();
-        const u64 first = s.key[0];
+        const u64 first = list[0];
         u64 differ = 0;
-        for (int i = t; i < n; i += G) differ |= s.key[i] ^ first;
+        for (int i = t; i < n; i += G) differ |= list[i] ^ first;
 #pragma unroll
         for (int d = kWave / 2; d > 0; d >>= 1) differ |= __shfl_xor(differ, d, kWave);
         if (lane == 0) atomicOr(&s.differ, differ);
@@ -106,7 +125,7 @@ __device__ void pick(Room<G>& s, int n, int k) {
             group_sync<G>();
             const u64 mask = top == 64 ? 0 : ~0ull << top;
             for (int i = t; i < n; i += G) {
-                const u64 key = s.key[i];
+                const u64 key = list[i];
                 if ((key & mask) == fixed) atomicAdd(&s.bins[(uint32_t)(key >> low) & (kBins - 1)], 1u);
             }
             group_sync<G>();
@@ -140,38 +159,49 @@ __device__ void pick(Room<G>& s, int n, int k) {
         if (t == 0) s.few_count = 0;
         group_sync<G>();
         for (int i = t; i < n; i += G) {
-            const u64 key = s.key[i];
+            const u64 key = list[i];
             if (key >= fixed) s.few[atomicAdd(&s.few_count, 1u)] = key;
         }
         group_sync<G>();
         n = (int)s.few_count;
         list = s.few;
     }
+    // whole steps of eight: keys of 0 are behind all others
+    if (t < 8 && n + t < ((n + 7) & ~7)) list[n + t] = 0;
+    group_sync<G>();
     for (int i = t; i < n; i += G) {
         const u64 mine = list[i];
         int place = 0;
-        for (int j = 0; j < n; ++j) place += list[j] > mine;
+        for (int j = 0; j < n; j += 8) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) place += list[j + u] > mine;
+        }
         if (place < k) s.top[place] = mine;
     }
     group_sync<G>();
 }
 
-// Goes through columns [v0, v1) of a row: the joined triple, the columns ahead of the label, and candidates
-// for the k largest, of which there are n <= kHold.  All of the group's threads get the same.
+// Columns [v0, v1) of a row: the joined triple, the columns ahead of the label (s.ahead), and in s.key the *n
+// candidates, the k largest among them, or *n > kKeys.  All of the group's threads get the same.
 template <typename T, bool ENT, bool RANK, int G>
 __device__ __forceinline__ Acc scan(const T* z, int64_t v0, int64_t v1, int32_t y, float zy, int kk, float k, Room<G>& s,
                                     int* n) {
     constexpr int N = Vec<T>::N;
     constexpr int kWavesIn = G / kWave;
     const int t = threadIdx.x & (G - 1), lane = threadIdx.x & (kWave - 1);
-    if (t == 0) s.count = s.ahead = 0;
+    const uint32_t none = ordered(lowest_of<T>());
+    const int share = (kk + kWavesIn - 1) / kWavesIn;      // threads of each wave that make k
+    if (t == 0) s.hits = s.count = s.ahead = 0;
     group_sync<G>();
     Acc r{kLowest, 0.0f, 0.0f};
     int ahead = 0;
     const int64_t whole = v0 + (v1 - v0) / N * N;
-    float bound = kNone;
+    auto load = [&](Vec<T>* w, int64_t v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) w[j] = load_vec<true>(z + at_most(v + j * G * N, whole - N));
+    };
     // a 16-byte group: its sums, its place beside the label's, and its largest
-    auto take = [&](const Vec<T>& w, int64_t v) {
+    auto take = [&](const Vec<T>& w, int64_t v) __attribute__((always_inline)) {
         float f[N], most = kNone;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
@@ -195,106 +225,169 @@ __device__ __forceinline__ Acc scan(const T* z, int64_t v0, int64_t v1, int32_t 
         }
         return most;
     };
-    auto load = [&](Vec<T>* w, int64_t v) {
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) w[j] = load_vec<true>(z + at_most(v + j * G * N, whole - N));
+    auto hit = [&](const Vec<T>& w, int64_t v) __attribute__((always_inline)) {
+        const uint32_t to = atomicAdd(&s.hits, 1u);
+        if (to < Room<G>::kHits) {
+            __builtin_memcpy(&s.hit[to], &w, 16);
+            s.hit_at[to] = (uint32_t)v;
+        }
     };
-    int64_t v = v0 + (int64_t)t * N;
-    if (v0 < whole) {     // uniform
+    // The bound that `share` threads of every wave reach, by the largest that each has met: what a wave has left
+    // here is true whenever another reads it.  Candidates are above the number below it.
+    auto bound = [&]() __attribute__((always_inline)) {
+        uint32_t o = wave_kth(ordered(r.m), share);
+        if (G > kWave) {
+            volatile uint32_t* const of = s.bound;
+            if (lane == 0) of[threadIdx.x / kWave] = o;
+            for (int i = 0; i < kWavesIn; ++i) o = of[i] < o ? of[i] : o;
+        }
+        return o;
+    };
+    auto joined_bound = [&](uint32_t o) __attribute__((always_inline)) {      // behind a meeting
+#pragma unroll
+        for (int i = 0; i < kWavesIn && G > kWave; ++i) o = s.bound[i] < o ? s.bound[i] : o;
+        return o;
+    };
+    auto limit_of = [&](uint32_t o) __attribute__((always_inline)) { return o > none + 1 ? unordered(o - 1 - (o - 1 == 0x7fffffffu)) : unordered(none); };
+    int64_t at = v0;
+    uint32_t o = 0;
+    // rounds behind which the group meets, until there is a bound
+    while (at < whole && o <= none) {     // uniform
+        const int64_t v = at + (int64_t)t * N;
         Vec<T> w[kAhead];
         load(w, v);
-        float most[kAhead], all = kNone;
+        float most[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            most[j] = kNone;
-            if (v + j * G * N < whole) most[j] = take(w[j], v + j * G * N);
-            all = fmaxf(all, most[j]);
-        }
-        // every wave gives its share of k threads, or one wave all of them
-        uint32_t o = wave_kth(ordered(all), (kk + kWavesIn - 1) / kWavesIn);
+        for (int j = 0; j < kAhead; ++j) most[j] = v + j * G * N < whole ? take(w[j], v + j * G * N) : kNone;
+        o = wave_kth(ordered(r.m), share);
         if (G > kWave) {
             if (lane == 0) s.bound[threadIdx.x / kWave] = o;
             __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kWavesIn; ++i) o = s.bound[i] < o ? s.bound[i] : o;
+            o = joined_bound(o);
+            __syncthreads();
         }
-        bound = o > ordered(kNone) ? unordered(o) : kNone;
+        const float limit = limit_of(o);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (most[j] >= bound && most[j] > kNone) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float f = (float)w[j].v[e];
-                    if (f >= bound && f > kNone) keep(s, key_of(f, v + j * G * N + e));
-                }
-            }
-        }
+        for (int j = 0; j < kAhead; ++j)
+            if (most[j] > limit) hit(w[j], v + j * G * N);
+        at += kAhead * G * N;
     }
-    // behind the first round k columns before these have reached the bound: equal ones come after them
-    for (v += kAhead * G * N; v < whole; v += kAhead * G * N) {
+    float limit = limit_of(o);
+    // the waves on their own, a round's loads under way beside the one before it; the bound again whenever the
+    // rounds have doubled
+    int rounds = 1;
+    int64_t v = at + (int64_t)t * N;
+    Vec<T> next[kAhead];
+    if (at < whole) load(next, v);
+    for (; at < whole; at += kAhead * G * N, v += kAhead * G * N) {
         Vec<T> w[kAhead];
-        load(w, v);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) w[j] = next[j];
+        if (at + kAhead * G * N < whole) load(next, v + kAhead * G * N);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             if (v + j * G * N >= whole) break;
-            if (take(w[j], v + j * G * N) > bound) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float f = (float)w[j].v[e];
-                    if (f > bound) keep(s, key_of(f, v + j * G * N + e));
-                }
-            }
+            if (take(w[j], v + j * G * N) > limit) hit(w[j], v + j * G * N);
         }
+        ++rounds;
+        if ((rounds & (rounds - 1)) == 0) limit = limit_of(bound());
     }
     if (whole + t < v1) {
         const float f = (float)z[whole + t];
         if (f > r.m) acc_rescale<ENT>(r, f, k);
         acc_term<ENT>(r, f, k);
         if (RANK) ahead += f > zy || (f == zy && whole + t < y);
-        if (f > bound) keep(s, key_of(f, whole + t));
+        if (f > limit) {
+            const uint32_t to = atomicAdd(&s.count, 1u);
+            if (to < (uint32_t)Room<G>::kKeys) s.key[to] = key_of(f, whole + t);
+        }
     }
     if (RANK) {
 #pragma unroll
         for (int d = kWave / 2; d > 0; d >>= 1) ahead += __shfl_xor(ahead, d, kWave);
         if (lane == 0) atomicAdd(&s.ahead, (uint32_t)ahead);
     }
+    o = wave_kth(ordered(r.m), share);
+    if (G > kWave && lane == 0) s.bound[threadIdx.x / kWave] = o;
     r = group_join<ENT, G>(r, s.acc, k);
     group_sync<G>();
-    int have = (int)s.count;
-    if (have > Room<G>::kHold) {
-        // again, a load a step, above the k-th largest so far
-        constexpr int kLanes = Room<G>::kLanes;
-        group_sync<G>();
-        u64 least = 0;
-        have = 0;
-        for (int64_t at = v0; at < v1; at += kLanes * N) {
-            if (t == 0) s.count = have;
-            group_sync<G>();
-            const int64_t mine = at + (int64_t)t * N;
-            for (int e = 0; t < kLanes && e < N && mine + e < v1; ++e) {
-                const float f = (float)z[mine + e];
-                const u64 key = key_of(f, mine + e);
-                if (f > kNone && key > least) keep(s, key);
+    // what of the groups is above the last bound
+    limit = limit_of(joined_bound(o));
+    const int hits = (int)s.hits;
+    for (int i = t; i < hits && hits <= Room<G>::kHits; i += G) {
+        Vec<T> w;
+        __builtin_memcpy(&w, &s.hit[i], 16);
+        const uint32_t v = s.hit_at[i];
+        uint32_t on = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) on |= (uint32_t)((float)w.v[e] > limit) << e;
+        if (!on) continue;
+        uint32_t to = atomicAdd(&s.count, (uint32_t)__builtin_popcount(on));
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            if (on >> e & 1) {
+                if (to < (uint32_t)Room<G>::kKeys) s.key[to] = key_of((float)w.v[e], v + e);
+                ++to;
             }
+        }
+    }
+    group_sync<G>();
+    *n = hits > Room<G>::kHits ? Room<G>::kKeys + 1 : (int)s.count;
+    return r;
+}
+
+// The k largest of columns [v0, v1), ordered, to s.top, and how many there are, from a list of n candidates that
+// scan left.  Where its room did not do, or fewer than k columns are above the type's lowest value, which masks
+// columns and is no candidate there, the row is gone through again, a load a step, above the k-th largest so far.
+template <typename T, int G>
+__device__ __forceinline__ int largest(const T* z, int64_t v0, int64_t v1, int kk, int n, Room<G>& s) {
+    constexpr int N = Vec<T>::N;
+    constexpr int kLanes = Room<G>::kLanes, kFull = Room<G>::kHold - kLanes * N;
+    const int t = threadIdx.x & (G - 1);
+    const bool again = n > Room<G>::kKeys || n < kk;
+    const int64_t whole = v0 + (v1 - v0) / N * N;
+    u64* const list = again ? s.hold : s.key;
+    u64 least = 0;
+    int64_t v = v0 + (int64_t)t * N, at = v0;
+    if (again) n = 0;
+    for (;;) {      // uniform: one round unless the row is gone through again
+        if (again) {
             group_sync<G>();
-            have = (int)s.count;
-            if (have > kk) {
-                pick(s, have, kk);
-                for (int i = t; i < kk; i += G) s.key[i] = s.top[i];
-                have = kk;
-                least = s.top[kk - 1];
+            if (t == 0) s.count = n;
+            Vec<T> next{};
+            if (t < kLanes && v < whole) next = load_vec<false>(z + v);
+            while (at < v1 && n <= kFull) {
+                const Vec<T> w = next;
+                if (t < kLanes && v + kLanes * N < whole) next = load_vec<false>(z + v + kLanes * N);
+                group_sync<G>();
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if (t >= kLanes || v + e >= v1) break;
+                    const float f = v < whole ? (float)w.v[e] : (float)z[v + e];
+                    const u64 key = key_of(f, v + e);
+                    if (f > kNone && key > least) {
+                        const uint32_t to = atomicAdd(&s.count, 1u);
+                        if (to < (uint32_t)Room<G>::kHold) s.hold[to] = key;     // always
+                    }
+                }
+                group_sync<G>();
+                n = (int)s.count;
+                at += kLanes * N;
+                v += kLanes * N;
             }
             group_sync<G>();
         }
+        pick(s, list, n, kk);
+        if (n > kk) n = kk;
+        if (!again || at >= v1) return n;
+        for (int i = t; i < n; i += G) s.hold[i] = s.top[i];
+        if (n == kk) least = s.top[kk - 1];
     }
-    *n = have;
-    return r;
 }
 
 // A token's outputs from the joined triple and the n <= k largest, ordered, in s.top.
 template <bool ENT, bool RANK, int G>
-__device__ __forceinline__ void leave(const TopArgs& A, int64_t q, const Acc& r, int32_t y, float zy, int n, uint32_t ahead,
-                                      const Room<G>& s) {
+__device__ __forceinline__ void leave(const TopArgs& A, int64_t q, const Acc& r, float zy, int n, const Room<G>& s) {
     const int t = threadIdx.x & (G - 1);
     const float a = (float)A.x.scale, lse = logf(r.s);
     const bool sound = r.s > 0.0f && r.s < HUGE_VALF;      // a NaN or +inf among the logits, or none above -inf
@@ -306,7 +399,7 @@ __device__ __forceinline__ void leave(const TopArgs& A, int64_t q, const Acc& r,
     }
     if (t == 0) {
         if (A.logprob) A.logprob[q] = (zy - r.m) * a - lse;
-        if (RANK) A.rank[q] = sound ? (int32_t)ahead : -1;
+        if (RANK) A.rank[q] = sound ? (int32_t)s.ahead : -1;
         if (A.stats) reinterpret_cast<float2*>(A.stats)[q] = make_float2(r.m, lse);
         if (ENT) A.entropy[q] = lse - r.t / r.s * kLn2;
     }
@@ -329,16 +422,16 @@ __device__ __forceinline__ void leave_none(const TopArgs& A, int64_t q) {
 
 // A group of G threads, a wave or a block, takes a position.
 template <typename T, bool ENT, bool RANK, int G>
-__global__ void __launch_bounds__(kBlock) top_kernel(TopArgs A) {
-    static_assert(G == kWave || G == kBlock, "a wave or a block");
-    __shared__ Room<G> s_room[kBlock / G];
+__global__ void __launch_bounds__(G > kBlock ? G : kBlock, ODB_TOP_WAVES) top_kernel(TopArgs A) {
+    constexpr int kThreads = G > kBlock ? G : kBlock;
+    __shared__ Room<G> s_room[kThreads / G];
     Room<G>& s = s_room[threadIdx.x / G];
     const odb_logits_t& x = A.x;
     const int64_t n = x.rows * x.cols, V = x.vocab;
     const int t = threadIdx.x & (G - 1);
     const float k = (float)x.scale * kLog2e;
-    for (int64_t q = (int64_t)blockIdx.x * (kBlock / G) + threadIdx.x / G; q < n;
-         q += (int64_t)gridDim.x * (kBlock / G)) {   // uniform over a group
+    for (int64_t q = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G; q < n;
+         q += (int64_t)gridDim.x * (kThreads / G)) {   // uniform over a group
         const uint32_t i = (uint32_t)q / (uint32_t)x.cols, c = (uint32_t)q - i * (uint32_t)x.cols;
         const int32_t y = c < (uint32_t)x.shift ? -1 : A.labels ? read_label(A.labels, q, V, A.status, t == 0) : 0;
         if (y < 0) {
@@ -350,8 +443,8 @@ __global__ void __launch_bounds__(kBlock) top_kernel(TopArgs A) {
         const float zy = (float)z[y];
         int have;
         const Acc r = scan<T, ENT, RANK, G>(z, 0, V, y, zy, A.k, k, s, &have);
-        pick(s, have, A.k);
-        leave<ENT, RANK, G>(A, q, r, y, zy, have < A.k ? have : A.k, s.ahead, s);
+        have = largest(z, 0, V, A.k, have, s);
+        leave<ENT, RANK, G>(A, q, r, zy, have, s);
         group_sync<G>();     // the next position writes where this one's are read
     }
 }
@@ -362,6 +455,8 @@ void launch(const TopArgs& a, hipStream_t s) {
     const int64_t row = a.x.vocab * (int64_t)sizeof(T);
     if (row <= 16384 && a.k <= kWave && n > 2 * num_cus())
         hipLaunchKernelGGL((top_kernel<T, ENT, RANK, kWave>), dim3(grid_for(n, kBlock / kWave)), dim3(kBlock), 0, s, a);
+    else if (ODB_TOP_G == 512)
+        hipLaunchKernelGGL((top_kernel<T, ENT, RANK, 512>), dim3(grid_for(n, 1)), dim3(512), 0, s, a);
     else
         hipLaunchKernelGGL((top_kernel<T, ENT, RANK, kBlock>), dim3(grid_for(n, 1)), dim3(kBlock), 0, s, a);
 }

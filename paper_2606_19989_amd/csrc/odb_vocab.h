@@ -129,10 +129,11 @@ __device__ __forceinline__ Acc group_join(Acc r, Acc* s_acc, float k) {
     if (G > kWave) {
         if ((threadIdx.x & (kWave - 1)) == 0) s_acc[threadIdx.x / kWave] = r;
         __syncthreads();
-        r = s_acc[0];
+        Acc all{s_acc[0].m, s_acc[0].s, s_acc[0].t};
 #pragma unroll
-        for (int j = 1; j < G / kWave; ++j) r = acc_join<ENT>(r, s_acc[j], k);
+        for (int j = 1; j < G / kWave; ++j) all = acc_join<ENT>(all, Acc{s_acc[j].m, s_acc[j].s, s_acc[j].t}, k);
         __syncthreads();
+        return all;
     }
     return r;
 }
