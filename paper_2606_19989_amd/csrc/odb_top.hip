@@ -9,6 +9,8 @@
 // keys are never equal, and of equal logits the first column's is the largest.
 // Where the list does not hold what passes (a first round far below the rest, rows of few different
 // values), the row is gone through again, with an exact bound behind every step.
+#include <algorithm>
+
 #include "odb_vocab.h"
 
 namespace odb {
@@ -18,6 +20,9 @@ namespace {
 typedef unsigned long long u64;
 #ifndef ODB_TOP_G
 #define ODB_TOP_G 256
+#endif
+#ifndef ODB_TOP_PART
+#define ODB_TOP_PART 8192
 #endif
 #ifndef ODB_TOP_WAVES
 #define ODB_TOP_WAVES 4
@@ -58,6 +63,18 @@ struct TopArgs {
     float* entropy;
     int32_t* status;
     int32_t k;
+    int32_t parts;          // blocks of a position, where it is more than one
+    int64_t part_len;       // their columns
+    struct Part* part;      // [positions * parts]
+    u64* part_key;          // [positions * parts * 2 k]
+};
+
+// What a block leaves of its part of a position's columns, beside its candidates.
+struct Part {
+    Acc acc;
+    float zy;               // the label's logit
+    uint32_t ahead;
+    int32_t n;              // candidates, in any order
 };
 
 // A group's LDS.
@@ -90,11 +107,9 @@ struct Room {
 // The largest whole number with its low 16 bits 0 that `kth` of the wave's lanes reach.
 __device__ __forceinline__ uint32_t wave_kth(uint32_t o, int kth) {
     uint32_t r = 0;
-#pragma unroll
-    for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t c = r | 1u << bit;
-        if (__builtin_popcountll(__ballot(o >= c)) >= kth) r = c;
-    }
+#pragma unroll 1
+    for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
+        if (__builtin_popcountll(__ballot(o >= (r | bit))) >= kth) r |= bit;
     return r;
 }
 
@@ -232,65 +247,49 @@ __device__ __forceinline__ Acc scan(const T* z, int64_t v0, int64_t v1, int32_t 
             s.hit_at[to] = (uint32_t)v;
         }
     };
-    // The bound that `share` threads of every wave reach, by the largest that each has met: what a wave has left
-    // here is true whenever another reads it.  Candidates are above the number below it.
-    auto bound = [&]() __attribute__((always_inline)) {
-        uint32_t o = wave_kth(ordered(r.m), share);
-        if (G > kWave) {
-            volatile uint32_t* const of = s.bound;
-            if (lane == 0) of[threadIdx.x / kWave] = o;
-            for (int i = 0; i < kWavesIn; ++i) o = of[i] < o ? of[i] : o;
-        }
-        return o;
+    auto limit_of = [&](uint32_t o) __attribute__((always_inline)) {
+        return o > none + 1 ? unordered(o - 1 - (o - 1 == 0x7fffffffu)) : unordered(none);
     };
-    auto joined_bound = [&](uint32_t o) __attribute__((always_inline)) {      // behind a meeting
-#pragma unroll
-        for (int i = 0; i < kWavesIn && G > kWave; ++i) o = s.bound[i] < o ? s.bound[i] : o;
-        return o;
-    };
-    auto limit_of = [&](uint32_t o) __attribute__((always_inline)) { return o > none + 1 ? unordered(o - 1 - (o - 1 == 0x7fffffffu)) : unordered(none); };
-    int64_t at = v0;
-    uint32_t o = 0;
-    // rounds behind which the group meets, until there is a bound
-    while (at < whole && o <= none) {     // uniform
-        const int64_t v = at + (int64_t)t * N;
-        Vec<T> w[kAhead];
-        load(w, v);
-        float most[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) most[j] = v + j * G * N < whole ? take(w[j], v + j * G * N) : kNone;
-        o = wave_kth(ordered(r.m), share);
-        if (G > kWave) {
-            if (lane == 0) s.bound[threadIdx.x / kWave] = o;
-            __syncthreads();
-            o = joined_bound(o);
-            __syncthreads();
-        }
-        const float limit = limit_of(o);
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (most[j] > limit) hit(w[j], v + j * G * N);
-        at += kAhead * G * N;
-    }
-    float limit = limit_of(o);
-    // the waves on their own, a round's loads under way beside the one before it; the bound again whenever the
-    // rounds have doubled
-    int rounds = 1;
-    int64_t v = at + (int64_t)t * N;
+    // The bound is what `share` threads of every wave reach with the largest that each has met; candidates are
+    // above the number below it.  Until there is one the group meets behind every round; then the waves go on by
+    // themselves and form it anew whenever their rounds have doubled, and in the last: what a wave has left is
+    // true whenever another reads it.
+    volatile uint32_t* const of = s.bound;
+    uint32_t met = 0;
+    float limit = unordered(none);
+    int rounds = 0;
+    int64_t v = v0 + (int64_t)t * N;
     Vec<T> next[kAhead];
-    if (at < whole) load(next, v);
-    for (; at < whole; at += kAhead * G * N, v += kAhead * G * N) {
+    if (v0 < whole) load(next, v);
+    for (int64_t at = v0; at < whole; at += kAhead * G * N, v += kAhead * G * N) {     // uniform
         Vec<T> w[kAhead];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) w[j] = next[j];
-        if (at + kAhead * G * N < whole) load(next, v + kAhead * G * N);
+        const bool last = at + kAhead * G * N >= whole;
+        if (!last) load(next, v + kAhead * G * N);     // under way beside this round
+        float most[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (v + j * G * N >= whole) break;
-            if (take(w[j], v + j * G * N) > limit) hit(w[j], v + j * G * N);
-        }
+        for (int j = 0; j < kAhead; ++j) most[j] = v + j * G * N < whole ? take(w[j], v + j * G * N) : kNone;
         ++rounds;
-        if ((rounds & (rounds - 1)) == 0) limit = limit_of(bound());
+        const bool meet = met <= none;
+        if (meet || last || (rounds & (rounds - 1)) == 0) {
+            uint32_t o = wave_kth(ordered(r.m), share);
+            if (G > kWave) {
+                if (lane == 0) of[threadIdx.x / kWave] = o;
+                if (meet) __syncthreads();
+#pragma unroll
+                for (int i = 0; i < kWavesIn; ++i) {
+                    const uint32_t other = of[i];
+                    o = other < o ? other : o;
+                }
+                if (meet) __syncthreads();
+            }
+            if (meet) met = o;
+            limit = limit_of(o);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (most[j] > limit) hit(w[j], v + j * G * N);
     }
     if (whole + t < v1) {
         const float f = (float)z[whole + t];
@@ -307,28 +306,20 @@ __device__ __forceinline__ Acc scan(const T* z, int64_t v0, int64_t v1, int32_t 
         for (int d = kWave / 2; d > 0; d >>= 1) ahead += __shfl_xor(ahead, d, kWave);
         if (lane == 0) atomicAdd(&s.ahead, (uint32_t)ahead);
     }
-    o = wave_kth(ordered(r.m), share);
-    if (G > kWave && lane == 0) s.bound[threadIdx.x / kWave] = o;
     r = group_join<ENT, G>(r, s.acc, k);
     group_sync<G>();
     // what of the groups is above the last bound
-    limit = limit_of(joined_bound(o));
-    const int hits = (int)s.hits;
-    for (int i = t; i < hits && hits <= Room<G>::kHits; i += G) {
-        Vec<T> w;
-        __builtin_memcpy(&w, &s.hit[i], 16);
-        const uint32_t v = s.hit_at[i];
-        uint32_t on = 0;
+    uint32_t o = s.bound[0];
 #pragma unroll
-        for (int e = 0; e < N; ++e) on |= (uint32_t)((float)w.v[e] > limit) << e;
-        if (!on) continue;
-        uint32_t to = atomicAdd(&s.count, (uint32_t)__builtin_popcount(on));
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            if (on >> e & 1) {
-                if (to < (uint32_t)Room<G>::kKeys) s.key[to] = key_of((float)w.v[e], v + e);
-                ++to;
-            }
+    for (int i = 1; i < kWavesIn; ++i) o = s.bound[i] < o ? s.bound[i] : o;
+    if (G > kWave && v0 < whole) limit = limit_of(o);
+    const int hits = (int)s.hits, found = hits <= Room<G>::kHits ? hits * N : 0;
+    const T* const of_hits = reinterpret_cast<const T*>(s.hit);
+    for (int i = t; i < found; i += G) {
+        const float f = (float)of_hits[i];
+        if (f > limit) {
+            const uint32_t to = atomicAdd(&s.count, 1u);
+            if (to < (uint32_t)Room<G>::kKeys) s.key[to] = key_of(f, s.hit_at[i / N] + i % N);
         }
     }
     group_sync<G>();
@@ -449,9 +440,83 @@ __global__ void __launch_bounds__(G > kBlock ? G : kBlock, ODB_TOP_WAVES) top_ke
     }
 }
 
+// Few positions: a block takes one of a position's parts, and leaves what it found in the workspace.
+template <typename T, bool ENT, bool RANK>
+__global__ void __launch_bounds__(kBlock) top_part_kernel(TopArgs A) {
+    __shared__ Room<kBlock> s;
+    const odb_logits_t& x = A.x;
+    const int64_t V = x.vocab;
+    const int64_t q = blockIdx.x / A.parts;
+    const int64_t v0 = (blockIdx.x - q * A.parts) * A.part_len, v1 = v0 + A.part_len < V ? v0 + A.part_len : V;
+    const uint32_t i = (uint32_t)q / (uint32_t)x.cols, c = (uint32_t)q - i * (uint32_t)x.cols;
+    const int32_t y =
+        c < (uint32_t)x.shift ? -1 : A.labels ? read_label(A.labels, q, V, A.status, threadIdx.x == 0) : 0;
+    if (y < 0) return;
+    const T* z = static_cast<const T*>(x.d_logits) + (int64_t)i * x.row_stride +
+                 (int64_t)(c - (uint32_t)x.shift) * x.col_stride;
+    const float zy = (float)z[y];
+    int n;
+    const Acc r = scan<T, ENT, RANK, kBlock>(z, v0, v1, y, zy, A.k, (float)x.scale * kLog2e, s, &n);
+    const u64* from = s.key;
+    if (n < A.k || n > 2 * A.k) {
+        n = largest(z, v0, v1, A.k, n, s);
+        from = s.top;
+    }
+    u64* to = A.part_key + (int64_t)blockIdx.x * 2 * A.k;
+    for (int j = threadIdx.x; j < n; j += kBlock) to[j] = from[j];
+    if (threadIdx.x == 0) A.part[blockIdx.x] = {r, zy, s.ahead, n};
+}
+
+// A position from its parts, in their order.
+template <bool ENT, bool RANK>
+__global__ void __launch_bounds__(kBlock) top_join_kernel(TopArgs A) {
+    __shared__ Room<kBlock> s;
+    const odb_logits_t& x = A.x;
+    const int64_t q = blockIdx.x;
+    const uint32_t c = (uint32_t)q % (uint32_t)x.cols;
+    const int32_t y = c < (uint32_t)x.shift ? -1 : A.labels ? read_label(A.labels, q, x.vocab, A.status, false) : 0;
+    if (y < 0) return leave_none<ENT, RANK, kBlock>(A, q);
+    const float k = (float)x.scale * kLog2e;
+    const Part* part = A.part + q * A.parts;
+    // a part a lane, in every wave; their candidates behind each other
+    const int lane = threadIdx.x & (kWave - 1);
+    Part w{{kLowest, 0.0f, 0.0f}, 0.0f, 0, 0};
+    if (lane < A.parts) w = part[lane];
+    const u64* from = A.part_key + q * A.parts * 2 * A.k;
+    int n = w.n;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int o = __shfl_up(n, d, kWave);
+        if (lane >= d) n += o;
+    }
+    if (threadIdx.x < kWave) {
+        s.bins[lane] = (uint32_t)(n - w.n);
+        s.bins[kWave + lane] = (uint32_t)w.n;
+    }
+    n = __shfl(n, kWave - 1, kWave);
+    const float zy = __shfl(w.zy, 0, kWave);
+    const Acc r = group_join<ENT, kWave>(w.acc, nullptr, k);
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d >>= 1) w.ahead += __shfl_xor(w.ahead, d, kWave);
+    if (threadIdx.x == 0) s.ahead = w.ahead;
+    __syncthreads();
+    for (int i = threadIdx.x; i < A.parts * 2 * A.k; i += kBlock) {
+        const int p = i / (2 * A.k), j = i - p * 2 * A.k;
+        if (j < (int)s.bins[kWave + p]) s.hold[s.bins[p] + j] = from[i];
+    }
+    __syncthreads();
+    pick(s, s.hold, n, A.k);
+    leave<ENT, RANK, kBlock>(A, q, r, zy, n < A.k ? n : A.k, s);
+}
+
 template <typename T, bool ENT, bool RANK>
 void launch(const TopArgs& a, hipStream_t s) {
     const int64_t n = a.x.rows * a.x.cols;
+    if (a.parts > 1) {
+        hipLaunchKernelGGL((top_part_kernel<T, ENT, RANK>), dim3((unsigned)(n * a.parts)), dim3(kBlock), 0, s, a);
+        hipLaunchKernelGGL((top_join_kernel<ENT, RANK>), dim3((unsigned)n), dim3(kBlock), 0, s, a);
+        return;
+    }
     const int64_t row = a.x.vocab * (int64_t)sizeof(T);
     if (row <= 16384 && a.k <= kWave && n > 2 * num_cus())
         hipLaunchKernelGGL((top_kernel<T, ENT, RANK, kWave>), dim3(grid_for(n, kBlock / kWave)), dim3(kBlock), 0, s, a);
@@ -475,7 +540,32 @@ int check_top(const odb_logits_t* x, int32_t k) {
     return ODB_OK;
 }
 
-size_t top_workspace(const odb_logits_t*, int32_t) { return 256; }
+// Blocks of a position: for fewer positions than would fill the chip, as many as have a round of loads each, as
+// far as their candidates go to one block's LDS.
+constexpr int64_t kFillBlocks = 512;
+int32_t parts_for(const odb_logits_t* x, int32_t k, int64_t* len) {
+    const int64_t n = x->rows * x->cols, round = x->dtype == ODB_FLOAT32 ? ODB_TOP_PART / 2 : ODB_TOP_PART;
+    int64_t parts = n > 0 ? kFillBlocks / n : 1;
+    parts = std::min({parts, (x->vocab + round - 1) / round, (int64_t)(Room<kBlock>::kHold / (2 * k)), (int64_t)kWave});
+    if (parts <= 1) return 1;
+    *len = ((x->vocab + parts - 1) / parts + 7) & ~(int64_t)7;
+    return (int32_t)((x->vocab + *len - 1) / *len);
+}
+
+struct TopLayout {
+    int32_t parts;
+    int64_t len;
+    size_t key, total;
+};
+
+TopLayout top_layout(const odb_logits_t* x, int32_t k) {
+    TopLayout L{};
+    L.parts = parts_for(x, k, &L.len);
+    const size_t all = L.parts > 1 ? (size_t)(x->rows * x->cols * L.parts) : 0;
+    L.key = (sizeof(Part) * all + 255) & ~size_t(255);
+    L.total = std::max(L.key + 16 * all * k, size_t(256));
+    return L;
+}
 
 }  // namespace
 
@@ -485,7 +575,7 @@ using namespace odb;
 
 extern "C" size_t odb_token_top_workspace_size(const odb_logits_t* x, int32_t k) {
     if (check_top(x, k) != ODB_OK) return 0;
-    return top_workspace(x, k);
+    return top_layout(x, k).total;
 }
 
 extern "C" int odb_token_top_logprobs(const odb_logits_t* x, const int32_t* d_labels, int32_t k, int32_t* d_top_ids,
@@ -502,8 +592,9 @@ extern "C" int odb_token_top_logprobs(const odb_logits_t* x, const int32_t* d_la
     if (!d_ws) return set_error(ODB_E_INVALID_ARG, "workspace is NULL");
     if (reinterpret_cast<uintptr_t>(d_ws) & 255)
         return set_error(ODB_E_INVALID_ARG, "workspace must be 256-byte aligned");
-    if (ws_bytes < top_workspace(x, k))
-        return set_error(ODB_E_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, top_workspace(x, k));
+    const TopLayout L = top_layout(x, k);
+    if (ws_bytes < L.total)
+        return set_error(ODB_E_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, L.total);
     TopArgs a{};
     a.x = *x;
     a.labels = d_labels;
@@ -515,6 +606,10 @@ extern "C" int odb_token_top_logprobs(const odb_logits_t* x, const int32_t* d_la
     a.entropy = d_entropy;
     a.status = d_status;
     a.k = k;
+    a.parts = L.parts;
+    a.part_len = L.len;
+    a.part = ws_at<Part>(d_ws, 0);
+    a.part_key = ws_at<u64>(d_ws, L.key);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (x->dtype == ODB_FLOAT32)
         launch<float>(a, s);
