@@ -1,14 +1,20 @@
 // The most probable tokens of every position of a tile, with log-probabilities, entropy and the label's rank.
 //
 // One pass over a position's logits forms the largest, the sum of exponentials and, for the entropy, their
-// weighted logs, as the label's log-probability does.  Beside it the k largest are found by a bound that
-// only a few candidates pass: k threads' largest of the first round of loads are k logits, so the k-th
-// of those is a bound that the row's k-th largest does not fall below.  What reaches it goes to a list in
-// LDS; behind the pass the list's k largest are picked by the digits of their keys and ordered by counting.
-// A key holds the logit, mapped to a whole number that grows with it, above the complement of the column:
-// keys are never equal, and of equal logits the first column's is the largest.
-// Where the list does not hold what passes (a first round far below the rest, rows of few different
-// values), the row is gone through again, with an exact bound behind every step.
+// weighted logs, as the label's log-probability does.  Beside it the k largest are found by a bound that only
+// few logits pass: with k cells of columns whose largest reach it, the row's k-th largest does not fall below
+// it.  A 16-byte group with a logit above the bound is set aside whole, in LDS, for about ten instructions;
+// behind the pass the groups are looked at once, under the last and highest bound, which leaves 1 to 2 k keys.
+// Their k largest are picked by the digits of the keys where they are many, and ordered by counting.
+// A key holds the logit, mapped to a whole number that grows with it, above the complement of the column: keys
+// are never equal, and of equal logits the first column's is the largest.
+// Where the room does not do (rows in ascending order, or with thousands of equal logits at the bound), the row
+// is gone through again, above the k-th largest key so far.
+//
+// Bound by the reads of the logits and, about as much, by the instructions: nine a logit as without the
+// alternatives (an exponential counts four), one more for its group's largest.  4,096 positions of 151,936 bf16
+// logits, k = 64: 210 us (5.7 TB/s of reads; 182 without alternatives), of which the groups set aside take
+// about 20 us and what is behind the pass 10.
 #include <algorithm>
 
 #include "odb_vocab.h"
@@ -18,17 +24,11 @@ namespace odb {
 namespace {
 
 typedef unsigned long long u64;
-#ifndef ODB_TOP_G
-#define ODB_TOP_G 256
-#endif
-#ifndef ODB_TOP_PART
-#define ODB_TOP_PART 8192
-#endif
-#ifndef ODB_TOP_WAVES
-#define ODB_TOP_WAVES 4
-#endif
 
 constexpr int kBins = 256;      // of a digit
+// Alternatives from which on a wave's cells are half a group of a thread's, 512, and not its 64 threads.  k = 20 / 40
+// of 36,621 positions of 8,192 bf16 logits: 130 / 390 us with threads, 173 / 185 with half groups.
+constexpr int kFine = 24;
 constexpr float kNone = -HUGE_VALF;
 
 template <typename T>
@@ -81,12 +81,11 @@ struct Part {
 template <int G>
 struct Room {
     static constexpr int kWaves = G / kWave;
-    static constexpr int kLanes = G < 256 ? G : 256;                // threads that load in a step of the second way
-    static constexpr int kHits = G < 256 ? 192 : 1024;
-    static constexpr int kKeys = G < 256 ? 256 : 512;               // all multiples of 8
-    static constexpr int kFew = G < 256 ? 128 : 256;                // candidates that are ordered by counting
+    static constexpr int kHits = G == kWave ? 192 : 1024;
+    static constexpr int kKeys = G == kWave ? 256 : 512;            // all multiples of 8
+    static constexpr int kFew = G == kWave ? 128 : 256;             // candidates that are ordered by counting
     static constexpr int kHold = kHits * 20 / 8 + kKeys;            // the second way's candidates
-    static_assert(kHold >= ODB_LIST_MAX + kLanes * 8 && kHold % 8 == 0, "k of them and a step's");
+    static_assert(kHold >= ODB_LIST_MAX + G * 8 && kHold % 8 == 0, "k of them and a step's");
     union {
         struct {
             uint4 hit[kHits];           // groups of 16 bytes with a candidate in them
@@ -104,12 +103,17 @@ struct Room {
     uint32_t hits, count, few_count, ahead;
 };
 
-// The largest whole number with its low 16 bits 0 that `kth` of the wave's lanes reach.
-__device__ __forceinline__ uint32_t wave_kth(uint32_t o, int kth) {
+// The largest whole number with its low 16 bits 0 that `kth` of the wave's C numbers a lane reach.
+template <int C>
+__device__ __forceinline__ uint32_t wave_kth(const uint32_t* o, int kth) {
     uint32_t r = 0;
 #pragma unroll 1
-    for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
-        if (__builtin_popcountll(__ballot(o >= (r | bit))) >= kth) r |= bit;
+    for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < C; ++i) n += __builtin_popcountll(__ballot(o[i] >= (r | bit)));
+        if (n >= kth) r |= bit;
+    }
     return r;
 }
 
@@ -198,14 +202,14 @@ __device__ __forceinline__ void pick(Room<G>& s, u64* list, int n, int k) {
 
 // Columns [v0, v1) of a row: the joined triple, the columns ahead of the label (s.ahead), and in s.key the *n
 // candidates, the k largest among them, or *n > kKeys.  All of the group's threads get the same.
-template <typename T, bool ENT, bool RANK, int G>
+template <typename T, bool ENT, bool RANK, bool FINE, int G>
 __device__ __forceinline__ Acc scan(const T* z, int64_t v0, int64_t v1, int32_t y, float zy, int kk, float k, Room<G>& s,
                                     int* n) {
     constexpr int N = Vec<T>::N;
     constexpr int kWavesIn = G / kWave;
     const int t = threadIdx.x & (G - 1), lane = threadIdx.x & (kWave - 1);
     const uint32_t none = ordered(lowest_of<T>());
-    const int share = (kk + kWavesIn - 1) / kWavesIn;      // threads of each wave that make k
+    const int share = (kk + kWavesIn - 1) / kWavesIn;      // cells of each wave that make k
     if (t == 0) s.hits = s.count = s.ahead = 0;
     group_sync<G>();
     Acc r{kLowest, 0.0f, 0.0f};
@@ -216,13 +220,18 @@ __device__ __forceinline__ Acc scan(const T* z, int64_t v0, int64_t v1, int32_t 
         for (int j = 0; j < kAhead; ++j) w[j] = load_vec<true>(z + at_most(v + j * G * N, whole - N));
     };
     // a 16-byte group: its sums, its place beside the label's, and its largest
-    auto take = [&](const Vec<T>& w, int64_t v) __attribute__((always_inline)) {
-        float f[N], most = kNone;
+    auto take = [&](const Vec<T>& w, int64_t v, float* cell) __attribute__((always_inline)) {
+        float f[N], half[2] = {kNone, kNone};
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             f[e] = (float)w.v[e];
-            most = fmaxf(most, f[e]);
+            half[2 * e / N] = fmaxf(half[2 * e / N], f[e]);
         }
+        if (FINE) {
+            cell[0] = fmaxf(cell[0], half[0]);
+            cell[1] = fmaxf(cell[1], half[1]);
+        }
+        const float most = fmaxf(half[0], half[1]);
         if (most > r.m) acc_rescale<ENT>(r, most, k);
 #pragma unroll
         for (int e = 0; e < N; ++e) acc_term<ENT>(r, f[e], k);
@@ -250,12 +259,16 @@ __device__ __forceinline__ Acc scan(const T* z, int64_t v0, int64_t v1, int32_t 
     auto limit_of = [&](uint32_t o) __attribute__((always_inline)) {
         return o > none + 1 ? unordered(o - 1 - (o - 1 == 0x7fffffffu)) : unordered(none);
     };
-    // The bound is what `share` threads of every wave reach with the largest that each has met; candidates are
-    // above the number below it.  Until there is one the group meets behind every round; then the waves go on by
+    // The bound is what `share` cells of every wave reach, a cell being the largest that one half of one of a
+    // thread's groups has held in any round, or, for few, a thread; candidates are above the number below it.
+    // Until there is one the group meets behind every round; then the waves go on by
     // themselves and form it anew whenever their rounds have doubled, and in the last: what a wave has left is
     // true whenever another reads it.
     volatile uint32_t* const of = s.bound;
     uint32_t met = 0;
+    float cell[2 * kAhead];
+#pragma unroll
+    for (int j = 0; j < 2 * kAhead; ++j) cell[j] = kNone;
     float limit = unordered(none);
     int rounds = 0;
     int64_t v = v0 + (int64_t)t * N;
@@ -269,11 +282,19 @@ __device__ __forceinline__ Acc scan(const T* z, int64_t v0, int64_t v1, int32_t 
         if (!last) load(next, v + kAhead * G * N);     // under way beside this round
         float most[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) most[j] = v + j * G * N < whole ? take(w[j], v + j * G * N) : kNone;
+        for (int j = 0; j < kAhead; ++j) most[j] = v + j * G * N < whole ? take(w[j], v + j * G * N, cell + 2 * j) : kNone;
         ++rounds;
         const bool meet = met <= none;
         if (meet || last || (rounds & (rounds - 1)) == 0) {
-            uint32_t o = wave_kth(ordered(r.m), share);
+            uint32_t o, c[2 * kAhead];
+            if (FINE) {
+#pragma unroll
+                for (int j = 0; j < 2 * kAhead; ++j) c[j] = ordered(cell[j]);
+                o = wave_kth<2 * kAhead>(c, share);
+            } else {
+                c[0] = ordered(r.m);
+                o = wave_kth<1>(c, share);
+            }
             if (G > kWave) {
                 if (lane == 0) of[threadIdx.x / kWave] = o;
                 if (meet) __syncthreads();
@@ -333,7 +354,7 @@ __device__ __forceinline__ Acc scan(const T* z, int64_t v0, int64_t v1, int32_t 
 template <typename T, int G>
 __device__ __forceinline__ int largest(const T* z, int64_t v0, int64_t v1, int kk, int n, Room<G>& s) {
     constexpr int N = Vec<T>::N;
-    constexpr int kLanes = Room<G>::kLanes, kFull = Room<G>::kHold - kLanes * N;
+    constexpr int kFull = Room<G>::kHold - G * N;
     const int t = threadIdx.x & (G - 1);
     const bool again = n > Room<G>::kKeys || n < kk;
     const int64_t whole = v0 + (v1 - v0) / N * N;
@@ -346,25 +367,32 @@ __device__ __forceinline__ int largest(const T* z, int64_t v0, int64_t v1, int k
             group_sync<G>();
             if (t == 0) s.count = n;
             Vec<T> next{};
-            if (t < kLanes && v < whole) next = load_vec<false>(z + v);
+            if (v < whole) next = load_vec<false>(z + v);
             while (at < v1 && n <= kFull) {
                 const Vec<T> w = next;
-                if (t < kLanes && v + kLanes * N < whole) next = load_vec<false>(z + v + kLanes * N);
+                if (v + G * N < whole) next = load_vec<false>(z + v + G * N);
                 group_sync<G>();
+                float f[N];
+                uint32_t on = 0;
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    if (t >= kLanes || v + e >= v1) break;
-                    const float f = v < whole ? (float)w.v[e] : (float)z[v + e];
-                    const u64 key = key_of(f, v + e);
-                    if (f > kNone && key > least) {
-                        const uint32_t to = atomicAdd(&s.count, 1u);
-                        if (to < (uint32_t)Room<G>::kHold) s.hold[to] = key;     // always
+                    f[e] = v < whole ? (float)w.v[e] : v + e < v1 ? (float)z[v + e] : kNone;
+                    on |= (uint32_t)(f[e] > kNone && key_of(f[e], v + e) > least) << e;
+                }
+                if (on) {
+                    uint32_t to = atomicAdd(&s.count, (uint32_t)__builtin_popcount(on));
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        if (on >> e & 1) {
+                            if (to < (uint32_t)Room<G>::kHold) s.hold[to] = key_of(f[e], v + e);     // always
+                            ++to;
+                        }
                     }
                 }
                 group_sync<G>();
                 n = (int)s.count;
-                at += kLanes * N;
-                v += kLanes * N;
+                at += G * N;
+                v += G * N;
             }
             group_sync<G>();
         }
@@ -412,17 +440,17 @@ __device__ __forceinline__ void leave_none(const TopArgs& A, int64_t q) {
 }
 
 // A group of G threads, a wave or a block, takes a position.
-template <typename T, bool ENT, bool RANK, int G>
-__global__ void __launch_bounds__(G > kBlock ? G : kBlock, ODB_TOP_WAVES) top_kernel(TopArgs A) {
-    constexpr int kThreads = G > kBlock ? G : kBlock;
-    __shared__ Room<G> s_room[kThreads / G];
+template <typename T, bool ENT, bool RANK, bool FINE, int G>
+__global__ void __launch_bounds__(kBlock, 4) top_kernel(TopArgs A) {
+    static_assert(G == kWave || G == kBlock, "a wave or a block");
+    __shared__ Room<G> s_room[kBlock / G];
     Room<G>& s = s_room[threadIdx.x / G];
     const odb_logits_t& x = A.x;
     const int64_t n = x.rows * x.cols, V = x.vocab;
     const int t = threadIdx.x & (G - 1);
     const float k = (float)x.scale * kLog2e;
-    for (int64_t q = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G; q < n;
-         q += (int64_t)gridDim.x * (kThreads / G)) {   // uniform over a group
+    for (int64_t q = (int64_t)blockIdx.x * (kBlock / G) + threadIdx.x / G; q < n;
+         q += (int64_t)gridDim.x * (kBlock / G)) {   // uniform over a group
         const uint32_t i = (uint32_t)q / (uint32_t)x.cols, c = (uint32_t)q - i * (uint32_t)x.cols;
         const int32_t y = c < (uint32_t)x.shift ? -1 : A.labels ? read_label(A.labels, q, V, A.status, t == 0) : 0;
         if (y < 0) {
@@ -433,7 +461,7 @@ __global__ void __launch_bounds__(G > kBlock ? G : kBlock, ODB_TOP_WAVES) top_ke
                      (int64_t)(c - (uint32_t)x.shift) * x.col_stride;
         const float zy = (float)z[y];
         int have;
-        const Acc r = scan<T, ENT, RANK, G>(z, 0, V, y, zy, A.k, k, s, &have);
+        const Acc r = scan<T, ENT, RANK, FINE, G>(z, 0, V, y, zy, A.k, k, s, &have);
         have = largest(z, 0, V, A.k, have, s);
         leave<ENT, RANK, G>(A, q, r, zy, have, s);
         group_sync<G>();     // the next position writes where this one's are read
@@ -441,7 +469,7 @@ __global__ void __launch_bounds__(G > kBlock ? G : kBlock, ODB_TOP_WAVES) top_ke
 }
 
 // Few positions: a block takes one of a position's parts, and leaves what it found in the workspace.
-template <typename T, bool ENT, bool RANK>
+template <typename T, bool ENT, bool RANK, bool FINE>
 __global__ void __launch_bounds__(kBlock) top_part_kernel(TopArgs A) {
     __shared__ Room<kBlock> s;
     const odb_logits_t& x = A.x;
@@ -456,7 +484,7 @@ __global__ void __launch_bounds__(kBlock) top_part_kernel(TopArgs A) {
                  (int64_t)(c - (uint32_t)x.shift) * x.col_stride;
     const float zy = (float)z[y];
     int n;
-    const Acc r = scan<T, ENT, RANK, kBlock>(z, v0, v1, y, zy, A.k, (float)x.scale * kLog2e, s, &n);
+    const Acc r = scan<T, ENT, RANK, FINE, kBlock>(z, v0, v1, y, zy, A.k, (float)x.scale * kLog2e, s, &n);
     const u64* from = s.key;
     if (n < A.k || n > 2 * A.k) {
         n = largest(z, v0, v1, A.k, n, s);
@@ -513,17 +541,30 @@ template <typename T, bool ENT, bool RANK>
 void launch(const TopArgs& a, hipStream_t s) {
     const int64_t n = a.x.rows * a.x.cols;
     if (a.parts > 1) {
-        hipLaunchKernelGGL((top_part_kernel<T, ENT, RANK>), dim3((unsigned)(n * a.parts)), dim3(kBlock), 0, s, a);
+        hipLaunchKernelGGL((a.k > kWave ? top_part_kernel<T, ENT, RANK, true> : top_part_kernel<T, ENT, RANK, false>),
+                           dim3((unsigned)(n * a.parts)), dim3(kBlock), 0, s, a);
         hipLaunchKernelGGL((top_join_kernel<ENT, RANK>), dim3((unsigned)n), dim3(kBlock), 0, s, a);
         return;
     }
+    // A wave or a block takes a position, by the bytes of its logits.  A wave leaves four positions to a block, so
+    // that one's wait behind its pass is another's reading; a block of four waves has cells for more alternatives,
+    // and needs 4 KB for all of its threads to have any.  us for 600 MB of bf16 logits, k = 5 / 20 / 64 / 128:
+    //   logits a row    wave                        block
+    //   1,024           279 / 330 /  630 / 1370     4890 / 4890 / 4890 / 5260
+    //   2,048           185 / 214 /  369 /  800      700 /  760 / 1020 / 1590
+    //   4,096           150 / 161 /  277 /  575      370 /  400 /  540 /  809
+    //   8,192           126 / 131 /  203 / 1195      208 /  225 /  293 /  422
+    //   16,384          115 / 115 /  434 /  818      155 /  167 /  200 /  301
+    //   32,768          118 / 125 /  397 /  652      126 /  131 /  147 /  214
+    //   65,536          137 / 144 /  420 /  613      114 /  116 /  125 /  162
     const int64_t row = a.x.vocab * (int64_t)sizeof(T);
-    if (row <= 16384 && a.k <= kWave && n > 2 * num_cus())
-        hipLaunchKernelGGL((top_kernel<T, ENT, RANK, kWave>), dim3(grid_for(n, kBlock / kWave)), dim3(kBlock), 0, s, a);
-    else if (ODB_TOP_G == 512)
-        hipLaunchKernelGGL((top_kernel<T, ENT, RANK, 512>), dim3(grid_for(n, 1)), dim3(512), 0, s, a);
+    const bool wave = row <= 4096 || (n > 2 * num_cus() && row <= (a.k <= kFine ? 32768 : a.k <= kWave ? 16384 : 8192));
+    if (wave)
+        hipLaunchKernelGGL((a.k > kFine ? top_kernel<T, ENT, RANK, true, kWave> : top_kernel<T, ENT, RANK, false, kWave>),
+                           dim3(grid_for(n, kBlock / kWave)), dim3(kBlock), 0, s, a);
     else
-        hipLaunchKernelGGL((top_kernel<T, ENT, RANK, kBlock>), dim3(grid_for(n, 1)), dim3(kBlock), 0, s, a);
+        hipLaunchKernelGGL((a.k > kWave ? top_kernel<T, ENT, RANK, true, kBlock> : top_kernel<T, ENT, RANK, false, kBlock>),
+                           dim3(grid_for(n, 1)), dim3(kBlock), 0, s, a);
 }
 
 template <typename T>
@@ -541,11 +582,13 @@ int check_top(const odb_logits_t* x, int32_t k) {
 }
 
 // Blocks of a position: for fewer positions than would fill the chip, as many as have a round of loads each, as
-// far as their candidates go to one block's LDS.
-constexpr int64_t kFillBlocks = 512;
+// far as their candidates go to one block's LDS.  In a graph, k = 20, 1 / 32 / 128 positions: of 151,936 bf16 logits
+// 12.7 / 14.8 / 17.4 us, with one block each 24 / 26 / 26; of 16,384 (two rounds) 10.6 / 11.3 / 11.9, with one 8 / 9 / 9.
+constexpr int64_t kFillBlocks = 1024;
 int32_t parts_for(const odb_logits_t* x, int32_t k, int64_t* len) {
-    const int64_t n = x->rows * x->cols, round = x->dtype == ODB_FLOAT32 ? ODB_TOP_PART / 2 : ODB_TOP_PART;
+    const int64_t n = x->rows * x->cols, round = x->dtype == ODB_FLOAT32 ? 4096 : 8192;
     int64_t parts = n > 0 ? kFillBlocks / n : 1;
+    if (x->vocab <= 3 * round) return 1;
     parts = std::min({parts, (x->vocab + round - 1) / round, (int64_t)(Room<kBlock>::kHold / (2 * k)), (int64_t)kWave});
     if (parts <= 1) return 1;
     *len = ((x->vocab + parts - 1) / parts + 7) & ~(int64_t)7;
