@@ -23,6 +23,8 @@
  *   odb_token_top_logprobs       the most probable tokens at every position, with their log-probabilities
  *   odb_token_list_logprobs      log-probabilities of a list of tokens at every position
  *   odb_token_list_logprobs_backward  their gradient with respect to the logits
+ *   odb_distill_loss             divergence of the student's lists from a teacher's, weighted per slot,
+ *                                and its gradient with respect to the student's log-probabilities
  *   odb_policy_loss              clipped policy loss with a KL term, weighted per slot, and its
  *                                gradient with respect to the log-probabilities
  *   odb_preference_loss          loss over pairs of rows (paired log ratios) and its gradient
@@ -795,6 +797,68 @@ int odb_preference_loss(const odb_tiles_t* t, const odb_preference_params_t* p, 
                         const float* d_ref_logprob, const int32_t* d_row_ids, int64_t num_ids, const int32_t* d_pair,
                         float* d_loss, float* d_row_loss, float* d_row_reward, int64_t* d_counts,
                         float* d_grad_logprob, int32_t* d_status, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Divergence between a teacher's probabilities p and a student's q. */
+typedef enum odb_distill {
+    ODB_DISTILL_FORWARD = 0,     /* sum p ln (p / q)                                           */
+    ODB_DISTILL_REVERSE = 1,     /* sum q ln (q / p)                                           */
+    ODB_DISTILL_MIXTURE = 2      /* w sum p ln (p / m) + (1 - w) sum q ln (q / m),
+                                    m = w p + (1 - w) q                                        */
+} odb_distill_t;
+
+/* What the sums run over.  A list holds part of each distribution: p_j = exp(teacher_j), q_j = exp(student_j). */
+typedef enum odb_support {
+    ODB_SUPPORT_LISTED = 0,      /* the list's entries as they are                             */
+    ODB_SUPPORT_RENORMALIZED = 1,/* the entries, p and q each divided by its sum over them     */
+    ODB_SUPPORT_REST = 2         /* the entries and what they leave out as one more,
+                                    max(1 - sum, 2^-24) of p and of q                          */
+} odb_support_t;
+
+typedef struct odb_distill_params {
+    int32_t kind;                /* odb_distill_t                                              */
+    int32_t support;             /* odb_support_t                                              */
+    int32_t reduce;              /* odb_reduce_t                                               */
+    int32_t reserved0;           /* must be 0                                                  */
+    double  mix;                 /* w of the mixture, inside (0, 1) also in fp32               */
+    double  loss_scale;          /* finite; factor of every slot's loss                        */
+} odb_distill_params_t;
+
+/* Bytes of device workspace odb_distill_loss needs: a function of num_slots, num_rows, num_elems and k alone.
+ * 0 on bad arguments. */
+size_t odb_distill_workspace_size(const odb_tiles_t* t, int32_t k);
+
+/*
+ * Distillation loss over lists of tokens, and its gradient.  With D the divergence of a counted token's lists
+ * and R the reduction over a slot's counted tokens, the loss of slot k is
+ *   loss_k = loss_scale * slot_weight_k * R(D)
+ * and the gradient is that of sum_k loss_k with respect to the student's log-probabilities, each an input of
+ * its own (odb_token_list_logprobs_backward brings them together).
+ *
+ *   k                 entries of a list, 1 <= k <= ODB_LIST_MAX
+ *   d_student         [num_elems * k], as odb_token_list_logprobs writes them for the teacher's ids
+ *   d_teacher         [num_elems * k], as odb_token_top_logprobs writes them; an entry of -inf is none: it adds
+ *                     nothing, has gradient 0, and the student's beside it may hold anything
+ *   d_slot_weight     [K] fp64 (odb_loss_weights), or NULL: 1
+ *   d_slot_loss       [K] out
+ *   d_slot_mean       [K] out: R(D)
+ *   d_slot_count      [K] int64 out: counted tokens
+ *   d_grad_student    [num_elems * k] out, or NULL
+ *   d_status          [1] device, or NULL: as odb_policy_loss
+ *   d_ws / ws_bytes   odb_distill_workspace_size(t, k) bytes, 256-B aligned; calls in flight at once (captured
+ *                     graphs too) need workspaces of their own
+ *
+ * num_elems <= 2^32.  A token that does not count contributes nothing, whatever its lists hold, and has
+ * gradient 0; one whose list has no entry counts with D = 0 (with ODB_SUPPORT_REST too: both rests are 1).  An
+ * entry to which the student gives no probability (-inf) makes a forward divergence infinite and adds nothing
+ * to a reverse one.  A rest that is held at 2^-24 has no gradient.  A slot without counted tokens has loss, mean and count 0.
+ * Elements behind the last slot are not written.  A token's terms and slopes are formed in 32 bits, what its
+ * list leaves out, weights and sums over tokens in 64, in a fixed order: results are the same bit for bit from
+ * call to call.  Asynchronous.
+ */
+int odb_distill_loss(const odb_tiles_t* t, const odb_distill_params_t* p, int32_t k, const float* d_student,
+                     const float* d_teacher, const double* d_slot_weight, float* d_slot_loss, float* d_slot_mean,
+                     int64_t* d_slot_count, float* d_grad_student, int32_t* d_status, void* d_ws, size_t ws_bytes,
+                     void* stream);
 
 #ifdef __cplusplus
 }

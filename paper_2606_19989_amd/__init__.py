@@ -39,6 +39,8 @@ ODB_LIST_MAX = 128
 ODB_FLOAT32, ODB_BFLOAT16, ODB_FLOAT16 = 0, 1, 2
 ODB_KL_NONE, ODB_KL_LINEAR, ODB_KL_SQUARE, ODB_KL_EXP = 0, 1, 2, 3
 ODB_REDUCE_TOKEN_MEAN, ODB_REDUCE_ROW_MEAN, ODB_REDUCE_SUM = 0, 1, 2
+ODB_DISTILL_FORWARD, ODB_DISTILL_REVERSE, ODB_DISTILL_MIXTURE = 0, 1, 2
+ODB_SUPPORT_LISTED, ODB_SUPPORT_RENORMALIZED, ODB_SUPPORT_REST = 0, 1, 2
 ODB_PREFERENCE_SIGMOID, ODB_PREFERENCE_HINGE, ODB_PREFERENCE_SQUARE = 0, 1, 2
 
 EXPORTED = [
@@ -47,7 +49,7 @@ EXPORTED = [
     "odb_length_sketch", "odb_stream_workspace_size", "odb_stream_plan", "odb_collate_static",
     "odb_token_logprobs", "odb_token_logprobs_backward", "odb_loss_workspace_size", "odb_policy_loss",
     "odb_preference_loss", "odb_token_list_logprobs", "odb_token_list_logprobs_backward",
-    "odb_token_top_workspace_size", "odb_token_top_logprobs",
+    "odb_token_top_workspace_size", "odb_token_top_logprobs", "odb_distill_workspace_size", "odb_distill_loss",
 ]
 ODB_COLLATE_STATIC_MAX_ROWS = 2097152
 
@@ -232,6 +234,21 @@ class PreferenceParams(ctypes.Structure):
         super().__init__(**{**dict(beta=0.1, loss_scale=1.0), **kw})
 
 
+class DistillParams(ctypes.Structure):
+    """Parameters of odb_distill_loss; keywords override the defaults below."""
+    _fields_ = [
+        ("kind", ctypes.c_int32),
+        ("support", ctypes.c_int32),
+        ("reduce", ctypes.c_int32),
+        ("reserved0", ctypes.c_int32),
+        ("mix", ctypes.c_double),
+        ("loss_scale", ctypes.c_double),
+    ]
+
+    def __init__(self, **kw):
+        super().__init__(**{**dict(mix=0.5, loss_scale=1.0), **kw})
+
+
 _lib = None
 
 
@@ -293,6 +310,10 @@ def load():
         lib.odb_preference_loss.restype = ctypes.c_int
         lib.odb_preference_loss.argtypes = [T, ctypes.POINTER(PreferenceParams), P, P, P, I64, P, P, P, P, P, P, P, P,
                                             SZ, P]
+        lib.odb_distill_workspace_size.restype = SZ
+        lib.odb_distill_workspace_size.argtypes = [T, I32]
+        lib.odb_distill_loss.restype = ctypes.c_int
+        lib.odb_distill_loss.argtypes = [T, ctypes.POINTER(DistillParams), I32, P, P, P, P, P, P, P, P, P, SZ, P]
         _lib = lib
     return _lib
 
@@ -702,9 +723,39 @@ def odb_preference_loss(tiles, params, logprob, pair, loss, row_loss, row_reward
         ws.numel() * ws.element_size(), _loss_stream(torch, stream, cur)))
 
 
+def odb_distill_workspace_size(tiles: Tiles, k: int) -> int:
+    v = load().odb_distill_workspace_size(tiles.ref, int(k))
+    if v == 0:
+        _check(ODB_E_INVALID_ARG)
+    return int(v)
+
+
+def odb_distill_loss(tiles, params, student, teacher, slot_loss, slot_mean, slot_count, ws, slot_weight=None,
+                     grad_student=None, status=None, stream=None):
+    """Divergence of the student's lists [num_elems, k] from the teacher's, reduced and weighted per slot, and
+    its gradient."""
+    torch, f32, f64, i32, i64, _ = _torch_types()
+    cur = _current(torch)
+    _tiles_here(tiles, cur)
+    K, E, a = tiles.num_slots, tiles.num_elems, _array
+    if student.dim() < 2:
+        raise ValueError(f"student: shape {tuple(student.shape)}, expected [{E}, k]")
+    k = student.size(-1)
+    for name, t in (("student", student), ("teacher", teacher), ("grad_student", grad_student)):
+        if t is not None and (t.numel() != E * k or t.size(-1) != k):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{E}, {k}]")
+    _check(load().odb_distill_loss(
+        tiles.ref, ctypes.byref(params), k, a(student, f32, E * k, "student", cur),
+        a(teacher, f32, E * k, "teacher", cur), a(slot_weight, f64, K, "slot_weight", cur),
+        a(slot_loss, f32, K, "slot_loss", cur), a(slot_mean, f32, K, "slot_mean", cur),
+        a(slot_count, i64, K, "slot_count", cur), a(grad_student, f32, E * k, "grad_student", cur),
+        a(status, i32, 1, "status", cur), a(ws, ws.dtype, 0, "ws", cur), ws.numel() * ws.element_size(),
+        _loss_stream(torch, stream, cur)))
+
+
 class _PlanLosses:
     """Losses over the tiles of a pipeline's plan.  Output buffers and workspaces are kept and
-    reused, one set for policy and one for preference losses, and views of them are returned: a
+    reused, one set for each kind of loss, and views of them are returned: a
     call overwrites what the last one of its kind returned, and two of one kind must not be under
     way at once.  A call that needs larger ones than any before it waits for the device and
     replaces them, so it cannot be captured, and a graph captured before it is no longer valid.
@@ -784,6 +835,20 @@ class _PlanLosses:
         odb_preference_loss(tiles, PreferenceParams() if params is None else params, logprob, pair, loss, row_loss,
                             reward, counts, ws, ref_logprob, self.emit_order[tiles.rows], grad, status, stream)
         return loss, row_loss, reward, counts, grad
+
+    def distill_loss(self, tiles: Tiles, student, teacher, params: Optional[DistillParams] = None, slot_weight=None,
+                     stream=None):
+        """odb_distill_loss of a run's tiles: the student's and the teacher's log-probabilities of each token's
+        list, [elements, k].  Returns (loss per slot, divergence per slot, counted tokens per slot, gradient of the
+        student's log-probabilities [elements, k])."""
+        K, E, k = tiles.num_slots, tiles.num_elems, student.size(-1)
+        (ws, loss, mean, count, grad), status = self._loss_outputs("distill", {
+            "ws": (odb_distill_workspace_size(tiles, k), "uint8"), "loss": (K, "float32"), "mean": (K, "float32"),
+            "count": (K, "int64"), "grad": (E * k, "float32")})
+        grad = grad.view(E, k)
+        odb_distill_loss(tiles, DistillParams() if params is None else params, student, teacher, loss, mean, count, ws,
+                         slot_weight, grad, status, stream)
+        return loss, mean, count, grad
 
     def check_losses(self, stream=None):
         """Synchronises `stream` and raises if a loss since the last check met bad tiles or pairs."""

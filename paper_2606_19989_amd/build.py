@@ -14,7 +14,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libodb.so")
 SOURCES = ["odb_common.hip", "odb_form.hip", "odb_align.hip", "odb_collate.hip", "odb_weights.hip", "odb_sketch.hip",
            "odb_stream.hip", "odb_logprobs.hip", "odb_losses.hip", "odb_lists.hip",
-           "odb_top.hip"]
+           "odb_top.hip", "odb_distill.hip"]
 ARCH = os.environ.get("ODB_OFFLOAD_ARCH", "gfx950")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

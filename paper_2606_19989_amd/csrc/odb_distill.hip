@@ -1,0 +1,558 @@
+// Distillation loss over a run of a plan's tiles, with its gradient: per counted token a divergence between the
+// teacher's and the student's log-probabilities of the token's list, reduced and weighted per slot.
+//
+// A token's k entries lie on a group of L lanes, four each; what a token needs as a whole (sums of
+// probabilities, the value, the sum of slopes) is joined by a butterfly over those lanes.  The run's
+// elements are cut into pieces wherever slots end, a block each; what a piece adds to a slot is a partial of its
+// own, named piece + slot as the chunks' partials are, and partials are summed in a fixed order in 64 bits.
+// A mean's weight is known after a pass over the labels, the one that the policy loss makes.
+//
+// Bound by the reads of both lists and the writes of the gradient, 12 k bytes an element.
+#include <algorithm>
+
+#include "odb_slots.h"
+
+namespace odb {
+
+namespace {
+
+constexpr float kNone = -HUGE_VALF;          // a teacher's entry that is none
+constexpr double kRestLeast = 0x1p-24;       // of what a list leaves out
+constexpr int kMaxPiece = 512;               // elements of a piece
+constexpr int64_t kMaxDistillElems = (int64_t)1 << 32;     // 2^23 pieces: a grid's threads stay below 2^32
+
+struct DistillPart {
+    double sum;
+    int64_t counted;
+};
+
+struct DistillArgs : SlotCounts {
+    const float* student;
+    const float* teacher;
+    const double* slot_weight;
+    float* slot_loss;
+    float* slot_mean;
+    int64_t* slot_counted;
+    float* grad;
+    DistillPart* part;
+    int64_t pieces;
+    double loss_scale, mix;
+    int32_t piece, piece_log2;
+    int32_t k, kind, reduce;
+};
+
+// ------------------------------------------------------------------ a token
+typedef float float4a __attribute__((ext_vector_type(4), aligned(4)));
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_of(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp_of(double v) {
+    const long long u = __double_as_longlong(v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)u, CTRL, 0xf, 0xf, true);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xf, 0xf, true);
+    return __longlong_as_double((long long)(((unsigned long long)hi << 32) | lo));
+}
+
+// f over a group's L lanes, the same on each: neighbours, pairs, quads and eights exchange (the mirrors swap
+// halves whose lanes hold the same by then).
+template <int L, typename T, typename F>
+__device__ __forceinline__ T over_lanes(T v, const F& f) {
+    if (L > 1) v = f(v, dpp_of<0xb1>(v));       // quad_perm 1 0 3 2
+    if (L > 2) v = f(v, dpp_of<0x4e>(v));       // quad_perm 2 3 0 1
+    if (L > 4) v = f(v, dpp_of<0x141>(v));      // row_half_mirror
+    if (L > 8) v = f(v, dpp_of<0x140>(v));      // row_mirror
+    if (L > 16) v = f(v, __shfl_xor(v, 16, kWave));
+    return v;
+}
+template <int L, typename T>
+__device__ __forceinline__ T lanes_sum(T v) {
+    return over_lanes<L>(v, [](T a, T b) { return a + b; });
+}
+template <int L>
+__device__ __forceinline__ float lanes_max(float v) {
+    return over_lanes<L>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// A lane's four entries of a list of k, 4 l and on; those from k on hold anything.
+__device__ __forceinline__ void load_entries(const float* p, int k, int l, float v[4]) {
+    if (k < 4) {        // uniform
+#pragma unroll
+        for (int i = 0; i < 3; ++i) v[i] = p[i < k ? i : k - 1];
+        v[3] = v[2];
+        return;
+    }
+    const int at = 4 * l < k - 4 ? 4 * l : k - 4, by = 4 * l - at;
+    const float4a w = __builtin_nontemporal_load(reinterpret_cast<const float4a*>(p + at));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = w[i];
+    if (k & 3) {        // the last lane's four start up to three entries early
+        if (by & 1) {
+            v[0] = v[1];
+            v[1] = v[2];
+            v[2] = v[3];
+        }
+        if (by & 2) {
+            v[0] = v[2];
+            v[1] = v[3];
+        }
+    }
+}
+
+__device__ __forceinline__ void store_entries(float* p, int k, int l, const float v[4]) {
+    if (4 * l + 4 <= k) {
+        const float4a w = {v[0], v[1], v[2], v[3]};
+        __builtin_nontemporal_store(w, reinterpret_cast<float4a*>(p + 4 * l));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (4 * l + i < k) p[4 * l + i] = v[i];
+    }
+}
+
+// -ln(v + w e^d), v + w = 1: how far a mixture with weight w of a probability e^d times this one lies below this
+// one.  Far above, by ln (w + v e^-d), which no power leaves.
+__device__ __forceinline__ float below_mixture(float w, float v, float d) {
+    return d > 30.0f ? -(d + logf(fmaf(v, exp_near(-d), w))) : -log1pf(w * expm1f(d));
+}
+
+struct Mixture {
+    float w, v;      // the teacher's weight and the student's
+};
+
+// A divergence's term of one entry with log-probabilities t and s, and its slope by s; `plus` is the
+// constant of the reverse divergence's slope, which probabilities that sum to 1 cancel.
+template <bool MIX>
+__device__ __forceinline__ void entry(int kind, const Mixture& m, float t, float s, float p, float q, float plus, float* term,
+                                      float* slope) {
+    if (MIX) {
+        const float d = t - s;
+        const float less_p = below_mixture(m.v, m.w, -d), less_q = below_mixture(m.w, m.v, d);
+        *slope = q == 0.0f ? 0.0f : m.v * q * less_q;
+        *term = (p == 0.0f ? 0.0f : m.w * p * less_p) + *slope;
+    } else if (kind == ODB_DISTILL_FORWARD) {
+        *term = p == 0.0f ? 0.0f : p * (t - s);
+        *slope = -p;
+    } else {
+        *term = q == 0.0f ? 0.0f : q * (s - t);
+        *slope = fmaf(q, plus, *term);
+    }
+}
+
+// A counted token: its value on every lane of the group, and this lane's slopes.
+template <bool MIX, int SUPPORT, int L>
+__device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, int64_t e, int l, float slope[4]) {
+    float t[4], s[4], term[4], p[4], q[4];
+    bool there[4];
+    load_entries(A.teacher + e * A.k, A.k, l, t);
+    load_entries(A.student + e * A.k, A.k, l, s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        there[i] = 4 * l + i < A.k && t[i] != kNone;
+        if (!there[i]) t[i] = s[i] = kNone;
+    }
+    if (SUPPORT == ODB_SUPPORT_RENORMALIZED) {
+        float mt = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), ms = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+        mt = lanes_max<L>(mt);
+        ms = lanes_max<L>(ms);
+        float st = 0.0f, ss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            st += there[i] ? exp_near(t[i] - mt) : 0.0f;
+            ss += there[i] ? exp_near(s[i] - ms) : 0.0f;
+        }
+        const float lt = logf(lanes_sum<L>(st)), ls = logf(lanes_sum<L>(ss));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            t[i] = (t[i] - mt) - lt;
+            s[i] = (s[i] - ms) - ls;
+        }
+    }
+    float value = 0.0f, slopes = 0.0f;
+    double sum_p = 0.0, sum_q = 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (SUPPORT == ODB_SUPPORT_REST) {
+            const double dp = there[i] ? exp((double)t[i]) : 0.0, dq = there[i] ? exp((double)s[i]) : 0.0;
+            sum_p += dp;
+            sum_q += dq;
+            p[i] = (float)dp;
+            q[i] = (float)dq;
+        } else {
+            p[i] = exp_near(t[i]);
+            q[i] = exp_near(s[i]);
+        }
+        entry<MIX>(A.kind, m, t[i], s[i], p[i], q[i], SUPPORT == ODB_SUPPORT_LISTED ? 1.0f : 0.0f, &term[i], &slope[i]);
+        if (!there[i]) term[i] = slope[i] = q[i] = 0.0f;
+        value += term[i];
+        slopes += slope[i];
+    }
+    value = lanes_sum<L>(value);
+    if (SUPPORT == ODB_SUPPORT_RENORMALIZED) {
+        slopes = lanes_sum<L>(slopes);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) slope[i] = fmaf(-q[i], slopes, slope[i]);
+    }
+    if (SUPPORT != ODB_SUPPORT_REST) return value;
+    // what the lists leave out, as one more entry: 1 - sum cancels, so in 64 bits
+    double rp = 1.0 - lanes_sum<L>(sum_p), rq = 1.0 - lanes_sum<L>(sum_q);
+    const bool held = rq < kRestLeast || rq == kRestLeast;
+    if (rp < kRestLeast) rp = kRestLeast;      // a NaN stays
+    if (rq < kRestLeast) rq = kRestLeast;
+    const double d = log(rp) - log(rq);
+    double rest, by_log;       // its term, and its slope by the log, over rq; the reverse's less 1
+    if (MIX) {
+        by_log = -(1.0 - A.mix) * log1p(A.mix * expm1(d));      // |d| <= ln 2^24
+        rest = -A.mix * rp * log1p((1.0 - A.mix) * expm1(-d)) + rq * by_log;
+    } else if (A.kind == ODB_DISTILL_FORWARD) {
+        rest = rp * d;
+        by_log = -rp / rq;
+    } else {
+        rest = -rq * d;
+        by_log = -d;
+    }
+    // d rq = -q_j d s_j, unless it is held at its least
+    const float moves = held ? (!MIX && A.kind == ODB_DISTILL_REVERSE ? -1.0f : 0.0f) : (float)by_log;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) slope[i] = fmaf(-q[i], moves, slope[i]);
+    return value + rest;
+}
+
+// The block's tokens of a slot's elements [a0, a1): weight(row) gives a token's weight in the reduction and the
+// factor of its gradient, by its row counted from the slot's first.
+struct DistillSum {
+    double sum;
+    int counted;
+};
+
+template <bool MIX, int SUPPORT, int L, typename Weight>
+__device__ __forceinline__ DistillSum distill_span(const DistillArgs& A, const SlotView& s, int64_t a0, int64_t a1,
+                                                   const Weight& weight) {
+    constexpr int kStep = kBlock / L;      // tokens of the block at once
+    const int l = threadIdx.x & (L - 1);
+    const int row_a = (int)((a0 - s.lo) / s.maxlen);
+    const uint32_t col_a = (uint32_t)((a0 - s.lo) - (int64_t)row_a * s.maxlen), maxlen = (uint32_t)s.maxlen;
+    const int n = (int)(a1 - a0);
+    const Mixture m{(float)A.mix, (float)(1.0 - A.mix)};
+    DistillSum S{0.0, 0};
+    int o = threadIdx.x / L;
+    int32_t y = o < n ? A.t.d_labels[a0 + o] : ODB_LABEL_IGNORE;
+    for (; o < n; o += kStep) {
+        const int32_t label = y;
+        if (o + kStep < n) y = A.t.d_labels[a0 + o + kStep];      // on its way beside this token
+        const uint32_t x = col_a + (uint32_t)o, r = x / maxlen;
+        const bool on = label != ODB_LABEL_IGNORE && x - r * maxlen >= (uint32_t)A.t.shift;
+        float g[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (on) {
+            const double value = token<MIX, SUPPORT, L>(A, m, a0 + o, l, g);
+            double f;
+            float gs;
+            weight(row_a + (int)r, &f, &gs);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) g[i] *= gs;
+            if (l == 0) {
+                S.sum += value * f;
+                ++S.counted;
+            }
+        }
+        if (A.grad) store_entries(A.grad + (a0 + o) * A.k, A.k, l, g);
+    }
+    return S;
+}
+
+__device__ __forceinline__ void leave_slot(const DistillArgs& A, int64_t k, double sum, int64_t counted) {
+    const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
+    A.slot_loss[k] = counted > 0 ? (float)(scale * sum) : 0.0f;
+    A.slot_mean[k] = (float)sum;
+    A.slot_counted[k] = counted;
+}
+
+// ------------------------------------------------------------------ the passes
+template <bool MIX, int SUPPORT, int L>
+__global__ void __launch_bounds__(kBlock) distill_kernel(DistillArgs A) {
+    __shared__ double s_weight[kMaxPiece];
+    const odb_tiles_t& t = A.t;
+    if (blockIdx.x >= A.pieces) return check_slots(t, blockIdx.x - A.pieces, A.disorder, A.check_blocks, NoVisit{});
+    const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
+    const int64_t total = run_elems(t, e_base);
+    const int64_t b = blockIdx.x, c0 = b << A.piece_log2, c1 = c0 + A.piece < total ? c0 + A.piece : total;
+    if (c0 >= c1) return;
+    each_slot(t, e_base, r_base, slot_at(t, e_base, A.reduce == ODB_REDUCE_SUM ? 0 : A.chunk_slot[c0 >> A.chunk_log2], c0),
+              c0, c1, [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+        const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
+        const int row_a = (int)((a0 - s.lo) / s.maxlen), here = (int)((a1 - 1 - s.lo) / s.maxlen) - row_a + 1;
+        double same = 1.0;       // weight of every token, where rows have none of their own
+        if (A.reduce == ODB_REDUCE_TOKEN_MEAN) {
+            const double n = slot_counted<false>(A, s, k);
+            same = n > 0 ? 1.0 / n : 0.0;
+        } else if (A.reduce == ODB_REDUCE_ROW_MEAN) {
+            const double rows = slot_counted<true>(A, s, k);
+            auto of_count = [&](double n) { return n > 0 ? 1.0 / (n * rows) : 0.0; };
+            // only the first and the last of the rows here may be long; below 0: not
+            double w_first = -1.0, w_last = -1.0;
+            const RowChunks first(A, s, row_a), last(A, s, row_a + here - 1);
+            if (first.last - first.first >= kLongRow) w_first = of_count(long_row_tokens(A, s, row_a, first));
+            if (here > 1 && last.last - last.first >= kLongRow)
+                w_last = of_count(long_row_tokens(A, s, row_a + here - 1, last));
+            __syncthreads();      // the slot before this one has read its weights
+            for (int i = threadIdx.x; i < here; i += kBlock) {
+                const double w = i == 0 ? w_first : i == here - 1 ? w_last : -1.0;
+                s_weight[i] = w >= 0.0 ? w : of_count(row_tokens(A, s, row_a + i));
+            }
+            __syncthreads();
+        }
+        const float factor = (float)(scale * same);
+        const DistillSum S = distill_span<MIX, SUPPORT, L>(A, s, a0, a1, [&](int row, double* f, float* gs) {
+            *f = same;
+            *gs = factor;
+            if (A.reduce == ODB_REDUCE_ROW_MEAN) {
+                *f = s_weight[row - row_a];
+                *gs = (float)(scale * *f);
+            }
+        });
+        const double sum = block_total(S.sum);
+        const int counted = block_total(S.counted);
+        if (threadIdx.x == 0) A.part[b + k] = {sum, counted};
+    });
+}
+
+// The slots' numbers from their pieces' partials, G threads a slot.
+template <int G>
+__global__ void __launch_bounds__(kBlock) distill_slots_kernel(DistillArgs A) {
+    const odb_tiles_t& t = A.t;
+    const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
+    const int i = threadIdx.x & (G - 1);
+    const uint32_t disorder = disorder_words(A.disorder, A.check_blocks);
+    for (int64_t k = (int64_t)blockIdx.x * (kBlock / G) + __builtin_amdgcn_readfirstlane(threadIdx.x / G); k < t.num_slots;
+         k += (int64_t)gridDim.x * (kBlock / G)) {
+        const SlotView s = slot_view(t, k, e_base, r_base);
+        double sum = 0.0, n = 0.0;      // whole numbers below 2^41
+        if (!s.ok) {
+            if (A.status && i == 0) *A.status = kErrTiles;
+        } else if (s.hi > s.lo) {
+#pragma unroll 4
+            for (int64_t j = (s.lo >> A.piece_log2) + i; j <= (s.hi - 1) >> A.piece_log2; j += G) {
+                sum += A.part[j + k].sum;
+                n += (double)A.part[j + k].counted;
+            }
+        }
+        sum = G == kBlock ? block_total(sum) : wave_total(sum);
+        n = G == kBlock ? block_total(n) : wave_total(n);
+        if (__any(disorder)) sum = n = 0.0;
+        if (i == 0) leave_slot(A, k, sum, (int64_t)n);
+    }
+}
+
+// A run of few elements, in one launch of one block.
+constexpr int kOneElems = 1024;
+constexpr int kOneEntries = 8192;
+constexpr int kOneSlots = 1024;
+
+template <bool MIX, int SUPPORT, int L>
+__global__ void __launch_bounds__(kBlock) distill_one_kernel(DistillArgs A) {
+    __shared__ int s_rows[kOneElems];
+    const odb_tiles_t& t = A.t;
+    const int64_t e_base = t.d_slot_tile_off[0], r_base = t.d_slot_row_off[0];
+    for (int64_t k = threadIdx.x; k < t.num_slots; k += kBlock) {
+        leave_slot(A, k, 0.0, 0);
+        if (A.status && !slot_view(t, k, e_base, r_base).ok) *A.status = kErrTiles;
+    }
+    __syncthreads();
+    if (t.num_elems == 0) return;
+    each_slot(t, e_base, r_base, first_slot(t, e_base, 0), 0, t.num_elems,
+              [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
+        const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
+        int count = 0;
+        if (A.reduce != ODB_REDUCE_SUM) {
+            __syncthreads();      // the slot before this one has read its rows
+            for (int i = threadIdx.x; i < s.rows; i += kBlock) s_rows[i] = 0;
+            __syncthreads();
+            for (int o = threadIdx.x; o < a1 - a0; o += kBlock) {
+                const int r = o / s.maxlen;
+                if (t.d_labels[a0 + o] != ODB_LABEL_IGNORE && o - r * s.maxlen >= t.shift) {
+                    ++count;
+                    if (A.reduce == ODB_REDUCE_ROW_MEAN) atomicAdd(&s_rows[r], 1);
+                }
+            }
+            __syncthreads();
+            if (A.reduce == ODB_REDUCE_ROW_MEAN) {
+                count = 0;
+                for (int i = threadIdx.x; i < s.rows; i += kBlock) count += s_rows[i] > 0;
+            }
+            count = block_total(count);
+        }
+        const double same = A.reduce == ODB_REDUCE_SUM ? 1.0 : count > 0 ? 1.0 / count : 0.0;
+        const DistillSum S = distill_span<MIX, SUPPORT, L>(A, s, a0, a1, [&](int row, double* f, float* gs) {
+            *f = A.reduce == ODB_REDUCE_ROW_MEAN ? 1.0 / ((double)s_rows[row] * count) : same;
+            *gs = (float)(scale * *f);
+        });
+        const double sum = block_total(S.sum);
+        const int counted = block_total(S.counted);
+        if (threadIdx.x == 0) leave_slot(A, k, sum, counted);
+    });
+}
+
+// ------------------------------------------------------------------ host
+// Elements of a piece, a power of two.
+int32_t piece_for(int64_t elems, int32_t k) {
+    int32_t piece = 32;
+#ifndef ODB_PIECE
+#define ODB_PIECE 4096
+#endif
+    while (piece < kMaxPiece && elems / piece >= ODB_PIECE) piece *= 2;
+    (void)k;
+    return piece;
+}
+
+struct DistillLayout {
+    size_t chunk_slot, slot_count, row_count, part, disorder, total;
+    int64_t chunks, pieces;
+    int32_t chunk, piece;
+};
+
+DistillLayout distill_layout(const odb_tiles_t* t, int32_t k) {
+    DistillLayout L;
+    size_t o = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t at = o;
+        o = (o + (size_t)(bytes > 0 ? bytes : 1) + 255) & ~size_t(255);
+        return at;
+    };
+    L.chunk = chunk_for(t->num_elems);
+    L.chunks = (t->num_elems + L.chunk - 1) / L.chunk;
+    L.piece = piece_for(t->num_elems, k);
+    L.pieces = (t->num_elems + L.piece - 1) / L.piece;
+    L.chunk_slot = take(4 * L.chunks);
+    L.slot_count = take(4 * (L.chunks + t->num_slots));
+    L.row_count = take(4 * (L.chunks + t->num_rows));
+    L.part = take((int64_t)sizeof(DistillPart) * (L.pieces + t->num_slots));
+    L.disorder = take(4 * kCheckBlocks * kWaves);
+    L.total = o;
+    return L;
+}
+
+int check_distill_tiles(const odb_tiles_t* t, int32_t k) {
+    ODB_TRY(check_tiles(t));
+    if (k < 1 || k > ODB_LIST_MAX) return set_error(ODB_E_INVALID_ARG, "k must be in [1, %d] (got %d)", ODB_LIST_MAX, k);
+    if (t->num_elems > kMaxDistillElems)
+        return set_error(ODB_E_INVALID_ARG, "num_elems must be at most 2^32 for lists");
+    return ODB_OK;
+}
+
+using DistillKernel = void (*)(DistillArgs);
+#define ODB_DISTILL_LANES(KERNEL, MIX, SUPPORT) \
+    {KERNEL<MIX, SUPPORT, 1>, KERNEL<MIX, SUPPORT, 2>, KERNEL<MIX, SUPPORT, 4>, KERNEL<MIX, SUPPORT, 8>, \
+     KERNEL<MIX, SUPPORT, 16>, KERNEL<MIX, SUPPORT, 32>}
+#define ODB_DISTILL_KERNELS(KERNEL) \
+    {{ODB_DISTILL_LANES(KERNEL, false, 0), ODB_DISTILL_LANES(KERNEL, false, 1), ODB_DISTILL_LANES(KERNEL, false, 2)}, \
+     {ODB_DISTILL_LANES(KERNEL, true, 0), ODB_DISTILL_LANES(KERNEL, true, 1), ODB_DISTILL_LANES(KERNEL, true, 2)}}
+// by mixture, odb_support_t and the log of a token's lanes
+const DistillKernel distill_kernels[2][3][6] = ODB_DISTILL_KERNELS(distill_kernel);
+const DistillKernel distill_one_kernels[2][3][6] = ODB_DISTILL_KERNELS(distill_one_kernel);
+#undef ODB_DISTILL_KERNELS
+#undef ODB_DISTILL_LANES
+
+}  // namespace
+
+}  // namespace odb
+
+using namespace odb;
+
+extern "C" size_t odb_distill_workspace_size(const odb_tiles_t* t, int32_t k) {
+    if (check_distill_tiles(t, k) != ODB_OK) return 0;
+    return distill_layout(t, k).total;
+}
+
+extern "C" int odb_distill_loss(const odb_tiles_t* t, const odb_distill_params_t* p, int32_t k, const float* d_student,
+                                const float* d_teacher, const double* d_slot_weight, float* d_slot_loss,
+                                float* d_slot_mean, int64_t* d_slot_count, float* d_grad_student, int32_t* d_status,
+                                void* d_ws, size_t ws_bytes, void* stream) {
+    ODB_TRY(check_distill_tiles(t, k));
+    if (!p) return set_error(ODB_E_INVALID_ARG, "params is NULL");
+    if (p->kind < ODB_DISTILL_FORWARD || p->kind > ODB_DISTILL_MIXTURE)
+        return set_error(ODB_E_INVALID_ARG, "unknown divergence %d", p->kind);
+    if (p->support < ODB_SUPPORT_LISTED || p->support > ODB_SUPPORT_REST)
+        return set_error(ODB_E_INVALID_ARG, "unknown support %d", p->support);
+    if (p->reduce < ODB_REDUCE_TOKEN_MEAN || p->reduce > ODB_REDUCE_SUM)
+        return set_error(ODB_E_INVALID_ARG, "unknown reduction %d", p->reduce);
+    if (p->reserved0 != 0) return set_error(ODB_E_INVALID_ARG, "params.reserved0 must be 0");
+    const bool mix = p->kind == ODB_DISTILL_MIXTURE;
+    // both weights are used in 32 bits
+    if (mix && !((float)p->mix > 0.0f && (float)(1.0 - p->mix) > 0.0f && p->mix < 1.0))
+        return set_error(ODB_E_INVALID_ARG, "mix must be inside (0, 1)");
+    if (!std::isfinite(p->loss_scale)) return set_error(ODB_E_INVALID_ARG, "loss_scale must be finite");
+    if (t->num_slots == 0) return ODB_OK;
+    ODB_TRY(check_tile_arrays(t));
+    if (!d_slot_loss || !d_slot_mean || !d_slot_count)
+        return set_error(ODB_E_INVALID_ARG, "d_slot_loss, d_slot_mean and d_slot_count must not be NULL");
+    if (t->num_elems > 0 && (!d_student || !d_teacher))
+        return set_error(ODB_E_INVALID_ARG, "d_student and d_teacher must not be NULL");
+    if (!d_ws) return set_error(ODB_E_INVALID_ARG, "workspace is NULL");
+    if (reinterpret_cast<uintptr_t>(d_ws) & 255)
+        return set_error(ODB_E_INVALID_ARG, "workspace must be 256-byte aligned");
+    const DistillLayout L = distill_layout(t, k);
+    if (ws_bytes < L.total)
+        return set_error(ODB_E_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, L.total);
+
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    DistillArgs a{};
+    a.t = *t;
+    a.chunk_slot = ws_at<int32_t>(d_ws, L.chunk_slot);
+    a.slot_count = ws_at<int32_t>(d_ws, L.slot_count);
+    a.row_count = ws_at<int32_t>(d_ws, L.row_count);
+    a.disorder = ws_at<uint32_t>(d_ws, L.disorder);
+    a.status = d_status;
+    a.chunks = L.chunks;
+    a.check_blocks = L.chunks > 0 ? check_blocks(t->num_slots) : 0;
+    a.counts = L.chunks >= kManyChunks ? kWave : kMaxElems;
+    a.chunk = L.chunk;
+    a.chunk_log2 = __builtin_ctz((unsigned)L.chunk);
+    a.student = d_student;
+    a.teacher = d_teacher;
+    a.slot_weight = d_slot_weight;
+    a.slot_loss = d_slot_loss;
+    a.slot_mean = d_slot_mean;
+    a.slot_counted = d_slot_count;
+    a.grad = d_grad_student;
+    a.part = ws_at<DistillPart>(d_ws, L.part);
+    a.pieces = L.pieces;
+    a.loss_scale = p->loss_scale;
+    a.mix = mix ? p->mix : 0.5;
+    a.piece = L.piece;
+    a.piece_log2 = __builtin_ctz((unsigned)L.piece);
+    a.k = k;
+    a.kind = p->kind;
+    a.reduce = p->reduce;
+    int lanes = 0;
+    while ((4 << lanes) < k) ++lanes;
+    const dim3 block(kBlock);
+    if (t->num_elems <= kOneElems && t->num_elems * k <= kOneEntries && t->num_slots <= kOneSlots) {
+        hipLaunchKernelGGL(distill_one_kernels[mix][p->support][lanes], dim3(1), block, 0, s, a);
+        ODB_LAUNCHED();
+        return ODB_OK;
+    }
+    if (L.chunks > 0 && p->reduce != ODB_REDUCE_SUM) {
+        hipLaunchKernelGGL((p->reduce == ODB_REDUCE_ROW_MEAN ? slot_count_kernel<true, false>
+                                                              : slot_count_kernel<false, false>),
+                           dim3((unsigned)(L.chunks + a.check_blocks)), block, 0, s, static_cast<const SlotCounts&>(a));
+        ODB_LAUNCHED();
+        if (a.counts == kWave) {
+            hipLaunchKernelGGL(p->reduce == ODB_REDUCE_ROW_MEAN ? slot_fold_kernel<true> : slot_fold_kernel<false>,
+                               dim3(grid_for(t->num_slots, 1)), block, 0, s, static_cast<const SlotCounts&>(a));
+            ODB_LAUNCHED();
+        }
+    }
+    if (L.pieces > 0) {     // at most 2^23 of them, and the blocks that look over the slots
+        hipLaunchKernelGGL(distill_kernels[mix][p->support][lanes],
+                           dim3((unsigned)(L.pieces + (p->reduce == ODB_REDUCE_SUM ? a.check_blocks : 0))), block, 0, s, a);
+        ODB_LAUNCHED();
+    }
+    if (t->num_slots <= 4096)
+        hipLaunchKernelGGL((distill_slots_kernel<kBlock>), dim3(grid_for(t->num_slots, 1)), block, 0, s, a);
+    else
+        hipLaunchKernelGGL((distill_slots_kernel<kWave>), dim3(grid_for(t->num_slots, kWaves)), block, 0, s, a);
+    ODB_LAUNCHED();
+    return ODB_OK;
+}

@@ -122,3 +122,75 @@ def test_reference_of_ties():
     row = np.array([1.0, 3.0, -np.inf, 3.0, 1.0, 0.0])
     assert ref.top(row, 4).tolist() == [1, 3, 0, 4] and ref.top(row, 9).tolist() == [1, 3, 0, 4, 5]
     assert [ref.rank(row, y) for y in range(6)] == [2, 0, 5, 1, 3, 4]
+
+
+def _tiles(**kw):
+    from test_losses_host import _tiles as tiles
+    return tiles(**kw)
+
+
+def _distill(t=None, p=None, k=4, student=P, teacher=P, w=None, loss=P, mean=P, count=P, grad=P, ws=P, ws_bytes=1 << 40):
+    return odb.load().odb_distill_loss(byref(t or _tiles()), byref(p or odb.DistillParams()), k, student, teacher, w, loss,
+                                       mean, count, grad, None, ws, ws_bytes, None)
+
+
+def test_distill_arguments_refused():
+    from test_losses_host import BAD_ARRAYS, BAD_TILES
+    lib = odb.load()
+    for bad in BAD_TILES + [dict(num_elems=(1 << 32) + 1)]:
+        assert _distill(_tiles(**bad)) == BAD, bad
+        assert lib.odb_distill_workspace_size(byref(_tiles(**bad)), 4) == 0
+    for bad in BAD_ARRAYS:
+        assert _distill(_tiles(**bad)) == BAD, bad
+    for bad in (dict(kind=3), dict(kind=-1), dict(support=3), dict(support=-1), dict(reduce=3), dict(reduce=-1),
+                dict(reserved0=1), dict(kind=2, mix=0.0), dict(kind=2, mix=1.0), dict(kind=2, mix=float("nan")),
+                dict(kind=2, mix=1e-60), dict(kind=2, mix=-0.5), dict(loss_scale=float("inf")),
+                dict(loss_scale=float("nan"))):
+        assert _distill(p=odb.DistillParams(**bad)) == BAD, bad
+    for bad in (dict(k=0), dict(k=odb.ODB_LIST_MAX + 1), dict(student=None), dict(teacher=None), dict(loss=None),
+                dict(mean=None), dict(count=None), dict(ws=None), dict(ws=P + 8)):
+        assert _distill(**bad) == BAD, bad
+    size = lib.odb_distill_workspace_size(byref(_tiles()), 4)
+    assert size > 0 and _distill(ws_bytes=size - 1) == odb.ODB_E_WORKSPACE
+    for k in (0, odb.ODB_LIST_MAX + 1):
+        assert lib.odb_distill_workspace_size(byref(_tiles()), k) == 0
+    assert lib.odb_distill_workspace_size(None, 4) == 0
+    # no slots: nothing to do
+    assert _distill(_tiles(num_slots=0), loss=None, mean=None, count=None, student=None, ws=None) == odb.ODB_OK
+    # a workspace grows with the run
+    sizes = [lib.odb_distill_workspace_size(byref(_tiles(num_elems=n)), 4) for n in (50, 1 << 20, 1 << 32)]
+    assert sizes[0] < sizes[1] < sizes[2]
+
+
+@pytest.mark.parametrize("kind", [0, 1, 2])
+@pytest.mark.parametrize("support", [0, 1, 2])
+def test_reference_divergence_is_one(kind, support):
+    """Against the definition in probabilities, its slopes against differences; 0 and flat where both agree."""
+    rng = np.random.default_rng(kind * 3 + support)
+    w = 0.3
+    for _ in range(20):
+        t = np.log(rng.dirichlet(np.ones(7))[:6] * 0.98)
+        s = np.log(rng.dirichlet(np.ones(7))[:6] * 0.98)
+        t[rng.integers(6)] = -np.inf
+        on = t > -np.inf
+
+        def value(s):
+            p, q = np.exp(t[on]), np.exp(s[on])
+            if support == 1:
+                p, q = p / p.sum(), q / q.sum()
+            elif support == 2:
+                p, q = np.append(p, 1 - p.sum()), np.append(q, 1 - q.sum())
+            kl = lambda a, b: float((a * np.log(a / b)).sum())
+            m = w * p + (1 - w) * q
+            return [kl(p, q), kl(q, p), w * kl(p, m) + (1 - w) * kl(q, m)][kind]
+
+        v, g, _, _ = ref.distill_token(t, s, kind, support, w)
+        assert abs(v - value(s)) < 1e-12
+        for j in range(6):
+            up, down = s.copy(), s.copy()
+            up[j] += 1e-6
+            down[j] -= 1e-6
+            assert abs((value(up) - value(down)) / 2e-6 - g[j]) < 1e-7
+        if support:
+            v, g, _, _ = ref.distill_token(t, np.where(on, t, 0.0), kind, support, w)
+            assert abs(v) < 1e-12 and np.abs(g).max() < 1e-12
