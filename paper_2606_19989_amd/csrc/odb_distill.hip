@@ -112,39 +112,69 @@ __device__ __forceinline__ void store_entries(float* p, int k, int l, const floa
     }
 }
 
-// -ln(v + w e^d), v + w = 1: how far a mixture with weight w of a probability e^d times this one lies below this
-// one.  Far above, by ln (w + v e^-d), which no power leaves.
-__device__ __forceinline__ float below_mixture(float w, float v, float d) {
-    return d > 30.0f ? -(d + logf(fmaf(v, exp_near(-d), w))) : -log1pf(w * expm1f(d));
-}
-
 struct Mixture {
     float w, v;      // the teacher's weight and the student's
 };
 
+// An entry's probabilities.  Both, and what the mixture is of them, need two powers: that of the larger log and of
+// the logs' distance d.
+struct Entry {
+    float p, q;
+    float d;         // ln p - ln q
+    float ratio;     // of the smaller to the larger
+};
+
+// How far the mixture lies below p and below q, in logs: -ln (w + v q / p), or the same from the other side; the
+// two differ by d.
+__device__ __forceinline__ void below(const Mixture& m, float d, float ratio, float* less_p, float* less_q) {
+    const bool more = d >= 0.0f;      // p is the larger
+    const float x = -logf(more ? fmaf(m.v, ratio, m.w) : fmaf(m.w, ratio, m.v));
+    *less_p = more ? x : x + d;
+    *less_q = more ? x - d : x;
+}
+
 // A divergence's term of one entry with log-probabilities t and s, and its slope by s; `plus` is the
 // constant of the reverse divergence's slope, which probabilities that sum to 1 cancel.
 template <bool MIX>
-__device__ __forceinline__ void entry(int kind, const Mixture& m, float t, float s, float p, float q, float plus, float* term,
-                                      float* slope) {
+__device__ __forceinline__ void entry(int kind, const Mixture& m, const Entry& x, float plus, float* term, float* slope) {
     if (MIX) {
-        const float d = t - s;
-        const float less_p = below_mixture(m.v, m.w, -d), less_q = below_mixture(m.w, m.v, d);
-        *slope = q == 0.0f ? 0.0f : m.v * q * less_q;
-        *term = (p == 0.0f ? 0.0f : m.w * p * less_p) + *slope;
+        float less_p, less_q;
+        below(m, x.d, x.ratio, &less_p, &less_q);
+        *slope = x.q == 0.0f ? 0.0f : m.v * x.q * less_q;
+        *term = (x.p == 0.0f ? 0.0f : m.w * x.p * less_p) + *slope;
     } else if (kind == ODB_DISTILL_FORWARD) {
-        *term = p == 0.0f ? 0.0f : p * (t - s);
-        *slope = -p;
+        *term = x.p == 0.0f ? 0.0f : x.p * x.d;
+        *slope = -x.p;
     } else {
-        *term = q == 0.0f ? 0.0f : q * (s - t);
-        *slope = fmaf(q, plus, *term);
+        *term = x.q == 0.0f ? 0.0f : -x.q * x.d;
+        *slope = fmaf(x.q, plus, *term);
     }
+}
+
+// exp in 64 bits to 2^-40, for sums of probabilities that are taken from 1: 2^n exp(g), |g| <= ln 2 / 2, by the
+// series up to g^10.
+__device__ __forceinline__ double exp_sum(float t) {
+    double u = (double)t * 1.4426950408889634074;
+    u = u < -1000.0 ? -1000.0 : u;      // 0; a NaN stays
+    const double n = rint(u), g = (u - n) * 0.69314718055994530942;
+    double e = 1.0 / 3628800.0;
+    e = fma(e, g, 1.0 / 362880.0);
+    e = fma(e, g, 1.0 / 40320.0);
+    e = fma(e, g, 1.0 / 5040.0);
+    e = fma(e, g, 1.0 / 720.0);
+    e = fma(e, g, 1.0 / 120.0);
+    e = fma(e, g, 1.0 / 24.0);
+    e = fma(e, g, 1.0 / 6.0);
+    e = fma(e, g, 0.5);
+    e = fma(e, g, 1.0);
+    e = fma(e, g, 1.0);
+    return ldexp(e, (int)n);
 }
 
 // A counted token: its value on every lane of the group, and this lane's slopes.
 template <bool MIX, int SUPPORT, int L>
 __device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, int64_t e, int l, float slope[4]) {
-    float t[4], s[4], term[4], p[4], q[4];
+    float t[4], s[4], q[4];
     bool there[4];
     load_entries(A.teacher + e * A.k, A.k, l, t);
     load_entries(A.student + e * A.k, A.k, l, s);
@@ -174,19 +204,28 @@ __device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, 
     double sum_p = 0.0, sum_q = 0.0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        Entry x{0.0f, 0.0f, t[i] - s[i], 0.0f};
         if (SUPPORT == ODB_SUPPORT_REST) {
-            const double dp = there[i] ? exp((double)t[i]) : 0.0, dq = there[i] ? exp((double)s[i]) : 0.0;
-            sum_p += dp;
-            sum_q += dq;
-            p[i] = (float)dp;
-            q[i] = (float)dq;
+            const double p = there[i] ? exp_sum(t[i]) : 0.0, q = there[i] ? exp_sum(s[i]) : 0.0;
+            sum_p += p;
+            sum_q += q;
+            x.p = (float)p;
+            x.q = (float)q;
+            if (MIX) x.ratio = exp_near(-fabsf(x.d));
+        } else if (MIX) {
+            const float larger = exp_near(x.d >= 0.0f ? t[i] : s[i]);
+            x.ratio = exp_near(-fabsf(x.d));
+            x.p = x.d >= 0.0f ? larger : larger * x.ratio;
+            x.q = x.d >= 0.0f ? larger * x.ratio : larger;
         } else {
-            p[i] = exp_near(t[i]);
-            q[i] = exp_near(s[i]);
+            x.p = exp_near(t[i]);
+            x.q = exp_near(s[i]);
         }
-        entry<MIX>(A.kind, m, t[i], s[i], p[i], q[i], SUPPORT == ODB_SUPPORT_LISTED ? 1.0f : 0.0f, &term[i], &slope[i]);
-        if (!there[i]) term[i] = slope[i] = q[i] = 0.0f;
-        value += term[i];
+        float term;
+        entry<MIX>(A.kind, m, x, SUPPORT == ODB_SUPPORT_LISTED ? 1.0f : 0.0f, &term, &slope[i]);
+        if (!there[i]) term = slope[i] = x.q = 0.0f;
+        q[i] = x.q;
+        value += term;
         slopes += slope[i];
     }
     value = lanes_sum<L>(value);
@@ -196,28 +235,22 @@ __device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, 
         for (int i = 0; i < 4; ++i) slope[i] = fmaf(-q[i], slopes, slope[i]);
     }
     if (SUPPORT != ODB_SUPPORT_REST) return value;
-    // what the lists leave out, as one more entry: 1 - sum cancels, so in 64 bits
+    // what the lists leave out, as one more entry: 1 - sum cancels, so it is taken in 64 bits
     double rp = 1.0 - lanes_sum<L>(sum_p), rq = 1.0 - lanes_sum<L>(sum_q);
-    const bool held = rq < kRestLeast || rq == kRestLeast;
+    const bool held = rq <= kRestLeast;
     if (rp < kRestLeast) rp = kRestLeast;      // a NaN stays
     if (rq < kRestLeast) rq = kRestLeast;
-    const double d = log(rp) - log(rq);
-    double rest, by_log;       // its term, and its slope by the log, over rq; the reverse's less 1
-    if (MIX) {
-        by_log = -(1.0 - A.mix) * log1p(A.mix * expm1(d));      // |d| <= ln 2^24
-        rest = -A.mix * rp * log1p((1.0 - A.mix) * expm1(-d)) + rq * by_log;
-    } else if (A.kind == ODB_DISTILL_FORWARD) {
-        rest = rp * d;
-        by_log = -rp / rq;
-    } else {
-        rest = -rq * d;
-        by_log = -d;
-    }
-    // d rq = -q_j d s_j, unless it is held at its least
-    const float moves = held ? (!MIX && A.kind == ODB_DISTILL_REVERSE ? -1.0f : 0.0f) : (float)by_log;
+    Entry rest{(float)rp, (float)rq, 0.0f, 0.0f};
+    const float times = rest.p / rest.q;
+    rest.d = logf(times);
+    if (MIX) rest.ratio = rest.d >= 0.0f ? rest.q / rest.p : times;
+    float term, by;
+    entry<MIX>(A.kind, m, rest, 0.0f, &term, &by);
+    // d rq = -q_j d s_j, unless it is held at its least; there the reverse's slopes keep their constant
+    const float moves = !held ? by / rest.q : !MIX && A.kind == ODB_DISTILL_REVERSE ? -1.0f : 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) slope[i] = fmaf(-q[i], moves, slope[i]);
-    return value + rest;
+    return (double)value + (double)term;
 }
 
 // The block's tokens of a slot's elements [a0, a1): weight(row) gives a token's weight in the reduction and the
