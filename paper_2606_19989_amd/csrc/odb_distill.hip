@@ -18,6 +18,9 @@ namespace {
 
 constexpr float kNone = -HUGE_VALF;          // a teacher's entry that is none
 constexpr double kRestLeast = 0x1p-24;       // of what a list leaves out
+#ifndef DW
+#define DW 1
+#endif
 constexpr int kMaxPiece = 512;               // elements of a piece
 constexpr int64_t kMaxDistillElems = (int64_t)1 << 32;     // 2^23 pieces: a grid's threads stay below 2^32
 
@@ -151,24 +154,27 @@ __device__ __forceinline__ void entry(int kind, const Mixture& m, const Entry& x
     }
 }
 
-// exp in 64 bits to 2^-40, for sums of probabilities that are taken from 1: 2^n exp(g), |g| <= ln 2 / 2, by the
-// series up to g^10.
-__device__ __forceinline__ double exp_sum(float t) {
-    double u = (double)t * 1.4426950408889634074;
-    u = u < -1000.0 ? -1000.0 : u;      // 0; a NaN stays
-    const double n = rint(u), g = (u - n) * 0.69314718055994530942;
-    double e = 1.0 / 3628800.0;
-    e = fma(e, g, 1.0 / 362880.0);
-    e = fma(e, g, 1.0 / 40320.0);
-    e = fma(e, g, 1.0 / 5040.0);
-    e = fma(e, g, 1.0 / 720.0);
-    e = fma(e, g, 1.0 / 120.0);
-    e = fma(e, g, 1.0 / 24.0);
-    e = fma(e, g, 1.0 / 6.0);
-    e = fma(e, g, 0.5);
-    e = fma(e, g, 1.0);
-    e = fma(e, g, 1.0);
-    return ldexp(e, (int)n);
+// exp of four numbers in 64 bits to 2^-40, for sums of probabilities that are taken from 1: 2^n exp(g),
+// |g| <= ln 2 / 2, by the series up to g^10.  Together, so that a coefficient is there for all.
+__device__ __forceinline__ void exp_sums(const float t[4], double e[4]) {
+    double g[4];
+    int n[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float x = t[i] < -700.0f ? -700.0f : t[i];      // as good as 0; a NaN stays
+        const float by = rintf(x * kLog2e);
+        n[i] = (int)by;
+        g[i] = fma((double)by, -0.69314718055994530942, (double)x);
+        e[i] = 1.0 / 3628800.0;
+    }
+    const double c[10] = {1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0,
+                          1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+#pragma unroll
+    for (int j = 0; j < 10; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = fma(e[i], g[i], c[j]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = ldexp(e[i], n[i]);
 }
 
 // A counted token: its value on every lane of the group, and this lane's slopes.
@@ -201,16 +207,19 @@ __device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, 
         }
     }
     float value = 0.0f, slopes = 0.0f;
-    double sum_p = 0.0, sum_q = 0.0;
+    double sum_p = 0.0, sum_q = 0.0, wide_p[4], wide_q[4];
+    if (SUPPORT == ODB_SUPPORT_REST) {
+        exp_sums(t, wide_p);
+        exp_sums(s, wide_q);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         Entry x{0.0f, 0.0f, t[i] - s[i], 0.0f};
         if (SUPPORT == ODB_SUPPORT_REST) {
-            const double p = there[i] ? exp_sum(t[i]) : 0.0, q = there[i] ? exp_sum(s[i]) : 0.0;
-            sum_p += p;
-            sum_q += q;
-            x.p = (float)p;
-            x.q = (float)q;
+            sum_p += wide_p[i];
+            sum_q += wide_q[i];
+            x.p = (float)wide_p[i];
+            x.q = (float)wide_q[i];
             if (MIX) x.ratio = exp_near(-fabsf(x.d));
         } else if (MIX) {
             const float larger = exp_near(x.d >= 0.0f ? t[i] : s[i]);
@@ -304,7 +313,7 @@ __device__ __forceinline__ void leave_slot(const DistillArgs& A, int64_t k, doub
 
 // ------------------------------------------------------------------ the passes
 template <bool MIX, int SUPPORT, int L>
-__global__ void __launch_bounds__(kBlock) distill_kernel(DistillArgs A) {
+__global__ void __launch_bounds__(kBlock, DW) distill_kernel(DistillArgs A) {
     __shared__ double s_weight[kMaxPiece];
     const odb_tiles_t& t = A.t;
     if (blockIdx.x >= A.pieces) return check_slots(t, blockIdx.x - A.pieces, A.disorder, A.check_blocks, NoVisit{});
