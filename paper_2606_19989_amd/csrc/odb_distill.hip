@@ -7,7 +7,11 @@
 // own, named piece + slot as the chunks' partials are, and partials are summed in a fixed order in 64 bits.
 // A mean's weight is known after a pass over the labels, the one that the policy loss makes.
 //
-// Bound by the reads of both lists and the writes of the gradient, 12 k bytes an element.
+// Bound by the reads of both lists and the writes of the gradient, 12 k bytes an element, and beside them by the
+// powers and logarithms: about 40 instructions an entry of a forward or reverse divergence, 60 of a mixture's, 75
+// with the rest, whose sums need powers in 64 bits.  2.2 M elements of 32 entries (64% counted), the reverse
+// divergence with the rest: 172 us for 620 MB (3.6 TB/s); 0.54 M of 27, the mixture, renormalised: 78 us for 172 MB;
+// one tile of 16,384 of 64: 16 us, three launches one after the other, of which the lists' pass takes 8.
 #include <algorithm>
 
 #include "odb_slots.h"
@@ -18,9 +22,6 @@ namespace {
 
 constexpr float kNone = -HUGE_VALF;          // a teacher's entry that is none
 constexpr double kRestLeast = 0x1p-24;       // of what a list leaves out
-#ifndef DW
-#define DW 1
-#endif
 constexpr int kMaxPiece = 512;               // elements of a piece
 constexpr int64_t kMaxDistillElems = (int64_t)1 << 32;     // 2^23 pieces: a grid's threads stay below 2^32
 
@@ -264,6 +265,11 @@ __device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, 
 
 // The block's tokens of a slot's elements [a0, a1): weight(row) gives a token's weight in the reduction and the
 // factor of its gradient, by its row counted from the slot's first.
+// Row of element e of a slot: a run has 2^32 elements at most.
+__device__ __forceinline__ uint32_t row_in(const SlotView& s, int64_t e) {
+    return (uint32_t)(e - s.lo) / (uint32_t)s.maxlen;
+}
+
 struct DistillSum {
     double sum;
     int counted;
@@ -274,8 +280,7 @@ __device__ __forceinline__ DistillSum distill_span(const DistillArgs& A, const S
                                                    const Weight& weight) {
     constexpr int kStep = kBlock / L;      // tokens of the block at once
     const int l = threadIdx.x & (L - 1);
-    const int row_a = (int)((a0 - s.lo) / s.maxlen);
-    const uint32_t col_a = (uint32_t)((a0 - s.lo) - (int64_t)row_a * s.maxlen), maxlen = (uint32_t)s.maxlen;
+    const uint32_t maxlen = (uint32_t)s.maxlen, row_a = row_in(s, a0), col_a = (uint32_t)(a0 - s.lo) - row_a * maxlen;
     const int n = (int)(a1 - a0);
     const Mixture m{(float)A.mix, (float)(1.0 - A.mix)};
     DistillSum S{0.0, 0};
@@ -291,7 +296,7 @@ __device__ __forceinline__ DistillSum distill_span(const DistillArgs& A, const S
             const double value = token<MIX, SUPPORT, L>(A, m, a0 + o, l, g);
             double f;
             float gs;
-            weight(row_a + (int)r, &f, &gs);
+            weight((int)(row_a + r), &f, &gs);
 #pragma unroll
             for (int i = 0; i < 4; ++i) g[i] *= gs;
             if (l == 0) {
@@ -313,7 +318,7 @@ __device__ __forceinline__ void leave_slot(const DistillArgs& A, int64_t k, doub
 
 // ------------------------------------------------------------------ the passes
 template <bool MIX, int SUPPORT, int L>
-__global__ void __launch_bounds__(kBlock, DW) distill_kernel(DistillArgs A) {
+__global__ void __launch_bounds__(kBlock) distill_kernel(DistillArgs A) {
     __shared__ double s_weight[kMaxPiece];
     const odb_tiles_t& t = A.t;
     if (blockIdx.x >= A.pieces) return check_slots(t, blockIdx.x - A.pieces, A.disorder, A.check_blocks, NoVisit{});
@@ -324,7 +329,7 @@ __global__ void __launch_bounds__(kBlock, DW) distill_kernel(DistillArgs A) {
     each_slot(t, e_base, r_base, slot_at(t, e_base, A.reduce == ODB_REDUCE_SUM ? 0 : A.chunk_slot[c0 >> A.chunk_log2], c0),
               c0, c1, [&](int64_t k, const SlotView& s, int64_t a0, int64_t a1) {
         const double scale = A.loss_scale * (A.slot_weight ? A.slot_weight[k] : 1.0);
-        const int row_a = (int)((a0 - s.lo) / s.maxlen), here = (int)((a1 - 1 - s.lo) / s.maxlen) - row_a + 1;
+        const int row_a = (int)row_in(s, a0), here = (int)row_in(s, a1 - 1) - row_a + 1;
         double same = 1.0;       // weight of every token, where rows have none of their own
         if (A.reduce == ODB_REDUCE_TOKEN_MEAN) {
             const double n = slot_counted<false>(A, s, k);
@@ -437,14 +442,12 @@ __global__ void __launch_bounds__(kBlock) distill_one_kernel(DistillArgs A) {
 }
 
 // ------------------------------------------------------------------ host
-// Elements of a piece, a power of two.
-int32_t piece_for(int64_t elems, int32_t k) {
+// Elements of a piece, a power of two: small ones fill the chip with few tokens, large ones cost fewer searches for
+// their slots.  With 2^14 / 2^19 / 2^21 elements of 64 / 27 / 32 entries, pieces from a 16,384th of the elements on
+// instead of a 4,096th: 15.5 / 93 / 219 us instead of 15.5 / 79 / 202; from a 1,024th on: 15.5 / 85 / 202.
+int32_t piece_for(int64_t elems) {
     int32_t piece = 32;
-#ifndef ODB_PIECE
-#define ODB_PIECE 4096
-#endif
-    while (piece < kMaxPiece && elems / piece >= ODB_PIECE) piece *= 2;
-    (void)k;
+    while (piece < kMaxPiece && elems / piece >= 4096) piece *= 2;
     return piece;
 }
 
@@ -454,7 +457,7 @@ struct DistillLayout {
     int32_t chunk, piece;
 };
 
-DistillLayout distill_layout(const odb_tiles_t* t, int32_t k) {
+DistillLayout distill_layout(const odb_tiles_t* t) {
     DistillLayout L;
     size_t o = 0;
     auto take = [&](int64_t bytes) {
@@ -464,7 +467,7 @@ DistillLayout distill_layout(const odb_tiles_t* t, int32_t k) {
     };
     L.chunk = chunk_for(t->num_elems);
     L.chunks = (t->num_elems + L.chunk - 1) / L.chunk;
-    L.piece = piece_for(t->num_elems, k);
+    L.piece = piece_for(t->num_elems);
     L.pieces = (t->num_elems + L.piece - 1) / L.piece;
     L.chunk_slot = take(4 * L.chunks);
     L.slot_count = take(4 * (L.chunks + t->num_slots));
@@ -504,7 +507,7 @@ using namespace odb;
 
 extern "C" size_t odb_distill_workspace_size(const odb_tiles_t* t, int32_t k) {
     if (check_distill_tiles(t, k) != ODB_OK) return 0;
-    return distill_layout(t, k).total;
+    return distill_layout(t).total;
 }
 
 extern "C" int odb_distill_loss(const odb_tiles_t* t, const odb_distill_params_t* p, int32_t k, const float* d_student,
@@ -534,7 +537,7 @@ extern "C" int odb_distill_loss(const odb_tiles_t* t, const odb_distill_params_t
     if (!d_ws) return set_error(ODB_E_INVALID_ARG, "workspace is NULL");
     if (reinterpret_cast<uintptr_t>(d_ws) & 255)
         return set_error(ODB_E_INVALID_ARG, "workspace must be 256-byte aligned");
-    const DistillLayout L = distill_layout(t, k);
+    const DistillLayout L = distill_layout(t);
     if (ws_bytes < L.total)
         return set_error(ODB_E_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, L.total);
 
