@@ -107,11 +107,12 @@ struct Room {
 template <int C>
 __device__ __forceinline__ uint32_t wave_kth(const uint32_t* o, int kth) {
     uint32_t r = 0;
-#pragma unroll 1
-    for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1) {
+#pragma unroll(C == 1 ? 16 : 1)
+    for (int i = 31; i >= 16; --i) {
+        const uint32_t bit = 1u << i;
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < C; ++i) n += __builtin_popcountll(__ballot(o[i] >= (r | bit)));
+        for (int j = 0; j < C; ++j) n += __builtin_popcountll(__ballot(o[j] >= (r | bit)));
         if (n >= kth) r |= bit;
     }
     return r;
@@ -185,16 +186,19 @@ __device__ __forceinline__ void pick(Room<G>& s, u64* list, int n, int k) {
         n = (int)s.few_count;
         list = s.few;
     }
-    // whole steps of eight: keys of 0 are behind all others
+    // Whole steps of eight: keys of 0 are behind all others.  As many threads count one key's place as there are.
     if (t < 8 && n + t < ((n + 7) & ~7)) list[n + t] = 0;
     group_sync<G>();
-    for (int i = t; i < n; i += G) {
+    int by = 0;     // 2^by threads
+    while (G > kWave && (n << (by + 1)) <= G && by < 3) ++by;
+    for (int i = t >> by; i < n; i += G >> by) {
         const u64 mine = list[i];
         int place = 0;
-        for (int j = 0; j < n; j += 8) {
+        for (int j = 8 * (t & ((1 << by) - 1)); j < n; j += 8 << by) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) place += list[j + u] > mine;
         }
+        for (int d = 0; d < by; ++d) place += __shfl_xor(place, 1 << d, kWave);
         if (place < k) s.top[place] = mine;
     }
     group_sync<G>();
@@ -249,13 +253,6 @@ __device__ __forceinline__ Acc scan(const T* z, int64_t v0, int64_t v1, int32_t 
         }
         return most;
     };
-    auto hit = [&](const Vec<T>& w, int64_t v) __attribute__((always_inline)) {
-        const uint32_t to = atomicAdd(&s.hits, 1u);
-        if (to < Room<G>::kHits) {
-            __builtin_memcpy(&s.hit[to], &w, 16);
-            s.hit_at[to] = (uint32_t)v;
-        }
-    };
     auto limit_of = [&](uint32_t o) __attribute__((always_inline)) {
         return o > none + 1 ? unordered(o - 1 - (o - 1 == 0x7fffffffu)) : unordered(none);
     };
@@ -308,9 +305,22 @@ __device__ __forceinline__ Acc scan(const T* z, int64_t v0, int64_t v1, int32_t 
             if (meet) met = o;
             limit = limit_of(o);
         }
+        int found = 0;
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (most[j] > limit) hit(w[j], v + j * G * N);
+        for (int j = 0; j < kAhead; ++j) found += most[j] > limit;
+        if (found) {
+            uint32_t to = atomicAdd(&s.hits, (uint32_t)found);
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                if (most[j] > limit) {
+                    if (to < (uint32_t)Room<G>::kHits) {
+                        __builtin_memcpy(&s.hit[to], &w[j], 16);
+                        s.hit_at[to] = (uint32_t)(v + j * G * N);
+                    }
+                    ++to;
+                }
+            }
+        }
     }
     if (whole + t < v1) {
         const float f = (float)z[whole + t];
