@@ -76,6 +76,9 @@ LIST_CASES = [
     (1, 6, 8191, "fp16", 1, 1.0, 0, 32, True), (2, 3, 32000, "fp32", 1, 1.0, 0, 2, True),
     (2, 4, 50021, "bf16", 1, 1.5, 11, 64, True), (1, 2, 151936, "bf16", 0, 1.0, 0, 128, False),
     (300, 3, 5, "bf16", 1, 1.0, 0, 4, True), (600, 2, 515, "bf16", 1, 0.8, 1, 9, True),
+    (600, 2, 200, "bf16", 1, 1.0, 0, 128, True), (600, 2, 77, "fp32", 0, 1.0, 2, 16, True),
+    (540, 2, 900, "bf16", 1, 1.0, 0, 33, True), (520, 2, 31, "fp16", 0, 1.0, 0, 64, False),
+    (270, 2, 4097, "bf16", 1, 1.0, 0, 128, True), (260, 2, 13001, "fp16", 1, 1.0, 1, 128, True),
     (300, 2, 1030, "fp16", 0, 1.0, 0, 16, True), (270, 2, 5003, "bf16", 0, 1.0, 3, 20, True),
 ]
 
