@@ -819,7 +819,7 @@ typedef struct odb_distill_params {
     int32_t support;             /* odb_support_t                                              */
     int32_t reduce;              /* odb_reduce_t                                               */
     int32_t reserved0;           /* must be 0                                                  */
-    double  mix;                 /* w of the mixture, inside (0, 1) also in fp32               */
+    double  mix;                 /* w of the mixture; w and 1 - w normal numbers of fp32       */
     double  loss_scale;          /* finite; factor of every slot's loss                        */
 } odb_distill_params_t;
 

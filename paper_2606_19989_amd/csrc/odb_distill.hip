@@ -8,10 +8,10 @@
 // A mean's weight is known after a pass over the labels, the one that the policy loss makes.
 //
 // Bound by the reads of both lists and the writes of the gradient, 12 k bytes an element, and beside them by the
-// powers and logarithms: about 40 instructions an entry of a forward or reverse divergence, 60 of a mixture's, 75
-// with the rest, whose sums need powers in 64 bits.  2.2 M elements of 32 entries (64% counted), the reverse
-// divergence with the rest: 172 us for 620 MB (3.6 TB/s); 0.54 M of 27, the mixture, renormalised: 69 us for 172 MB;
-// one tile of 16,384 of 64: 16 us, three launches one after the other, of which the lists' pass takes 8.
+// powers and logarithms: some 40 to 100 instructions an entry, with the rest most, whose sums need powers in 64
+// bits.  2.1 M elements of 32 entries (64% counted), the reverse divergence with the rest: 170 us for 620 MB
+// (3.6 TB/s, instructions two thirds of the time); 0.54 M of 27, the mixture, renormalised: 60 us for 172 MB; one
+// tile of 16,384 of 64: 15 us, three launches one after the other, of which the lists' pass takes 8.
 #include <algorithm>
 
 #include "odb_slots.h"
@@ -89,8 +89,8 @@ __device__ __forceinline__ void load_entries(const float* p, int k, int l, float
         return;
     }
     const int at = 4 * l < k - 4 ? 4 * l : k - 4, by = 4 * l - at;
-    // lists whose fours share lines with their neighbours' are better kept near: 0.54 M lists of 27 take 69 us, past
-    // the caches' usual order 79; 2.2 M of 32 take 177 and 172
+    // lists whose fours share lines with their neighbours' are better kept near: 0.54 M lists of 27 took 69 us, past
+    // the caches' usual order 79; 2.1 M of 32 took 177 and 172
     const float4a* const from = reinterpret_cast<const float4a*>(p + at);
     const float4a w = k & 3 ? *from : __builtin_nontemporal_load(from);
 #pragma unroll
@@ -119,6 +119,17 @@ __device__ __forceinline__ void store_entries(float* p, int k, int l, const floa
     }
 }
 
+// exp(d) for d <= 0 as exp_near gives it; below e^-150 a number as good as 0.  A NaN stays.
+__device__ __forceinline__ float exp_below(float d) {
+    d = d < -150.0f ? -150.0f : d;
+    const float u = d * kLog2e;
+    const float e = __builtin_amdgcn_exp2f(u);
+    return fmaf(e * fmaf(d, kLog2eLow, fmaf(d, kLog2e, -u)), kLn2, e);
+}
+
+// ln x of a normal number to two roundings.
+__device__ __forceinline__ float log_near(float x) { return __builtin_amdgcn_logf(x) * kLn2; }
+
 struct Mixture {
     float w, v;      // the teacher's weight and the student's
 };
@@ -134,7 +145,7 @@ struct Entry {
 // two differ by d.
 __device__ __forceinline__ void below(const Mixture& m, float d, float ratio, float* less_p, float* less_q) {
     const bool more = d >= 0.0f;      // p is the larger
-    const float x = -logf(more ? fmaf(m.v, ratio, m.w) : fmaf(m.w, ratio, m.v));
+    const float x = -log_near(more ? fmaf(m.v, ratio, m.w) : fmaf(m.w, ratio, m.v));
     *less_p = more ? x : x + d;
     *less_q = more ? x - d : x;
 }
@@ -200,14 +211,15 @@ __device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, 
         float st = 0.0f, ss = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            share_p[i] = there[i] ? exp_near(t[i] - mt) : 0.0f;
-            share_q[i] = there[i] ? exp_near(s[i] - ms) : 0.0f;
+            share_p[i] = there[i] ? exp_below(t[i] - mt) : 0.0f;
+            share_q[i] = there[i] ? exp_below(s[i] - ms) : 0.0f;
             st += share_p[i];
             ss += share_q[i];
         }
         st = lanes_sum<L>(st);
         ss = lanes_sum<L>(ss);
-        const float lt = logf(st), ls = logf(ss), over_t = 1.0f / st, over_s = 1.0f / ss;
+        const float lt = log_near(st), ls = log_near(ss);      // 1 to k
+        const float over_t = __builtin_amdgcn_rcpf(st), over_s = __builtin_amdgcn_rcpf(ss);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             t[i] = (t[i] - mt) - lt;
@@ -230,14 +242,14 @@ __device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, 
             sum_q += wide_q[i];
             x.p = (float)wide_p[i];
             x.q = (float)wide_q[i];
-            if (MIX) x.ratio = exp_near(-fabsf(x.d));
+            if (MIX) x.ratio = exp_below(-fabsf(x.d));
         } else if (SUPPORT == ODB_SUPPORT_RENORMALIZED) {
             x.p = share_p[i];
             x.q = share_q[i];
-            if (MIX) x.ratio = exp_near(-fabsf(x.d));
+            if (MIX) x.ratio = exp_below(-fabsf(x.d));
         } else if (MIX) {
             const float larger = exp_near(x.d >= 0.0f ? t[i] : s[i]);
-            x.ratio = exp_near(-fabsf(x.d));
+            x.ratio = exp_below(-fabsf(x.d));
             x.p = x.d >= 0.0f ? larger : larger * x.ratio;
             x.q = x.d >= 0.0f ? larger * x.ratio : larger;
         } else {
@@ -264,13 +276,13 @@ __device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, 
     if (rp < kRestLeast) rp = kRestLeast;      // a NaN stays
     if (rq < kRestLeast) rq = kRestLeast;
     Entry rest{(float)rp, (float)rq, 0.0f, 0.0f};
-    const float times = rest.p / rest.q;
-    rest.d = logf(times);
-    if (MIX) rest.ratio = rest.d >= 0.0f ? rest.q / rest.p : times;
+    const float over_q = __builtin_amdgcn_rcpf(rest.q), times = rest.p * over_q;     // 2^-24 to 2^24
+    rest.d = log_near(times);
+    if (MIX) rest.ratio = rest.d >= 0.0f ? rest.q * __builtin_amdgcn_rcpf(rest.p) : times;
     float term, by;
     entry<MIX>(A.kind, m, rest, 0.0f, &term, &by);
     // d rq = -q_j d s_j, unless it is held at its least; there the reverse's slopes keep their constant
-    const float moves = !held ? by / rest.q : !MIX && A.kind == ODB_DISTILL_REVERSE ? -1.0f : 0.0f;
+    const float moves = !held ? by * over_q : !MIX && A.kind == ODB_DISTILL_REVERSE ? -1.0f : 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) slope[i] = fmaf(-q[i], moves, slope[i]);
     return (double)value + (double)term;
@@ -299,11 +311,21 @@ __device__ __forceinline__ DistillSum distill_span(const DistillArgs& A, const S
     DistillSum S{0.0, 0};
     int o = threadIdx.x / L;
     int32_t y = o < n ? A.t.d_labels[a0 + o] : ODB_LABEL_IGNORE;
-    for (; o < n; o += kStep) {
+    // row and column of the thread's token, and from one to its next
+    const uint32_t rows_by = kStep / maxlen, cols_by = kStep - rows_by * maxlen;
+    uint32_t r = (col_a + (uint32_t)o) / maxlen, col = col_a + (uint32_t)o - r * maxlen;
+    auto advance = [&]() {
+        r += rows_by;
+        col += cols_by;      // below 2 maxlen < 2^32
+        if (col >= maxlen) {
+            col -= maxlen;
+            ++r;
+        }
+    };
+    for (; o < n; o += kStep, advance()) {
         const int32_t label = y;
         if (o + kStep < n) y = A.t.d_labels[a0 + o + kStep];      // on its way beside this token
-        const uint32_t x = col_a + (uint32_t)o, r = x / maxlen;
-        const bool on = label != ODB_LABEL_IGNORE && x - r * maxlen >= (uint32_t)A.t.shift;
+        const bool on = label != ODB_LABEL_IGNORE && col >= (uint32_t)A.t.shift;
         float g[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (on) {
             const double value = token<MIX, SUPPORT, L>(A, m, a0 + o, l, g);
@@ -537,8 +559,8 @@ extern "C" int odb_distill_loss(const odb_tiles_t* t, const odb_distill_params_t
         return set_error(ODB_E_INVALID_ARG, "unknown reduction %d", p->reduce);
     if (p->reserved0 != 0) return set_error(ODB_E_INVALID_ARG, "params.reserved0 must be 0");
     const bool mix = p->kind == ODB_DISTILL_MIXTURE;
-    // both weights are used in 32 bits
-    if (mix && !((float)p->mix > 0.0f && (float)(1.0 - p->mix) > 0.0f && p->mix < 1.0))
+    // both weights are used in 32 bits, as normal numbers
+    if (mix && !((float)p->mix >= 0x1p-126f && (float)(1.0 - p->mix) >= 0x1p-126f && p->mix < 1.0))
         return set_error(ODB_E_INVALID_ARG, "mix must be inside (0, 1)");
     if (!std::isfinite(p->loss_scale)) return set_error(ODB_E_INVALID_ARG, "loss_scale must be finite");
     if (t->num_slots == 0) return ODB_OK;

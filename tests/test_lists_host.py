@@ -144,7 +144,7 @@ def test_distill_arguments_refused():
         assert _distill(_tiles(**bad)) == BAD, bad
     for bad in (dict(kind=3), dict(kind=-1), dict(support=3), dict(support=-1), dict(reduce=3), dict(reduce=-1),
                 dict(reserved0=1), dict(kind=2, mix=0.0), dict(kind=2, mix=1.0), dict(kind=2, mix=float("nan")),
-                dict(kind=2, mix=1e-60), dict(kind=2, mix=-0.5), dict(loss_scale=float("inf")),
+                dict(kind=2, mix=1e-60), dict(kind=2, mix=1e-40), dict(kind=2, mix=-0.5), dict(loss_scale=float("inf")),
                 dict(loss_scale=float("nan"))):
         assert _distill(p=odb.DistillParams(**bad)) == BAD, bad
     for bad in (dict(k=0), dict(k=odb.ODB_LIST_MAX + 1), dict(student=None), dict(teacher=None), dict(loss=None),
