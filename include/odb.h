@@ -595,7 +595,7 @@ size_t odb_token_top_workspace_size(const odb_logits_t* x, int32_t k);
  * A logit of -inf is no alternative.  Entries that a position does not have, and all of a token that does
  * not count, have id ODB_LABEL_IGNORE and log-probability -inf (no entries for the calls that take lists);
  * such a token's rank is -1 and its other outputs are 0.  A token whose logits have no distribution (all
- * -inf, a NaN, +inf) has no ids, rank -1, and NaN elsewhere.  Asynchronous.
+ * -inf, a NaN, +inf) has no ids, rank -1, and NaN for its log-probabilities and entropy.  Asynchronous.
  */
 int odb_token_top_logprobs(const odb_logits_t* x, const int32_t* d_labels, int32_t k, int32_t* d_top_ids,
                            float* d_top_logprob, float* d_logprob, int32_t* d_rank, float* d_stats, float* d_entropy,

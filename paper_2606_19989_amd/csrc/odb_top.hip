@@ -13,8 +13,7 @@
 //
 // Bound by the reads of the logits and, about as much, by the instructions: nine a logit as without the
 // alternatives (an exponential counts four), one more for its group's largest.  4,096 positions of 151,936 bf16
-// logits, k = 64: 210 us (5.7 TB/s of reads; 182 without alternatives), of which the groups set aside take
-// about 20 us and what is behind the pass 10.
+// logits, k = 64: 203 us (5.9 TB/s of reads; 182 without alternatives).
 #include <algorithm>
 
 #include "odb_vocab.h"
@@ -26,9 +25,10 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int kBins = 256;      // of a digit
-// Alternatives from which on a wave's cells are half a group of a thread's, 512, and not its 64 threads.  k = 20 / 40
-// of 36,621 positions of 8,192 bf16 logits: 130 / 390 us with threads, 173 / 185 with half groups.
-constexpr int kFine = 24;
+// Alternatives from which on a wave's cells are half a group of a thread's, 512, and not its 64 threads.  k = 20 / 32
+// / 40 / 56 of 36,621 positions of 8,192 bf16 logits: 130 / 135 / 151 / 464 us with threads, 170 / 177 / 182 / 190 with
+// half groups; of 1,024 logits (131,072 positions) 157 / 186 / 238 / 365 and 215 / 232 / 241 / 283.
+constexpr int kFine = 32;
 constexpr float kNone = -HUGE_VALF;
 
 template <typename T>
@@ -560,13 +560,13 @@ void launch(const TopArgs& a, hipStream_t s) {
     // that one's wait behind its pass is another's reading; a block of four waves has cells for more alternatives,
     // and needs 4 KB for all of its threads to have any.  us for 600 MB of bf16 logits, k = 5 / 20 / 64 / 128:
     //   logits a row    wave                        block
-    //   1,024           279 / 330 /  630 / 1370     4890 / 4890 / 4890 / 5260
-    //   2,048           185 / 214 /  369 /  800      700 /  760 / 1020 / 1590
-    //   4,096           150 / 161 /  277 /  575      370 /  400 /  540 /  809
-    //   8,192           126 / 131 /  203 / 1195      208 /  225 /  293 /  422
-    //   16,384          115 / 115 /  434 /  818      155 /  167 /  200 /  301
-    //   32,768          118 / 125 /  397 /  652      126 /  131 /  147 /  214
-    //   65,536          137 / 144 /  420 /  613      114 /  116 /  125 /  162
+    //   1,024           272 / 314 /  631 / 1349     4815 / 4815 / 4823 / 5253
+    //   2,048           177 / 199 /  369 /  783      690 /  711 /  865 / 1596
+    //   4,096           139 / 152 /  277 /  566      366 /  377 /  459 /  812
+    //   8,192           126 / 126 /  204 / 1123      207 /  214 /  254 /  425
+    //   16,384          112 / 116 /  413 /  771      154 /  157 /  175 /  302
+    //   32,768          117 / 123 /  381 /  609      123 /  124 /  136 /  214
+    //   65,536          135 / 142 /  408 /  578      116 /  115 /  121 /  162
     const int64_t row = a.x.vocab * (int64_t)sizeof(T);
     const bool wave = row <= 4096 || (n > 2 * num_cus() && row <= (a.k <= kFine ? 32768 : a.k <= kWave ? 16384 : 8192));
     if (wave)
@@ -592,13 +592,15 @@ int check_top(const odb_logits_t* x, int32_t k) {
 }
 
 // Blocks of a position: for fewer positions than would fill the chip, as many as have a round of loads each, as
-// far as their candidates go to one block's LDS.  In a graph, k = 20, 1 / 32 / 128 positions: of 151,936 bf16 logits
-// 12.7 / 14.8 / 17.4 us, with one block each 24 / 26 / 26; of 16,384 (two rounds) 10.6 / 11.3 / 11.9, with one 8 / 9 / 9.
+// far as their candidates go to one block's LDS.  In a graph, k = 20, 1 / 32 / 128 positions, with one block and with
+// parts: of 32,000 bf16 logits (four rounds) 10.0 / 10.6 / 11.2 and 9.8 / 12.0 / 13.3 us; of 50,000 12.6 / 13.9 / 13.6
+// and 11.8 / 14.1 / 16.2; of 100,000 18.7 / 19.7 / 20.1 and 12.1 / 13.9 / 19.8; of 151,936 24.3 / 25.4 / 26.2 and
+// 13.2 / 15.6 / 18 to 23.
 constexpr int64_t kFillBlocks = 1024;
 int32_t parts_for(const odb_logits_t* x, int32_t k, int64_t* len) {
     const int64_t n = x->rows * x->cols, round = x->dtype == ODB_FLOAT32 ? 4096 : 8192;
     int64_t parts = n > 0 ? kFillBlocks / n : 1;
-    if (x->vocab <= 3 * round) return 1;
+    if (x->vocab <= 6 * round) return 1;
     parts = std::min({parts, (x->vocab + round - 1) / round, (int64_t)(Room<kBlock>::kHold / (2 * k)), (int64_t)kWave});
     if (parts <= 1) return 1;
     *len = ((x->vocab + parts - 1) / parts + 7) & ~(int64_t)7;

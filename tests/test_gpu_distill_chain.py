@@ -59,7 +59,7 @@ def _step(s):
 
 
 # one block's loss; parts of a position and the passes; a wave a position
-SHAPES = [(3, 9, 50, 5), (2, 5, 40000, 20), (6, 300, 3000, 64)]
+SHAPES = [(3, 9, 50, 5), (2, 5, 60000, 20), (6, 300, 3000, 64)]
 
 
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
