@@ -333,7 +333,7 @@ __device__ __forceinline__ DistillSum distill_span(const DistillArgs& A, const S
             float gs;
             weight((int)(row_a + r), &f, &gs);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) g[i] *= gs;
+            for (int i = 0; i < 4; ++i) g[i] = g[i] == 0.0f ? 0.0f : g[i] * gs;      // no entry beside a weight of infinity
             if (l == 0) {
                 S.sum += value * f;
                 ++S.counted;

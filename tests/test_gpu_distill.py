@@ -214,6 +214,23 @@ def test_a_nan_stays():
                 assert np.isfinite(grad[np.arange(plan.E) != 2]).all()
 
 
+@pytest.mark.parametrize("n", [3, 900])
+def test_no_entry_has_gradient_0_beside_weights_that_are_not_finite(n):
+    import paper_2606_19989_amd as odb
+    plan = Plan([[5] * n, [4]])
+    rng = np.random.default_rng(8)
+    y = plan.labels(rng)
+    t, s = _lists(rng, plan.E, 6, short=0.5)
+    on = plan.counted(y, 1)
+    for support in range(3):
+        for w in (math.inf, math.nan):
+            run = Run(plan, y, t, s, 6, odb.DistillParams(kind=1, support=support), np.array([w, 1.0]))
+            run()
+            loss, mean, count, grad = run.numpy()
+            assert not math.isfinite(loss[0]) and math.isfinite(loss[1]) and np.isfinite(mean).all()
+            assert np.all(grad[~on] == 0) and np.all(grad[t == -math.inf] == 0)
+
+
 def test_without_gradient_and_weights():
     import paper_2606_19989_amd as odb
     rng = np.random.default_rng(4)
