@@ -823,8 +823,8 @@ typedef struct odb_distill_params {
     double  loss_scale;          /* finite; factor of every slot's loss                        */
 } odb_distill_params_t;
 
-/* Bytes of device workspace odb_distill_loss needs: a function of num_slots, num_rows and num_elems alone.  0 on
- * bad arguments. */
+/* Bytes of device workspace odb_distill_loss needs: a function of num_slots, num_rows, num_elems and k alone.
+ * 0 on bad arguments. */
 size_t odb_distill_workspace_size(const odb_tiles_t* t, int32_t k);
 
 /*

@@ -478,11 +478,12 @@ __global__ void __launch_bounds__(kBlock) distill_one_kernel(DistillArgs A) {
 
 // ------------------------------------------------------------------ host
 // Elements of a piece, a power of two: small ones fill the chip with few tokens, large ones cost fewer searches for
-// their slots.  With 2^14 / 2^19 / 2^21 elements of 64 / 27 / 32 entries, pieces from a 16,384th of the elements on
-// instead of a 4,096th: 15.5 / 93 / 219 us instead of 15.5 / 79 / 202; from a 1,024th on: 15.5 / 85 / 202.
-int32_t piece_for(int64_t elems) {
+// their slots and fewer sums of their counts.  us with pieces of a 4,096th of the elements, and with larger ones while
+// they have fewer than 4,096 entries and are 512 or more: 2^17 elements of 11 entries (mean over rows) 42.0 and 25.3, of
+// 7 (sum) 21.1 and 12.1, 2^16 of 32 21.7 and 18.1; 2^14 of 64 18 and 18, 2^19 of 27 73 and 73.
+int32_t piece_for(int64_t elems, int32_t k) {
     int32_t piece = 32;
-    while (piece < kMaxPiece && elems / piece >= 4096) piece *= 2;
+    while (piece < kMaxPiece && (elems / piece >= 4096 || (piece * k < 4096 && elems / piece >= 512))) piece *= 2;
     return piece;
 }
 
@@ -492,7 +493,7 @@ struct DistillLayout {
     int32_t chunk, piece;
 };
 
-DistillLayout distill_layout(const odb_tiles_t* t) {
+DistillLayout distill_layout(const odb_tiles_t* t, int32_t k) {
     DistillLayout L;
     size_t o = 0;
     auto take = [&](int64_t bytes) {
@@ -502,7 +503,7 @@ DistillLayout distill_layout(const odb_tiles_t* t) {
     };
     L.chunk = chunk_for(t->num_elems);
     L.chunks = (t->num_elems + L.chunk - 1) / L.chunk;
-    L.piece = piece_for(t->num_elems);
+    L.piece = piece_for(t->num_elems, k);
     L.pieces = (t->num_elems + L.piece - 1) / L.piece;
     L.chunk_slot = take(4 * L.chunks);
     L.slot_count = take(4 * (L.chunks + t->num_slots));
@@ -542,7 +543,7 @@ using namespace odb;
 
 extern "C" size_t odb_distill_workspace_size(const odb_tiles_t* t, int32_t k) {
     if (check_distill_tiles(t, k) != ODB_OK) return 0;
-    return distill_layout(t).total;
+    return distill_layout(t, k).total;
 }
 
 extern "C" int odb_distill_loss(const odb_tiles_t* t, const odb_distill_params_t* p, int32_t k, const float* d_student,
@@ -572,7 +573,7 @@ extern "C" int odb_distill_loss(const odb_tiles_t* t, const odb_distill_params_t
     if (!d_ws) return set_error(ODB_E_INVALID_ARG, "workspace is NULL");
     if (reinterpret_cast<uintptr_t>(d_ws) & 255)
         return set_error(ODB_E_INVALID_ARG, "workspace must be 256-byte aligned");
-    const DistillLayout L = distill_layout(t);
+    const DistillLayout L = distill_layout(t, k);
     if (ws_bytes < L.total)
         return set_error(ODB_E_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, L.total);
 
