@@ -124,7 +124,32 @@ template <int G>
 __device__ __forceinline__ void pick(Room<G>& s, u64* list, int n, int k) {
     constexpr int kFew = Room<G>::kFew;
     const int t = threadIdx.x & (G - 1), lane = threadIdx.x & (kWave - 1);
-    if (n > kFew) {
+    if (G > kWave && n > kFew) {
+        // a bound as in the pass, with the threads' largest keys for cells (a wave has too few for many alternatives)
+        uint32_t o = 0;
+        for (int i = t; i < n; i += G) {
+            const uint32_t high = (uint32_t)(list[i] >> 32);
+            o = high > o ? high : o;
+        }
+        o = wave_kth<1>(&o, (k + Room<G>::kWaves - 1) / Room<G>::kWaves);
+        if (t == 0) s.few_count = 0;
+        if (lane == 0) s.bound[t / kWave] = o;
+        group_sync<G>();
+#pragma unroll
+        for (int i = 0; i < Room<G>::kWaves; ++i) o = s.bound[i] < o ? s.bound[i] : o;
+        for (int i = t; i < n; i += G) {
+            const u64 key = list[i];
+            if ((uint32_t)(key >> 32) < o) continue;
+            const uint32_t to = atomicAdd(&s.few_count, 1u);
+            if (to < (uint32_t)kFew) s.few[to] = key;
+        }
+        group_sync<G>();
+    }
+    const int cut = G > kWave && n > kFew ? (int)s.few_count : kFew + 1;
+    if (cut <= kFew) {
+        n = cut;
+        list = s.few;
+    } else if (n > kFew) {
         // digits of 8 bits from the highest bit that differs
         if (t == 0) s.differ = 0;
         group_sync<G>();
