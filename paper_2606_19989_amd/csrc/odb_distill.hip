@@ -22,7 +22,7 @@ namespace {
 
 constexpr float kNone = -HUGE_VALF;          // a teacher's entry that is none
 constexpr double kRestLeast = 0x1p-24;       // of what a list leaves out
-constexpr int kMaxPiece = 512;               // elements of a piece
+constexpr int kMaxPiece = 2048;              // elements of a piece; with 4,096 their weights leave too few blocks
 constexpr int64_t kMaxDistillElems = (int64_t)1 << 32;     // 2^23 pieces: a grid's threads stay below 2^32
 
 struct DistillPart {
@@ -480,10 +480,12 @@ __global__ void __launch_bounds__(kBlock) distill_one_kernel(DistillArgs A) {
 // Elements of a piece, a power of two: small ones fill the chip with few tokens, large ones cost fewer searches for
 // their slots and fewer sums of their counts.  us with pieces of a 4,096th of the elements, and with larger ones while
 // they have fewer than 4,096 entries and are 512 or more: 2^17 elements of 11 entries (mean over rows) 42.0 and 25.3, of
-// 7 (sum) 21.1 and 12.1, 2^16 of 32 21.7 and 18.1; 2^14 of 64 18 and 18, 2^19 of 27 73 and 73.
+// 7 (sum) 21.1 and 12.1, 2^16 of 32 21.7 and 18.1; 2^14 of 64 18 and 18, 2^19 of 27 73 and 73.  Up to 2,048
+// elements instead of 512: 3.0e7 elements of 1 entry 342 and 532, 2^22 of 4 75 and 89.
 int32_t piece_for(int64_t elems, int32_t k) {
     int32_t piece = 32;
-    while (piece < kMaxPiece && (elems / piece >= 4096 || (piece * k < 4096 && elems / piece >= 512))) piece *= 2;
+    while ((piece < 512 && elems / piece >= 4096) || (piece < kMaxPiece && piece * k < 4096 && elems / piece >= 512))
+        piece *= 2;
     return piece;
 }
 

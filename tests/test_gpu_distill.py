@@ -138,6 +138,43 @@ def test_slots_and_rows_across_pieces(shape, reduce):
         assert all(np.array_equal(a, b) for a, b in zip(first, run.numpy())), "not the same bit for bit"
 
 
+@pytest.mark.parametrize("reduce", [0, 1, 2])
+def test_many_short_rows(reduce):
+    """A million elements in rows of 1 to 5, with few entries: thousands of rows in a piece, rows cut by its ends."""
+    import paper_2606_19989_amd as odb
+    rng = np.random.default_rng(11)
+    plan = Plan([[1] * 100_001, [5] * 70_003, [], [3] * 120_007, [2] * 70_001, [40_000] * 2])
+    log(f"distill: {plan.E} elements in {plan.R} rows")
+    y = plan.labels(rng, prompt=0.9, empty=0.2)
+    k = 2
+    t, s = _lists(rng, plan.E, k)
+    w = rng.random(plan.K)
+    run = Run(plan, y, t, s, k, odb.DistillParams(reduce=reduce, loss_scale=2.0), w)
+    run()
+    loss, mean, count, grad = run.numpy()
+    assert int(run.status.item()) == 0
+    on = plan.counted(y, 1)
+    there = t != -math.inf
+    t64, s64 = np.where(there, t, 0.0).astype(np.float64), np.where(there, s, 0.0).astype(np.float64)
+    p = np.where(there, np.exp(t64), 0.0)
+    D = (p * (t64 - s64)).sum(-1)
+    slot = plan.slot_of_row[plan.row_of]
+    n = np.bincount(slot[on], minlength=plan.K)
+    per_row = np.bincount(plan.row_of[on], minlength=plan.R)
+    rows = np.bincount(plan.slot_of_row[per_row > 0], minlength=plan.K)
+    with np.errstate(divide="ignore"):
+        f = [1.0 / n[slot], 1.0 / (per_row[plan.row_of] * rows[slot]), np.ones(plan.E)][reduce]
+    f = np.where(on, f, 0.0)
+    assert np.array_equal(count, n)
+    size = (p * (np.abs(t64) + np.abs(s64) + 4) * (1 + np.abs(t64 - s64))).sum(-1)      # as in the oracle's bounds
+    want = np.bincount(slot, weights=f * D, minlength=plan.K)
+    tol = U * np.bincount(slot, weights=f * (4 * size + 12 * np.abs(D)), minlength=plan.K) + 2 * U * np.abs(want)
+    assert np.all(np.abs(mean - want) <= tol)
+    assert np.all(np.abs(loss - 2 * w * want) <= 2 * w * tol + 2 * U * np.abs(2 * w * want))
+    want = -(2 * w[slot] * f)[:, None] * p
+    assert np.all(np.abs(grad - want) <= U * np.abs(want) * (4 * (np.abs(t64) + np.abs(s64) + 4) + 4) + 2.0 ** -115)
+
+
 def test_nothing_counts_and_no_slots():
     import paper_2606_19989_amd as odb
     plan = Plan([[4, 3], [], [2]])
