@@ -8,7 +8,8 @@ fails to load, every call raises.
 
 :class:`Pipeline` owns the device buffers of one window and runs the three stages
 (grouping, alignment, collation) in order on one stream, and on request the loss-scaling
-weights of the aligned plan, a policy loss and a preference loss over its tiles.
+weights of the aligned plan, a policy loss, a preference loss and a distillation loss over its
+tiles.
 """
 from __future__ import annotations
 
