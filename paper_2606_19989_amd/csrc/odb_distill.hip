@@ -8,9 +8,9 @@
 // A mean's weight is known after a pass over the labels, the one that the policy loss makes.
 //
 // Bound by the reads of both lists and the writes of the gradient, 12 k bytes an element, and beside them by the
-// powers and logarithms: some 40 to 100 instructions an entry, with the rest most, whose sums need powers in 64
+// powers, logarithms and series: some 40 to 100 instructions an entry, with the rest most, whose sums need powers in 64
 // bits.  2.1 M elements of 32 entries (64% counted), the reverse divergence with the rest: 170 us for 620 MB
-// (3.6 TB/s, instructions two thirds of the time); 0.54 M of 27, the mixture, renormalised: 60 us for 172 MB; one
+// (3.6 TB/s, instructions two thirds of the time); 0.54 M of 27, the mixture, renormalised: 76 us for 172 MB; one
 // tile of 16,384 of 64: 15 us, three launches one after the other, of which the lists' pass takes 8.
 #include <algorithm>
 
@@ -30,6 +30,14 @@ struct DistillPart {
     int64_t counted;
 };
 
+// A mixture's weights, the teacher's w and the student's v, and its series (mixture_entry): with cumulants w v c_n,
+//   K(d) = w d (1 + d log_by(d)),   d K' - K = w v d^2 term_by(d).
+struct Mixture {
+    float w, v;
+    float log_by[7];      // of |d| < 1/2: what follows is below 2^-25 of the sum
+    float term_by[8];
+};
+
 struct DistillArgs : SlotCounts {
     const float* student;
     const float* teacher;
@@ -40,7 +48,8 @@ struct DistillArgs : SlotCounts {
     float* grad;
     DistillPart* part;
     int64_t pieces;
-    double loss_scale, mix;
+    double loss_scale;
+    Mixture mix;
     int32_t piece, piece_log2;
     int32_t k, kind, reduce;
 };
@@ -119,7 +128,7 @@ __device__ __forceinline__ void store_entries(float* p, int k, int l, const floa
     }
 }
 
-// exp(d) for d <= 0 as exp_near gives it; below e^-150 a number as good as 0.  A NaN stays.
+// exp(d) for d <= 16 as exp_near gives it; below e^-150 a number as good as 0.  A NaN stays.
 __device__ __forceinline__ float exp_below(float d) {
     d = d < -150.0f ? -150.0f : d;
     const float u = d * kLog2e;
@@ -127,38 +136,53 @@ __device__ __forceinline__ float exp_below(float d) {
     return fmaf(e * fmaf(d, kLog2eLow, fmaf(d, kLog2e, -u)), kLn2, e);
 }
 
-// ln x of a normal number to two roundings.
+// ln x of a normal number to two roundings of x's logarithm.
 __device__ __forceinline__ float log_near(float x) { return __builtin_amdgcn_logf(x) * kLn2; }
 
-struct Mixture {
-    float w, v;      // the teacher's weight and the student's
-};
-
-// An entry's probabilities, and what its part of the mixture needs of them.
+// An entry's probabilities, and ln p - ln q.
 struct Entry {
-    float p, q;
-    float d;         // ln p - ln q
-    float ratio;     // of the smaller to the larger
+    float p, q, d;
 };
 
-// How far the mixture lies below p and below q, in logs: -ln (w + v q / p), or the same from the other side; the
-// two differ by d.
-__device__ __forceinline__ void below(const Mixture& m, float d, float ratio, float* less_p, float* less_q) {
-    const bool more = d >= 0.0f;      // p is the larger
-    const float x = -log_near(more ? fmaf(m.v, ratio, m.w) : fmaf(m.w, ratio, m.v));
-    *less_p = more ? x : x + d;
-    *less_q = more ? x - d : x;
+// c[0] + c[1] d + ...
+template <int N>
+__device__ __forceinline__ float series(const float (&c)[N], float d) {
+    float r = c[N - 1];
+#pragma unroll
+    for (int i = N - 2; i >= 0; --i) r = fmaf(r, d, c[i]);
+    return r;
 }
 
-// A divergence's term of one entry with log-probabilities t and s, and its slope by s; `plus` is the
-// constant of the reverse divergence's slope, which probabilities that sum to 1 cancel.
+// With m = w p + v q and K(d) = ln (v + w e^d) = ln (m / q): the slope v q ln (q / m) is -v q K, and the term
+// w p ln (p / m) + v q ln (q / m) is m (d K' - K).  Both come from numbers of d's size, which the term, of d^2's,
+// would be the difference of; so for |d| < kNear they are series in d with the cumulants of a weight of w, right
+// to themselves however near the student is.  Beyond, ln (m / p) or ln (m / q) is taken where m's other part has the
+// smaller weight, in at most half of the distance, which gives the other; past kFar where it is the smaller part.
+constexpr float kNear = 0.5f, kFar = 16.0f;
+__device__ __forceinline__ void mixture_entry(const Mixture& m, const Entry& x, float* term, float* slope) {
+    const float d = x.d, size = fabsf(d);
+    // near
+    const float near_q = m.w * d * fmaf(d, series(m.log_by, d), 1.0f);
+    const float part = m.w * m.v * (d * d) * fmaf(m.w, x.p, m.v * x.q) * series(m.term_by, d);
+    // far: from p's side, or from q's
+    const bool from_p = size < kFar ? m.w >= 0.5f : d >= 0.0f;
+    const float along = from_p ? -d : d, c = from_p ? m.v : m.w, rest = from_p ? m.w : m.v;
+    const float power = exp_below(along), u = fmaf(c, power, rest);
+    const float lost = fmaf(c, power, -c) - (u - 1.0f);      // of u, which counts where u is next to 1
+    const float here = log_near(u) + (u < 2.0f ? lost : 0.0f);
+    const float there = here - along;
+    const float of_p = from_p ? here : there, of_q = from_p ? there : here;
+    const bool near = size < kNear;
+    *slope = x.q == 0.0f ? 0.0f : -m.v * x.q * (near ? near_q : of_q);
+    *term = near ? part : (x.p == 0.0f ? 0.0f : -m.w * x.p * of_p) + *slope;
+}
+
+// A divergence's term of one entry, and its slope by the student's log; `plus` is the constant of the reverse
+// divergence's slope, which probabilities that sum to 1 cancel.
 template <bool MIX>
 __device__ __forceinline__ void entry(int kind, const Mixture& m, const Entry& x, float plus, float* term, float* slope) {
     if (MIX) {
-        float less_p, less_q;
-        below(m, x.d, x.ratio, &less_p, &less_q);
-        *slope = x.q == 0.0f ? 0.0f : m.v * x.q * less_q;
-        *term = (x.p == 0.0f ? 0.0f : m.w * x.p * less_p) + *slope;
+        mixture_entry(m, x, term, slope);
     } else if (kind == ODB_DISTILL_FORWARD) {
         *term = x.p == 0.0f ? 0.0f : x.p * x.d;
         *slope = -x.p;
@@ -193,7 +217,8 @@ __device__ __forceinline__ void exp_sums(const float t[4], double e[4]) {
 
 // A counted token: its value on every lane of the group, and this lane's slopes.
 template <bool MIX, int SUPPORT, int L>
-__device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, int64_t e, int l, float slope[4]) {
+__device__ __forceinline__ double token(const DistillArgs& A, int64_t e, int l, float slope[4]) {
+    const Mixture& m = A.mix;
     float t[4], s[4], q[4];
     bool there[4];
     load_entries(A.teacher + e * A.k, A.k, l, t);
@@ -236,22 +261,15 @@ __device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, 
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        Entry x{0.0f, 0.0f, t[i] - s[i], 0.0f};
+        Entry x{0.0f, 0.0f, t[i] - s[i]};
         if (SUPPORT == ODB_SUPPORT_REST) {
             sum_p += wide_p[i];
             sum_q += wide_q[i];
             x.p = (float)wide_p[i];
             x.q = (float)wide_q[i];
-            if (MIX) x.ratio = exp_below(-fabsf(x.d));
         } else if (SUPPORT == ODB_SUPPORT_RENORMALIZED) {
             x.p = share_p[i];
             x.q = share_q[i];
-            if (MIX) x.ratio = exp_below(-fabsf(x.d));
-        } else if (MIX) {
-            const float larger = exp_near(x.d >= 0.0f ? t[i] : s[i]);
-            x.ratio = exp_below(-fabsf(x.d));
-            x.p = x.d >= 0.0f ? larger : larger * x.ratio;
-            x.q = x.d >= 0.0f ? larger * x.ratio : larger;
         } else {
             x.p = exp_near(t[i]);
             x.q = exp_near(s[i]);
@@ -275,10 +293,9 @@ __device__ __forceinline__ double token(const DistillArgs& A, const Mixture& m, 
     const bool held = rq <= kRestLeast;
     if (rp < kRestLeast) rp = kRestLeast;      // a NaN stays
     if (rq < kRestLeast) rq = kRestLeast;
-    Entry rest{(float)rp, (float)rq, 0.0f, 0.0f};
+    Entry rest{(float)rp, (float)rq, 0.0f};
     const float over_q = __builtin_amdgcn_rcpf(rest.q), times = rest.p * over_q;     // 2^-24 to 2^24
     rest.d = log_near(times);
-    if (MIX) rest.ratio = rest.d >= 0.0f ? rest.q * __builtin_amdgcn_rcpf(rest.p) : times;
     float term, by;
     entry<MIX>(A.kind, m, rest, 0.0f, &term, &by);
     // d rq = -q_j d s_j, unless it is held at its least; there the reverse's slopes keep their constant
@@ -307,7 +324,6 @@ __device__ __forceinline__ DistillSum distill_span(const DistillArgs& A, const S
     const int l = threadIdx.x & (L - 1);
     const uint32_t maxlen = (uint32_t)s.maxlen, row_a = row_in(s, a0), col_a = (uint32_t)(a0 - s.lo) - row_a * maxlen;
     const int n = (int)(a1 - a0);
-    const Mixture m{(float)A.mix, (float)(1.0 - A.mix)};
     DistillSum S{0.0, 0};
     int o = threadIdx.x / L;
     int32_t y = o < n ? A.t.d_labels[a0 + o] : ODB_LABEL_IGNORE;
@@ -328,7 +344,7 @@ __device__ __forceinline__ DistillSum distill_span(const DistillArgs& A, const S
         const bool on = label != ODB_LABEL_IGNORE && col >= (uint32_t)A.t.shift;
         float g[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (on) {
-            const double value = token<MIX, SUPPORT, L>(A, m, a0 + o, l, g);
+            const double value = token<MIX, SUPPORT, L>(A, a0 + o, l, g);
             double f;
             float gs;
             weight((int)(row_a + r), &f, &gs);
@@ -489,6 +505,30 @@ int32_t piece_for(int64_t elems, int32_t k) {
     return piece;
 }
 
+// The cumulants of a weight w are w, w v, w v (1 - 2 w), ...: each is w v times the derivative by w of the one before,
+// and c_n = (that) / (w v) a polynomial in w, c_{n+1} = (1 - 2 w) c_n + w v c_n'.
+Mixture mixture_of(double w) {
+    constexpr int kTerms = 9;      // c_2 to c_10
+    Mixture m;
+    const double v = 1.0 - w;
+    m.w = (float)w;
+    m.v = (float)v;
+    double by[kTerms] = {1.0}, factorial = 1.0;      // c_n's coefficients, n!
+    for (int n = 2; n < 10; ++n) {
+        double c = 0.0, next[kTerms] = {};
+        factorial *= n;
+        for (int i = kTerms - 1; i >= 0; --i) c = c * w + by[i];
+        if (n - 2 < 7) m.log_by[n - 2] = (float)(v * c / factorial);
+        m.term_by[n - 2] = (float)(c * (n - 1) / factorial);
+        for (int i = 0; i < n - 1; ++i) {      // (1 - 2 w) by + (w - w^2) by'
+            next[i] += by[i] * (1 + i);
+            next[i + 1] -= by[i] * (2 + i);
+        }
+        std::copy(next, next + kTerms, by);
+    }
+    return m;
+}
+
 struct DistillLayout {
     size_t chunk_slot, slot_count, row_count, part, disorder, total;
     int64_t chunks, pieces;
@@ -602,7 +642,7 @@ extern "C" int odb_distill_loss(const odb_tiles_t* t, const odb_distill_params_t
     a.part = ws_at<DistillPart>(d_ws, L.part);
     a.pieces = L.pieces;
     a.loss_scale = p->loss_scale;
-    a.mix = mix ? p->mix : 0.5;
+    if (mix) a.mix = mixture_of(p->mix);
     a.piece = L.piece;
     a.piece_log2 = __builtin_ctz((unsigned)L.piece);
     a.k = k;

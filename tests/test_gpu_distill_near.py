@@ -1,0 +1,100 @@
+"""The distillation loss beside the teacher: a student that starts from its weights or has nearly learned it.  There
+a divergence falls with the square of the distance and its slopes with the distance; both are compared relative to
+themselves, with the definition in extended precision.
+
+A probability costs up to 7 roundings, the series of a term or a logarithm and its products 11 more, a sum over a
+list at most nine (three adds of a lane, six over the lanes): values and slopes are right to C = 40 roundings of
+themselves where nothing but products stands between them and the inputs."""
+import math
+
+import numpy as np
+import pytest
+
+from _losses import U, Plan
+from _parity import log
+from test_gpu_distill import Run
+
+pytestmark = pytest.mark.gpu
+
+X = np.longdouble
+C = 40
+LISTED, RENORMALIZED, REST = 0, 1, 2
+NOISE = [0.05, 1e-2, 1e-3, 1e-4]
+
+
+def _near(rng, E, k, noise):
+    """A teacher's lists and those of a student beside it: likeliest first, some lists end early."""
+    z = -np.cumsum(rng.exponential(0.5, (E, k)), -1)
+    t = z - np.log(np.exp(z).sum(-1, keepdims=True)) + np.log(rng.uniform(0.6, 0.999, (E, 1)))
+    s = t + noise * (rng.standard_normal((E, k)).clip(-4, 4) + rng.standard_normal((E, 1)).clip(-4, 4))
+    t, s = t.astype(np.float32), s.astype(np.float32)
+    none = np.arange(k)[None] >= np.where(rng.random(E) < 0.3, rng.integers(1, k + 1, E), k)[:, None]
+    t[none] = -math.inf
+    return t, s
+
+
+def _extended(t, s):
+    """Logs and probabilities of the entries, 0 for those that are none."""
+    there = t != -math.inf
+    t, s = np.where(there, t, 0).astype(X), np.where(there, s, 0).astype(X)
+    return t, s, np.where(there, np.exp(t), 0), np.where(there, np.exp(s), 0), there
+
+
+def _mixture(w, p, q, d):
+    """Terms of the divergence from the mixture, and ln(q / m)."""
+    w = X(w)
+    less_p, less_q = -np.log1p((1 - w) * np.expm1(-d)), -np.log1p(w * np.expm1(d))
+    return w * p * less_p + (1 - w) * q * less_q, less_q
+
+
+def _run(t, s, kind, support, w):
+    """Every token's value, in a slot of its own, and the slopes."""
+    import paper_2606_19989_amd as odb
+    E, k = t.shape
+    params = odb.DistillParams(kind=kind, support=support, reduce=2, mix=w)
+    y = np.zeros(E, np.int32)
+    each, all_ = Run(Plan([[1]] * E), y, t, s, k, params, shift=0), Run(Plan([[1] * E]), y, t, s, k, params, shift=0)
+    each()
+    all_()
+    value, slope = each.numpy()[1], each.numpy()[3]
+    assert np.array_equal(slope, all_.numpy()[3])
+    return value, slope
+
+
+def _hold(name, got, want, tol):
+    ratio = np.abs(got - want) / tol
+    log(f"  {name}: {float(ratio.max()):.3f} of the tolerance")
+    assert np.all(ratio <= 1), (name, float(ratio.max()))
+
+
+@pytest.mark.parametrize("noise", NOISE)
+@pytest.mark.parametrize("w", [0.3, 0.5, 1e-3, 0.999])
+def test_mixture_of_listed_entries(w, noise):
+    rng = np.random.default_rng(31)
+    for E, k in ((700, 16), (200, 100), (900, 3)):
+        log(f"distill near: mixture {w}, noise {noise}, k {k}")
+        t, s = _near(rng, E, k, noise)
+        value, grad = _run(t, s, 2, LISTED, w)
+        t64, s64, p, q, _ = _extended(t, s)
+        term, less_q = _mixture(w, p, q, t64 - s64)
+        _hold("values", value, term.sum(-1), C * U * term.sum(-1) + 1e-37)
+        assert np.all(value >= 0)
+        slope = (1 - X(w)) * q * less_q
+        _hold("slopes", grad, slope, C * U * np.abs(slope) + 2.0 ** -115)
+
+
+@pytest.mark.parametrize("noise", [0.7, 3.0])
+@pytest.mark.parametrize("w", [0.3, 1e-3, 0.999, 1e-6])
+def test_mixture_of_a_small_weight(w, noise):
+    """Away from the teacher a term is a sum of two of either sign, right to 100 roundings of those, and a logarithm
+    to 100 of itself: one side's is taken, right to 3 of at most 16, and the distance leaves the other's, ln 2 or more."""
+    rng = np.random.default_rng(32)
+    t, s = _near(rng, 700, 16, noise)
+    log(f"distill: mixture {w}, noise {noise}")
+    value, grad = _run(t, s, 2, LISTED, w)
+    t64, s64, p, q, _ = _extended(t, s)
+    term, less_q = _mixture(w, p, q, t64 - s64)
+    slope = (1 - X(w)) * q * less_q
+    sizes = np.abs(slope) + np.abs(term - slope)
+    _hold("values", value, term.sum(-1), 100 * U * sizes.sum(-1) + 1e-37)
+    _hold("slopes", grad, slope, 100 * U * np.abs(slope) + 2.0 ** -115)
