@@ -9,8 +9,8 @@
 //
 // Bound by the reads of both lists and the writes of the gradient, 12 k bytes an element, and beside them by the
 // powers, logarithms and series: some 40 to 100 instructions an entry, with the rest most, whose sums need powers in 64
-// bits.  2.1 M elements of 32 entries (64% counted), the reverse divergence with the rest: 170 us for 620 MB
-// (3.6 TB/s, instructions two thirds of the time); 0.54 M of 27, the mixture, renormalised: 76 us for 172 MB; one
+// bits.  2.1 M elements of 32 entries (64% counted), the reverse divergence with the rest: 184 us for 620 MB
+// (3.4 TB/s, instructions most of the time); 0.54 M of 27, the mixture, renormalised: 76 us for 172 MB; one
 // tile of 16,384 of 64: 15 us, three launches one after the other, of which the lists' pass takes 8.
 #include <algorithm>
 
@@ -177,6 +177,23 @@ __device__ __forceinline__ void mixture_entry(const Mixture& m, const Entry& x, 
     *term = near ? part : (x.p == 0.0f ? 0.0f : -m.w * x.p * of_p) + *slope;
 }
 
+// ln (1 + x), |x| < 1/2: the logarithm of the rounded sum, and what that lost.
+__device__ __forceinline__ float log_beside(float x) {
+    const float u = 1.0f + x;
+    return log_near(u) + (x - (u - 1.0f));
+}
+
+// Where a and b both sum to 1, sum a ln (a / b) is the sum of a ln (a / b) + b - a = a (e^r - 1 - r), r = ln (b / a):
+// of none below 0, where the logs' own sum is the small difference of numbers of either sign.  Next to r = 0 a series,
+// whose rest is below 2^-27 of it.  *rise: b - a, right to itself there.
+__device__ __forceinline__ float excess(float a, float b, float r, float* rise) {
+    const float c[8] = {1.0f / 2, 1.0f / 6, 1.0f / 24, 1.0f / 120, 1.0f / 720, 1.0f / 5040, 1.0f / 40320, 1.0f / 362880};
+    const float bend = r * r * series(c, r);
+    const bool near = fabsf(r) < kNear;
+    *rise = near ? a * (r + bend) : b - a;
+    return near ? a * bend : a == 0.0f ? b : (b - a) - a * r;
+}
+
 // A divergence's term of one entry, and its slope by the student's log; `plus` is the constant of the reverse
 // divergence's slope, which probabilities that sum to 1 cancel.
 template <bool MIX>
@@ -192,8 +209,9 @@ __device__ __forceinline__ void entry(int kind, const Mixture& m, const Entry& x
     }
 }
 
-// exp of four numbers in 64 bits to 2^-40, for sums of probabilities that are taken from 1: 2^n exp(g),
-// |g| <= ln 2 / 2, by the series up to g^10.  Together, so that a coefficient is there for all.
+// exp of four numbers in 64 bits to 2^-46, for sums of probabilities that are taken from 1: 2^n exp(g),
+// |g| <= ln 2 / 2, by the polynomial of degree 9 whose largest relative error there is least (the series needs degree
+// 11: 186 us where this takes 184, 2.1 M lists of 32).  Together, so that a coefficient is there for all.
 __device__ __forceinline__ void exp_sums(const float t[4], double e[4]) {
     double g[4];
     int n[4];
@@ -203,16 +221,79 @@ __device__ __forceinline__ void exp_sums(const float t[4], double e[4]) {
         const float by = rintf(x * kLog2e);
         n[i] = (int)by;
         g[i] = fma((double)by, -0.69314718055994530942, (double)x);
-        e[i] = 1.0 / 3628800.0;
+        e[i] = 2.7482089332277467e-06;
     }
-    const double c[10] = {1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0,
-                          1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+    const double c[9] = {2.4884117327236977e-05, 0.00019841597248962728, 0.0013888802604866363, 0.00833333300152798,
+                         0.041666667033890305, 0.1666666666783302, 0.4999999999945516, 0.9999999999998921,
+                         1.0000000000000129};
 #pragma unroll
-    for (int j = 0; j < 10; ++j)
+    for (int j = 0; j < 9; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) e[i] = fma(e[i], g[i], c[j]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) e[i] = ldexp(e[i], n[i]);
+}
+
+// A counted token's lists with what they leave out as one more entry.  1 - sum cancels, and so does the difference of
+// the rests, which stands for the distance of their logs beside the teacher: both in 64 bits.
+template <bool MIX, int L>
+__device__ __forceinline__ double token_with_rest(const DistillArgs& A, const float t[4], const float s[4],
+                                                  const bool there[4], float slope[4]) {
+    const Mixture& m = A.mix;
+    const bool forward = A.kind == ODB_DISTILL_FORWARD;
+    double wide_p[4], wide_q[4], rp = 0.0, rq = 0.0;
+    exp_sums(t, wide_p);
+    exp_sums(s, wide_q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        rp += wide_p[i];
+        rq += wide_q[i];
+    }
+    rp = 1.0 - lanes_sum<L>(rp);
+    rq = 1.0 - lanes_sum<L>(rq);
+    const bool held = rq <= kRestLeast;
+    double over = 0.0;      // by how much the teacher's sum is above 1, less the student's
+    if (rp < kRestLeast) {      // a NaN stays
+        over += kRestLeast - rp;
+        rp = kRestLeast;
+    }
+    if (rq < kRestLeast) {
+        over -= kRestLeast - rq;
+        rq = kRestLeast;
+    }
+    Entry rest{(float)rp, (float)rq, 0.0f};
+    const float over_q = __builtin_amdgcn_rcpf(rest.q), times = rest.p * over_q;     // 2^-24 to 2^24
+    const float apart = (float)(rp - rq) * over_q;      // p / q - 1
+    const bool beside = fabsf(apart) < kNear;
+    rest.d = beside ? log_beside(apart) : log_near(times);
+    float value = 0.0f, term, rise, q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Entry x{(float)wide_p[i], (float)wide_q[i], t[i] - s[i]};
+        q[i] = x.q;
+        if (MIX) {
+            mixture_entry(m, x, &term, &slope[i]);
+        } else if (forward) {
+            term = excess(x.p, x.q, -x.d, &rise);
+            // -p + q rp / rq, unless the student's rest is held
+            slope[i] = beside && !held ? fmaf(x.q, apart, rise) : fmaf(x.q, held ? 0.0f : times, -x.p);
+        } else {
+            term = excess(x.q, x.p, x.d, &rise);
+            slope[i] = x.q == 0.0f ? 0.0f : x.q * ((held ? 1.0f : rest.d) - x.d);
+        }
+        if (!there[i]) term = slope[i] = 0.0f;
+        value += term;
+    }
+    value = lanes_sum<L>(value);
+    if (MIX) {
+        mixture_entry(m, rest, &term, &rise);
+        const float moves = held ? 0.0f : rise * over_q;      // d rq = -q_j d s_j
+#pragma unroll
+        for (int i = 0; i < 4; ++i) slope[i] = there[i] ? fmaf(-q[i], moves, slope[i]) : 0.0f;
+        return (double)value + (double)term;
+    }
+    term = forward ? excess(rest.p, rest.q, -rest.d, &rise) : excess(rest.q, rest.p, rest.d, &rise);
+    return (double)value + (double)term + (forward ? over : -over);
 }
 
 // A counted token: its value on every lane of the group, and this lane's slopes.
@@ -228,6 +309,7 @@ __device__ __forceinline__ double token(const DistillArgs& A, int64_t e, int l, 
         there[i] = 4 * l + i < A.k && t[i] != kNone;
         if (!there[i]) t[i] = s[i] = kNone;
     }
+    if (SUPPORT == ODB_SUPPORT_REST) return token_with_rest<MIX, L>(A, t, s, there, slope);
     float share_p[4], share_q[4];
     if (SUPPORT == ODB_SUPPORT_RENORMALIZED) {
         float mt = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), ms = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
@@ -254,20 +336,10 @@ __device__ __forceinline__ double token(const DistillArgs& A, int64_t e, int l, 
         }
     }
     float value = 0.0f, slopes = 0.0f;
-    double sum_p = 0.0, sum_q = 0.0, wide_p[4], wide_q[4];
-    if (SUPPORT == ODB_SUPPORT_REST) {
-        exp_sums(t, wide_p);
-        exp_sums(s, wide_q);
-    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         Entry x{0.0f, 0.0f, t[i] - s[i]};
-        if (SUPPORT == ODB_SUPPORT_REST) {
-            sum_p += wide_p[i];
-            sum_q += wide_q[i];
-            x.p = (float)wide_p[i];
-            x.q = (float)wide_q[i];
-        } else if (SUPPORT == ODB_SUPPORT_RENORMALIZED) {
+        if (SUPPORT == ODB_SUPPORT_RENORMALIZED) {
             x.p = share_p[i];
             x.q = share_q[i];
         } else {
@@ -287,22 +359,7 @@ __device__ __forceinline__ double token(const DistillArgs& A, int64_t e, int l, 
 #pragma unroll
         for (int i = 0; i < 4; ++i) slope[i] = fmaf(-q[i], slopes, slope[i]);
     }
-    if (SUPPORT != ODB_SUPPORT_REST) return value;
-    // what the lists leave out, as one more entry: 1 - sum cancels, so it is taken in 64 bits
-    double rp = 1.0 - lanes_sum<L>(sum_p), rq = 1.0 - lanes_sum<L>(sum_q);
-    const bool held = rq <= kRestLeast;
-    if (rp < kRestLeast) rp = kRestLeast;      // a NaN stays
-    if (rq < kRestLeast) rq = kRestLeast;
-    Entry rest{(float)rp, (float)rq, 0.0f};
-    const float over_q = __builtin_amdgcn_rcpf(rest.q), times = rest.p * over_q;     // 2^-24 to 2^24
-    rest.d = log_near(times);
-    float term, by;
-    entry<MIX>(A.kind, m, rest, 0.0f, &term, &by);
-    // d rq = -q_j d s_j, unless it is held at its least; there the reverse's slopes keep their constant
-    const float moves = !held ? by * over_q : !MIX && A.kind == ODB_DISTILL_REVERSE ? -1.0f : 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) slope[i] = fmaf(-q[i], moves, slope[i]);
-    return (double)value + (double)term;
+    return value;
 }
 
 // The block's tokens of a slot's elements [a0, a1): weight(row) gives a token's weight in the reduction and the

@@ -22,10 +22,10 @@ LISTED, RENORMALIZED, REST = 0, 1, 2
 NOISE = [0.05, 1e-2, 1e-3, 1e-4]
 
 
-def _near(rng, E, k, noise):
+def _near(rng, E, k, noise, mass=(0.6, 0.999)):
     """A teacher's lists and those of a student beside it: likeliest first, some lists end early."""
     z = -np.cumsum(rng.exponential(0.5, (E, k)), -1)
-    t = z - np.log(np.exp(z).sum(-1, keepdims=True)) + np.log(rng.uniform(0.6, 0.999, (E, 1)))
+    t = z - np.log(np.exp(z).sum(-1, keepdims=True)) + np.log(rng.uniform(*mass, (E, 1)))
     s = t + noise * (rng.standard_normal((E, k)).clip(-4, 4) + rng.standard_normal((E, 1)).clip(-4, 4))
     t, s = t.astype(np.float32), s.astype(np.float32)
     none = np.arange(k)[None] >= np.where(rng.random(E) < 0.3, rng.integers(1, k + 1, E), k)[:, None]
@@ -98,3 +98,52 @@ def test_mixture_of_a_small_weight(w, noise):
     sizes = np.abs(slope) + np.abs(term - slope)
     _hold("values", value, term.sum(-1), 100 * U * sizes.sum(-1) + 1e-37)
     _hold("slopes", grad, slope, 100 * U * np.abs(slope) + 2.0 ** -115)
+
+
+# Powers whose sums are taken from 1 are right to 2^-46.
+WIDE = 2.0 ** -46
+
+
+@pytest.mark.parametrize("mass", [(0.6, 0.999), (1 - 1e-3, 1 - 1e-5)])
+@pytest.mark.parametrize("noise", NOISE)
+@pytest.mark.parametrize("kind", [0, 1, 2])
+def test_with_the_rest(kind, noise, mass):
+    """What the lists leave out is one entry more; its log's distance is right to a few roundings and to what the powers
+    leave of it.  Where it is more than 1/2, or the rest is held, the rest's probabilities stand in its place."""
+    w = 0.3
+    rng = np.random.default_rng(33)
+    for E, k in ((700, 16), (200, 100), (900, 3)):
+        log(f"distill near: kind {kind} with the rest of {mass}, noise {noise}, k {k}")
+        t, s = _near(rng, E, k, noise, mass)
+        value, grad = _run(t, s, kind, REST, w)
+        t64, s64, p, q, there = _extended(t, s)
+        d = t64 - s64
+        rp, rq = 1 - p.sum(-1), 1 - q.sum(-1)
+        held = rq <= 2.0 ** -24
+        rp, rq = np.maximum(rp, 2.0 ** -24), np.maximum(rq, 2.0 ** -24)
+        x0, d0 = (rp - rq) / rq, np.log(rp) - np.log(rq)
+        near = (np.abs(x0) < 0.49) & (np.abs(d0) < 0.49)
+        assert near.any()
+        if kind == 0:
+            D = (p * d).sum(-1) + rp * d0
+            slope = -p + q * np.where(held, 0, rp / rq)[:, None]
+            size = np.where(near & ~held, p.T * np.abs(np.expm1(-d.T)) + q.T * np.abs(x0), p.T + q.T * rp / rq)
+        elif kind == 1:
+            D = -(q * d).sum(-1) - rq * d0
+            slope = q * (np.where(held, 1, d0)[:, None] - d)
+            size = q.T * (np.abs(d.T) + np.where(held, 1, np.abs(d0)))
+        else:
+            term, less_q = _mixture(w, p, q, d)
+            term0, less_q0 = _mixture(w, rp, rq, d0)
+            D = term.sum(-1) + term0
+            slope = (1 - w) * q * (less_q - np.where(held, 0, less_q0)[:, None])
+            size = (1 - w) * q.T * (np.abs(less_q.T) + np.abs(less_q0))
+        wide = WIDE / np.minimum(rp, rq)
+        # D is the sum of terms of none below 0 and of what the held rests add to the sums, `over`; that may be below 0
+        # and leave less of D than the terms are, whose roundings count: they are D - over or D + over
+        over = np.abs(p.sum(-1) + rp - q.sum(-1) - rq)
+        tol = C * U * (np.abs(D) + 2 * over + np.where(near, 0, rp + rq)) + 4 * WIDE * np.abs(d0) + 1e-37
+        _hold("values", value, D, tol)
+        assert np.all(value[near & ~held] >= 0)
+        tol = C * U * size.T + (4 * q * wide[:, None]) + 2.0 ** -115
+        _hold("slopes", grad, np.where(there, slope, 0), tol)
