@@ -10,7 +10,7 @@
 // Bound by the reads of both lists and the writes of the gradient, 12 k bytes an element, and beside them by the
 // powers, logarithms and series: some 40 to 100 instructions an entry, with the rest most, whose sums need powers in 64
 // bits.  2.1 M elements of 32 entries (64% counted), the reverse divergence with the rest: 184 us for 620 MB
-// (3.4 TB/s, instructions most of the time); 0.54 M of 27, the mixture, renormalised: 76 us for 172 MB; one
+// (3.4 TB/s, instructions most of the time); 0.54 M of 27, the mixture, renormalised: 80 us for 172 MB; one
 // tile of 16,384 of 64: 15 us, three launches one after the other, of which the lists' pass takes 8.
 #include <algorithm>
 
@@ -194,21 +194,6 @@ __device__ __forceinline__ float excess(float a, float b, float r, float* rise) 
     return near ? a * bend : a == 0.0f ? b : (b - a) - a * r;
 }
 
-// A divergence's term of one entry, and its slope by the student's log; `plus` is the constant of the reverse
-// divergence's slope, which probabilities that sum to 1 cancel.
-template <bool MIX>
-__device__ __forceinline__ void entry(int kind, const Mixture& m, const Entry& x, float plus, float* term, float* slope) {
-    if (MIX) {
-        mixture_entry(m, x, term, slope);
-    } else if (kind == ODB_DISTILL_FORWARD) {
-        *term = x.p == 0.0f ? 0.0f : x.p * x.d;
-        *slope = -x.p;
-    } else {
-        *term = x.q == 0.0f ? 0.0f : -x.q * x.d;
-        *slope = fmaf(x.q, plus, *term);
-    }
-}
-
 // exp of four numbers in 64 bits to 2^-46, for sums of probabilities that are taken from 1: 2^n exp(g),
 // |g| <= ln 2 / 2, by the polynomial of degree 9 whose largest relative error there is least (the series needs degree
 // 11: 186 us where this takes 184, 2.1 M lists of 32).  Together, so that a coefficient is there for all.
@@ -296,11 +281,73 @@ __device__ __forceinline__ double token_with_rest(const DistillArgs& A, const fl
     return (double)value + (double)term + (forward ? over : -over);
 }
 
+// A counted token's lists, each divided by its sum.  The logs of the sums are off by roundings, and with them, beside the
+// teacher, all of a token's distances d by the same much more than their own.  By how much, e, is what is left of the sum
+// of p - q, which is 0, when one side comes from the other with these distances: the forward and the reverse divergence,
+// as sums of their excess, are too large by e^2 / 2 then, their slopes have it taken off.  The mixture, whose
+// terms do not show it, has the sums' distance from the sum of the entries' differences, to begin with.
+template <bool MIX, int L>
+__device__ __forceinline__ double token_renormalized(const DistillArgs& A, const float t[4], const float s[4],
+                                                     const bool there[4], float slope[4]) {
+    const bool forward = A.kind == ODB_DISTILL_FORWARD;
+    const float mt = lanes_max<L>(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
+    const float ms = lanes_max<L>(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
+    Entry x[4];
+    float sum_t = 0.0f, sum_s = 0.0f, more = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i].p = there[i] ? exp_below(t[i] - mt) : 0.0f;
+        x[i].q = there[i] ? exp_below(s[i] - ms) : 0.0f;
+        x[i].d = (t[i] - s[i]) - (mt - ms);
+        sum_t += x[i].p;
+        sum_s += x[i].q;
+        if (MIX) {      // p - q; next to each other q (e^d - 1), the series to 2^-24 of it
+            const float c[5] = {1.0f, 1.0f / 2, 1.0f / 6, 1.0f / 24, 1.0f / 120};
+            more += fabsf(x[i].d) < 0.125f ? x[i].q * (x[i].d * series(c, x[i].d)) : x[i].p - x[i].q;
+        }
+    }
+    sum_t = lanes_sum<L>(sum_t);      // 1 to k
+    sum_s = lanes_sum<L>(sum_s);
+    const float over_t = __builtin_amdgcn_rcpf(sum_t), over_s = __builtin_amdgcn_rcpf(sum_s);
+    float by = log_near(sum_t * over_s);
+    if (MIX) {
+        const float apart = lanes_sum<L>(more) * over_s;
+        if (fabsf(apart) < kNear) by = log_beside(apart);
+    }
+    float value = 0.0f, rises = 0.0f, term;      // MIX: rises are slopes
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i].p *= over_t;
+        x[i].q *= over_s;
+        x[i].d -= by;
+        if (MIX)
+            mixture_entry(A.mix, x[i], &term, &slope[i]);
+        else
+            term = excess(forward ? x[i].p : x[i].q, forward ? x[i].q : x[i].p, forward ? -x[i].d : x[i].d, &slope[i]);
+        if (!there[i]) term = slope[i] = x[i].q = 0.0f;
+        value += term;
+        rises += slope[i];
+    }
+    value = lanes_sum<L>(value);
+    rises = lanes_sum<L>(rises);
+    if (!MIX) {
+        value = fmaf(-0.5f * rises, rises, value);
+        if (value < 0.0f) value = 0.0f;      // of no distance but e; a NaN stays
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (MIX || forward)
+            slope[i] = fmaf(-x[i].q, rises, slope[i]);
+        else
+            slope[i] = x[i].q == 0.0f ? 0.0f : -x[i].q * ((x[i].d - rises) + value);
+    }
+    return value;
+}
+
 // A counted token: its value on every lane of the group, and this lane's slopes.
 template <bool MIX, int SUPPORT, int L>
 __device__ __forceinline__ double token(const DistillArgs& A, int64_t e, int l, float slope[4]) {
-    const Mixture& m = A.mix;
-    float t[4], s[4], q[4];
+    float t[4], s[4];
     bool there[4];
     load_entries(A.teacher + e * A.k, A.k, l, t);
     load_entries(A.student + e * A.k, A.k, l, s);
@@ -310,56 +357,25 @@ __device__ __forceinline__ double token(const DistillArgs& A, int64_t e, int l, 
         if (!there[i]) t[i] = s[i] = kNone;
     }
     if (SUPPORT == ODB_SUPPORT_REST) return token_with_rest<MIX, L>(A, t, s, there, slope);
-    float share_p[4], share_q[4];
-    if (SUPPORT == ODB_SUPPORT_RENORMALIZED) {
-        float mt = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), ms = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-        mt = lanes_max<L>(mt);
-        ms = lanes_max<L>(ms);
-        float st = 0.0f, ss = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            share_p[i] = there[i] ? exp_below(t[i] - mt) : 0.0f;
-            share_q[i] = there[i] ? exp_below(s[i] - ms) : 0.0f;
-            st += share_p[i];
-            ss += share_q[i];
-        }
-        st = lanes_sum<L>(st);
-        ss = lanes_sum<L>(ss);
-        const float lt = log_near(st), ls = log_near(ss);      // 1 to k
-        const float over_t = __builtin_amdgcn_rcpf(st), over_s = __builtin_amdgcn_rcpf(ss);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            t[i] = (t[i] - mt) - lt;
-            s[i] = (s[i] - ms) - ls;
-            share_p[i] *= over_t;      // exp(t), without another power
-            share_q[i] *= over_s;
-        }
-    }
-    float value = 0.0f, slopes = 0.0f;
+    if (SUPPORT == ODB_SUPPORT_RENORMALIZED) return token_renormalized<MIX, L>(A, t, s, there, slope);
+    float value = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        Entry x{0.0f, 0.0f, t[i] - s[i]};
-        if (SUPPORT == ODB_SUPPORT_RENORMALIZED) {
-            x.p = share_p[i];
-            x.q = share_q[i];
-        } else {
-            x.p = exp_near(t[i]);
-            x.q = exp_near(s[i]);
-        }
+        const Entry x{exp_near(t[i]), exp_near(s[i]), t[i] - s[i]};
         float term;
-        entry<MIX>(A.kind, m, x, SUPPORT == ODB_SUPPORT_LISTED ? 1.0f : 0.0f, &term, &slope[i]);
-        if (!there[i]) term = slope[i] = x.q = 0.0f;
-        q[i] = x.q;
+        if (MIX) {
+            mixture_entry(A.mix, x, &term, &slope[i]);
+        } else if (A.kind == ODB_DISTILL_FORWARD) {
+            term = x.p == 0.0f ? 0.0f : x.p * x.d;
+            slope[i] = -x.p;
+        } else {
+            term = x.q == 0.0f ? 0.0f : -x.q * x.d;
+            slope[i] = x.q + term;
+        }
+        if (!there[i]) term = slope[i] = 0.0f;
         value += term;
-        slopes += slope[i];
     }
-    value = lanes_sum<L>(value);
-    if (SUPPORT == ODB_SUPPORT_RENORMALIZED) {
-        slopes = lanes_sum<L>(slopes);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) slope[i] = fmaf(-q[i], slopes, slope[i]);
-    }
-    return value;
+    return lanes_sum<L>(value);
 }
 
 // The block's tokens of a slot's elements [a0, a1): weight(row) gives a token's weight in the reduction and the

@@ -147,3 +147,42 @@ def test_with_the_rest(kind, noise, mass):
         assert np.all(value[near & ~held] >= 0)
         tol = C * U * size.T + (4 * q * wide[:, None]) + 2.0 ** -115
         _hold("slopes", grad, np.where(there, slope, 0), tol)
+
+
+@pytest.mark.parametrize("noise", NOISE)
+@pytest.mark.parametrize("kind", [0, 1, 2])
+def test_renormalized(kind, noise):
+    """Each side divided by its sum.  With G the largest distance of an entry's logs as they are, a distance less that of
+    the sums' logs is right to d = 2 U G (S + 25): two roundings of G each for the entry's and the largest entries'
+    distances, and powers whose exponents, S at most, are rounded, times distances of 2 G at most.  A value moves with
+    the square of a distance that all entries are off by, and by 2 G U times the distances with each one's own."""
+    w = 0.3
+    rng = np.random.default_rng(34)
+    for E, k in ((700, 16), (200, 100), (900, 3)):
+        log(f"distill near: kind {kind} renormalised, noise {noise}, k {k}")
+        t, s = _near(rng, E, k, noise)
+        value, grad = _run(t, s, kind, RENORMALIZED, w)
+        t64, s64, p, q, there = _extended(t, s)
+        d = np.where(there, t64 - s64, 0)
+        G = np.abs(d).max(-1, keepdims=True)
+        S = np.where(there, np.maximum(t64.max(-1, keepdims=True, where=there, initial=-1e9) - t64,
+                                       s64.max(-1, keepdims=True, where=there, initial=-1e9) - s64), 0).max(-1, keepdims=True)
+        sp, sq = p.sum(-1, keepdims=True), q.sum(-1, keepdims=True)
+        d, p, q = np.where(there, d - (np.log(sp) - np.log(sq)), 0), p / sp, q / sq
+        assert np.abs(d).max() < 0.5
+        off = 2 * U * G * (S + 25)
+        if kind == 0:
+            D, slope = (p * d).sum(-1), q - p
+        elif kind == 1:
+            D = -(q * d).sum(-1)
+            slope = -q * (d + D[:, None])
+        else:
+            term, less_q = _mixture(w, p, q, d)
+            D, slope = term.sum(-1), (1 - w) * q * (less_q - (q * less_q).sum(-1, keepdims=True))
+        both = p + q
+        # a list of one entry has D = 0, of which the oracle's own roundings (2^-63 of logs below 8) leave something
+        tol = U * ((C + S[:, 0]) * D + 8 * G[:, 0] * (both * np.abs(d)).sum(-1)) + off[:, 0] ** 2 + 2.0 ** -60
+        _hold("values", value, D, tol)
+        assert np.all(value >= 0)
+        far = np.abs(d) + (q * np.abs(d)).sum(-1, keepdims=True)
+        _hold("slopes", grad, slope, both * (2 * off + (C + S) * U * far) + 2.0 ** -115)
