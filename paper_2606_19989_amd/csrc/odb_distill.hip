@@ -185,13 +185,14 @@ __device__ __forceinline__ float log_beside(float x) {
 
 // Where a and b both sum to 1, sum a ln (a / b) is the sum of a ln (a / b) + b - a = a (e^r - 1 - r), r = ln (b / a):
 // of none below 0, where the logs' own sum is the small difference of numbers of either sign.  Next to r = 0 a series,
-// whose rest is below 2^-27 of it.  *rise: b - a, right to itself there.
+// whose rest is below 2^-27 of it.  *rise: b - a, right to itself there.  Infinite where b has nothing (r = -inf),
+// however little a has; past r = 200 a is 0 in 32 bits.
 __device__ __forceinline__ float excess(float a, float b, float r, float* rise) {
     const float c[8] = {1.0f / 2, 1.0f / 6, 1.0f / 24, 1.0f / 120, 1.0f / 720, 1.0f / 5040, 1.0f / 40320, 1.0f / 362880};
     const float bend = r * r * series(c, r);
     const bool near = fabsf(r) < kNear;
     *rise = near ? a * (r + bend) : b - a;
-    return near ? a * bend : a == 0.0f ? b : (b - a) - a * r;
+    return near ? a * bend : r == -HUGE_VALF ? HUGE_VALF : (b - a) - a * fminf(r, 200.0f);
 }
 
 // exp of four numbers in 64 bits to 2^-46, for sums of probabilities that are taken from 1: 2^n exp(g),
@@ -366,7 +367,7 @@ __device__ __forceinline__ double token(const DistillArgs& A, int64_t e, int l, 
         if (MIX) {
             mixture_entry(A.mix, x, &term, &slope[i]);
         } else if (A.kind == ODB_DISTILL_FORWARD) {
-            term = x.p == 0.0f ? 0.0f : x.p * x.d;
+            term = x.d == HUGE_VALF ? HUGE_VALF : x.p * x.d;      // p may be 0 in 32 bits
             slope[i] = -x.p;
         } else {
             term = x.q == 0.0f ? 0.0f : -x.q * x.d;

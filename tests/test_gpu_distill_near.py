@@ -186,3 +186,16 @@ def test_renormalized(kind, noise):
         assert np.all(value >= 0)
         far = np.abs(d) + (q * np.abs(d)).sum(-1, keepdims=True)
         _hold("slopes", grad, slope, both * (2 * off + (C + S) * U * far) + 2.0 ** -115)
+
+
+@pytest.mark.parametrize("low", [-60.0, -95.0, -200.0, -1000.0])
+@pytest.mark.parametrize("support", [LISTED, RENORMALIZED, REST])
+def test_an_entry_that_only_the_teacher_gives(support, low):
+    """However little the teacher gives it: a forward divergence is infinite, the others and all slopes are not."""
+    t = np.tile(np.float32([-0.7, low, -1.5, -math.inf]), (300, 1))
+    s = np.tile(np.float32([-0.6, -math.inf, -1.75, -math.inf]), (300, 1))
+    for kind in range(3):
+        value, slope = _run(t, s, kind, support, 0.3)
+        assert np.all(value == math.inf) if kind == 0 else np.all((value > 0) & (value < 2)) or support == LISTED
+        assert np.all(np.isfinite(value)) or kind == 0
+        assert np.all(np.isfinite(slope)) and np.all(slope[:, 3] == 0)
