@@ -637,7 +637,8 @@ int odb_token_list_logprobs(const odb_logits_t* x, const int32_t* d_labels, int3
  *   grad strides
  *   d_status           as in the forward call
  *
- * Where all of a token's g_j are 0 its gradient is 0.  Sums run in 32 bits, in the list's order.
+ * Where all of a token's g_j are 0 its gradient is 0.  Sums run in 32 bits, in an order that type, sizes and the
+ * token's ids alone decide (it is not the list's): results are the same bit for bit from call to call.
  * Asynchronous (one kernel); needs no workspace.
  */
 int odb_token_list_logprobs_backward(const odb_logits_t* x, const int32_t* d_labels, int32_t k, const int32_t* d_ids,
