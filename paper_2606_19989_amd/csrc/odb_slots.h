@@ -261,7 +261,8 @@ __device__ __forceinline__ void add_to_rows(int* s_rows, Group q, uint32_t on, i
 // Bound by the reads of the labels: 67 M elements in 2,080 tiles take 59 us (5.1 TB/s).
 template <bool ROWS, bool BITS>
 __global__ void __launch_bounds__(kBlock) slot_count_kernel(SlotCounts A) {
-    __shared__ alignas(16) uint8_t s_nibble[kMaxChunk / 4];
+    constexpr bool kNibbles = ROWS || BITS;      // who reads them
+    __shared__ alignas(16) uint8_t s_nibble[kNibbles ? kMaxChunk / 4 : 4];
     __shared__ int s_rows[ROWS ? kLdsRows : 1];
     const odb_tiles_t& t = A.t;
     if (blockIdx.x >= A.chunks) return check_slots(t, blockIdx.x - A.chunks, A.disorder, A.check_blocks, NoVisit{});
@@ -271,7 +272,7 @@ __global__ void __launch_bounds__(kBlock) slot_count_kernel(SlotCounts A) {
     if (c0 >= c1) return;
     const int32_t* labels = t.d_labels + c0;
     const int last = last_four(t, c0);
-    for (int i = threadIdx.x; i < A.chunk / 16; i += kBlock) reinterpret_cast<uint32_t*>(s_nibble)[i] = 0;
+    for (int i = threadIdx.x; kNibbles && i < A.chunk / 16; i += kBlock) reinterpret_cast<uint32_t*>(s_nibble)[i] = 0;
     const int64_t k0 = first_slot(t, e_base, c0);
     if (threadIdx.x == 0) A.chunk_slot[b] = (int32_t)k0;
     __syncthreads();
@@ -287,7 +288,7 @@ __global__ void __launch_bounds__(kBlock) slot_count_kernel(SlotCounts A) {
         Group q = p.first((int)threadIdx.x);
         auto take = [&](const int4u& y) {
             const uint32_t on = count_mask(q, y, p.maxlen, t.shift);
-            if (on) s_nibble[q.o / 4] |= (uint8_t)on;
+            if (kNibbles && on) s_nibble[q.o / 4] |= (uint8_t)on;
             if (lds)
                 add_to_rows(s_rows, q, on, p.maxlen, p.row_a);
             else
