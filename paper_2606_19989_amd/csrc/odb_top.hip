@@ -617,15 +617,20 @@ int check_top(const odb_logits_t* x, int32_t k) {
 }
 
 // Blocks of a position: for fewer positions than would fill the chip, as many as have a round of loads each, as
-// far as their candidates go to one block's LDS.  In a graph, k = 20, 1 / 32 / 128 positions, with one block and with
-// parts: of 32,000 bf16 logits (four rounds) 10.0 / 10.6 / 11.2 and 9.8 / 12.0 / 13.3 us; of 50,000 12.6 / 13.9 / 13.6
-// and 11.8 / 14.1 / 16.2; of 100,000 18.7 / 19.7 / 20.1 and 12.1 / 13.9 / 19.8; of 151,936 24.3 / 25.4 / 26.2 and
-// 13.2 / 15.6 / 18 to 23.
+// far as their candidates go to one block's LDS.  The join costs what six rounds do, and the parts of many positions take
+// turns: a position is split if it has more than six rounds and an eighth as many as there are positions (long lists,
+// which a part cuts to 2 k before the join, a 32nd).  us in a graph with parts / with one block, 1 / 32 / 128 / 512
+// positions of bf16 logits:
+//   logits (rounds)    k = 20                                             k = 128
+//   50,000 (6.1)       12.5/12.4  13.7/13.0  16.1/13.6  21.0/16.4         17.6/24.2  19.3/26.1  23.4/27.0  36.9/29.5
+//   100,000 (12.2)     10.3/17.9  13.0/19.3  18.9/19.6  29.9/24.3         22.0/33.5  25.8/35.0  29.8/35.4  49.4/40.5
+//   151,936 (18.5)     11.8/23.8  14.0/25.2  22.4/25.1  38.4/34.6         23.7/41.5  27.2/44.3  36.2/44.1  61.3/90.0
+//   250,000 (30.5)     12.6/33.6  15.6/34.2  25.5/35.5  54.9/51.8         27.6/61.4  32.1/154   42.3/199   153/213
 constexpr int64_t kFillBlocks = 1024;
 int32_t parts_for(const odb_logits_t* x, int32_t k, int64_t* len) {
     const int64_t n = x->rows * x->cols, round = x->dtype == ODB_FLOAT32 ? 4096 : 8192;
     int64_t parts = n > 0 ? kFillBlocks / n : 1;
-    if (x->vocab <= 6 * round) return 1;
+    if (x->vocab <= 6 * round || x->vocab * (k > kWave ? 32 : 8) < n * round) return 1;
     parts = std::min({parts, (x->vocab + round - 1) / round, (int64_t)(Room<kBlock>::kHold / (2 * k)), (int64_t)kWave});
     if (parts <= 1) return 1;
     *len = ((x->vocab + parts - 1) / parts + 7) & ~(int64_t)7;
