@@ -8,8 +8,8 @@
 // A mean's weight is known after a pass over the labels, the one that the policy loss makes.
 //
 // Bound by the reads of both lists and the writes of the gradient, 12 k bytes an element, and beside them by the
-// powers, logarithms and series: some 40 to 100 instructions an entry, with the rest most, whose sums need powers in 64
-// bits.  2.1 M elements of 32 entries (64% counted), the reverse divergence with the rest: 184 us for 620 MB
+// powers, logarithms and series: some 40 to 150 instructions an entry, with the rest most, whose sums need powers in 64
+// bits.  2.1 M elements of 32 entries (64% counted), the reverse divergence with the rest: 185 us for 620 MB
 // (3.4 TB/s, instructions most of the time); 0.54 M of 27, the mixture, renormalised: 80 us for 172 MB; one
 // tile of 16,384 of 64: 15 us, three launches one after the other, of which the lists' pass takes 8.
 #include <algorithm>
@@ -105,8 +105,8 @@ __device__ __forceinline__ void load_entries(const float* p, int k, int l, float
         return;
     }
     const int at = 4 * l < k - 4 ? 4 * l : k - 4, by = 4 * l - at;
-    // lists whose fours share lines with their neighbours' are better kept near: 0.54 M lists of 27 took 69 us, past
-    // the caches' usual order 79; 2.1 M of 32 took 177 and 172
+    // lists whose fours share lines with their neighbours' are better kept near: 0.52 M lists of 27 take 71 us (mixture,
+    // renormalised) and 41 (reverse, as they are), past the caches' usual order 80 and 57; 2.1 M of 32 219 and 217
     const float4a* const from = reinterpret_cast<const float4a*>(p + at);
     const float4a w = k & 3 ? *from : __builtin_nontemporal_load(from);
 #pragma unroll
@@ -143,7 +143,7 @@ __device__ __forceinline__ float exp_below(float d) {
     return fmaf(e * fmaf(d, kLog2eLow, fmaf(d, kLog2e, -u)), kLn2, e);
 }
 
-// ln x of a normal number to two roundings of x's logarithm.
+// ln x of a normal number to three roundings of it, next to x = 1 too: the hardware's is right to two of itself there.
 __device__ __forceinline__ float log_near(float x) { return __builtin_amdgcn_logf(x) * kLn2; }
 
 // An entry's probabilities, and ln p - ln q.
@@ -575,10 +575,11 @@ __global__ void __launch_bounds__(kBlock) distill_one_kernel(DistillArgs A) {
 
 // ------------------------------------------------------------------ host
 // Elements of a piece, a power of two: small ones fill the chip with few tokens, large ones cost fewer searches for
-// their slots and fewer sums of their counts.  us with pieces of a 4,096th of the elements, and with larger ones while
-// they have fewer than 4,096 entries and are 512 or more: 2^17 elements of 11 entries (mean over rows) 42.0 and 25.3, of
-// 7 (sum) 21.1 and 12.1, 2^16 of 32 21.7 and 18.1; 2^14 of 64 18 and 18, 2^19 of 27 73 and 73.  Up to 2,048
-// elements instead of 512: 3.0e7 elements of 1 entry 342 and 532, 2^22 of 4 75 and 89.
+// their slots and fewer sums of their counts.  us in a graph (forward, renormalised; rows of 512 in slots of 32,768) with
+// pieces of a 4,096th of the elements, and with larger ones while they have fewer than 4,096 entries and are 512 or more:
+// 3.0e7 elements of 1 entry (mean over rows) 525 and 338, 2^22 of 4 72 and 61, 2^16 of 32 20.5 and 18.3, 2^17 of 7 (sum)
+// 14.7 and 13.8, 2^17 of 11 (mean over rows) 24.1 and 26.1, 2^14 of 64 (mean over rows) 14.6 and 15.3.  Up to 2,048
+// elements and not 512: 526 for the first, 72 for the second.
 int32_t piece_for(int64_t elems, int32_t k) {
     int32_t piece = 32;
     while ((piece < 512 && elems / piece >= 4096) || (piece < kMaxPiece && piece * k < 4096 && elems / piece >= 512))
