@@ -854,9 +854,10 @@ size_t odb_distill_workspace_size(const odb_tiles_t* t, int32_t k);
  * to a reverse one.  A rest that is held at 2^-24 has no gradient.  A slot without counted tokens has loss, mean and count 0.
  * Elements behind the last slot are not written.  A token's terms and slopes are formed in 32 bits, what its
  * list leaves out, weights and sums over tokens in 64, in a fixed order: results are the same bit for bit from
- * call to call.  However near the student is, a divergence and its slopes are right to a few roundings of themselves
- * and no divergence of lists that sum to 1 or from the mixture is below 0; the forward and the reverse one of entries
- * as they are (ODB_SUPPORT_LISTED), and of lists with a held rest, may be.  Asynchronous.
+ * call to call.  However near the student is, a divergence from the mixture or of lists that sum to 1 (renormalised
+ * or with a rest that is not held) is not below 0 and right to a few roundings of itself, its slopes to a few
+ * roundings of their two parts.  Entries as they are have forward and reverse divergences of either sign, sums of
+ * terms that are right to a few roundings each.  Asynchronous.
  */
 int odb_distill_loss(const odb_tiles_t* t, const odb_distill_params_t* p, int32_t k, const float* d_student,
                      const float* d_teacher, const double* d_slot_weight, float* d_slot_loss, float* d_slot_mean,

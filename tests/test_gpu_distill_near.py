@@ -199,3 +199,21 @@ def test_an_entry_that_only_the_teacher_gives(support, low):
         assert np.all(value == math.inf) if kind == 0 else np.all((value > 0) & (value < 2)) or support == LISTED
         assert np.all(np.isfinite(value)) or kind == 0
         assert np.all(np.isfinite(slope)) and np.all(slope[:, 3] == 0)
+
+
+@pytest.mark.parametrize("support", [LISTED, RENORMALIZED, REST])
+def test_a_student_that_is_the_teacher(support):
+    """Distances of 0.  Renormalised lists' are off by e, 2 U at most (a reciprocal's and a product's rounding), which the
+    slopes have taken off to 8 U e."""
+    rng = np.random.default_rng(35)
+    for E, k in ((500, 16), (100, 128), (300, 1)):
+        t, _ = _near(rng, E, k, 0.1)
+        s = np.where(t == -math.inf, 3.0, t).astype(np.float32)
+        for kind in range(3):
+            value, slope = _run(t, s, kind, support, 0.3)
+            assert np.all((value >= 0) & (value <= U * U)), (kind, k)
+            if support == LISTED and kind < 2:
+                p = np.where(t == -math.inf, 0, np.exp(t.astype(X)))
+                assert np.all(np.abs(slope - (p if kind else -p)) <= 4 * U * p + 2.0 ** -115)
+            else:
+                assert np.all(np.abs(slope) <= 16 * U * U), (kind, k)
