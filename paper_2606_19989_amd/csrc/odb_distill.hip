@@ -26,10 +26,11 @@ constexpr int kMaxPiece = 2048;              // elements of a piece; with 4,096 
 constexpr int64_t kMaxDistillElems = (int64_t)1 << 32;     // 2^23 pieces: a grid's threads stay below 2^32
 
 // Chunks of a run from which on what they counted is folded (kManyChunks), unless its slots are many and so, nearly
-// all, short: here every piece adds up its slot's counts, four to sixteen times as often as the other losses'
-// chunks.  us a call without and with it, one slot of 2^24 / 2^26 / 2^27 elements of 8 entries: mean over tokens
-// 524 / 3,264 / 8,898 and 365 / 1,405 / 2,790, over rows of 512 625 / 5,464 / 19,474 and 377 / 1,445 / 2,898; in slots of 2^20 elements
-// 371 / 1,416 / 2,898 and 365 / 1,411 / 2,873, 393 / 1,501 / 3,049 and 388 / 1,471 / 2,987.
+// all, short: here every piece adds up its slot's counts, four to sixteen times as often as the other losses' chunks.
+// us a call without it and with it, one slot of 2^24 / 2^26 / 2^27 elements of 8 entries:
+//   mean over tokens         524 / 3,264 /  8,898    365 / 1,405 / 2,790
+//   over rows of 512         625 / 5,464 / 19,474    377 / 1,445 / 2,898
+// and in slots of 2^20 elements 371 / 1,416 / 2,898, 365 / 1,411 / 2,873 and 393 / 1,501 / 3,049, 388 / 1,471 / 2,987.
 constexpr int64_t kManyCounts = 2048;
 
 struct DistillPart {
